@@ -564,6 +564,87 @@ windq_status windq_greedy_allocate(windq_ctx* ctx, const float* saliency, const 
 windq_status windq_fallback(windq_ctx* ctx, const float* err, const float* energy, const uint8_t* actions, int64_t U,
                             float theta, uint8_t* actions_out, int64_t* n_changed_out, void* stream);
 
+/* ---- after the plan: low-rank adapters over the quantised model ------------------------------------
+ *
+ * The consumer of a plan serves the fake-quantised weights (Wq_out of windq_apply_plan) to many requests at once, each
+ * with a low-rank adapter of its own, and trains such adapters to win back what quantisation lost.  (The paper has no
+ * counterpart.)  The three calls below are the shared projection with its adapters, its gradients, and the optimiser. */
+typedef enum { WINDQ_F16 = 0, WINDQ_BF16 = 1, WINDQ_F32 = 2 } windq_dtype;
+
+/* Shared projection with one low-rank adapter per token.  With a = adapter_of[t]:
+ *   u_t = scaling[a] * A[a] x_t              (rank values, binary32)
+ *   Y[t] = W x_t + B[a] u_t                  (binary32 accumulation, one rounding to the type of Y)
+ * A token whose adapter_of is outside [0, n_adapters) has no adapter: Y[t] = W x_t.  Tokens may come in any order;
+ * a batch in which neighbouring tokens share an adapter (prompts one after another) runs fastest.
+ *   dtype       WINDQ_F16 or WINDQ_BF16, the type of X, W, A, B and Y
+ *   X [T][ldx], W [R][ldw], Y [T][ldy]       row-major; ldx, ldw >= C, ldy >= R, all multiples of 8; C % 8 == 0
+ *   A [n_adapters][rank][C], B [n_adapters][R][rank]   contiguous; rank a multiple of 8 in [8, 128] (adapters of
+ *                                            smaller rank are padded with zeros)
+ *   scaling     fp32 [n_adapters];  adapter_of  i32 [T]
+ * T = 0 is allowed and does nothing.  Y must not overlap an input.  Columns of Y at and beyond R are not written.
+ * On WINDQ_F16, u_t is carried as the sum of two fp16 values and therefore saturates at +-131008; inputs must be finite
+ * (an adapter with a non-finite weight spoils the rows of every token within 256 tokens of one of its own).
+ * Scratch: windq_scratch_bytes_lora_forward. */
+int64_t windq_scratch_bytes_lora_forward(int64_t T, int64_t R, int64_t C, int rank);
+windq_status windq_lora_forward(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx, const void* W,
+                                int64_t R, int64_t ldw, const void* A, const void* B, int64_t n_adapters, int rank,
+                                const float* scaling, const int32_t* adapter_of, void* Y, int64_t ldy, void* stream);
+
+/* Gradients of windq_lora_forward for a frozen W, given dY = the gradient of Y.  With u_t as above and
+ *   v_t = scaling[a] * B[a]^T dY[t]          (rank values, binary32):
+ *   dX[t] = W^T dY[t] + A[a]^T v_t           type `dtype`, [T][lddx], nullable
+ *   dA[a] = sum over the tokens t of a  of  v_t x_t^T      fp32 [n_adapters][rank][C], nullable
+ *   dB[a] = sum over the tokens t of a  of  dY[t] u_t^T    fp32 [n_adapters][R][rank], nullable
+ * u_t is computed again from X; nothing has to be kept from the forward call.  The outputs are overwritten (an adapter
+ * without tokens gets zeros).  Every sum is taken in an order fixed by the sizes: equal calls give equal bits.
+ * Arguments as windq_lora_forward; lddy >= R, lddx >= C, multiples of 8.  With T = 0 dA and dB become zero.
+ * Scratch: windq_scratch_bytes_lora_backward. */
+int64_t windq_scratch_bytes_lora_backward(int64_t T, int64_t R, int64_t C, int64_t n_adapters, int rank);
+windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx, const void* W,
+                                 int64_t R, int64_t ldw, const void* A, const void* B, int64_t n_adapters, int rank,
+                                 const float* scaling, const int32_t* adapter_of, const void* dY, int64_t lddy, void* dX,
+                                 int64_t lddx, float* dA, float* dB, void* stream);
+
+/* One AdamW step (decoupled weight decay) over any number of tensors.  Per element, in binary32, every operation
+ * rounded as written:
+ *   g = grad * grad_scale[0]                      (no product when grad_scale is NULL)
+ *   m = m * beta1 + g * (1 - beta1);   v = v * beta2 + (g * g) * (1 - beta2);   r = sqrt(v)
+ *   param = param * (1 - lr * weight_decay) - (m * (lr / (1 - beta1^step))) / (r * (1 / sqrt(1 - beta2^step)) + eps)
+ *   copy = param rounded to the copy's type       (e.g. the 16-bit adapters windq_lora_forward reads)
+ * The factors of the hyperparameters are formed in double and rounded to binary32 once.
+ *   jobs: HOST array of n_jobs descriptors (n_jobs >= 1, no upper limit), read during the call only; all jobs share the
+ *         types.  Tensors are flat, 16-byte aligned, of any length n >= 0 (0 does nothing); none may overlap.
+ *   param_dtype WINDQ_F32, _F16 or _BF16 (16-bit parameters are rounded once per step);  grad_dtype likewise
+ *   copy_dtype  WINDQ_F16 or WINDQ_BF16; read only by jobs whose copy is not NULL
+ *   state_bits  32: m and v are fp32 [n]; m_scale and r_scale are not read.
+ *               8:  every block of 256 elements of a tensor (the last may be shorter) keeps m as i8 codes q with one
+ *                   scale, m = sign(q) (q/127)^2 * m_scale, and r = sqrt(v) as u8 codes, r = (q/255)^2 * r_scale.  The
+ *                   scales are the block's largest |m| and r (0, with codes 0, where that is below 2^-100); codes are
+ *                   rounded to nearest in the square-root domain, and an r above zero in such a block never gets code 0
+ *                   (its element would divide by eps).  The step itself uses m and r before they are rounded to codes.
+ *                   All-zero codes and scales are the empty state.
+ *   step >= 1 counts from one;  lr >= 0, 0 <= beta1, beta2 < 1, eps > 0, weight_decay >= 0, all finite;
+ *   grad_scale  fp32 [1] on the device, or NULL: an unscaling and / or clipping factor formed there */
+typedef struct {
+  void* param;
+  const void* grad;
+  void* m;         /* fp32 [n], or i8 [n] */
+  void* v;         /* fp32 [n], or u8 [n] (codes of sqrt(v)) */
+  float* m_scale;  /* fp32 [ceil(n / 256)] with 8-bit states */
+  float* r_scale;  /* likewise */
+  void* copy;      /* 16-bit [n], nullable */
+  int64_t n;
+} windq_adamw_job;
+windq_status windq_adamw_step(windq_ctx* ctx, const windq_adamw_job* jobs, int n_jobs, int param_dtype, int grad_dtype,
+                              int copy_dtype, int state_bits, int64_t step, double lr, double beta1, double beta2, double eps,
+                              double weight_decay, const float* grad_scale, void* stream);
+
+/* The values 8-bit states stand for (to inspect or to save them): m_out[j], v_out[j] receive m and v of job j as fp32 [n].
+ * jobs as in windq_adamw_step with state_bits 8 (param, grad and copy are not read); m_out, v_out: HOST arrays of n_jobs
+ * device pointers, 16-byte aligned. */
+windq_status windq_adamw_states(windq_ctx* ctx, const windq_adamw_job* jobs, int n_jobs, float* const* m_out,
+                                float* const* v_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

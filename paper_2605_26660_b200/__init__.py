@@ -96,6 +96,15 @@ def _load() -> ctypes.CDLL:
     lib.windq_apply_plan.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.windq_apply_plan_multi.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, i32, vp, vp, vp, i32, vp]
     lib.windq_apply_plan_searched.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    f64 = ctypes.c_double
+    lib.windq_lora_forward.argtypes = [vp, i32, vp, i64, i64, i64, vp, i64, i64, vp, vp, i64, i32, vp, vp, vp, i64, vp]
+    lib.windq_lora_backward.argtypes = [vp, i32, vp, i64, i64, i64, vp, i64, i64, vp, vp, i64, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp]
+    lib.windq_scratch_bytes_lora_forward.argtypes = [i64, i64, i64, i32]
+    lib.windq_scratch_bytes_lora_forward.restype = i64
+    lib.windq_scratch_bytes_lora_backward.argtypes = [i64, i64, i64, i64, i32]
+    lib.windq_scratch_bytes_lora_backward.restype = i64
+    lib.windq_adamw_step.argtypes = [vp, vp, i32, i32, i32, i32, i32, i64, f64, f64, f64, f64, f64, vp, vp]
+    lib.windq_adamw_states.argtypes = [vp, vp, i32, vp, vp, vp]
     lib.windq_fit_ternary_search.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
     lib.windq_scratch_bytes_fit_ternary_search.argtypes = [i64, i64, i32]
     lib.windq_scratch_bytes_fit_ternary_search.restype = i64
@@ -933,3 +942,211 @@ def windq_features_fit_batch(ctx: Context, Ws, G: int, ss, clip_grid: torch.Tens
     ctx._check(_lib.windq_features_fit_batch(ctx._h, ctypes.cast(jobs, ctypes.c_void_p), len(Ws), int(G), _ptr(clip_grid),
                                              clip_grid.numel(), _stream(stream)))
     return feat_list, results
+
+
+# ---- low-rank adapters over the quantised model, and their optimiser ----
+
+_DTYPE_CODES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}   # windq_dtype of the header
+
+
+def windq_scratch_bytes_lora_forward(T: int, R: int, C: int, rank: int) -> int:
+    return int(_lib.windq_scratch_bytes_lora_forward(T, R, C, rank))
+
+
+def windq_scratch_bytes_lora_backward(T: int, R: int, C: int, n_adapters: int, rank: int) -> int:
+    return int(_lib.windq_scratch_bytes_lora_backward(T, R, C, n_adapters, rank))
+
+
+def _lora_args(X, W, A, B, scaling, adapter_of):
+    """Checks the arguments the two adapter calls share; returns (dtype code, T, C, ldx, R, ldw, n_adapters, rank)."""
+    dt = X.dtype
+    if dt is not torch.float16 and dt is not torch.bfloat16:
+        raise TypeError("X must be torch.float16 or torch.bfloat16, got %s" % dt)
+    if X.dim() != 2 or W.dim() != 2 or A.dim() != 3 or B.dim() != 3 or scaling.dim() != 1 or adapter_of.dim() != 1:
+        raise ValueError("X and W have 2 dimensions, A and B 3, scaling and adapter_of 1")
+    T, C = X.shape
+    R, n, rank = W.shape[0], A.shape[0], A.shape[1]
+    ldx, ldw = X.stride(0), W.stride(0)
+    if not (X.is_cuda and W.is_cuda and A.is_cuda and B.is_cuda and scaling.is_cuda and adapter_of.is_cuda):
+        raise TypeError("X, W, A, B, scaling and adapter_of must be CUDA tensors")
+    if W.dtype is not dt or A.dtype is not dt or B.dtype is not dt:
+        raise TypeError("W, A and B must have the type of X, %s" % dt)
+    if scaling.dtype is not torch.float32 or adapter_of.dtype is not torch.int32:
+        raise TypeError("scaling must be torch.float32 and adapter_of torch.int32")
+    if W.shape[1] != C or A.shape[2] != C or B.shape != (n, R, rank) or scaling.shape[0] != n or adapter_of.shape[0] != T:
+        raise ValueError("shapes do not fit: X [T, C], W [R, C], A [n, rank, C], B [n, R, rank], scaling [n], adapter_of [T]")
+    if (X.stride(1) != 1 and C > 1) or (W.stride(1) != 1 and C > 1):
+        raise ValueError("X and W must be row-major (unit stride along columns)")
+    if not (A.is_contiguous() and B.is_contiguous() and scaling.is_contiguous() and adapter_of.is_contiguous()):
+        raise ValueError("A, B, scaling and adapter_of must be contiguous")
+    if T == 1:      # the stride of a single row means nothing, and torch may report any
+        ldx = max(ldx, C)
+        ldx += -ldx % 8
+    return _DTYPE_CODES[dt], T, C, ldx, R, (ldw if R > 1 else C), n, rank
+
+
+def _row_output(t, rows, cols, dtype, device, name):
+    """A caller's [rows, cols] output, or a new one whose rows are padded to a multiple of 8 elements."""
+    if t is None:
+        if cols % 8 == 0:
+            return torch.empty((rows, cols), dtype=dtype, device=device), cols
+        ld = cols + -cols % 8
+        return torch.empty((rows, ld), dtype=dtype, device=device)[:, :cols], ld
+    _need(t, dtype, name, 2)
+    if t.shape != (rows, cols) or (t.stride(1) != 1 and cols > 1):
+        raise ValueError("%s must be a row-major [%d, %d] tensor" % (name, rows, cols))
+    return t, (t.stride(0) if rows > 1 else cols + -cols % 8)
+
+
+def windq_lora_forward(ctx: Context, X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                       scaling: torch.Tensor, adapter_of: torch.Tensor, *, out: torch.Tensor | None = None,
+                       stream=None) -> torch.Tensor:
+    """Y[t] = W x_t + B[a] (scaling[a] A[a] x_t) with a = adapter_of[t] (outside [0, n): no adapter).
+
+    X [T, C], W [R, C] (as windq_apply_plan leaves it), A [n, rank, C], B [n, R, rank], all fp16 or all bf16;
+    scaling fp32 [n]; adapter_of int32 [T].  Returns Y [T, R] of the same type (``out`` if given)."""
+    code, T, C, ldx, R, ldw, n, rank = _lora_args(X, W, A, B, scaling, adapter_of)
+    out, ldy = _row_output(out, T, R, X.dtype, X.device, "out")
+    ctx._check(_lib.windq_lora_forward(ctx._h, code, X.data_ptr(), T, C, ldx, W.data_ptr(), R, ldw, A.data_ptr(), B.data_ptr(),
+                                       n, rank, scaling.data_ptr(), adapter_of.data_ptr(), out.data_ptr(), ldy,
+                                       _stream(stream)))
+    return out
+
+
+def windq_lora_backward(ctx: Context, X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                        scaling: torch.Tensor, adapter_of: torch.Tensor, dY: torch.Tensor, *, want_dx: bool = True,
+                        want_dab: bool = True, out: dict | None = None, stream=None) -> dict:
+    """Gradients of windq_lora_forward for a frozen W, from dY [T, R] (the gradient of Y).
+
+    Returns dict(dx [T, C] of X's type | None, dA fp32 [n, rank, C] | None, dB fp32 [n, R, rank] | None), overwritten,
+    not added to.  ``out`` may hold preallocated tensors under the same keys."""
+    code, T, C, ldx, R, ldw, n, rank = _lora_args(X, W, A, B, scaling, adapter_of)
+    _need(dY, X.dtype, "dY", 2)
+    if dY.shape != (T, R) or (dY.stride(1) != 1 and R > 1):
+        raise ValueError("dY must be a row-major [T, R] tensor")
+    lddy = dY.stride(0) if T > 1 else R + -R % 8
+    out = dict(out) if out else {}
+    dx, lddx = _row_output(out.get("dx"), T, C, X.dtype, X.device, "dx") if want_dx else (None, 0)
+    dA, dB = (out.get("dA"), out.get("dB")) if want_dab else (None, None)
+    if want_dab:
+        if dA is None:
+            dA = torch.empty((n, rank, C), dtype=torch.float32, device=X.device)
+        if dB is None:
+            dB = torch.empty((n, R, rank), dtype=torch.float32, device=X.device)
+        _need(dA, torch.float32, "dA", 3)
+        _need(dB, torch.float32, "dB", 3)
+        if dA.shape != A.shape or dB.shape != B.shape or not (dA.is_contiguous() and dB.is_contiguous()):
+            raise ValueError("dA and dB must be contiguous and have the shapes of A and B")
+    ctx._check(_lib.windq_lora_backward(ctx._h, code, X.data_ptr(), T, C, ldx, W.data_ptr(), R, ldw, A.data_ptr(), B.data_ptr(),
+                                        n, rank, scaling.data_ptr(), adapter_of.data_ptr(), dY.data_ptr(), lddy, _ptr(dx), lddx,
+                                        _ptr(dA), _ptr(dB), _stream(stream)))
+    return dict(dx=dx, dA=dA, dB=dB)
+
+
+ADAMW_BLOCK = 256   # elements of a tensor that share the scales of 8-bit states
+
+
+class _AdamwJob(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("r_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64)]
+
+
+class AdamwTensors:
+    """The tensors one optimiser steps, as windq_adamw_step takes them: checked once, kept alive, and described in the
+    array the C call reads.
+
+    ``params``, ``grads``: lists of contiguous CUDA tensors (fp32, fp16 or bf16; one type for all params, one for all
+    grads).  ``m``, ``v``: fp32 tensors of the same sizes, or int8 ``m`` and uint8 ``v`` (codes of sqrt(v)) together with
+    ``m_scale`` and ``r_scale``, fp32, one entry per 256 elements.  ``copies``: None or a list of fp16 / bf16 tensors
+    (or None) that receive the rounded parameters."""
+
+    def __init__(self, params, grads, m, v, *, m_scale=None, r_scale=None, copies=None):
+        k = len(params)
+        if k == 0:
+            raise ValueError("params must be non-empty")
+        for name, ts in (("grads", grads), ("m", m), ("v", v), ("m_scale", m_scale), ("r_scale", r_scale), ("copies", copies)):
+            if ts is not None and len(ts) != k:
+                raise ValueError("%s must have one entry per parameter" % name)
+        if m[0].dtype not in (torch.float32, torch.int8):
+            raise TypeError("m must be torch.float32 or torch.int8, got %s" % m[0].dtype)
+        self.state_bits = 8 if m[0].dtype == torch.int8 else 32
+        if self.state_bits == 8 and (m_scale is None or r_scale is None):
+            raise ValueError("8-bit states need m_scale and r_scale")
+        self.param_dtype, self.grad_dtype = params[0].dtype, grads[0].dtype
+        if self.param_dtype not in _DTYPE_CODES or self.grad_dtype not in _DTYPE_CODES:
+            raise TypeError("params and grads must be fp32, fp16 or bf16")
+        self.copy_dtype = next((c.dtype for c in copies or [] if c is not None), torch.float16)
+        if self.copy_dtype not in (torch.float16, torch.bfloat16):
+            raise TypeError("copies must be fp16 or bf16")
+        state = (torch.int8, torch.uint8) if self.state_bits == 8 else (torch.float32, torch.float32)
+        self._jobs = (_AdamwJob * k)()
+        for j in range(k):
+            n = params[j].numel()
+            self._flat(params[j], self.param_dtype, n, "params")
+            self._flat(m[j], state[0], n, "m")
+            self._flat(v[j], state[1], n, "v")
+            scales = (None, None)
+            if self.state_bits == 8:
+                scales = (m_scale[j], r_scale[j])
+                for t, name in zip(scales, ("m_scale", "r_scale")):
+                    self._flat(t, torch.float32, -(-n // ADAMW_BLOCK), name)
+            copy = copies[j] if copies else None
+            if copy is not None:
+                self._flat(copy, self.copy_dtype, n, "copies")
+            self._jobs[j] = _AdamwJob(params[j].data_ptr(), None, m[j].data_ptr(), v[j].data_ptr(),
+                                      *(None if t is None else t.data_ptr() for t in scales),
+                                      None if copy is None else copy.data_ptr(), n)
+        self._keep = (list(params), list(m), list(v), m_scale, r_scale, copies)
+        self._codes = (_DTYPE_CODES[self.param_dtype], _DTYPE_CODES[self.grad_dtype], _DTYPE_CODES[self.copy_dtype], self.state_bits)
+        self.set_grads(grads)
+
+    @staticmethod
+    def _flat(t, dtype, n, name):
+        _need(t, dtype, name)
+        if t.numel() != n or not t.is_contiguous():
+            raise ValueError("%s: a tensor is not contiguous or has %d elements where %d are needed" % (name, t.numel(), n))
+
+    def __len__(self):
+        return len(self._jobs)
+
+    def set_grads(self, grads) -> None:
+        """Takes other gradient tensors from the next step on."""
+        if len(grads) != len(self._jobs):
+            raise ValueError("grads must have one entry per parameter")
+        for j, g in enumerate(grads):
+            self._flat(g, self.grad_dtype, self._jobs[j].n, "grads")
+        for j, g in enumerate(grads):
+            self._jobs[j].grad = g.data_ptr()
+        self._grads = list(grads)
+
+
+def windq_adamw_step(ctx: Context, tensors: AdamwTensors, *, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+                     eps: float = 1e-8, weight_decay: float = 0.0, grad_scale: torch.Tensor | None = None, stream=None) -> None:
+    """One AdamW step over all tensors, in place.  ``step`` counts from one; ``grad_scale`` (fp32 [1] on the device)
+    multiplies every gradient first."""
+    if grad_scale is not None:
+        _need(grad_scale, torch.float32, "grad_scale")
+        if grad_scale.numel() != 1:
+            raise ValueError("grad_scale must hold one value")
+    ctx._check(_lib.windq_adamw_step(ctx._h, tensors._jobs, len(tensors._jobs), *tensors._codes, int(step), lr, beta1, beta2, eps,
+                                     weight_decay, _ptr(grad_scale), _stream(stream)))
+
+
+def windq_adamw_states(ctx: Context, tensors: AdamwTensors, m_out=None, v_out=None, *, stream=None):
+    """The fp32 values that 8-bit states stand for: (list of m, list of v), written to the given tensors if any."""
+    if tensors.state_bits != 8:
+        raise ValueError("the states are not held in 8 bits")
+    params, k = tensors._keep[0], len(tensors)
+    outs, arrays = [], []
+    for given, name in ((m_out, "m_out"), (v_out, "v_out")):
+        if given is None:
+            given = [torch.empty(p.shape, dtype=torch.float32, device=p.device) for p in params]
+        elif len(given) != k:
+            raise ValueError("%s must have one entry per parameter" % name)
+        else:
+            for t, p in zip(given, params):
+                AdamwTensors._flat(t, torch.float32, p.numel(), name)
+        outs.append(given)
+        arrays.append((ctypes.c_void_p * k)(*[t.data_ptr() for t in given]))
+    ctx._check(_lib.windq_adamw_states(ctx._h, tensors._jobs, k, arrays[0], arrays[1], _stream(stream)))
+    return tuple(outs)
