@@ -88,6 +88,12 @@ windq_status windq_selfcheck(windq_ctx* ctx, int64_t* n_failures_out, void* stre
  * Synchronises the device (a blocking copy). */
 windq_status windq_fit_work(windq_ctx* ctx, int64_t* evaluated_out, int64_t* searched_out, int reset);
 
+/* Thread blocks of windq_lora_forward / windq_lora_backward in which a wait on a copy or a matrix product gave up after
+ * about two seconds: 0 unless the GPU or the library is broken; the results of a call that adds to it are invalid.  (Every
+ * wait of a kernel is bounded, so that such a fault ends the kernel instead of hanging the GPU.)
+ *   n_out: HOST pointer to one int64; reset != 0 puts the counter back to zero.  Synchronises the device. */
+windq_status windq_stalls(windq_ctx* ctx, int64_t* n_out, int reset);
+
 /* Grows the context's scratch buffer to at least `bytes` now (synchronises the device), so that
  * later calls do not allocate.  windq_scratch_bytes_* tell how much a call will need. */
 windq_status windq_reserve(windq_ctx* ctx, int64_t bytes);

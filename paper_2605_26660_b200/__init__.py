@@ -97,6 +97,7 @@ def _load() -> ctypes.CDLL:
     lib.windq_apply_plan_multi.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, i32, vp, vp, vp, i32, vp]
     lib.windq_apply_plan_searched.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
     f64 = ctypes.c_double
+    lib.windq_stalls.argtypes = [vp, ctypes.POINTER(i64), i32]
     lib.windq_lora_forward.argtypes = [vp, i32, vp, i64, i64, i64, vp, i64, i64, vp, vp, i64, i32, vp, vp, vp, i64, vp]
     lib.windq_lora_backward.argtypes = [vp, i32, vp, i64, i64, i64, vp, i64, i64, vp, vp, i64, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp]
     lib.windq_scratch_bytes_lora_forward.argtypes = [i64, i64, i64, i32]
@@ -198,6 +199,13 @@ def windq_fit_work(ctx: Context, reset: bool = False):
     a, b = ctypes.c_int64(0), ctypes.c_int64(0)
     ctx._check(_lib.windq_fit_work(ctx._h, ctypes.byref(a), ctypes.byref(b), 1 if reset else 0))
     return int(a.value), int(b.value)
+
+
+def windq_stalls(ctx: Context, reset: bool = False) -> int:
+    """Thread blocks of the adapter calls whose bounded waits gave up (0 is expected).  Synchronises the device."""
+    n = ctypes.c_int64(0)
+    ctx._check(_lib.windq_stalls(ctx._h, ctypes.byref(n), 1 if reset else 0))
+    return int(n.value)
 
 
 def windq_scratch_bytes_act_stats(T: int, C: int) -> int:

@@ -146,6 +146,18 @@ windq_status windq_fit_work(windq_ctx* ctx, int64_t* evaluated_out, int64_t* sea
   return WINDQ_OK;
 }
 
+windq_status windq_stalls(windq_ctx* ctx, int64_t* n_out, int reset) {
+  using namespace windq;
+  if (!ctx) return fail(nullptr, WINDQ_ERR_NULL, "windq_stalls: ctx is NULL");
+  WINDQ_REQUIRE(ctx, n_out, WINDQ_ERR_NULL, "windq_stalls: n_out is NULL");
+  DeviceGuard guard(ctx->device);
+  unsigned long long host = 0;
+  WINDQ_CUDA(ctx, cudaMemcpy(&host, stall_counter(ctx), sizeof(host), cudaMemcpyDeviceToHost));
+  if (reset) WINDQ_CUDA(ctx, cudaMemset(stall_counter(ctx), 0, sizeof(host)));
+  *n_out = (int64_t)host;
+  return WINDQ_OK;
+}
+
 windq_status windq_reserve(windq_ctx* ctx, int64_t bytes) {
   if (!ctx) return windq::fail(nullptr, WINDQ_ERR_NULL, "windq_reserve: ctx is NULL");
   WINDQ_REQUIRE(ctx, bytes >= 0, WINDQ_ERR_ARG, "windq_reserve: bytes = %lld", (long long)bytes);

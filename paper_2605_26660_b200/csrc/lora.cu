@@ -1,5 +1,6 @@
 // The shared projection with one low-rank adapter per token, and its gradients.
-#include "typed.cuh"
+#include "lora.cuh"
+#include "tcgen05.cuh"
 
 namespace windq {
 namespace {
@@ -7,9 +8,36 @@ namespace {
 __device__ __forceinline__ float value(const void* base, int64_t i, int dt) { return load1(base, i, dt); }
 
 // S[t][j] = scaling[a] * sum_k Z[t][k] * P[a](k, j), P[a](k, j) = P[a * pa + k * pk + j * pj]; zeros without an adapter.
-__global__ void low_rank_kernel(const void* Z, int64_t ldz, int64_t K, const void* P, int64_t pa, int64_t pk, int64_t pj, int dt,
-                                int64_t n_adapters, int rank, const float* scaling, const int32_t* adapter_of, float* S) {
+// The blocks past the tokens write the lists of adapters of the token tiles.
+__global__ void low_rank_kernel(const void* Z, int64_t ldz, int64_t T, int64_t K, const void* P, int64_t pa, int64_t pk, int64_t pj,
+                                int dt, int64_t n_adapters, int rank, const float* scaling, const int32_t* adapter_of, float* S,
+                                int* lists, int rows) {
+  launch_dependents();
   const int64_t t = blockIdx.x;
+  if (t >= T) {
+    // adapters in the order of their first token; a thread per token (blockDim.x >= rows)
+    __shared__ int ids[256], taken[8];
+    const int tile = (int)(t - T), i = threadIdx.x;
+    const int64_t at = (int64_t)tile * rows + i;
+    int id = i < rows && at < T ? adapter_of[at] : -1;
+    if (id >= n_adapters) id = -1;
+    ids[i] = id;
+    __syncthreads();
+    bool first = id >= 0;
+    for (int k = 0; k < i && first; k++) first = ids[k] != id;
+    const unsigned vote = __ballot_sync(0xffffffffu, first);
+    if ((i & 31) == 0) taken[i >> 5] = __popc(vote);
+    __syncthreads();
+    int before = __popc(vote & ((1u << (i & 31)) - 1)), all = 0;
+    for (int w = 0; w < 8; w++) {
+      if (w < i >> 5) before += taken[w];
+      all += taken[w];
+    }
+    int* list = lists + (int64_t)tile * (rows + 1);
+    if (first) list[1 + before] = id;
+    if (i == 0) list[0] = all;
+    return;
+  }
   const int a = adapter_of[t];
   for (int j = threadIdx.x >> 5; j < rank; j += blockDim.x >> 5) {
     float acc = 0.0f;
@@ -21,33 +49,6 @@ __global__ void low_rank_kernel(const void* Z, int64_t ldz, int64_t K, const voi
     }
     if ((threadIdx.x & 31) == 0) S[t * rank + j] = acc;
   }
-}
-
-// O[t][n] = sum_k Z[t][k] * W(k, n) + sum_j S[t][j] * P[a](j, n), one output a thread, 32 x 8 tiles.
-__global__ void project_kernel(const void* Z, int64_t ldz, int64_t T, int64_t K, int64_t N, const void* W, int64_t wk, int64_t wn,
-                               const void* P, int64_t pa, int64_t pj, int64_t pn, int dt, int64_t n_adapters, int rank,
-                               const int32_t* adapter_of, const float* S, void* O, int64_t ldo) {
-  __shared__ float zs[8][33], ws[32][33];
-  const int64_t n = (int64_t)blockIdx.x * 32 + threadIdx.x, t = (int64_t)blockIdx.y * 8 + threadIdx.y;
-  float acc = 0.0f;
-  for (int64_t k0 = 0; k0 < K; k0 += 32) {
-    const int64_t k = k0 + threadIdx.x;
-    zs[threadIdx.y][threadIdx.x] = (t < T && k < K) ? value(Z, t * ldz + k, dt) : 0.0f;
-    for (int y = threadIdx.y; y < 32; y += 8) {
-      const int64_t kk = k0 + (wk == 1 ? threadIdx.x : y), nn = (int64_t)blockIdx.x * 32 + (wk == 1 ? y : threadIdx.x);
-      const float w = (kk < K && nn < N) ? value(W, kk * wk + nn * wn, dt) : 0.0f;
-      if (wk == 1) ws[threadIdx.x][y] = w;
-      else ws[y][threadIdx.x] = w;
-    }
-    __syncthreads();
-    for (int k1 = 0; k1 < 32; k1++) acc = fmaf(zs[threadIdx.y][k1], ws[k1][threadIdx.x], acc);
-    __syncthreads();
-  }
-  if (t >= T || n >= N) return;
-  const int a = adapter_of[t];
-  if (a >= 0 && a < n_adapters)
-    for (int j = 0; j < rank; j++) acc = fmaf(S[t * rank + j], value(P, a * pa + j * pj + n * pn, dt), acc);
-  store1(O, t * ldo + n, dt, acc);
 }
 
 // D[a][..] = sum over the tokens of a of S[t][j] * Z[t][c]; j contiguous (dB) or c contiguous (dA).
@@ -107,7 +108,7 @@ extern "C" {
 
 int64_t windq_scratch_bytes_lora_forward(int64_t T, int64_t R, int64_t C, int rank) {
   if (T < 0 || R <= 0 || C <= 0 || rank <= 0) return 0;
-  return 4 * T * rank;
+  return windq::round_up(4 * T * rank, 256) + windq::list_bytes(T);
 }
 
 windq_status windq_lora_forward(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx, const void* W,
@@ -127,16 +128,17 @@ windq_status windq_lora_forward(windq_ctx* ctx, int dtype, const void* X, int64_
   if (room != WINDQ_OK) return room;
   cudaStream_t st = (cudaStream_t)stream;
   float* U = (float*)ctx->scratch;
-  low_rank_kernel<<<(unsigned)T, 256, 0, st>>>(X, ldx, C, A, rank * C, 1, C, dtype, n_adapters, rank, scaling, adapter_of, U);
-  project_kernel<<<dim3((unsigned)((R + 31) / 32), (unsigned)((T + 7) / 8)), dim3(32, 8), 0, st>>>(
-      X, ldx, T, C, R, W, 1, ldw, B, R * rank, 1, rank, dtype, n_adapters, rank, adapter_of, U, Y, ldy);
+  int* lists = (int*)((char*)ctx->scratch + round_up(4 * T * rank, 256));
+  const int rows = token_tile(T), tiles = (int)((T + rows - 1) / rows);
+  low_rank_kernel<<<(unsigned)(T + tiles), 256, 0, st>>>(X, ldx, T, C, A, rank * C, 1, C, dtype, n_adapters, rank, scaling, adapter_of,
+                                                         U, lists, rows);
   WINDQ_CUDA(ctx, cudaGetLastError());
-  return WINDQ_OK;
+  return launch_projection(ctx, Projection{dtype, false, X, T, C, R, ldx, W, ldw, B, n_adapters, rank, adapter_of, U, lists, Y, ldy}, st);
 }
 
 int64_t windq_scratch_bytes_lora_backward(int64_t T, int64_t R, int64_t C, int64_t n_adapters, int rank) {
   if (T < 0 || R <= 0 || C <= 0 || rank <= 0 || n_adapters <= 0) return 0;
-  return 2 * windq::round_up(4 * T * rank, 256);
+  return 2 * windq::round_up(4 * T * rank, 256) + windq::list_bytes(T);
 }
 
 windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx, const void* W,
@@ -166,12 +168,20 @@ windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64
   if (room != WINDQ_OK) return room;
   float* U = (float*)ctx->scratch;
   float* V = (float*)((char*)ctx->scratch + round_up(4 * T * rank, 256));
-  if (dB) low_rank_kernel<<<(unsigned)T, 256, 0, st>>>(X, ldx, C, A, rank * C, 1, C, dtype, n_adapters, rank, scaling, adapter_of, U);
+  int* lists = (int*)((char*)V + round_up(4 * T * rank, 256));
+  const int rows = token_tile(T), tiles = (int)((T + rows - 1) / rows);
+  if (dB)
+    low_rank_kernel<<<(unsigned)T, 256, 0, st>>>(X, ldx, T, C, A, rank * C, 1, C, dtype, n_adapters, rank, scaling, adapter_of, U,
+                                                 nullptr, rows);
   if (dX || dA)
-    low_rank_kernel<<<(unsigned)T, 256, 0, st>>>(dY, lddy, R, B, R * rank, rank, 1, dtype, n_adapters, rank, scaling, adapter_of, V);
-  if (dX)
-    project_kernel<<<dim3((unsigned)((C + 31) / 32), (unsigned)((T + 7) / 8)), dim3(32, 8), 0, st>>>(
-        dY, lddy, T, R, C, W, ldw, 1, A, rank * C, C, 1, dtype, n_adapters, rank, adapter_of, V, dX, lddx);
+    low_rank_kernel<<<(unsigned)(T + tiles), 256, 0, st>>>(dY, lddy, T, R, B, R * rank, rank, 1, dtype, n_adapters, rank, scaling,
+                                                           adapter_of, V, lists, rows);
+  WINDQ_CUDA(ctx, cudaGetLastError());
+  if (dX) {
+    const windq_status done = launch_projection(
+        ctx, Projection{dtype, true, dY, T, R, C, lddy, W, ldw, A, n_adapters, rank, adapter_of, V, lists, dX, lddx}, st);
+    if (done != WINDQ_OK) return done;
+  }
   if (dA)
     gradient_kernel<<<dim3((unsigned)((C + 31) / 32), rank / 8, (unsigned)n_adapters), dim3(32, 8), 0, st>>>(
         X, ldx, T, C, V, rank, dtype, adapter_of, dA, C, 1);

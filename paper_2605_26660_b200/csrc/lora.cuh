@@ -1,0 +1,38 @@
+// Declarations shared by the translation units of the adapter calls.
+#pragma once
+
+#include "typed.cuh"
+
+namespace windq {
+
+// O[t][n] = sum_k Z[t][k] W(n, k) + sum_j S[t][j] P[a](n, j), a = adapter_of[t]; S is fp32 and already scaled.
+//   forward:  Z = X,  W(n, k) = W[n][k], P[a](n, j) = B[a][n][j]     (k and j contiguous)
+//   backward: Z = dY, W(n, k) = W[k][n], P[a](n, j) = A[a][j][n]     (n contiguous: transposed)
+struct Projection {
+  int dtype;
+  bool transposed;
+  const void* Z;
+  int64_t T, K, N, ldz;
+  const void* W;
+  int64_t ldw;
+  const void* P;
+  int64_t n_adapters;
+  int rank;
+  const int32_t* adapter_of;
+  const float* S;
+  const int* lists;  // see token_tile
+  void* O;
+  int64_t ldo;
+};
+
+// Rows of the token tiles of a projection over T tokens; the kernel that writes S also writes, for every tile, the
+// adapters its tokens use: lists[tile * (rows + 1)] their number, then their indices.
+int token_tile(int64_t T);
+inline int64_t list_bytes(int64_t T) {
+  const int64_t rows = token_tile(T);
+  return round_up(4 * ((T + rows - 1) / rows) * (rows + 1), 256);
+}
+
+windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t st);
+
+}  // namespace windq

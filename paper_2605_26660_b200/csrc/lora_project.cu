@@ -1,0 +1,472 @@
+// The product of the adapter calls: tokens times the shared weight, plus every token's low-rank term, in one kernel on
+// the tensor cores (tcgen05, accumulators in tensor memory, operands by TMA).
+//
+// A low-rank term is more reduction dimension: after the chunks of K the accumulator takes, for every adapter a that the
+// tile's tokens use, S (tokens x rank, zero in the rows of other tokens' adapters) times P[a].  So a tile whose tokens
+// share an adapter costs rank / K more than the bare product, any mix of adapters is right, and there is no second pass
+// over the output.  S is binary32; the tensor cores take 16 bits, so it enters as the sum of two 16-bit values (22 bits
+// for fp16, 16 for bf16), which keeps the rounding of the low-rank term below that of the result.
+//
+// Warps: one issues TMA copies, one issues matrix products, four write the S tiles and, after the tile, read the
+// accumulators and store.  Two layouts of a tile:
+//   wide  128 tokens x 256 outputs; persistent over tiles with two accumulators, so that storing a tile overlaps the next
+//   tall  (at most 256 tokens) 128 outputs x all tokens: the weight is read once and the tokens cost little -- the shape
+//         of decoding, bound by the bytes of W
+// Where the tiles do not fill the GPU, `splits` thread blocks (a cluster) share a tile along K and add their
+// accumulators through distributed shared memory, in rank order: equal calls give equal bits.
+#include <algorithm>
+
+#include "lora.cuh"
+#include "tcgen05.cuh"
+
+namespace windq {
+namespace {
+
+constexpr int kThreads = 192;
+constexpr int kMaxStages = 8;
+constexpr int kSmemLimit = 227 * 1024 - 2048;       // dynamic shared memory of one thread block per SM
+constexpr int kSmemLimitTwo = 112 * 1024;           // of two
+
+struct ProjectArgs {
+  int T, N, chunks, rank, n_adapters, dtype;
+  const int32_t* adapter_of;
+  const float* S;
+  const int* lists;
+  void* O;
+  int64_t ldo;
+  int token_rows, weight_rows, token_tiles, weight_tiles, group;
+  int splits, stages, accumulators, columns;  // columns: of tensor memory
+  unsigned long long* stalls;
+};
+
+struct Barriers {
+  uint64_t full[kMaxStages], empty[kMaxStages], granted[kMaxStages], written[kMaxStages], done[2], free[2];
+};
+
+// Tiles in an order that keeps a group of token tiles in L2 while the weight streams by.
+__device__ __forceinline__ void tile_at(const ProjectArgs& p, int tile, int& tt, int& wt) {
+  const int per = p.group * p.weight_tiles, g = tile / per, rest = tile - g * per;
+  const int rows = min(p.group, p.token_tiles - g * p.group);
+  wt = rest / rows;
+  tt = g * p.group + rest - wt * rows;
+}
+
+template <bool TALL, bool TRANS>
+__global__ void __launch_bounds__(kThreads, 1)
+    project_kernel(const __grid_constant__ CUtensorMap zmap, const __grid_constant__ CUtensorMap wmap,
+                   const __grid_constant__ CUtensorMap pmap, const __grid_constant__ ProjectArgs p) {
+  extern __shared__ uint8_t raw[];
+  __shared__ Barriers bars;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int dead;
+  const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t token_bytes = p.token_rows * 128, weight_bytes = p.weight_rows * 128, stage_bytes = token_bytes + weight_bytes;
+  auto full = [&](int s) { return smem_addr(&bars.full[s]); };
+  auto empty = [&](int s) { return smem_addr(&bars.empty[s]); };
+  auto granted = [&](int s) { return smem_addr(&bars.granted[s]); };
+  auto written = [&](int s) { return smem_addr(&bars.written[s]); };
+  auto done = [&](int b) { return smem_addr(&bars.done[b]); };
+  auto free_ = [&](int b) { return smem_addr(&bars.free[b]); };
+
+  if (threadIdx.x == 0) {
+    prefetch_map(&zmap);
+    prefetch_map(&wmap);
+    prefetch_map(&pmap);
+    for (int s = 0; s < p.stages; s++) {
+      mbar_init(full(s), 1);
+      mbar_init(empty(s), 1);
+      mbar_init(granted(s), 1);
+      mbar_init(written(s), 4);
+    }
+    for (int b = 0; b < 2; b++) {
+      mbar_init(done(b), 1);
+      mbar_init(free_(b), 4);
+    }
+    dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_shared();
+  }
+  if (warp == 1) tmem_alloc(smem_addr(&tmem_slot), p.columns);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+
+  const int split = blockIdx.x % p.splits, step = gridDim.x / p.splits, tiles = p.token_tiles * p.weight_tiles;
+  const int c0 = (int)((int64_t)p.chunks * split / p.splits), c1 = (int)((int64_t)p.chunks * (split + 1) / p.splits);
+  const int rank_chunks = (p.rank + 63) >> 6;
+  const bool paired = p.rank <= 32;  // both halves of S in one stage, at columns 0 and 32
+  const int parts = paired ? 1 : 2;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int it = 0;
+      bool waited = false, ok = true;
+      for (int tile = blockIdx.x / p.splits; ok && tile < tiles; tile += step) {
+        int tt, wt;
+        tile_at(p, tile, tt, wt);
+        for (int c = c0; ok && c < c1; c++, it++) {
+          const int s = it % p.stages;
+          if (!(ok = mbar_wait(empty(s), ((it / p.stages) & 1) ^ 1, &dead))) break;
+          const uint32_t at = base + s * stage_bytes;
+          mbar_expect(full(s), stage_bytes);
+          tma_load_2d(at, &zmap, c * 64, tt * p.token_rows, full(s));
+          if (TRANS) {
+            for (int b = 0; b < p.weight_rows / 64; b++)
+              tma_load_2d(at + token_bytes + b * 8192, &wmap, wt * p.weight_rows + b * 64, c * 64, full(s));
+          } else {
+            tma_load_2d(at + token_bytes, &wmap, c * 64, wt * p.weight_rows, full(s));
+          }
+        }
+        if (!ok) break;
+        if (!waited) {
+          wait_for_predecessor();
+          waited = true;
+        }
+        const int* list = p.lists + (int64_t)tt * (p.token_rows + 1);
+        const int n_list = __ldcg(list);
+        for (int i = split; ok && i < n_list; i += p.splits) {
+          const int a = __ldcg(list + 1 + i);
+          for (int e = 0; ok && e < rank_chunks * parts; e++, it++) {
+            const int rc = e / parts, s = it % p.stages;
+            if (!(ok = mbar_wait(empty(s), ((it / p.stages) & 1) ^ 1, &dead))) break;
+            const uint32_t at = base + s * stage_bytes + token_bytes;
+            mbar_arrive(granted(s));  // the stage's token tile is the writers' now
+            mbar_expect(full(s), weight_bytes);
+            if (TRANS) {
+              for (int b = 0; b < p.weight_rows / 64; b++)
+                tma_load_3d(at + b * 8192, &pmap, wt * p.weight_rows + b * 64, rc * 64, a, full(s));
+            } else {
+              tma_load_3d(at, &pmap, rc * 64, wt * p.weight_rows, a, full(s));
+            }
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const int columns = TALL ? p.token_rows : p.weight_rows;
+      const uint32_t idesc = TALL ? instr_desc(p.dtype, TRANS, false, 128, columns) : instr_desc(p.dtype, false, TRANS, 128, columns);
+      // 16 values of K further: 32 bytes in a K-major tile, two groups of 8 rows in an MN-major one
+      const uint32_t weight_step = TRANS ? 2048 >> 4 : 32 >> 4, token_step = 32 >> 4;
+      int it = 0, turn = 0;
+      uint32_t written_phase = 0;
+      bool waited = false, ok = true;
+      for (int tile = blockIdx.x / p.splits; ok && tile < tiles; tile += step, turn++) {
+        int tt, wt;
+        tile_at(p, tile, tt, wt);
+        const int b = p.accumulators == 2 ? turn & 1 : 0, use = p.accumulators == 2 ? turn >> 1 : turn;
+        if (!(ok = mbar_wait(free_(b), (use & 1) ^ 1, &dead))) break;
+        tc_fence_after();
+        const uint32_t d = tmem + b * 256;
+        bool some = false;
+        auto product = [&](uint32_t at, int k_token, int k_weight) {
+          const uint64_t z = smem_desc(at, 16) + (uint64_t)(k_token * token_step);
+          const uint64_t w = smem_desc(at + token_bytes, TRANS ? 8192 : 16) + (uint64_t)(k_weight * weight_step);
+          mma_f16(d, TALL ? w : z, TALL ? z : w, idesc, some);
+          some = true;
+        };
+        for (int c = c0; c < c1; c++, it++) {
+          const int s = it % p.stages;
+          if (!(ok = mbar_wait(full(s), (it / p.stages) & 1, &dead))) break;
+          tc_fence_after();
+#pragma unroll
+          for (int k = 0; k < 4; k++) product(base + s * stage_bytes, k, k);
+          mma_commit(empty(s));
+        }
+        if (!ok) break;
+        if (!waited) {
+          wait_for_predecessor();
+          waited = true;
+        }
+        const int n_list = __ldcg(p.lists + (int64_t)tt * (p.token_rows + 1));
+        for (int i = split; ok && i < n_list; i += p.splits) {
+          for (int e = 0; e < rank_chunks * parts; e++, it++) {
+            const int rc = e / parts, s = it % p.stages;
+            if (!(ok = mbar_wait(full(s), (it / p.stages) & 1, &dead) && mbar_wait(written(s), (written_phase >> s) & 1, &dead))) break;
+            written_phase ^= 1u << s;
+            tc_fence_after();
+            const int steps = (min(64, p.rank - rc * 64) + 15) >> 4;
+            for (int k = 0; k < steps; k++) product(base + s * stage_bytes, k, k);
+            if (paired)
+              for (int k = 0; k < steps; k++) product(base + s * stage_bytes, k + 2, k);
+            mma_commit(empty(s));
+          }
+        }
+        if (!ok) break;
+        mma_commit(done(b));
+      }
+    }
+  } else {
+    const int e = threadIdx.x - 64, quarter = warp & 3;
+    // The writers take part in few of a stage's rounds, so they cannot follow its `empty` barrier by parity; the copying
+    // warp, which follows every round, grants them the stage.
+    int it = 0, turn = 0;
+    uint32_t granted_phase = 0;
+    bool waited = false, ok = true;
+    for (int tile = blockIdx.x / p.splits; tile < tiles; tile += step, turn++) {
+      int tt, wt;
+      tile_at(p, tile, tt, wt);
+      it += c1 - c0;
+      if (!waited) {
+        wait_for_predecessor();
+        waited = true;
+      }
+      // S: a thread writes rows e and e + 128 of the token tile
+      int mine[2];
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        const int row = e + h * 128, t = tt * p.token_rows + row;
+        mine[h] = row < p.token_rows && t < p.T ? p.adapter_of[t] : -1;
+        if (mine[h] >= 0 && mine[h] < p.n_adapters)
+          for (int j = 0; j < p.rank; j += 32) asm volatile("prefetch.global.L1 [%0];" ::"l"(p.S + (int64_t)t * p.rank + j));
+      }
+      const int* list = p.lists + (int64_t)tt * (p.token_rows + 1);
+      const int n_list = __ldcg(list);
+      for (int i = split; ok && i < n_list; i += p.splits) {
+        const int a = __ldcg(list + 1 + i);
+        for (int x = 0; x < rank_chunks * parts; x++, it++) {
+          const int rc = x / parts, s = it % p.stages;
+          ok = mbar_wait(granted(s), (granted_phase >> s) & 1, &dead);
+          granted_phase ^= 1u << s;
+          if (!__all_sync(0xffffffffu, ok)) {
+            ok = false;
+            break;
+          }
+          const int wide = ((min(64, p.rank - rc * 64) + 15) & ~15) >> 3;  // 16-byte pieces of a row, whole steps of K
+#pragma unroll
+          for (int h = 0; h < 2; h++) {
+            const int row = e + h * 128;
+            if (row >= p.token_rows) continue;
+            const float* src = p.S + (int64_t)(tt * p.token_rows + row) * p.rank + rc * 64;
+            const uint32_t dst = base + s * stage_bytes + row * 128;
+            for (int g = 0; g < wide; g++) {
+              uint4 hi = make_uint4(0, 0, 0, 0), lo = hi;
+              if (mine[h] == a && rc * 64 + g * 8 < p.rank) {
+                const float4 u = *reinterpret_cast<const float4*>(src + g * 8), v = *reinterpret_cast<const float4*>(src + g * 8 + 4);
+                float y[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+                if (p.dtype == WINDQ_F16) {
+#pragma unroll
+                  for (int k = 0; k < 8; k++) y[k] = fminf(fmaxf(y[k], -131008.0f), 131008.0f);
+                }
+                uint32_t w[4], r[4];
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                  float2 first = make_float2(y[2 * k], y[2 * k + 1]);
+                  if (p.dtype == WINDQ_F16) {
+                    first.x = fminf(fmaxf(first.x, -65504.0f), 65504.0f);
+                    first.y = fminf(fmaxf(first.y, -65504.0f), 65504.0f);
+                  }
+                  w[k] = pack2(first.x, first.y, p.dtype);
+                  const float2 back = unpack2(w[k], p.dtype);
+                  r[k] = pack2(y[2 * k] - back.x, y[2 * k + 1] - back.y, p.dtype);
+                }
+                hi = make_uint4(w[0], w[1], w[2], w[3]);
+                lo = make_uint4(r[0], r[1], r[2], r[3]);
+              }
+              auto put = [&](int piece, const uint4& q) {
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + ((piece ^ (row & 7)) << 4)), "r"(q.x), "r"(q.y),
+                             "r"(q.z), "r"(q.w)
+                             : "memory");
+              };
+              put(g, paired || (x & 1) == 0 ? hi : lo);
+              if (paired) put(g + 4, lo);
+            }
+          }
+          fence_async_shared();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(written(s));
+        }
+      }
+      // the accumulators of the tile
+      const int b = p.accumulators == 2 ? turn & 1 : 0, use = p.accumulators == 2 ? turn >> 1 : turn;
+      ok = ok && mbar_wait(done(b), use & 1, &dead);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      tc_fence_after();
+      const uint32_t d = tmem + b * 256 + ((uint32_t)(quarter * 32) << 16);
+      const int columns = TALL ? p.token_rows : p.weight_rows, at = quarter * 32 + lane;
+      for (int c = 0; c < columns; c += 16) {
+        uint32_t r[16];
+        tmem_load16(d + c, r);
+        tmem_load_wait();
+        if (p.splits > 1) {
+          // [column][lane], 129 apart: free of bank conflicts along either
+#pragma unroll
+          for (int k = 0; k < 16; k++)
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + ((c + k) * 129 + at) * 4), "r"(r[k]) : "memory");
+        } else if (TALL) {
+          const int n = wt * 128 + at;
+          if (n < p.N) {
+#pragma unroll
+            for (int k = 0; k < 16; k++) {
+              const int t = tt * p.token_rows + c + k;
+              if (t < p.T) store1(p.O, t * p.ldo + n, p.dtype, __uint_as_float(r[k]));
+            }
+          }
+        } else {
+          const int t = tt * 128 + at, n = wt * p.weight_rows + c;
+          if (t < p.T) {
+#pragma unroll
+            for (int k = 0; k < 16; k += 8) {
+              float x[8];
+#pragma unroll
+              for (int j = 0; j < 8; j++) x[j] = __uint_as_float(r[k + j]);
+              if (n + k + 8 <= p.N) store8(p.O, t * p.ldo + n + k, p.dtype, x);
+              else if (n + k < p.N) store_some(p.O, t * p.ldo + n + k, p.dtype, p.N - n - k, x);
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(free_(b));
+    }
+  }
+  __syncwarp();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_free(tmem, p.columns);
+  }
+  if (dead && threadIdx.x == 0) {
+    // copies this thread block has issued may still be landing in its shared memory
+    const long long begin = clock64();
+    while (clock64() - begin < 4000000) {
+    }
+    atomicAdd(p.stalls, 1ull);
+  }
+  if (p.splits > 1) {
+    __syncwarp();
+    cluster_sync();
+    // one tile a cluster: this block adds and stores its share of it
+    int tt, wt;
+    tile_at(p, blockIdx.x / p.splits, tt, wt);
+    if (TALL) {
+      const int columns = min(p.token_rows, p.T - tt * p.token_rows);
+      for (int i = threadIdx.x; i < (columns - split + p.splits - 1) / p.splits * 128; i += kThreads) {
+        const int c = split + (i >> 7) * p.splits, at = i & 127, n = wt * 128 + at;
+        float x = 0.0f;
+        for (int q = 0; q < p.splits; q++) x += cluster_load(base + (c * 129 + at) * 4, q);
+        if (n < p.N) store1(p.O, (int64_t)(tt * p.token_rows + c) * p.ldo + n, p.dtype, x);
+      }
+    } else {
+      const int share = 128 / p.splits;
+      for (int i = threadIdx.x; i < share * p.weight_rows; i += kThreads) {
+        const int c = i % p.weight_rows, at = split * share + i / p.weight_rows, n = wt * p.weight_rows + c, t = tt * 128 + at;
+        float x = 0.0f;
+        for (int q = 0; q < p.splits; q++) x += cluster_load(base + (c * 129 + at) * 4, q);
+        if (t < p.T && n < p.N) store1(p.O, t * p.ldo + n, p.dtype, x);
+      }
+    }
+    cluster_sync();  // no block leaves while another reads its shared memory
+  }
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+  static const EncodeTiled fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      p = nullptr;
+    }
+    return (EncodeTiled)p;
+  }();
+  return fn;
+}
+
+// A row-major array of 16-bit values [planes][rows][inner], copied in boxes of box_rows x 64 with the 128-byte swizzle;
+// what lies outside the array reads as zero.
+bool make_map(CUtensorMap* map, int dtype, const void* base, int64_t inner, int64_t rows, int64_t planes, int64_t row_stride,
+              int64_t plane_stride, int box_rows) {
+  const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)planes};
+  const cuuint64_t strides[2] = {(cuuint64_t)(2 * row_stride), (cuuint64_t)(2 * plane_stride)};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, ones[3] = {1, 1, 1};
+  return encode_tiled()(map, dtype == WINDQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                        planes > 0 ? 3 : 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool TALL, bool TRANS>
+windq_status launch(windq_ctx* ctx, const CUtensorMap& z, const CUtensorMap& w, const CUtensorMap& pm, const ProjectArgs& p,
+                    int blocks, int smem, cudaStream_t st) {
+  const windq_status ready = prepare_kernel(ctx, kProject + 2 * TALL + TRANS, project_kernel<TALL, TRANS>, kThreads, kSmemLimit, false);
+  if (ready != WINDQ_OK) return ready;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attrs[2];
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = p.splits;
+  attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+  cfg.attrs = attrs;
+  cfg.numAttrs = p.splits > 1 ? 2 : 1;
+  WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, project_kernel<TALL, TRANS>, z, w, pm, p));
+  return WINDQ_OK;
+}
+
+}  // namespace
+
+int token_tile(int64_t T) { return T <= 256 ? (int)round_up(std::max<int64_t>(T, 1), 16) : 128; }
+
+windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t st) {
+  const bool tall = q.T <= 256;
+  ProjectArgs p = {};
+  p.T = (int)q.T;
+  p.N = (int)q.N;
+  p.chunks = (int)((q.K + 63) / 64);
+  p.rank = q.rank;
+  p.n_adapters = (int)q.n_adapters;
+  p.dtype = q.dtype;
+  p.adapter_of = q.adapter_of;
+  p.S = q.S;
+  p.lists = q.lists;
+  p.O = q.O;
+  p.ldo = q.ldo;
+  p.stalls = stall_counter(ctx);
+  p.token_rows = token_tile(q.T);
+  p.weight_rows = tall ? 128 : 256;
+  p.token_tiles = (int)((q.T + p.token_rows - 1) / p.token_rows);
+  p.weight_tiles = (int)((q.N + p.weight_rows - 1) / p.weight_rows);
+  p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.token_tiles, (48ll << 20) / (2 * q.K * p.token_rows)));
+  const int stage = (p.token_rows + p.weight_rows) * 128;
+  const bool two = tall && p.token_rows <= 64;  // thread blocks an SM
+  const int limit = two ? kSmemLimitTwo : kSmemLimit;
+  p.stages = std::min(kMaxStages, (limit - 1024) / stage);
+  const int64_t tiles = (int64_t)p.token_tiles * p.weight_tiles, slots = (int64_t)ctx->sm_count * (two ? 2 : 1);
+  p.splits = 1;
+  while (p.splits < 8 && tiles * p.splits * 2 <= slots && p.chunks >= p.splits * 2 * 4) p.splits *= 2;
+  p.accumulators = !tall && p.splits == 1 ? 2 : 1;
+  p.columns = tall ? (p.token_rows <= 32 ? 32 : p.token_rows <= 64 ? 64 : p.token_rows <= 128 ? 128 : 256) : 256 * p.accumulators;
+  const int64_t blocks = p.splits > 1 ? tiles * p.splits : std::min(tiles, slots);
+  const int smem = 1024 + p.stages * stage;
+
+  CUtensorMap z, w, pm;
+  WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+  bool ok = make_map(&z, q.dtype, q.Z, q.K, q.T, 0, q.ldz, 0, p.token_rows);
+  if (q.transposed) {
+    ok = ok && make_map(&w, q.dtype, q.W, q.N, q.K, 0, q.ldw, 0, 64);
+    ok = ok && make_map(&pm, q.dtype, q.P, q.N, q.rank, q.n_adapters, q.N, q.N * q.rank, 64);
+  } else {
+    ok = ok && make_map(&w, q.dtype, q.W, q.K, q.N, 0, q.ldw, 0, p.weight_rows);
+    ok = ok && make_map(&pm, q.dtype, q.P, q.rank, q.N, q.n_adapters, q.rank, q.N * q.rank, p.weight_rows);
+  }
+  WINDQ_REQUIRE(ctx, ok, WINDQ_ERR_CUDA, "a tensor map could not be made");
+  if (tall) return q.transposed ? launch<true, true>(ctx, z, w, pm, p, (int)blocks, smem, st)
+                                : launch<true, false>(ctx, z, w, pm, p, (int)blocks, smem, st);
+  return q.transposed ? launch<false, true>(ctx, z, w, pm, p, (int)blocks, smem, st)
+                      : launch<false, false>(ctx, z, w, pm, p, (int)blocks, smem, st);
+}
+
+}  // namespace windq

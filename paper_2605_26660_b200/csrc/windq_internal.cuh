@@ -14,7 +14,7 @@ struct windq_ctx {
   int sm_count;
   void* scratch;
   int64_t scratch_bytes;
-  unsigned int* sync;  // kSyncCounters arrival counters, zero between launches; two 64-bit work counters follow them
+  unsigned int* sync;  // kSyncCounters arrival counters, zero between launches; two 64-bit work counters and one of stalls follow them
   unsigned long long prepared[2];  // kernels whose attributes have been set on this context's device (bit per KernelId)
   int occupancy[128];              // resident blocks per SM of those kernels (0 where not asked)
   char err[256];
@@ -23,13 +23,15 @@ struct windq_ctx {
 namespace windq {
 
 constexpr int64_t kSyncCounters = 16384;
-constexpr int64_t kSyncBytes = kSyncCounters * (int64_t)sizeof(unsigned int) + 2 * (int64_t)sizeof(unsigned long long);
+constexpr int64_t kSyncBytes = kSyncCounters * (int64_t)sizeof(unsigned int) + 3 * (int64_t)sizeof(unsigned long long);
 
 windq_status fail(windq_ctx* ctx, windq_status st, const char* fmt, ...);
 // Where the fits count their clip candidates: [0] those evaluated in full, [1] all of them (see windq_fit_work).
 inline unsigned long long* fit_work_counters(windq_ctx* ctx) {
   return reinterpret_cast<unsigned long long*>(ctx->sync + kSyncCounters);
 }
+// Thread blocks whose bounded waits gave up (see windq_stalls).
+inline unsigned long long* stall_counter(windq_ctx* ctx) { return fit_work_counters(ctx) + 2; }
 // Makes the context's scratch at least `bytes` large (may cudaMalloc).
 windq_status ensure_scratch(windq_ctx* ctx, int64_t bytes);
 
@@ -64,7 +66,7 @@ struct DeviceGuard {
 // attributes belong to a device, so the record is kept in the context, not in a process-wide static.
 enum KernelId { kFitG32 = 0, kApplyG32 = 5, kApplySearchG32 = 10, kHistG32 = 15, kFinalize = 20, kFitProtectG32 = 21, kApplyProtectG32 = 26, kApplyProtectSearchG32 = 31,
                 kFitBatchG32 = 41 /* 41..45 whole items, 46..50 in parts */, kApplyBatchG32 = 51 /* 51..55 */, kFitPartsOffset = 36 /* kFitG32 + 36 .. and kFitProtectG32 + 36 ..: the in-parts instantiations (36..40, 57..61) */,
-                kApplyStreamG32 = 64 /* 64..68 */, kFitFeatG32 = 79 /* 79..83 whole items, 84..88 in parts */, kTernarySearchG32 = 69 /* 69..73 plain, 74..78 protected */, kFinalize2 = 89, kKernelIds = 128 };
+                kApplyStreamG32 = 64 /* 64..68 */, kFitFeatG32 = 79 /* 79..83 whole items, 84..88 in parts */, kTernarySearchG32 = 69 /* 69..73 plain, 74..78 protected */, kFinalize2 = 89, kProject = 90 /* 90..93 */, kKernelIds = 128 };
 inline int g_index(int G) { return G == 32 ? 0 : G == 64 ? 1 : G == 128 ? 2 : G == 256 ? 3 : 4; }
 
 // Sets the dynamic shared-memory limit of `kernel` once per context and, if asked, records how many

@@ -108,7 +108,7 @@ SHAPES = [  # T, R, C, rank, adapters, kind
     (65, 384, 96, 128, 3, "mixed"), (100, 256, 256, 32, 100, "distinct"), (128, 264, 392, 16, 9, "mixed"), (129, 136, 512, 40, 3, "none"),
     (200, 264, 72, 72, 6, "mixed"), (255, 513, 128, 8, 2, "segments"), (256, 248, 456, 16, 64, "distinct"), (257, 96, 640, 24, 3, "mixed"),
     (300, 520, 648, 64, 40, "mixed"), (511, 40, 88, 16, 2, "segments"), (640, 777, 320, 120, 5, "segments"), (1025, 512, 1032, 16, 4, "invalid"),
-    (2100, 264, 520, 32, 3, "segments"), (3000, 1288, 136, 8, 1, "one"),
+    (2100, 264, 520, 32, 3, "segments"), (48, 640, 4160, 16, 24, "mixed"), (203, 1200, 8192, 32, 48, "mixed"), (330, 520, 6000, 16, 30, "mixed"), (3000, 1288, 136, 8, 1, "one"),
 ]
 
 
@@ -293,3 +293,7 @@ def test_refusals(wq, ctx):
     assert e.value.status == 1
     torch.cuda.synchronize()
     assert bool((out == 7).all())
+
+
+def test_no_wait_gave_up(wq, ctx):
+    assert wq.windq_stalls(ctx) == 0
