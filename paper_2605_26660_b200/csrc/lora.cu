@@ -1,67 +1,8 @@
-// The shared projection with one low-rank adapter per token, and its gradients.
+// The shared projection with one low-rank adapter per token, and its gradients: checks and the order of the kernels.
 #include "lora.cuh"
-#include "tcgen05.cuh"
 
 namespace windq {
 namespace {
-
-__device__ __forceinline__ float value(const void* base, int64_t i, int dt) { return load1(base, i, dt); }
-
-// S[t][j] = scaling[a] * sum_k Z[t][k] * P[a](k, j), P[a](k, j) = P[a * pa + k * pk + j * pj]; zeros without an adapter.
-// The blocks past the tokens write the lists of adapters of the token tiles.
-__global__ void low_rank_kernel(const void* Z, int64_t ldz, int64_t T, int64_t K, const void* P, int64_t pa, int64_t pk, int64_t pj,
-                                int dt, int64_t n_adapters, int rank, const float* scaling, const int32_t* adapter_of, float* S,
-                                int* lists, int rows) {
-  launch_dependents();
-  const int64_t t = blockIdx.x;
-  if (t >= T) {
-    // adapters in the order of their first token; a thread per token (blockDim.x >= rows)
-    __shared__ int ids[256], taken[8];
-    const int tile = (int)(t - T), i = threadIdx.x;
-    const int64_t at = (int64_t)tile * rows + i;
-    int id = i < rows && at < T ? adapter_of[at] : -1;
-    if (id >= n_adapters) id = -1;
-    ids[i] = id;
-    __syncthreads();
-    bool first = id >= 0;
-    for (int k = 0; k < i && first; k++) first = ids[k] != id;
-    const unsigned vote = __ballot_sync(0xffffffffu, first);
-    if ((i & 31) == 0) taken[i >> 5] = __popc(vote);
-    __syncthreads();
-    int before = __popc(vote & ((1u << (i & 31)) - 1)), all = 0;
-    for (int w = 0; w < 8; w++) {
-      if (w < i >> 5) before += taken[w];
-      all += taken[w];
-    }
-    int* list = lists + (int64_t)tile * (rows + 1);
-    if (first) list[1 + before] = id;
-    if (i == 0) list[0] = all;
-    return;
-  }
-  const int a = adapter_of[t];
-  for (int j = threadIdx.x >> 5; j < rank; j += blockDim.x >> 5) {
-    float acc = 0.0f;
-    if (a >= 0 && a < n_adapters) {
-      for (int64_t k = threadIdx.x & 31; k < K; k += 32)
-        acc = fmaf(value(Z, t * ldz + k, dt), value(P, a * pa + k * pk + j * pj, dt), acc);
-      for (int d = 16; d; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
-      acc *= scaling[a];
-    }
-    if ((threadIdx.x & 31) == 0) S[t * rank + j] = acc;
-  }
-}
-
-// D[a][..] = sum over the tokens of a of S[t][j] * Z[t][c]; j contiguous (dB) or c contiguous (dA).
-__global__ void gradient_kernel(const void* Z, int64_t ldz, int64_t T, int64_t K, const float* S, int rank, int dt,
-                                const int32_t* adapter_of, float* D, int64_t dj, int64_t dc) {
-  const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
-  const int j = blockIdx.y * 8 + threadIdx.y, a = blockIdx.z;
-  if (c >= K) return;
-  float acc = 0.0f;
-  for (int64_t t = 0; t < T; t++)
-    if (adapter_of[t] == a) acc = fmaf(S[t * rank + j], value(Z, t * ldz + c, dt), acc);
-  D[a * (int64_t)rank * K + j * dj + c * dc] = acc;
-}
 
 struct LoraArgs {
   const char* who;
@@ -129,16 +70,15 @@ windq_status windq_lora_forward(windq_ctx* ctx, int dtype, const void* X, int64_
   cudaStream_t st = (cudaStream_t)stream;
   float* U = (float*)ctx->scratch;
   int* lists = (int*)((char*)ctx->scratch + round_up(4 * T * rank, 256));
-  const int rows = token_tile(T), tiles = (int)((T + rows - 1) / rows);
-  low_rank_kernel<<<(unsigned)(T + tiles), 256, 0, st>>>(X, ldx, T, C, A, rank * C, 1, C, dtype, n_adapters, rank, scaling, adapter_of,
-                                                         U, lists, rows);
-  WINDQ_CUDA(ctx, cudaGetLastError());
+  const windq_status low = launch_low_rank(
+      ctx, LowRank{dtype, false, X, T, C, ldx, A, n_adapters, rank, scaling, adapter_of, U, nullptr, lists}, st);
+  if (low != WINDQ_OK) return low;
   return launch_projection(ctx, Projection{dtype, false, X, T, C, R, ldx, W, ldw, B, n_adapters, rank, adapter_of, U, lists, Y, ldy}, st);
 }
 
 int64_t windq_scratch_bytes_lora_backward(int64_t T, int64_t R, int64_t C, int64_t n_adapters, int rank) {
   if (T < 0 || R <= 0 || C <= 0 || rank <= 0 || n_adapters <= 0) return 0;
-  return 2 * windq::round_up(4 * T * rank, 256) + windq::list_bytes(T);
+  return 2 * (windq::round_up(4 * T * rank, 256) + windq::round_up(4 * T, 256)) + windq::list_bytes(T);
 }
 
 windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx, const void* W,
@@ -166,30 +106,30 @@ windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64
   }
   const windq_status room = ensure_scratch(ctx, windq_scratch_bytes_lora_backward(T, R, C, n_adapters, rank));
   if (room != WINDQ_OK) return room;
-  float* U = (float*)ctx->scratch;
-  float* V = (float*)((char*)ctx->scratch + round_up(4 * T * rank, 256));
-  int* lists = (int*)((char*)V + round_up(4 * T * rank, 256));
-  const int rows = token_tile(T), tiles = (int)((T + rows - 1) / rows);
+  char* at = (char*)ctx->scratch;
+  auto take = [&](int64_t bytes) {
+    char* p = at;
+    at += round_up(bytes, 256);
+    return p;
+  };
+  float* U = (float*)take(4 * T * rank);
+  float* V = (float*)take(4 * T * rank);
+  float* top_u = (float*)take(4 * T);
+  float* top_v = (float*)take(4 * T);
+  int* lists = (int*)at;
+  windq_status done = WINDQ_OK;
   if (dB)
-    low_rank_kernel<<<(unsigned)T, 256, 0, st>>>(X, ldx, T, C, A, rank * C, 1, C, dtype, n_adapters, rank, scaling, adapter_of, U,
-                                                 nullptr, rows);
-  if (dX || dA)
-    low_rank_kernel<<<(unsigned)(T + tiles), 256, 0, st>>>(dY, lddy, T, R, B, R * rank, rank, 1, dtype, n_adapters, rank, scaling,
-                                                           adapter_of, V, lists, rows);
-  WINDQ_CUDA(ctx, cudaGetLastError());
-  if (dX) {
-    const windq_status done = launch_projection(
+    done = launch_low_rank(ctx, LowRank{dtype, false, X, T, C, ldx, A, n_adapters, rank, scaling, adapter_of, U, top_u, nullptr}, st);
+  if (done == WINDQ_OK && (dX || dA))
+    done = launch_low_rank(ctx, LowRank{dtype, true, dY, T, R, lddy, B, n_adapters, rank, scaling, adapter_of, V, top_v, lists}, st);
+  if (done == WINDQ_OK && dX)
+    done = launch_projection(
         ctx, Projection{dtype, true, dY, T, R, C, lddy, W, ldw, A, n_adapters, rank, adapter_of, V, lists, dX, lddx}, st);
-    if (done != WINDQ_OK) return done;
+  if (done == WINDQ_OK && (dA || dB)) {
+    const Gradient ga{X, C, ldx, V, top_v, dA}, gb{dY, R, lddy, U, top_u, dB};
+    done = launch_gradients(ctx, dA ? &ga : nullptr, dB ? &gb : nullptr, dtype, T, rank, n_adapters, adapter_of, st);
   }
-  if (dA)
-    gradient_kernel<<<dim3((unsigned)((C + 31) / 32), rank / 8, (unsigned)n_adapters), dim3(32, 8), 0, st>>>(
-        X, ldx, T, C, V, rank, dtype, adapter_of, dA, C, 1);
-  if (dB)
-    gradient_kernel<<<dim3((unsigned)((R + 31) / 32), rank / 8, (unsigned)n_adapters), dim3(32, 8), 0, st>>>(
-        dY, lddy, T, R, U, rank, dtype, adapter_of, dB, 1, rank);
-  WINDQ_CUDA(ctx, cudaGetLastError());
-  return WINDQ_OK;
+  return done;
 }
 
 }  // extern "C"

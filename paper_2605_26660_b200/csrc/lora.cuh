@@ -33,6 +33,35 @@ inline int64_t list_bytes(int64_t T) {
   return round_up(4 * ((T + rows - 1) / rows) * (rows + 1), 256);
 }
 
+// S[t][j] = scaling[a] * sum_k Z[t][k] P[a](j, k): forward P[a](j, k) = A[a][j][k], backward (transposed) B[a][k][j].
+// Rows of tokens without an adapter are not written.
+struct LowRank {
+  int dtype;
+  bool transposed;
+  const void* Z;
+  int64_t T, K, ldz;
+  const void* P;
+  int64_t n_adapters;
+  int rank;
+  const float* scaling;
+  const int32_t* adapter_of;
+  float* S;
+  float* top;  // fp32 [T], the largest |S[t][j]| of every token; nullable
+  int* lists;  // nullable
+};
+windq_status launch_low_rank(windq_ctx* ctx, const LowRank& q, cudaStream_t st);
+
+// D[a] = sum over the tokens of a of S[t] (x) Z[t]; dA is [a][j][c], dB is [a][c][j].  Either may be NULL.
+struct Gradient {
+  const void* Z;
+  int64_t cols, ldz;
+  const float* S;
+  const float* top;
+  float* D;
+};
+windq_status launch_gradients(windq_ctx* ctx, const Gradient* dA, const Gradient* dB, int dtype, int64_t T, int rank,
+                              int64_t n_adapters, const int32_t* adapter_of, cudaStream_t st);
+
 windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t st);
 
 }  // namespace windq
