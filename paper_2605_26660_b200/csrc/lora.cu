@@ -71,7 +71,7 @@ windq_status windq_lora_forward(windq_ctx* ctx, int dtype, const void* X, int64_
   float* U = (float*)ctx->scratch;
   int* lists = (int*)((char*)ctx->scratch + round_up(4 * T * rank, 256));
   const windq_status low = launch_low_rank(
-      ctx, LowRank{dtype, false, X, T, C, ldx, A, n_adapters, rank, scaling, adapter_of, U, nullptr, lists}, st);
+      ctx, LowRank{dtype, T, n_adapters, rank, scaling, adapter_of, lists, 1, {{false, X, C, ldx, A, U, nullptr}}}, st);
   if (low != WINDQ_OK) return low;
   return launch_projection(ctx, Projection{dtype, false, X, T, C, R, ldx, W, ldw, B, n_adapters, rank, adapter_of, U, lists, Y, ldy}, st);
 }
@@ -117,18 +117,18 @@ windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64
   float* top_u = (float*)take(4 * T);
   float* top_v = (float*)take(4 * T);
   int* lists = (int*)at;
-  windq_status done = WINDQ_OK;
-  if (dB)
-    done = launch_low_rank(ctx, LowRank{dtype, false, X, T, C, ldx, A, n_adapters, rank, scaling, adapter_of, U, top_u, nullptr}, st);
-  if (done == WINDQ_OK && (dX || dA))
-    done = launch_low_rank(ctx, LowRank{dtype, true, dY, T, R, lddy, B, n_adapters, rank, scaling, adapter_of, V, top_v, lists}, st);
-  if (done == WINDQ_OK && dX)
-    done = launch_projection(
-        ctx, Projection{dtype, true, dY, T, R, C, lddy, W, ldw, A, n_adapters, rank, adapter_of, V, lists, dX, lddx}, st);
+  LowRank low = {dtype, T, n_adapters, rank, scaling, adapter_of, dX ? lists : nullptr, 0, {}};
+  if (dB) low.job[low.jobs++] = LowRankJob{false, X, C, ldx, A, U, top_u};
+  if (dX || dA) low.job[low.jobs++] = LowRankJob{true, dY, R, lddy, B, V, top_v};
+  windq_status done = launch_low_rank(ctx, low, st);
+  // the gradients before dX: the projection's first tiles then start while the last of them finish
   if (done == WINDQ_OK && (dA || dB)) {
     const Gradient ga{X, C, ldx, V, top_v, dA}, gb{dY, R, lddy, U, top_u, dB};
     done = launch_gradients(ctx, dA ? &ga : nullptr, dB ? &gb : nullptr, dtype, T, rank, n_adapters, adapter_of, st);
   }
+  if (done == WINDQ_OK && dX)
+    done = launch_projection(
+        ctx, Projection{dtype, true, dY, T, R, C, lddy, W, ldw, A, n_adapters, rank, adapter_of, V, lists, dX, lddx}, st);
   return done;
 }
 

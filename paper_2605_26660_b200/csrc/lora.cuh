@@ -34,20 +34,24 @@ inline int64_t list_bytes(int64_t T) {
 }
 
 // S[t][j] = scaling[a] * sum_k Z[t][k] P[a](j, k): forward P[a](j, k) = A[a][j][k], backward (transposed) B[a][k][j].
-// Rows of tokens without an adapter are not written.
-struct LowRank {
-  int dtype;
+// One or two of them for the same tokens.  Rows of tokens without an adapter are not written.
+struct LowRankJob {
   bool transposed;
   const void* Z;
-  int64_t T, K, ldz;
+  int64_t K, ldz;
   const void* P;
-  int64_t n_adapters;
+  float* S;
+  float* top;  // fp32 [T], the largest |S[t][j]| of every token; nullable
+};
+struct LowRank {
+  int dtype;
+  int64_t T, n_adapters;
   int rank;
   const float* scaling;
   const int32_t* adapter_of;
-  float* S;
-  float* top;  // fp32 [T], the largest |S[t][j]| of every token; nullable
   int* lists;  // nullable
+  int jobs;
+  LowRankJob job[2];
 };
 windq_status launch_low_rank(windq_ctx* ctx, const LowRank& q, cudaStream_t st);
 

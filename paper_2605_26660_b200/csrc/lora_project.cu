@@ -9,7 +9,9 @@
 //
 // Warps: one issues TMA copies, one issues matrix products, four write the S tiles and, after the tile, read the
 // accumulators and store.  Two layouts of a tile:
-//   wide  128 tokens x 256 outputs; persistent over tiles with two accumulators, so that storing a tile overlaps the next
+//   wide  256 tokens x up to 256 outputs on a pair of thread blocks (cta_group::2: each holds half of either operand, so
+//         that a block's shared memory feeds a product twice as large); persistent over tiles with two accumulators, so
+//         that storing a tile overlaps the next
 //   tall  (at most 256 tokens) 128 outputs x all tokens: the weight is read once and the tokens cost little -- the shape
 //         of decoding, bound by the bytes of W
 // Where the tiles do not fill the GPU, `splits` thread blocks (a cluster) share a tile along K and add their
@@ -43,6 +45,25 @@ struct Barriers {
   uint64_t full[kMaxStages], empty[kMaxStages], granted[kMaxStages], written[kMaxStages], done[2], free[2];
 };
 
+// A place in the ring of stages.  The roles step through it thousands of times in one thread each, where a division by the
+// number of stages would be most of the time (measured: 0.52 us a chunk of K with it).
+struct Ring {
+  int s = 0, n;
+  uint32_t phase = 0;
+  __device__ explicit Ring(int stages) : n(stages) {}
+  __device__ __forceinline__ void next() {
+    if (++s == n) {
+      s = 0;
+      phase ^= 1;
+    }
+  }
+  __device__ __forceinline__ void skip(int k) {
+    k += s;
+    phase ^= (k / n) & 1;
+    s = k % n;
+  }
+};
+
 // Tiles in an order that keeps a group of token tiles in L2 while the weight streams by.
 __device__ __forceinline__ void tile_at(const ProjectArgs& p, int tile, int& tt, int& wt) {
   const int per = p.group * p.weight_tiles, g = tile / per, rest = tile - g * per;
@@ -60,8 +81,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ uint32_t tmem_slot;
   __shared__ int dead;
   const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
+  constexpr bool PAIR = !TALL;
+  constexpr int kBlocks = PAIR ? 2 : 1;  // thread blocks that share a tile's products
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t token_bytes = p.token_rows * 128, weight_bytes = p.weight_rows * 128, stage_bytes = token_bytes + weight_bytes;
+  const uint32_t rank = PAIR || p.splits > 1 ? cluster_rank() : 0, me = PAIR ? rank & 1 : 0, leader = rank & ~1u;
+  const uint32_t token_bytes = p.token_rows * 128;
+  const int weight_boxes = (p.weight_rows + 63) / 64;  // of a transposed weight
+  const uint32_t weight_bytes = TRANS ? weight_boxes * 8192 : p.weight_rows * 128, stage_bytes = token_bytes + weight_bytes;
   auto full = [&](int s) { return smem_addr(&bars.full[s]); };
   auto empty = [&](int s) { return smem_addr(&bars.empty[s]); };
   auto granted = [&](int s) { return smem_addr(&bars.granted[s]); };
@@ -77,23 +103,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
       mbar_init(granted(s), 1);
-      mbar_init(written(s), 4);
+      mbar_init(written(s), 4 * kBlocks);
     }
     for (int b = 0; b < 2; b++) {
       mbar_init(done(b), 1);
-      mbar_init(free_(b), 4);
+      mbar_init(free_(b), 4 * kBlocks);
     }
     dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
   }
-  if (warp == 1) tmem_alloc(smem_addr(&tmem_slot), p.columns);
+  __syncwarp();
+  if (warp == 1) tmem_alloc<PAIR>(smem_addr(&tmem_slot), p.columns);
   tc_fence_before();
   __syncthreads();
+  if (PAIR) cluster_sync();  // the other block's barriers are ready
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
 
-  const int split = blockIdx.x % p.splits, step = gridDim.x / p.splits, tiles = p.token_tiles * p.weight_tiles;
+  const int team = kBlocks * p.splits;  // thread blocks of a tile
+  const int split = (blockIdx.x % team) / kBlocks, step = gridDim.x / team, tiles = p.token_tiles * p.weight_tiles;
   const int c0 = (int)((int64_t)p.chunks * split / p.splits), c1 = (int)((int64_t)p.chunks * (split + 1) / p.splits);
   const int rank_chunks = (p.rank + 63) >> 6;
   const bool paired = p.rank <= 32;  // both halves of S in one stage, at columns 0 and 32
@@ -101,22 +130,22 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == 0) {
     if (lane == 0) {
-      int it = 0;
+      Ring at(p.stages);
+      const uint32_t to = PAIR ? cluster_addr(full(0), leader) : full(0);  // barriers of the issuing block
       bool waited = false, ok = true;
-      for (int tile = blockIdx.x / p.splits; ok && tile < tiles; tile += step) {
+      for (int tile = blockIdx.x / team; ok && tile < tiles; tile += step) {
         int tt, wt;
         tile_at(p, tile, tt, wt);
-        for (int c = c0; ok && c < c1; c++, it++) {
-          const int s = it % p.stages;
-          if (!(ok = mbar_wait(empty(s), ((it / p.stages) & 1) ^ 1, &dead))) break;
-          const uint32_t at = base + s * stage_bytes;
-          mbar_expect(full(s), stage_bytes);
-          tma_load_2d(at, &zmap, c * 64, tt * p.token_rows, full(s));
+        const int t0 = (tt * kBlocks + me) * p.token_rows, n0 = (wt * kBlocks + me) * p.weight_rows;
+        for (int c = c0; c < c1; c++, at.next()) {
+          if (!(ok = mbar_wait(empty(at.s), at.phase ^ 1, &dead))) break;
+          const uint32_t dst = base + at.s * stage_bytes, bar = to + at.s * 8;
+          if (me == 0) mbar_expect(full(at.s), kBlocks * stage_bytes);
+          tma_load_2d<PAIR>(dst, &zmap, c * 64, t0, bar);
           if (TRANS) {
-            for (int b = 0; b < p.weight_rows / 64; b++)
-              tma_load_2d(at + token_bytes + b * 8192, &wmap, wt * p.weight_rows + b * 64, c * 64, full(s));
+            for (int b = 0; b < weight_boxes; b++) tma_load_2d<PAIR>(dst + token_bytes + b * 8192, &wmap, n0 + b * 64, c * 64, bar);
           } else {
-            tma_load_2d(at + token_bytes, &wmap, c * 64, wt * p.weight_rows, full(s));
+            tma_load_2d<PAIR>(dst + token_bytes, &wmap, c * 64, n0, bar);
           }
         }
         if (!ok) break;
@@ -124,110 +153,113 @@ __global__ void __launch_bounds__(kThreads, 1)
           wait_for_predecessor();
           waited = true;
         }
-        const int* list = p.lists + (int64_t)tt * (p.token_rows + 1);
+        const int* list = p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1);
         const int n_list = __ldcg(list);
         for (int i = split; ok && i < n_list; i += p.splits) {
           const int a = __ldcg(list + 1 + i);
-          for (int e = 0; ok && e < rank_chunks * parts; e++, it++) {
-            const int rc = e / parts, s = it % p.stages;
-            if (!(ok = mbar_wait(empty(s), ((it / p.stages) & 1) ^ 1, &dead))) break;
-            const uint32_t at = base + s * stage_bytes + token_bytes;
-            mbar_arrive(granted(s));  // the stage's token tile is the writers' now
-            mbar_expect(full(s), weight_bytes);
+          for (int e = 0; e < rank_chunks * parts; e++, at.next()) {
+            const int rc = e / parts;
+            if (!(ok = mbar_wait(empty(at.s), at.phase ^ 1, &dead))) break;
+            const uint32_t dst = base + at.s * stage_bytes + token_bytes, bar = to + at.s * 8;
+            mbar_arrive(granted(at.s));  // the stage's token tile is the writers' now
+            if (me == 0) mbar_expect(full(at.s), kBlocks * weight_bytes);
             if (TRANS) {
-              for (int b = 0; b < p.weight_rows / 64; b++)
-                tma_load_3d(at + b * 8192, &pmap, wt * p.weight_rows + b * 64, rc * 64, a, full(s));
+              for (int b = 0; b < weight_boxes; b++) tma_load_3d<PAIR>(dst + b * 8192, &pmap, n0 + b * 64, rc * 64, a, bar);
             } else {
-              tma_load_3d(at, &pmap, rc * 64, wt * p.weight_rows, a, full(s));
+              tma_load_3d<PAIR>(dst, &pmap, rc * 64, n0, a, bar);
             }
           }
         }
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const int columns = TALL ? p.token_rows : p.weight_rows;
-      const uint32_t idesc = TALL ? instr_desc(p.dtype, TRANS, false, 128, columns) : instr_desc(p.dtype, false, TRANS, 128, columns);
+    if (lane == 0 && me == 0) {
+      const uint32_t idesc = TALL ? instr_desc(p.dtype, TRANS, false, 128, p.token_rows)
+                                  : instr_desc(p.dtype, false, TRANS, 256, 2 * p.weight_rows);
+      const uint32_t mask = 3u << leader;
       // 16 values of K further: 32 bytes in a K-major tile, two groups of 8 rows in an MN-major one
       const uint32_t weight_step = TRANS ? 2048 >> 4 : 32 >> 4, token_step = 32 >> 4;
-      int it = 0, turn = 0;
+      const uint64_t z_desc = smem_desc(base, 16), w_desc = smem_desc(base + token_bytes, TRANS ? 8192 : 16);
+      Ring at(p.stages);
+      int turn = 0;
       uint32_t written_phase = 0;
       bool waited = false, ok = true;
-      for (int tile = blockIdx.x / p.splits; ok && tile < tiles; tile += step, turn++) {
+      for (int tile = blockIdx.x / team; ok && tile < tiles; tile += step, turn++) {
         int tt, wt;
         tile_at(p, tile, tt, wt);
         const int b = p.accumulators == 2 ? turn & 1 : 0, use = p.accumulators == 2 ? turn >> 1 : turn;
         if (!(ok = mbar_wait(free_(b), (use & 1) ^ 1, &dead))) break;
         tc_fence_after();
         const uint32_t d = tmem + b * 256;
-        bool some = false;
-        auto product = [&](uint32_t at, int k_token, int k_weight) {
-          const uint64_t z = smem_desc(at, 16) + (uint64_t)(k_token * token_step);
-          const uint64_t w = smem_desc(at + token_bytes, TRANS ? 8192 : 16) + (uint64_t)(k_weight * weight_step);
-          mma_f16(d, TALL ? w : z, TALL ? z : w, idesc, some);
-          some = true;
-        };
-        for (int c = c0; c < c1; c++, it++) {
-          const int s = it % p.stages;
-          if (!(ok = mbar_wait(full(s), (it / p.stages) & 1, &dead))) break;
+        auto product = [&](uint64_t z, uint64_t w, bool accumulate) { mma_f16<PAIR>(d, TALL ? w : z, TALL ? z : w, idesc, accumulate); };
+        for (int c = c0; c < c1; c++, at.next()) {
+          if (!(ok = mbar_wait(full(at.s), at.phase, &dead))) break;
           tc_fence_after();
+          const uint64_t off = (uint64_t)(at.s * stage_bytes >> 4);
 #pragma unroll
-          for (int k = 0; k < 4; k++) product(base + s * stage_bytes, k, k);
-          mma_commit(empty(s));
+          for (int k = 0; k < 4; k++) product(z_desc + off + k * token_step, w_desc + off + k * weight_step, c > c0 || k > 0);
+          mma_commit<PAIR>(empty(at.s), mask);
         }
         if (!ok) break;
         if (!waited) {
           wait_for_predecessor();
           waited = true;
         }
-        const int n_list = __ldcg(p.lists + (int64_t)tt * (p.token_rows + 1));
+        const int n_list = __ldcg(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1));
         for (int i = split; ok && i < n_list; i += p.splits) {
-          for (int e = 0; e < rank_chunks * parts; e++, it++) {
-            const int rc = e / parts, s = it % p.stages;
-            if (!(ok = mbar_wait(full(s), (it / p.stages) & 1, &dead) && mbar_wait(written(s), (written_phase >> s) & 1, &dead))) break;
-            written_phase ^= 1u << s;
+          for (int e = 0; e < rank_chunks * parts; e++, at.next()) {
+            const int rc = e / parts;
+            if (!(ok = mbar_wait(full(at.s), at.phase, &dead) && mbar_wait(written(at.s), (written_phase >> at.s) & 1, &dead))) break;
+            written_phase ^= 1u << at.s;
             tc_fence_after();
+            const uint64_t off = (uint64_t)(at.s * stage_bytes >> 4);
             const int steps = (min(64, p.rank - rc * 64) + 15) >> 4;
-            for (int k = 0; k < steps; k++) product(base + s * stage_bytes, k, k);
+            for (int k = 0; k < steps; k++) product(z_desc + off + k * token_step, w_desc + off + k * weight_step, true);
             if (paired)
-              for (int k = 0; k < steps; k++) product(base + s * stage_bytes, k + 2, k);
-            mma_commit(empty(s));
+              for (int k = 0; k < steps; k++) product(z_desc + off + (k + 2) * token_step, w_desc + off + k * weight_step, true);
+            mma_commit<PAIR>(empty(at.s), mask);
           }
         }
         if (!ok) break;
-        mma_commit(done(b));
+        mma_commit<PAIR>(done(b), mask);
       }
     }
   } else {
     const int e = threadIdx.x - 64, quarter = warp & 3;
     // The writers take part in few of a stage's rounds, so they cannot follow its `empty` barrier by parity; the copying
     // warp, which follows every round, grants them the stage.
-    int it = 0, turn = 0;
+    Ring ring(p.stages);
+    int turn = 0;
     uint32_t granted_phase = 0;
+    auto tell = [&](uint32_t bar) {  // the block that issues the products
+      if (PAIR) cluster_arrive(cluster_addr(bar, leader));
+      else mbar_arrive(bar);
+    };
     bool waited = false, ok = true;
-    for (int tile = blockIdx.x / p.splits; tile < tiles; tile += step, turn++) {
+    for (int tile = blockIdx.x / team; tile < tiles; tile += step, turn++) {
       int tt, wt;
       tile_at(p, tile, tt, wt);
-      it += c1 - c0;
+      ring.skip(c1 - c0);
       if (!waited) {
         wait_for_predecessor();
         waited = true;
       }
+      const int t0 = (tt * kBlocks + me) * p.token_rows;
       // S: a thread writes rows e and e + 128 of the token tile
       int mine[2];
 #pragma unroll
       for (int h = 0; h < 2; h++) {
-        const int row = e + h * 128, t = tt * p.token_rows + row;
+        const int row = e + h * 128, t = t0 + row;
         mine[h] = row < p.token_rows && t < p.T ? p.adapter_of[t] : -1;
         if (mine[h] >= 0 && mine[h] < p.n_adapters)
           for (int j = 0; j < p.rank; j += 32) asm volatile("prefetch.global.L1 [%0];" ::"l"(p.S + (int64_t)t * p.rank + j));
       }
-      const int* list = p.lists + (int64_t)tt * (p.token_rows + 1);
+      const int* list = p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1);
       const int n_list = __ldcg(list);
       for (int i = split; ok && i < n_list; i += p.splits) {
         const int a = __ldcg(list + 1 + i);
-        for (int x = 0; x < rank_chunks * parts; x++, it++) {
-          const int rc = x / parts, s = it % p.stages;
+        for (int x = 0; x < rank_chunks * parts; x++, ring.next()) {
+          const int rc = x / parts, s = ring.s;
           ok = mbar_wait(granted(s), (granted_phase >> s) & 1, &dead);
           granted_phase ^= 1u << s;
           if (!__all_sync(0xffffffffu, ok)) {
@@ -239,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int h = 0; h < 2; h++) {
             const int row = e + h * 128;
             if (row >= p.token_rows) continue;
-            const float* src = p.S + (int64_t)(tt * p.token_rows + row) * p.rank + rc * 64;
+            const float* src = p.S + (int64_t)(t0 + row) * p.rank + rc * 64;
             const uint32_t dst = base + s * stage_bytes + row * 128;
             for (int g = 0; g < wide; g++) {
               uint4 hi = make_uint4(0, 0, 0, 0), lo = hi;
@@ -276,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           fence_async_shared();
           __syncwarp();
-          if (lane == 0) mbar_arrive(written(s));
+          if (lane == 0) tell(written(s));
         }
       }
       // the accumulators of the tile
@@ -285,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
       const uint32_t d = tmem + b * 256 + ((uint32_t)(quarter * 32) << 16);
-      const int columns = TALL ? p.token_rows : p.weight_rows, at = quarter * 32 + lane;
+      const int columns = TALL ? p.token_rows : 2 * p.weight_rows, at = quarter * 32 + lane;
       for (int c = 0; c < columns; c += 16) {
         uint32_t r[16];
         tmem_load16(d + c, r);
@@ -300,12 +332,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (n < p.N) {
 #pragma unroll
             for (int k = 0; k < 16; k++) {
-              const int t = tt * p.token_rows + c + k;
+              const int t = t0 + c + k;
               if (t < p.T) store1(p.O, t * p.ldo + n, p.dtype, __uint_as_float(r[k]));
             }
           }
         } else {
-          const int t = tt * 128 + at, n = wt * p.weight_rows + c;
+          const int t = t0 + at, n = wt * 2 * p.weight_rows + c;
           if (t < p.T) {
 #pragma unroll
             for (int k = 0; k < 16; k += 8) {
@@ -320,15 +352,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(free_(b));
+      if (lane == 0) tell(free_(b));
     }
   }
   __syncwarp();
   __syncthreads();
-  if (warp == 1) {
-    tc_fence_after();
-    tmem_free(tmem, p.columns);
-  }
   if (dead && threadIdx.x == 0) {
     // copies this thread block has issued may still be landing in its shared memory
     const long long begin = clock64();
@@ -336,12 +364,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     atomicAdd(p.stalls, 1ull);
   }
+  __syncwarp();
+  if (team > 1) cluster_sync();  // no more arrivals from other blocks; their sums are in shared memory
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_free<PAIR>(tmem, p.columns);
+  }
   if (p.splits > 1) {
-    __syncwarp();
-    cluster_sync();
-    // one tile a cluster: this block adds and stores its share of it
+    // one tile a team: this block adds and stores its share of it
     int tt, wt;
-    tile_at(p, blockIdx.x / p.splits, tt, wt);
+    tile_at(p, blockIdx.x / team, tt, wt);
     if (TALL) {
       const int columns = min(p.token_rows, p.T - tt * p.token_rows);
       for (int i = threadIdx.x; i < (columns - split + p.splits - 1) / p.splits * 128; i += kThreads) {
@@ -351,47 +383,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (n < p.N) store1(p.O, (int64_t)(tt * p.token_rows + c) * p.ldo + n, p.dtype, x);
       }
     } else {
-      const int share = 128 / p.splits;
-      for (int i = threadIdx.x; i < share * p.weight_rows; i += kThreads) {
-        const int c = i % p.weight_rows, at = split * share + i / p.weight_rows, n = wt * p.weight_rows + c, t = tt * 128 + at;
+      const int share = 128 / p.splits, columns = 2 * p.weight_rows;
+      for (int i = threadIdx.x; i < share * columns; i += kThreads) {
+        const int c = i % columns, at = split * share + i / columns, n = wt * columns + c, t = (tt * 2 + me) * 128 + at;
         float x = 0.0f;
-        for (int q = 0; q < p.splits; q++) x += cluster_load(base + (c * 129 + at) * 4, q);
+        for (int q = 0; q < p.splits; q++) x += cluster_load(base + (c * 129 + at) * 4, 2 * q + me);
         if (t < p.T && n < p.N) store1(p.O, t * p.ldo + n, p.dtype, x);
       }
     }
+    __syncwarp();
     cluster_sync();  // no block leaves while another reads its shared memory
   }
-}
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-  static const EncodeTiled fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess) {
-      cudaGetLastError();
-      p = nullptr;
-    }
-    return (EncodeTiled)p;
-  }();
-  return fn;
-}
-
-// A row-major array of 16-bit values [planes][rows][inner], copied in boxes of box_rows x 64 with the 128-byte swizzle;
-// what lies outside the array reads as zero.
-bool make_map(CUtensorMap* map, int dtype, const void* base, int64_t inner, int64_t rows, int64_t planes, int64_t row_stride,
-              int64_t plane_stride, int box_rows) {
-  const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)planes};
-  const cuuint64_t strides[2] = {(cuuint64_t)(2 * row_stride), (cuuint64_t)(2 * plane_stride)};
-  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, ones[3] = {1, 1, 1};
-  return encode_tiled()(map, dtype == WINDQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
-                        planes > 0 ? 3 : 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <bool TALL, bool TRANS>
@@ -408,17 +410,17 @@ windq_status launch(windq_ctx* ctx, const CUtensorMap& z, const CUtensorMap& w, 
   attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attrs[0].val.programmaticStreamSerializationAllowed = 1;
   attrs[1].id = cudaLaunchAttributeClusterDimension;
-  attrs[1].val.clusterDim.x = p.splits;
+  attrs[1].val.clusterDim.x = (TALL ? 1 : 2) * p.splits;
   attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
   cfg.attrs = attrs;
-  cfg.numAttrs = p.splits > 1 ? 2 : 1;
+  cfg.numAttrs = attrs[1].val.clusterDim.x > 1 ? 2 : 1;
   WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, project_kernel<TALL, TRANS>, z, w, pm, p));
   return WINDQ_OK;
 }
 
 }  // namespace
 
-int token_tile(int64_t T) { return T <= 256 ? (int)round_up(std::max<int64_t>(T, 1), 16) : 128; }
+int token_tile(int64_t T) { return T <= 256 ? (int)round_up(std::max<int64_t>(T, 1), 16) : 256; }
 
 windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t st) {
   const bool tall = q.T <= 256;
@@ -435,21 +437,41 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   p.O = q.O;
   p.ldo = q.ldo;
   p.stalls = stall_counter(ctx);
-  p.token_rows = token_tile(q.T);
-  p.weight_rows = tall ? 128 : 256;
-  p.token_tiles = (int)((q.T + p.token_rows - 1) / p.token_rows);
-  p.weight_tiles = (int)((q.N + p.weight_rows - 1) / p.weight_rows);
-  p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.token_tiles, (48ll << 20) / (2 * q.K * p.token_rows)));
-  const int stage = (p.token_rows + p.weight_rows) * 128;
+  const int blocks_of_tile = tall ? 1 : 2;
+  p.token_rows = tall ? token_tile(q.T) : 128;
+  p.weight_rows = 128;
+  p.token_tiles = (int)((q.T + p.token_rows * blocks_of_tile - 1) / (p.token_rows * blocks_of_tile));
   const bool two = tall && p.token_rows <= 64;  // thread blocks an SM
+  const int64_t slots = (int64_t)ctx->sm_count * (two ? 2 : 1) / blocks_of_tile;
+  p.splits = 1;
+  if (!tall) {
+    // outputs of a tile: the width that takes the fewest rounds over the GPU, a chunk of K costing 600 + width (0.39 us at
+    // 128, 0.42 at 192, 0.47 at 256).  Tiles that fill less than half of the GPU are split along K instead.
+    int64_t best = INT64_MAX;
+    for (int rows = 128; rows >= 48; rows -= 16) {
+      const int64_t tiles = p.token_tiles * ((q.N + 2 * rows - 1) / (2 * rows));
+      int splits = 1;
+      while (splits < 4 && tiles * splits * 2 <= slots && p.chunks >= splits * 2 * 4) splits *= 2;
+      const int64_t waves = (tiles * splits + slots - 1) / slots;
+      const int64_t cost = waves * ((p.chunks + splits - 1) / splits * (600 + 2 * rows) + (splits > 1 ? 9000 : 4000));
+      if (cost < best) {
+        best = cost;
+        p.weight_rows = rows;
+        p.splits = splits;
+      }
+    }
+  }
+  p.weight_tiles = (int)((q.N + p.weight_rows * blocks_of_tile - 1) / (p.weight_rows * blocks_of_tile));
+  p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.token_tiles, (48ll << 20) / (2 * q.K * p.token_rows * blocks_of_tile)));
+  const int stage = p.token_rows * 128 + (q.transposed ? (p.weight_rows + 63) / 64 * 8192 : p.weight_rows * 128);
   const int limit = two ? kSmemLimitTwo : kSmemLimit;
   p.stages = std::min(kMaxStages, (limit - 1024) / stage);
-  const int64_t tiles = (int64_t)p.token_tiles * p.weight_tiles, slots = (int64_t)ctx->sm_count * (two ? 2 : 1);
-  p.splits = 1;
-  while (p.splits < 8 && tiles * p.splits * 2 <= slots && p.chunks >= p.splits * 2 * 4) p.splits *= 2;
+  const int64_t tiles = (int64_t)p.token_tiles * p.weight_tiles;
+  if (tall)
+    while (p.splits < 8 && tiles * p.splits * 2 <= slots && p.chunks >= p.splits * 2 * 4) p.splits *= 2;
   p.accumulators = !tall && p.splits == 1 ? 2 : 1;
   p.columns = tall ? (p.token_rows <= 32 ? 32 : p.token_rows <= 64 ? 64 : p.token_rows <= 128 ? 128 : 256) : 256 * p.accumulators;
-  const int64_t blocks = p.splits > 1 ? tiles * p.splits : std::min(tiles, slots);
+  const int64_t blocks = (p.splits > 1 ? tiles * p.splits : std::min(tiles, slots)) * blocks_of_tile;
   const int smem = 1024 + p.stages * stage;
 
   CUtensorMap z, w, pm;
