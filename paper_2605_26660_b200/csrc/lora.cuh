@@ -5,7 +5,7 @@
 
 namespace windq {
 
-// O[t][n] = sum_k Z[t][k] W(n, k) + sum_j S[t][j] P[a](n, j), a = adapter_of[t]; S is fp32 and already scaled.
+// O[t][n] = sum_k Z[t][k] W(n, k) + sum_j S[t][j] P[a](n, j), a = adapter_of[t]; S is already scaled.
 //   forward:  Z = X,  W(n, k) = W[n][k], P[a](n, j) = B[a][n][j]     (k and j contiguous)
 //   backward: Z = dY, W(n, k) = W[k][n], P[a](n, j) = A[a][j][n]     (n contiguous: transposed)
 struct Projection {
@@ -19,7 +19,7 @@ struct Projection {
   int64_t n_adapters;
   int rank;
   const int32_t* adapter_of;
-  const float* S;
+  const void* pair;  // S as launch_low_rank leaves it
   const int* lists;  // see token_tile
   void* O;
   int64_t ldo;
@@ -40,7 +40,8 @@ struct LowRankJob {
   const void* Z;
   int64_t K, ldz;
   const void* P;
-  float* S;
+  float* S;    // nullable
+  void* pair;  // 16-bit [T][2][rank]: first and second term of S, for the projection; nullable
   float* top;  // fp32 [T], the largest |S[t][j]| of every token; nullable
 };
 struct LowRank {

@@ -14,9 +14,13 @@ namespace {
 
 // ---- D[a][j][c] = sum over the tokens t of a of S[t][j] Z[t][c] ----------------------------------------------------
 
-constexpr int kGradWarps = 8, kGradCols = 128, kGradTokens = 64, kGradStages = 3;
+constexpr int kGradWarps = 8, kGradThreads = 256, kGradCols = 128;
 constexpr int kZPitch = kGradCols * 2 + 16;  // bytes
 constexpr int kWindow = 64;                  // blocks of tokens whose adapters are looked up at a time
+
+// Blocks of tokens and stages of copies in flight, by the rank / 8 that a kernel is made for: two thread blocks an SM.
+__host__ __device__ constexpr int grad_tokens(int nb) { return nb <= 4 ? 64 : 32; }
+__host__ __device__ constexpr int grad_stages(int nb) { return nb <= 2 ? 4 : nb <= 4 ? 3 : nb <= 8 ? 4 : 2; }
 
 struct GradJob {
   const uint16_t* Z;
@@ -35,15 +39,17 @@ struct GradArgs {
 
 // A thread block owns 128 columns of Z for one adapter; a cluster of `splits` shares the tokens.  The tokens that are not
 // the adapter's are left out as rows of zeros (copied with size zero, so that what they hold cannot spoil a sum), blocks
-// of 64 tokens without any of its tokens are skipped.  Z is the transposed left operand (ldmatrix.trans); S enters as two
+// of tokens without any of its tokens are skipped.  Z is the transposed left operand (ldmatrix.trans); S enters as two
 // fp16 or three bf16 values whose sum is S to 22 or 24 bits -- fp16 ones after a scaling by a power of two that puts the
-// block's largest |S| near 2^13, undone at the end, so that small gradients keep their bits.
+// adapter's largest |S| near 2^13, undone at the end, so that small gradients keep their bits.
 template <int NB, bool BF>
-__global__ void __launch_bounds__(kGradWarps * 32) gradient_kernel(const __grid_constant__ GradArgs p) {
-  constexpr int kTerms = BF ? 3 : 2;
+__global__ void __launch_bounds__(kGradThreads) gradient_kernel(const __grid_constant__ GradArgs p) {
+  constexpr int kTerms = BF ? 3 : 2, kTokens = grad_tokens(NB), kStages = grad_stages(NB);
+  constexpr int kHalves = kTokens / 32;                                                  // of a block's tokens, 32 each
+  constexpr int kPieces = (kTokens * NB + kGradThreads - 1) / kGradThreads;              // of eight values of S, a thread
   extern __shared__ uint4 shared[];
-  __shared__ int ids[kWindow * kGradTokens];
-  __shared__ short active[kWindow], flags[kWindow];
+  __shared__ unsigned masks[kWindow][kHalves];  // tokens of the adapter
+  __shared__ short active[kWindow];
   __shared__ int n_active;
   __shared__ float tops[kGradWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
@@ -53,14 +59,14 @@ __global__ void __launch_bounds__(kGradWarps * 32) gradient_kernel(const __grid_
   const GradJob& job = p.job[second];
   if (second) tile -= p.job[0].tiles;
   const int c0 = tile * kGradCols;
-  const int all = (p.T + kGradTokens - 1) / kGradTokens;
+  const int all = (p.T + kTokens - 1) / kTokens;
   launch_dependents();
   wait_for_predecessor();
 
   float up = 1.0f, down = 1.0f;
   if (!BF) {
     float top = 0.0f;
-    for (int t = tid; t < p.T; t += kGradWarps * 32) {
+    for (int t = tid; t < p.T; t += kGradThreads) {
       const float x = job.top[t];
       if (p.adapter_of[t] == a) top = fmaxf(top, x);
     }
@@ -75,8 +81,10 @@ __global__ void __launch_bounds__(kGradWarps * 32) gradient_kernel(const __grid_
     down = __uint_as_float((uint32_t)(127 - k) << 23);
   }
 
-  const int s_pitch = r * 2 + 16;
-  const uint32_t z_base = smem_addr(shared), s_base = z_base + kGradStages * kGradTokens * kZPitch;
+  // a stage: Z [token][column], then S [token][j] in binary32; after the stages two buffers of S in 16-bit terms
+  const int s_pitch = r * 2 + 16, s_raw = kTokens * r * 4, s_terms = kTerms * kTokens * s_pitch;
+  const int stage_bytes = kTokens * kZPitch + s_raw;
+  const uint32_t base = smem_addr(shared), terms = base + kStages * stage_bytes;
   float acc[NB][4];
 #pragma unroll
   for (int n = 0; n < NB; n++)
@@ -86,19 +94,16 @@ __global__ void __launch_bounds__(kGradWarps * 32) gradient_kernel(const __grid_
   for (int w0 = 0; w0 < all; w0 += kWindow) {
     const int count = min(kWindow, all - w0);
     __syncthreads();
-    for (int b = warp; b < count; b += kGradWarps) {
-      const int i = b * kGradTokens + lane, t = w0 * kGradTokens + i;
-      const int x = t < p.T ? p.adapter_of[t] : -1, y = t + 32 < p.T ? p.adapter_of[t + 32] : -1;
-      ids[i] = x;
-      ids[i + 32] = y;
-      const unsigned vote = __ballot_sync(0xffffffffu, x == a || y == a);
-      if (lane == 0) flags[b] = vote != 0;
+    for (int i = warp; i < count * kHalves; i += kGradWarps) {
+      const int t = w0 * kTokens + i * 32 + lane;
+      const unsigned vote = __ballot_sync(0xffffffffu, t < p.T && p.adapter_of[t] == a);
+      if (lane == 0) masks[i / kHalves][i % kHalves] = vote;
     }
     __syncthreads();
     if (warp == 0) {
       int n = 0;
       for (int h = 0; h < count; h += 32) {
-        const bool on = h + lane < count && flags[h + lane];
+        const bool on = h + lane < count && (masks[h + lane][0] | masks[h + lane][kHalves - 1]);
         const unsigned vote = __ballot_sync(0xffffffffu, on);
         if (on) active[n + __popc(vote & ((1u << lane) - 1))] = (short)(h + lane);
         n += __popc(vote);
@@ -107,45 +112,43 @@ __global__ void __launch_bounds__(kGradWarps * 32) gradient_kernel(const __grid_
     }
     __syncthreads();
     const int n_blocks = (n_active - split + p.splits - 1) / p.splits;  // every splits-th of them is this block's
-    auto block_at = [&](int i) { return (int)active[split + i * p.splits]; };
-    auto copy_z = [&](int i) {
+    auto copy_block = [&](int i) {
       if (i < n_blocks) {
-        const int b = block_at(i), t0 = (w0 + b) * kGradTokens;
-        const uint32_t at = z_base + (i % kGradStages) * kGradTokens * kZPitch;
+        const int b = active[split + i * p.splits], t0 = (w0 + b) * kTokens;
+        const uint32_t at = base + (i % kStages) * stage_bytes;
 #pragma unroll
-        for (int h = 0; h < 4; h++) {
-          const int x = h * kGradWarps * 32 + tid, row = x >> 4, piece = x & 15, t = t0 + row, c = c0 + piece * 8;
-          const bool on = c < job.cols && ids[b * kGradTokens + row] == a;
-          const int bytes = on ? min(16, (job.cols - c) * 2) : 0;
-          copy16(at + row * kZPitch + piece * 16, on ? job.Z + t * job.ldz + c : job.Z, bytes);
+        for (int h = 0; h < kTokens * 16 / kGradThreads; h++) {
+          const int x = h * kGradThreads + tid, row = x >> 4, piece = x & 15, c = c0 + piece * 8;
+          const bool on = c < job.cols && (masks[b][row >> 5] >> (row & 31) & 1);
+          copy16(at + row * kZPitch + piece * 16, on ? job.Z + (t0 + row) * job.ldz + c : job.Z, on ? min(16, (job.cols - c) * 2) : 0);
+        }
+#pragma unroll
+        for (int h = 0; h < kPieces; h++) {
+          const int x = h * kGradThreads + tid, row = x / NB, piece = x % NB;
+          if (row >= kTokens || piece * 8 >= r) continue;
+          const bool on = masks[b][row >> 5] >> (row & 31) & 1;
+          const float* src = on ? job.S + (int64_t)(t0 + row) * r + piece * 8 : job.S;
+          const uint32_t dst = at + kTokens * kZPitch + (row * r + piece * 8) * 4;
+          copy16(dst, src, on ? 16 : 0);
+          copy16(dst + 16, src + 4, on ? 16 : 0);
         }
       }
       copy_commit();
     };
-    // S of a block: pieces of eight values, kGradTokens * rank / 8 of them over 256 threads
-    constexpr int kPieces = (kGradTokens * NB + kGradWarps * 32 - 1) / (kGradWarps * 32);
-    float4 s_next[kPieces][2];
-    auto load_s = [&](int i) {
-      if (i >= n_blocks) return;
-      const int b = block_at(i), t0 = (w0 + b) * kGradTokens;
+    // The thread that copied a piece of S also splits it into terms.
+    auto split_s = [&](int i) {
+      const uint32_t at = base + (i % kStages) * stage_bytes + kTokens * kZPitch, to = terms + (i & 1) * s_terms;
 #pragma unroll
       for (int h = 0; h < kPieces; h++) {
-        const int x = h * kGradWarps * 32 + tid, row = x / NB, piece = x % NB, t = t0 + row;
-        s_next[h][0] = s_next[h][1] = make_float4(0, 0, 0, 0);
-        if (row < kGradTokens && piece * 8 < r && ids[b * kGradTokens + row] == a) {
-          const float4* src = reinterpret_cast<const float4*>(job.S + (int64_t)t * r + piece * 8);
-          s_next[h][0] = src[0];
-          s_next[h][1] = src[1];
-        }
-      }
-    };
-    auto write_s = [&] {
+        const int x = h * kGradThreads + tid, row = x / NB, piece = x % NB;
+        if (row >= kTokens || piece * 8 >= r) continue;
+        float y[8];
 #pragma unroll
-      for (int h = 0; h < kPieces; h++) {
-        const int x = h * kGradWarps * 32 + tid, row = x / NB, piece = x % NB;
-        if (row >= kGradTokens || piece * 8 >= r) continue;
-        float y[8] = {s_next[h][0].x, s_next[h][0].y, s_next[h][0].z, s_next[h][0].w,
-                      s_next[h][1].x, s_next[h][1].y, s_next[h][1].z, s_next[h][1].w};
+        for (int k = 0; k < 8; k += 4)
+          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(y[k]), "=f"(y[k + 1]), "=f"(y[k + 2]), "=f"(y[k + 3])
+                       : "r"(at + (row * r + piece * 8 + k) * 4)
+                       : "memory");
 #pragma unroll
         for (int k = 0; k < 8; k++) y[k] *= up;
 #pragma unroll
@@ -158,29 +161,28 @@ __global__ void __launch_bounds__(kGradWarps * 32) gradient_kernel(const __grid_
             y[2 * k] -= back.x;
             y[2 * k + 1] -= back.y;
           }
-          const uint32_t at = s_base + (term * kGradTokens + row) * s_pitch + piece * 16;
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (term * kTokens + row) * s_pitch + piece * 16), "r"(w[0]),
+                       "r"(w[1]), "r"(w[2]), "r"(w[3])
+                       : "memory");
         }
       }
     };
-    copy_z(0);
-    copy_z(1);
-    load_s(0);
-    for (int i = 0; i < n_blocks; i++) {
-      write_s();
-      copy_wait<1>();
-      __syncthreads();
-      copy_z(i + 2);
-      load_s(i + 1);
-      const uint32_t z_at = z_base + (i % kGradStages) * kGradTokens * kZPitch;
 #pragma unroll
-      for (int k = 0; k < kGradTokens / 16; k++) {
+    for (int i = 0; i < kStages - 1; i++) copy_block(i);
+    for (int i = 0; i < n_blocks; i++) {
+      copy_wait<kStages - 2>();
+      split_s(i);
+      __syncthreads();
+      copy_block(i + kStages - 1);  // into the stage that every warp left before the barrier
+      const uint32_t z_at = base + (i % kStages) * stage_bytes, s_at0 = terms + (i & 1) * s_terms;
+#pragma unroll
+      for (int k = 0; k < kTokens / 16; k++) {
         // left operand: columns 16 warp .. + 15 (rows of the product), tokens 16 k .. + 15
         uint32_t za[4];
         ldmatrix_trans(z_at + (k * 16 + (lane & 7) + (lane >> 4) * 8) * kZPitch + (warp * 16 + ((lane >> 3) & 1) * 8) * 2, za);
 #pragma unroll
         for (int term = 0; term < kTerms; term++) {
-          const uint32_t s_at = s_base + (term * kGradTokens + k * 16 + (lane & 15)) * s_pitch + (lane >> 4) * 16;
+          const uint32_t s_at = s_at0 + (term * kTokens + k * 16 + (lane & 15)) * s_pitch + (lane >> 4) * 16;
 #pragma unroll
           for (int n = 0; n < NB; n += 2) {
             if (n * 8 < r) {
@@ -193,32 +195,45 @@ __global__ void __launch_bounds__(kGradWarps * 32) gradient_kernel(const __grid_
           }
         }
       }
-      __syncthreads();
     }
     copy_wait<0>();
   }
-  // join the cluster, [j][column] 129 apart
   __syncthreads();
-  float* out = reinterpret_cast<float*>(shared);
+  // join the cluster: [column][j] for dB, [j][column] for dA, as the result lies
+  const int pitch = job.j_first ? r + 4 : kGradCols + 4;
 #pragma unroll
   for (int n = 0; n < NB; n++)
     if (n * 8 < r) {
 #pragma unroll
-      for (int k = 0; k < 4; k++) out[(n * 8 + q * 2 + (k & 1)) * 129 + warp * 16 + g + (k >> 1) * 8] = acc[n][k] * down;
+      for (int k = 0; k < 4; k++) {
+        const int j = n * 8 + q * 2 + (k & 1), c = warp * 16 + g + (k >> 1) * 8;
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(base + (job.j_first ? c * pitch + j : j * pitch + c) * 4), "f"(acc[n][k] * down)
+                     : "memory");
+      }
     }
+  __syncwarp();
   if (p.splits > 1) cluster_sync();
   else __syncthreads();
   const int cols = min(kGradCols, job.cols - c0);
+  const int quads = (job.j_first ? r : cols) / 4, items = (job.j_first ? cols : r) * quads;  // four values each
   float* D = job.D + (int64_t)a * r * job.cols;
-  for (int i = split * kGradWarps * 32 + tid; i < cols * r; i += p.splits * kGradWarps * 32) {
-    const int j = job.j_first ? i % r : i / cols, c = job.j_first ? i / r : i % cols;
-    float x = 0.0f;
-    if (p.splits > 1) {
-      for (int s = 0; s < p.splits; s++) x += cluster_load(smem_addr(&out[j * 129 + c]), s);
-    } else {
-      x = out[j * 129 + c];
+  constexpr int U = 4;
+  for (int i = split * kGradThreads + tid; i < items; i += U * p.splits * kGradThreads) {
+    uint32_t offset[U];
+    float4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int e = min(i + u * p.splits * kGradThreads, items - 1);
+      offset[u] = (uint32_t)(e / quads * pitch + e % quads * 4) * 4;
     }
-    D[job.j_first ? (int64_t)(c0 + c) * r + j : (int64_t)j * job.cols + c0 + c] = x;
+    cluster_sum<U>(base, offset, p.splits, 0, 1, x);
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int e = i + u * p.splits * kGradThreads;
+      if (e >= items) continue;
+      const int row = e / quads, col = e % quads * 4;
+      *reinterpret_cast<float4*>(D + (job.j_first ? (int64_t)(c0 + row) * r + col : (int64_t)row * job.cols + c0 + col)) = x[u];
+    }
   }
   __syncwarp();
   if (p.splits > 1) cluster_sync();
@@ -226,18 +241,20 @@ __global__ void __launch_bounds__(kGradWarps * 32) gradient_kernel(const __grid_
 
 template <int NB, bool BF>
 windq_status launch_gradients(windq_ctx* ctx, int id, GradArgs p, cudaStream_t st) {
-  const int tiles = p.job[0].tiles + p.job[1].tiles, blocks = (p.T + kGradTokens - 1) / kGradTokens;
+  const int tiles = p.job[0].tiles + p.job[1].tiles, blocks = (p.T + grad_tokens(NB) - 1) / grad_tokens(NB);
   // every token has one adapter, so the work of a column tile over all adapters is about one pass over the tokens
   p.splits = 1;
   while (p.splits < 8 && tiles * p.splits * 2 <= 3 * ctx->sm_count && blocks >= p.splits * 2 * 4) p.splits *= 2;
-  const int loop = kGradStages * kGradTokens * kZPitch + (BF ? 3 : 2) * kGradTokens * (p.rank * 2 + 16);
-  const int smem = std::max(loop, p.rank * 129 * 4);
-  constexpr int kMost = 108 * 1024;
-  const windq_status ready = prepare_kernel(ctx, id, gradient_kernel<NB, BF>, kGradWarps * 32, kMost, false);
+  const int tokens = grad_tokens(NB), terms = BF ? 3 : 2;
+  const int loop = grad_stages(NB) * tokens * (kZPitch + p.rank * 4) + 2 * terms * tokens * (p.rank * 2 + 16);
+  const int smem = std::max(loop, std::max(kGradCols * (p.rank + 4), p.rank * (kGradCols + 4)) * 4);
+  constexpr int kMost = 112 * 1024;
+  static_assert(grad_stages(NB) * grad_tokens(NB) * (kZPitch + NB * 32) + 6 * grad_tokens(NB) * (NB * 16 + 16) <= kMost, "two an SM");
+  const windq_status ready = prepare_kernel(ctx, id, gradient_kernel<NB, BF>, kGradThreads, kMost, false);
   if (ready != WINDQ_OK) return ready;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * p.splits), (unsigned)p.n_adapters);
-  cfg.blockDim = dim3(kGradWarps * 32);
+  cfg.blockDim = dim3(kGradThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attrs[2];
@@ -247,7 +264,7 @@ windq_status launch_gradients(windq_ctx* ctx, int id, GradArgs p, cudaStream_t s
   attrs[1].val.clusterDim.x = p.splits;
   attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
   cfg.attrs = attrs;
-  cfg.numAttrs = p.splits > 1 ? 2 : 1;
+  cfg.numAttrs = 2;
   WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, gradient_kernel<NB, BF>, p));
   return WINDQ_OK;
 }

@@ -19,8 +19,9 @@ struct LowJob {
   const uint16_t* Z;
   int64_t ldz;
   const uint16_t* P;  // [a][j][k], or transposed [a][k][j]
-  float* S;
-  float* top;  // largest |S[t][j]| of a token, or NULL
+  float* S;        // binary32, or NULL
+  uint16_t* pair;  // [t][2][j]: the two 16-bit values whose sum stands for S, or NULL
+  float* top;      // largest |S[t][j]| of a token, or NULL
   int K, transposed;
 };
 struct LowRankArgs {
@@ -69,35 +70,52 @@ __device__ void write_list(const LowRankArgs& p, int tile, int* ids, int* taken)
   if (threadIdx.x == 0) list[0] = all;
 }
 
-// S of the tokens of this block from the sums of the cluster's blocks, [token][pitch] at `sums`; a warp a token.  kept(i)
-// tells whether token t0 + i is to be written.
+// S of the tokens of this block from the sums of the cluster's blocks, [token][pitch] at `sums`: four values a thread.
+// kept(i) tells whether token t0 + i is to be written; tops: one word a token, zero.
 template <class Kept>
 __device__ __forceinline__ void finish_tokens(const LowRankArgs& p, const LowJob& job, int t0, int tokens, uint32_t sums, int pitch,
-                                              int split, const int* ids, Kept kept) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = split + warp * p.splits; i < tokens; i += kLowWarps * p.splits) {
-    if (!kept(i)) continue;  // the same for the whole warp
+                                              int split, const int* ids, int* tops, Kept kept) {
+  const int quads = p.rank / 4, share = (tokens - split + p.splits - 1) / p.splits;
+  for (int x = threadIdx.x; x < share * quads; x += kLowThreads) {
+    const int i = split + x / quads * p.splits, j = x % quads * 4;
+    if (!kept(i)) continue;
+    const uint32_t offset[1] = {(uint32_t)(i * pitch + j) * 4};
+    float4 y[1];
+    if (p.splits > 1) cluster_sum<1>(sums, offset, p.splits, 0, 1, y);
+    else asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y[0].x), "=f"(y[0].y), "=f"(y[0].z), "=f"(y[0].w) : "r"(sums + offset[0]) : "memory");
     const float scale = p.scaling[ids[i]];
-    float top = 0.0f;
-    for (int j = lane; j < p.rank; j += 32) {
-      const uint32_t at = sums + (i * pitch + j) * 4;
-      float x = 0.0f;
-      if (p.splits > 1) {
-        for (int s = 0; s < p.splits; s++) x += cluster_load(at, s);
-      } else {
-        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
-      }
-      x *= scale;
-      job.S[(int64_t)(t0 + i) * p.rank + j] = x;
-      top = fmaxf(top, fabsf(x));
-    }
-    if (job.top) {
+    float v[4] = {y[0].x * scale, y[0].y * scale, y[0].z * scale, y[0].w * scale};
+    const int64_t at = (int64_t)(t0 + i) * p.rank + j;
+    if (job.S) *reinterpret_cast<float4*>(job.S + at) = make_float4(v[0], v[1], v[2], v[3]);
+    if (job.top) atomicMax(&tops[i], __float_as_int(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])))));
+    if (job.pair) {
+      // 22 bits of fp16 (saturating: the first value takes what it can, the second up to as much again), 16 of bf16
+      uint32_t hi[2], lo[2];
 #pragma unroll
-      for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-      if (lane == 0) job.top[t0 + i] = top;
+      for (int k = 0; k < 2; k++) {
+        float a = v[2 * k], b = v[2 * k + 1];
+        if (p.dtype == WINDQ_F16) {
+          a = fminf(fmaxf(a, -131008.0f), 131008.0f);
+          b = fminf(fmaxf(b, -131008.0f), 131008.0f);
+          hi[k] = pack2(fminf(fmaxf(a, -65504.0f), 65504.0f), fminf(fmaxf(b, -65504.0f), 65504.0f), p.dtype);
+        } else {
+          hi[k] = pack2(a, b, p.dtype);
+        }
+        const float2 back = unpack2(hi[k], p.dtype);
+        lo[k] = pack2(a - back.x, b - back.y, p.dtype);
+      }
+      uint16_t* out = job.pair + (int64_t)(t0 + i) * 2 * p.rank + j;
+      *reinterpret_cast<uint2*>(out) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2*>(out + p.rank) = make_uint2(lo[0], lo[1]);
     }
   }
-  __syncwarp();
+  if (job.top) {
+    __syncthreads();
+    for (int x = threadIdx.x; x < share; x += kLowThreads) {
+      const int i = split + x * p.splits;
+      if (kept(i)) job.top[t0 + i] = __int_as_float(tops[i]);
+    }
+  }
 }
 
 // ---- up to 256 tokens ----------------------------------------------------------------------------------------------
@@ -115,7 +133,7 @@ __host__ __device__ constexpr int few_batch(int nb) { return nb <= 4 ? 4 : nb <=
 // matrix product with 64-byte pieces of every row.  Transposed P[a] (k rows of j) goes through shared memory.
 template <int NB, bool TRANS>
 __device__ __forceinline__ void few_tokens(const LowRankArgs& p, const LowJob& job, uint4* shared, const int* ids, const int* used,
-                                           int n_used, int t0, int split) {
+                                           int* tops, int n_used, int t0, int split) {
   constexpr int kBatch = few_batch(NB);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
   const bool bf = p.dtype == WINDQ_BF16;
@@ -211,7 +229,7 @@ __device__ __forceinline__ void few_tokens(const LowRankArgs& p, const LowJob& j
       }
       __syncthreads();
     }
-    constexpr int kRow = NB * 8 + 1;  // [token][j]
+    constexpr int kRow = NB * 8 + 4;  // [token][j]
     if (warp == 0) {
 #pragma unroll
       for (int n = 0; n < NB; n++)
@@ -221,7 +239,8 @@ __device__ __forceinline__ void few_tokens(const LowRankArgs& p, const LowJob& j
     __syncwarp();
     if (p.splits > 1) cluster_sync();
     else __syncthreads();
-    finish_tokens(p, job, t0, kFew, smem_addr(sums), kRow, split, ids, [&](int i) { return ids[i] == a; });
+    finish_tokens(p, job, t0, kFew, smem_addr(sums), kRow, split, ids, tops, [&](int i) { return ids[i] == a; });
+    __syncwarp();
     if (p.splits > 1) cluster_sync();
     else __syncthreads();
   }
@@ -230,7 +249,7 @@ __device__ __forceinline__ void few_tokens(const LowRankArgs& p, const LowJob& j
 template <int NB>
 __global__ void __launch_bounds__(kLowThreads) few_tokens_kernel(const __grid_constant__ LowRankArgs p) {
   extern __shared__ uint4 shared[];
-  __shared__ int ids[256], used[kFew], taken[kLowWarps];
+  __shared__ int ids[256], used[kFew], tops[kFew], taken[kLowWarps];
   launch_dependents();
   const int split = blockIdx.x % p.splits, tile = blockIdx.x / p.splits;
   if (blockIdx.y == p.slots) {
@@ -241,10 +260,11 @@ __global__ void __launch_bounds__(kLowThreads) few_tokens_kernel(const __grid_co
   int n_used;
   const int id = threadIdx.x < kFew ? valid_id(p, t0 + threadIdx.x) : -1, place = first_place(id, kFew, ids, taken, &n_used);
   if (place >= 0) used[place] = id;
+  if (threadIdx.x < kFew) tops[threadIdx.x] = 0;
   __syncthreads();
   const LowJob& job = p.job[blockIdx.z];
-  if (job.transposed) few_tokens<NB, true>(p, job, shared, ids, used, n_used, t0, split);
-  else few_tokens<NB, false>(p, job, shared, ids, used, n_used, t0, split);
+  if (job.transposed) few_tokens<NB, true>(p, job, shared, ids, used, tops, n_used, t0, split);
+  else few_tokens<NB, false>(p, job, shared, ids, used, tops, n_used, t0, split);
 }
 
 template <int NB>
@@ -257,7 +277,7 @@ windq_status launch_few(windq_ctx* ctx, int id, LowRankArgs p, cudaStream_t st) 
   while (p.splits < 8 && (int64_t)tiles * p.slots * p.jobs * p.splits * 2 <= 4 * ctx->sm_count &&
          (most + 31) / 32 >= 2 * kLowWarps * p.splits)
     p.splits *= 2;
-  const int sums = std::max(kLowWarps / 2 * NB * 128, kFew * (NB * 8 + 1)) * 4;
+  const int sums = std::max(kLowWarps / 2 * NB * 128, kFew * (NB * 8 + 4)) * 4;
   const bool trans = p.job[0].transposed || (p.jobs > 1 && p.job[1].transposed);
   const int smem = std::max(sums, trans ? kLowWarps * few_batch(NB) * 32 * (p.rank * 2 + 16) : 0);
   constexpr int kMost = 128 * 1024;
@@ -286,7 +306,9 @@ constexpr int kManyStages = 8;
 constexpr int kManySmem = 227 * 1024 - 3072;
 
 // A tile of 128 tokens (rows of the accumulator) times the P of its adapters (columns, 16-padded): as many adapters at a
-// time as 64 columns hold, one pass over K each -- prompts need one.  Blocks of a cluster share K.  Warps: one issues TMA
+// time as 128 columns hold (transposed, where an adapter takes a block of 64 columns of shared memory: two), one pass over
+// K each.  A tile in which one prompt ends and the next begins then still takes one pass; with one adapter a pass such
+// tiles took twice as long and with them the whole kernel (41 against 22 us for 8192 tokens of 4096 values, rank 64).  Blocks of a cluster share K.  Warps: one issues TMA
 // copies, one the products, four take the rows of their own adapter out of tensor memory.
 __global__ void __launch_bounds__(kLowThreads, 1)
     many_tokens_kernel(const __grid_constant__ CUtensorMap z0, const __grid_constant__ CUtensorMap p0,
@@ -295,7 +317,7 @@ __global__ void __launch_bounds__(kLowThreads, 1)
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t full_[kManyStages], empty_[kManyStages], done_, free_;
   __shared__ uint32_t tmem_slot;
-  __shared__ int dead, ids[256], used[kMany], taken[kLowWarps];
+  __shared__ int dead, ids[256], used[kMany], tops[kMany], taken[kLowWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   launch_dependents();
   const int split = blockIdx.x % p.splits, tile = blockIdx.x / p.splits;
@@ -308,8 +330,9 @@ __global__ void __launch_bounds__(kLowThreads, 1)
   const CUtensorMap* pmap = blockIdx.y ? &p1 : &p0;
   const bool trans = job.transposed;
   const int r = p.rank, wide = (r + 15) & ~15;
-  const int pack = trans ? 1 : max(1, 64 / wide);               // adapters of a pass
-  const uint32_t p_bytes = r > 64 ? 16384 : 8192, stage_bytes = kMany * 128 + p_bytes, columns = r > 64 ? 128 : 64;
+  const int pack = trans ? (r > 64 ? 1 : 2) : 128 / wide;      // adapters of a pass
+  const int apart = trans ? 64 : wide;                          // their columns
+  constexpr uint32_t stage_bytes = kMany * 128 + 16384, columns = 128;
   const uint32_t base = (smem_addr(raw) + 1023) & ~1023u, sums = base + p.stages * stage_bytes;
   auto full = [&](int s) { return smem_addr(&full_[s]); };
   auto empty = [&](int s) { return smem_addr(&empty_[s]); };
@@ -334,6 +357,7 @@ __global__ void __launch_bounds__(kLowThreads, 1)
   int n_used;
   const int id = tid < kMany ? valid_id(p, t0 + tid) : -1, place = first_place(id, kMany, ids, taken, &n_used);
   if (place >= 0) used[place] = id;
+  if (tid < kMany) tops[tid] = 0;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -348,18 +372,21 @@ __global__ void __launch_bounds__(kLowThreads, 1)
       bool ok = true;
       for (int pass = 0; ok && pass < passes; pass++) {
         const int count = min(pack, n_used - pass * pack);
-        const uint32_t bytes = kMany * 128 + (trans ? (r > 64 ? 16384 : 8192) : count * wide * 128);
-        for (int c = c0; c < c1; c++) {
+        const uint32_t bytes = kMany * 128 + (trans ? (r > 64 ? 16384 : count * 8192) : count * wide * 128);
+        // every block begins elsewhere in its part of K: rows are a power of two apart in most models, and blocks that
+        // walk them in step would meet on few memory channels
+        int c = c0 + (tile * 5 + split * 3) % max(1, c1 - c0);
+        for (int i = c0; i < c1; i++, c = c + 1 < c1 ? c + 1 : c0) {
           if (!(ok = mbar_wait(empty(s), phase ^ 1, &dead))) break;
           const uint32_t at = base + s * stage_bytes;
           mbar_expect(full(s), bytes);
           tma_load_2d<false>(at, zmap, c * 64, t0, full(s));
           if (trans) {
-            tma_load_3d<false>(at + kMany * 128, pmap, 0, c * 64, used[pass], full(s));
+            for (int u = 0; u < count; u++) tma_load_3d<false>(at + kMany * 128 + u * 8192, pmap, 0, c * 64, used[pass * pack + u], full(s));
             if (r > 64) tma_load_3d<false>(at + kMany * 128 + 8192, pmap, 64, c * 64, used[pass], full(s));
           } else {
-            for (int i = 0; i < count; i++)
-              tma_load_3d<false>(at + kMany * 128 + i * wide * 128, pmap, c * 64, 0, used[pass * pack + i], full(s));
+            for (int u = 0; u < count; u++)
+              tma_load_3d<false>(at + kMany * 128 + u * wide * 128, pmap, c * 64, 0, used[pass * pack + u], full(s));
           }
           if (++s == p.stages) s = 0, phase ^= 1;
         }
@@ -374,7 +401,7 @@ __global__ void __launch_bounds__(kLowThreads, 1)
       bool ok = true;
       for (int pass = 0; ok && pass < passes; pass++) {
         const int count = min(pack, n_used - pass * pack);
-        const uint32_t idesc = instr_desc(p.dtype, false, trans, 128, count * wide);
+        const uint32_t idesc = instr_desc(p.dtype, false, trans, 128, trans ? wide : count * wide);
         if (!(ok = mbar_wait(free, (pass & 1) ^ 1, &dead))) break;
         tc_fence_after();
         for (int c = c0; c < c1; c++) {
@@ -384,6 +411,11 @@ __global__ void __launch_bounds__(kLowThreads, 1)
 #pragma unroll
           for (int k = 0; k < 4; k++)
             mma_f16<false>(tmem, z_desc + off + k * (32 >> 4), p_desc + off + k * p_step, idesc, c > c0 || k > 0);
+          if (trans && count > 1) {
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+              mma_f16<false>(tmem + 64, z_desc + off + k * (32 >> 4), p_desc + off + (8192 >> 4) + k * p_step, idesc, c > c0 || k > 0);
+          }
           mma_commit<false>(empty(s), 0);
           if (++s == p.stages) s = 0, phase ^= 1;
         }
@@ -402,12 +434,12 @@ __global__ void __launch_bounds__(kLowThreads, 1)
         if (!__any_sync(0xffffffffu, keep)) continue;
         for (int c = 0; c < wide; c += 16) {
           uint32_t x[16];
-          tmem_load16(tmem + ((uint32_t)(quarter * 32) << 16) + i * wide + c, x);
+          tmem_load16(tmem + ((uint32_t)(quarter * 32) << 16) + i * apart + c, x);
           tmem_load_wait();
           if (keep) {
 #pragma unroll
             for (int k = 0; k < 16; k++)
-              if (c + k < r) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sums + (row * (r + 1) + c + k) * 4), "r"(x[k]) : "memory");
+              if (c + k < r) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sums + (row * (r + 4) + c + k) * 4), "r"(x[k]) : "memory");
           }
         }
       }
@@ -430,7 +462,8 @@ __global__ void __launch_bounds__(kLowThreads, 1)
     tc_fence_after();
     tmem_free<false>(tmem, columns);
   }
-  finish_tokens(p, job, t0, kMany, sums, r + 1, split, ids, [&](int i) { return ids[i] >= 0; });
+  finish_tokens(p, job, t0, kMany, sums, r + 4, split, ids, tops, [&](int i) { return ids[i] >= 0; });
+  __syncwarp();
   if (p.splits > 1) cluster_sync();
 }
 
@@ -440,7 +473,7 @@ windq_status launch_many(windq_ctx* ctx, LowRankArgs p, cudaStream_t st) {
   if (p.jobs > 1) least = std::min(least, (p.job[1].K + 63) / 64);
   p.splits = 1;
   while (p.splits < 8 && (int64_t)tiles * p.jobs * p.splits * 2 <= ctx->sm_count && least >= p.splits * 2 * 4) p.splits *= 2;
-  const int stage = kMany * 128 + (p.rank > 64 ? 16384 : 8192), sums = kMany * (p.rank + 1) * 4;
+  const int stage = kMany * 128 + 16384, sums = kMany * (p.rank + 4) * 4;
   p.stages = std::min(kManyStages, (kManySmem - 1024 - sums) / stage);
   const windq_status ready = prepare_kernel(ctx, kLowRankMany, many_tokens_kernel, kLowThreads, kManySmem, false);
   if (ready != WINDQ_OK) return ready;
@@ -474,7 +507,7 @@ windq_status launch_low_rank(windq_ctx* ctx, const LowRank& q, cudaStream_t st) 
   LowRankArgs p = {};
   for (int k = 0; k < q.jobs; k++) {
     const LowRankJob& j = q.job[k];
-    p.job[k] = LowJob{(const uint16_t*)j.Z, j.ldz, (const uint16_t*)j.P, j.S, j.top, (int)j.K, j.transposed};
+    p.job[k] = LowJob{(const uint16_t*)j.Z, j.ldz, (const uint16_t*)j.P, j.S, (uint16_t*)j.pair, j.top, (int)j.K, j.transposed};
   }
   p.jobs = q.jobs;
   p.T = (int)q.T;

@@ -4,8 +4,8 @@
 // A low-rank term is more reduction dimension: after the chunks of K the accumulator takes, for every adapter a that the
 // tile's tokens use, S (tokens x rank, zero in the rows of other tokens' adapters) times P[a].  So a tile whose tokens
 // share an adapter costs rank / K more than the bare product, any mix of adapters is right, and there is no second pass
-// over the output.  S is binary32; the tensor cores take 16 bits, so it enters as the sum of two 16-bit values (22 bits
-// for fp16, 16 for bf16), which keeps the rounding of the low-rank term below that of the result.
+// over the output.  S enters as the sum of two 16-bit values (22 bits for fp16, 16 for bf16; written by the low-rank
+// kernel), which keeps the rounding of the low-rank term below that of the result.
 //
 // Warps: one issues TMA copies, one issues matrix products, four write the S tiles and, after the tile, read the
 // accumulators and store.  Two layouts of a tile:
@@ -27,12 +27,13 @@ namespace {
 constexpr int kThreads = 192;
 constexpr int kMaxStages = 8;
 constexpr int kSmemLimit = 227 * 1024 - 2048;       // dynamic shared memory of one thread block per SM
+constexpr int kTallPitch = 132, kWidePitch = 260;    // binary32 sums of a split tile, rows free of bank conflicts
 constexpr int kSmemLimitTwo = 112 * 1024;           // of two
 
 struct ProjectArgs {
   int T, N, chunks, rank, n_adapters, dtype;
   const int32_t* adapter_of;
-  const float* S;
+  const uint16_t* pair;
   const int* lists;
   void* O;
   int64_t ldo;
@@ -73,7 +74,7 @@ __device__ __forceinline__ void tile_at(const ProjectArgs& p, int tile, int& tt,
 }
 
 template <bool TALL, bool TRANS>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
     project_kernel(const __grid_constant__ CUtensorMap zmap, const __grid_constant__ CUtensorMap wmap,
                    const __grid_constant__ CUtensorMap pmap, const __grid_constant__ ProjectArgs p) {
   extern __shared__ uint8_t raw[];
@@ -155,8 +156,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         const int* list = p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1);
         const int n_list = __ldcg(list);
+        int next = split < n_list ? __ldcg(list + 1 + split) : 0;
         for (int i = split; ok && i < n_list; i += p.splits) {
-          const int a = __ldcg(list + 1 + i);
+          const int a = next;
+          if (i + p.splits < n_list) next = __ldcg(list + 1 + i + p.splits);
           for (int e = 0; e < rank_chunks * parts; e++, at.next()) {
             const int rc = e / parts;
             if (!(ok = mbar_wait(empty(at.s), at.phase ^ 1, &dead))) break;
@@ -245,65 +248,58 @@ __global__ void __launch_bounds__(kThreads, 1)
         waited = true;
       }
       const int t0 = (tt * kBlocks + me) * p.token_rows;
-      // S: a thread writes rows e and e + 128 of the token tile
-      int mine[2];
+      // S: a thread writes rows e and e + 128 of the token tile, 16-byte pieces of eight values
+      constexpr int kRows = TALL ? 2 : 1;
+      int mine[kRows];
+      uint4 pieces[kRows][8];  // paired: the first terms, then the second; otherwise one of them
+      const uint16_t* src[kRows];
 #pragma unroll
-      for (int h = 0; h < 2; h++) {
+      for (int h = 0; h < kRows; h++) {
         const int row = e + h * 128, t = t0 + row;
         mine[h] = row < p.token_rows && t < p.T ? p.adapter_of[t] : -1;
-        if (mine[h] >= 0 && mine[h] < p.n_adapters)
-          for (int j = 0; j < p.rank; j += 32) asm volatile("prefetch.global.L1 [%0];" ::"l"(p.S + (int64_t)t * p.rank + j));
+        if (mine[h] >= p.n_adapters) mine[h] = -1;
+        src[h] = p.pair + (int64_t)(mine[h] >= 0 ? t : 0) * 2 * p.rank;
       }
+      auto load = [&](int rc, int part) {
+#pragma unroll
+        for (int h = 0; h < kRows; h++)
+#pragma unroll
+          for (int g = 0; g < 8; g++) {
+            const int j = paired ? (g & 3) * 8 : rc * 64 + g * 8;
+            pieces[h][g] = mine[h] >= 0 && j < p.rank
+                               ? __ldcg(reinterpret_cast<const uint4*>(src[h] + (paired ? g >> 2 : part) * p.rank + j))
+                               : make_uint4(0, 0, 0, 0);
+          }
+      };
       const int* list = p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1);
       const int n_list = __ldcg(list);
+      if (n_list > split && paired) load(0, 0);
+      int next = split < n_list ? __ldcg(list + 1 + split) : 0;
       for (int i = split; ok && i < n_list; i += p.splits) {
-        const int a = __ldcg(list + 1 + i);
+        const int a = next;
+        if (i + p.splits < n_list) next = __ldcg(list + 1 + i + p.splits);
         for (int x = 0; x < rank_chunks * parts; x++, ring.next()) {
           const int rc = x / parts, s = ring.s;
+          if (!paired) load(rc, x & 1);
           ok = mbar_wait(granted(s), (granted_phase >> s) & 1, &dead);
           granted_phase ^= 1u << s;
           if (!__all_sync(0xffffffffu, ok)) {
             ok = false;
             break;
           }
-          const int wide = ((min(64, p.rank - rc * 64) + 15) & ~15) >> 3;  // 16-byte pieces of a row, whole steps of K
+          const int wide = ((min(64, p.rank - rc * 64) + 15) & ~15) >> 3;  // pieces of whole steps of K
 #pragma unroll
-          for (int h = 0; h < 2; h++) {
+          for (int h = 0; h < kRows; h++) {
             const int row = e + h * 128;
             if (row >= p.token_rows) continue;
-            const float* src = p.S + (int64_t)(t0 + row) * p.rank + rc * 64;
             const uint32_t dst = base + s * stage_bytes + row * 128;
-            for (int g = 0; g < wide; g++) {
-              uint4 hi = make_uint4(0, 0, 0, 0), lo = hi;
-              if (mine[h] == a && rc * 64 + g * 8 < p.rank) {
-                const float4 u = *reinterpret_cast<const float4*>(src + g * 8), v = *reinterpret_cast<const float4*>(src + g * 8 + 4);
-                float y[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-                if (p.dtype == WINDQ_F16) {
 #pragma unroll
-                  for (int k = 0; k < 8; k++) y[k] = fminf(fmaxf(y[k], -131008.0f), 131008.0f);
-                }
-                uint32_t w[4], r[4];
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                  float2 first = make_float2(y[2 * k], y[2 * k + 1]);
-                  if (p.dtype == WINDQ_F16) {
-                    first.x = fminf(fmaxf(first.x, -65504.0f), 65504.0f);
-                    first.y = fminf(fmaxf(first.y, -65504.0f), 65504.0f);
-                  }
-                  w[k] = pack2(first.x, first.y, p.dtype);
-                  const float2 back = unpack2(w[k], p.dtype);
-                  r[k] = pack2(y[2 * k] - back.x, y[2 * k + 1] - back.y, p.dtype);
-                }
-                hi = make_uint4(w[0], w[1], w[2], w[3]);
-                lo = make_uint4(r[0], r[1], r[2], r[3]);
-              }
-              auto put = [&](int piece, const uint4& q) {
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + ((piece ^ (row & 7)) << 4)), "r"(q.x), "r"(q.y),
-                             "r"(q.z), "r"(q.w)
-                             : "memory");
-              };
-              put(g, paired || (x & 1) == 0 ? hi : lo);
-              if (paired) put(g + 4, lo);
+            for (int g = 0; g < 8; g++) {
+              if ((paired ? g & 3 : g) >= wide) continue;
+              const uint4 v = mine[h] == a ? pieces[h][g] : make_uint4(0, 0, 0, 0);
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + ((g ^ (row & 7)) << 4)), "r"(v.x), "r"(v.y), "r"(v.z),
+                           "r"(v.w)
+                           : "memory");
             }
           }
           fence_async_shared();
@@ -323,10 +319,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_load16(d + c, r);
         tmem_load_wait();
         if (p.splits > 1) {
-          // [column][lane], 129 apart: free of bank conflicts along either
+          // as the result lies: [token][output], the outputs of a tall tile being the lanes
+          if (TALL) {
 #pragma unroll
-          for (int k = 0; k < 16; k++)
-            asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + ((c + k) * 129 + at) * 4), "r"(r[k]) : "memory");
+            for (int k = 0; k < 16; k++)
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + ((c + k) * kTallPitch + at) * 4), "r"(r[k]) : "memory");
+          } else {
+#pragma unroll
+            for (int k = 0; k < 16; k += 4)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (at * kWidePitch + c + k) * 4), "r"(r[k]),
+                           "r"(r[k + 1]), "r"(r[k + 2]), "r"(r[k + 3])
+                           : "memory");
+          }
         } else if (TALL) {
           const int n = wt * 128 + at;
           if (n < p.N) {
@@ -374,21 +378,32 @@ __global__ void __launch_bounds__(kThreads, 1)
     // one tile a team: this block adds and stores its share of it
     int tt, wt;
     tile_at(p, blockIdx.x / team, tt, wt);
-    if (TALL) {
-      const int columns = min(p.token_rows, p.T - tt * p.token_rows);
-      for (int i = threadIdx.x; i < (columns - split + p.splits - 1) / p.splits * 128; i += kThreads) {
-        const int c = split + (i >> 7) * p.splits, at = i & 127, n = wt * 128 + at;
-        float x = 0.0f;
-        for (int q = 0; q < p.splits; q++) x += cluster_load(base + (c * 129 + at) * 4, q);
-        if (n < p.N) store1(p.O, (int64_t)(tt * p.token_rows + c) * p.ldo + n, p.dtype, x);
+    const int outputs = TALL ? 128 : 2 * p.weight_rows, quads = outputs / 4, pitch = TALL ? kTallPitch : kWidePitch;
+    const int t0 = TALL ? tt * p.token_rows : (tt * 2 + me) * 128, n0 = wt * outputs;
+    const int rows = min(TALL ? p.token_rows : 128, p.T - t0), items = max(0, (rows - split + p.splits - 1) / p.splits) * quads;
+    constexpr int U = 4;
+    for (int i = threadIdx.x; i < items; i += U * kThreads) {
+      uint32_t offset[U];
+      float4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const int q = min(i + u * kThreads, items - 1);
+        offset[u] = (uint32_t)((split + q / quads * p.splits) * pitch + q % quads * 4) * 4;
       }
-    } else {
-      const int share = 128 / p.splits, columns = 2 * p.weight_rows;
-      for (int i = threadIdx.x; i < share * columns; i += kThreads) {
-        const int c = i % columns, at = split * share + i / columns, n = wt * columns + c, t = (tt * 2 + me) * 128 + at;
-        float x = 0.0f;
-        for (int q = 0; q < p.splits; q++) x += cluster_load(base + (c * 129 + at) * 4, 2 * q + me);
-        if (t < p.T && n < p.N) store1(p.O, t * p.ldo + n, p.dtype, x);
+      cluster_sum<U>(base, offset, p.splits, me, kBlocks, x);
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const int q = i + u * kThreads, t = t0 + split + q / quads * p.splits, n = n0 + q % quads * 4;
+        if (q >= items || n >= p.N) continue;
+        if (n + 4 <= p.N) {
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.O) + t * p.ldo + n) =
+              make_uint2(pack2(x[u].x, x[u].y, p.dtype), pack2(x[u].z, x[u].w, p.dtype));
+        } else {
+          const float v[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+          for (int k = 0; k < 4; k++)
+            if (n + k < p.N) store1(p.O, t * p.ldo + n + k, p.dtype, v[k]);
+        }
       }
     }
     __syncwarp();
@@ -432,7 +447,7 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   p.n_adapters = (int)q.n_adapters;
   p.dtype = q.dtype;
   p.adapter_of = q.adapter_of;
-  p.S = q.S;
+  p.pair = (const uint16_t*)q.pair;
   p.lists = q.lists;
   p.O = q.O;
   p.ldo = q.ldo;

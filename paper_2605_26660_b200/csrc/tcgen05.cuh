@@ -162,11 +162,23 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void cluster_arrive(uint32_t remote_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote_bar) : "memory");
 }
-__device__ __forceinline__ float cluster_load(uint32_t addr, uint32_t rank) {
-  const uint32_t remote = cluster_addr(addr, rank);
-  float x;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(remote) : "memory");
-  return x;
+// Distributed shared memory answers after the better part of a microsecond, so sums over a cluster's blocks have several
+// loads in flight: `U` of them, at base + offset[u] in each of the n blocks of ranks first, first + stride, ...
+template <int U>
+__device__ __forceinline__ void cluster_sum(uint32_t base, const uint32_t (&offset)[U], int n, int first, int stride, float4 (&x)[U]) {
+#pragma unroll
+  for (int u = 0; u < U; u++) x[u] = make_float4(0, 0, 0, 0);
+  for (int q = 0; q < n; q++) {
+    const uint32_t from = cluster_addr(base, first + q * stride);
+    float4 y[U];
+#pragma unroll
+    for (int u = 0; u < U; u++)
+      asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                   : "=f"(y[u].x), "=f"(y[u].y), "=f"(y[u].z), "=f"(y[u].w)
+                   : "r"(from + offset[u]));
+#pragma unroll
+    for (int u = 0; u < U; u++) x[u].x += y[u].x, x[u].y += y[u].y, x[u].z += y[u].z, x[u].w += y[u].w;
+  }
 }
 
 // Programmatic dependent launch: the kernel may start before its predecessor in the stream has ended; it waits here
