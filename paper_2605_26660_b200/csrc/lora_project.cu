@@ -84,11 +84,12 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
   const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
   constexpr bool PAIR = !TALL;
   constexpr int kBlocks = PAIR ? 2 : 1;  // thread blocks that share a tile's products
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t rank = PAIR || p.splits > 1 ? cluster_rank() : 0, me = PAIR ? rank & 1 : 0, leader = rank & ~1u;
   const uint32_t token_bytes = p.token_rows * 128;
   const int weight_boxes = (p.weight_rows + 63) / 64;  // of a transposed weight
   const uint32_t weight_bytes = TRANS ? weight_boxes * 8192 : p.weight_rows * 128, stage_bytes = token_bytes + weight_bytes;
+  const uint32_t dead_ = smem_addr(&dead);
   auto full = [&](int s) { return smem_addr(&bars.full[s]); };
   auto empty = [&](int s) { return smem_addr(&bars.empty[s]); };
   auto granted = [&](int s) { return smem_addr(&bars.granted[s]); };
@@ -130,17 +131,17 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
   const int parts = paired ? 1 : 2;
 
   if (warp == 0) {
-    if (lane == 0) {
-      Ring at(p.stages);
-      const uint32_t to = PAIR ? cluster_addr(full(0), leader) : full(0);  // barriers of the issuing block
-      bool waited = false, ok = true;
-      for (int tile = blockIdx.x / team; ok && tile < tiles; tile += step) {
-        int tt, wt;
-        tile_at(p, tile, tt, wt);
-        const int t0 = (tt * kBlocks + me) * p.token_rows, n0 = (wt * kBlocks + me) * p.weight_rows;
-        for (int c = c0; c < c1; c++, at.next()) {
-          if (!(ok = mbar_wait(empty(at.s), at.phase ^ 1, &dead))) break;
-          const uint32_t dst = base + at.s * stage_bytes, bar = to + at.s * 8;
+    Ring at(p.stages);
+    const uint32_t to = PAIR ? cluster_addr(full(0), leader) : full(0);  // barriers of the issuing block
+    bool waited = false;
+    for (int tile = blockIdx.x / team; tile < tiles; tile += step) {
+      int tt, wt;
+      tile_at(p, tile, tt, wt);
+      const int t0 = (tt * kBlocks + me) * p.token_rows, n0 = (wt * kBlocks + me) * p.weight_rows;
+      for (int c = c0; c < c1; c++, at.next()) {
+        mbar_wait(empty(at.s), at.phase ^ 1, dead_);
+        const uint32_t dst = base + at.s * stage_bytes, bar = to + at.s * 8;
+        if (elect_one() && !*(volatile int*)&dead) {
           if (me == 0) mbar_expect(full(at.s), kBlocks * stage_bytes);
           tma_load_2d<PAIR>(dst, &zmap, c * 64, t0, bar);
           if (TRANS) {
@@ -149,21 +150,23 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
             tma_load_2d<PAIR>(dst + token_bytes, &wmap, c * 64, n0, bar);
           }
         }
-        if (!ok) break;
-        if (!waited) {
-          wait_for_predecessor();
-          waited = true;
-        }
-        const int* list = p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1);
-        const int n_list = __ldcg(list);
-        int next = split < n_list ? __ldcg(list + 1 + split) : 0;
-        for (int i = split; ok && i < n_list; i += p.splits) {
-          const int a = next;
-          if (i + p.splits < n_list) next = __ldcg(list + 1 + i + p.splits);
-          for (int e = 0; e < rank_chunks * parts; e++, at.next()) {
-            const int rc = e / parts;
-            if (!(ok = mbar_wait(empty(at.s), at.phase ^ 1, &dead))) break;
-            const uint32_t dst = base + at.s * stage_bytes + token_bytes, bar = to + at.s * 8;
+        __syncwarp();
+      }
+      if (!waited) {
+        wait_for_predecessor();
+        waited = true;
+      }
+      const int* list = p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1);
+      const int n_list = uniform(__ldcg(list));
+      int next = split < n_list ? __ldcg(list + 1 + split) : 0;
+      for (int i = split; i < n_list; i += p.splits) {
+        const int a = uniform(next);
+        if (i + p.splits < n_list) next = __ldcg(list + 1 + i + p.splits);
+        for (int e = 0; e < rank_chunks * parts; e++, at.next()) {
+          const int rc = e / parts;
+          mbar_wait(empty(at.s), at.phase ^ 1, dead_);
+          const uint32_t dst = base + at.s * stage_bytes + token_bytes, bar = to + at.s * 8;
+          if (elect_one() && !*(volatile int*)&dead) {
             mbar_arrive(granted(at.s));  // the stage's token tile is the writers' now
             if (me == 0) mbar_expect(full(at.s), kBlocks * weight_bytes);
             if (TRANS) {
@@ -172,59 +175,66 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
               tma_load_3d<PAIR>(dst, &pmap, rc * 64, n0, a, bar);
             }
           }
+          __syncwarp();
         }
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && me == 0) {
+    if (me == 0) {
       const uint32_t idesc = TALL ? instr_desc(p.dtype, TRANS, false, 128, p.token_rows)
                                   : instr_desc(p.dtype, false, TRANS, 256, 2 * p.weight_rows);
       const uint32_t mask = 3u << leader;
       // 16 values of K further: 32 bytes in a K-major tile, two groups of 8 rows in an MN-major one
-      const uint32_t weight_step = TRANS ? 2048 >> 4 : 32 >> 4, token_step = 32 >> 4;
+      constexpr uint32_t weight_step = TRANS ? 2048 >> 4 : 32 >> 4, token_step = 32 >> 4;
       const uint64_t z_desc = smem_desc(base, 16), w_desc = smem_desc(base + token_bytes, TRANS ? 8192 : 16);
       Ring at(p.stages);
       int turn = 0;
       uint32_t written_phase = 0;
-      bool waited = false, ok = true;
-      for (int tile = blockIdx.x / team; ok && tile < tiles; tile += step, turn++) {
+      bool waited = false;
+      for (int tile = blockIdx.x / team; tile < tiles; tile += step, turn++) {
         int tt, wt;
         tile_at(p, tile, tt, wt);
         const int b = p.accumulators == 2 ? turn & 1 : 0, use = p.accumulators == 2 ? turn >> 1 : turn;
-        if (!(ok = mbar_wait(free_(b), (use & 1) ^ 1, &dead))) break;
+        mbar_wait(free_(b), (use & 1) ^ 1, dead_);
         tc_fence_after();
         const uint32_t d = tmem + b * 256;
         auto product = [&](uint64_t z, uint64_t w, bool accumulate) { mma_f16<PAIR>(d, TALL ? w : z, TALL ? z : w, idesc, accumulate); };
         for (int c = c0; c < c1; c++, at.next()) {
-          if (!(ok = mbar_wait(full(at.s), at.phase, &dead))) break;
+          mbar_wait(full(at.s), at.phase, dead_);
           tc_fence_after();
           const uint64_t off = (uint64_t)(at.s * stage_bytes >> 4);
+          if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < 4; k++) product(z_desc + off + k * token_step, w_desc + off + k * weight_step, c > c0 || k > 0);
-          mma_commit<PAIR>(empty(at.s), mask);
+            for (int k = 0; k < 4; k++) product(z_desc + off + k * token_step, w_desc + off + k * weight_step, c > c0 || k > 0);
+            mma_commit<PAIR>(empty(at.s), mask);
+          }
+          __syncwarp();
         }
-        if (!ok) break;
         if (!waited) {
           wait_for_predecessor();
           waited = true;
         }
-        const int n_list = __ldcg(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1));
-        for (int i = split; ok && i < n_list; i += p.splits) {
+        const int n_list = uniform(__ldcg(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1)));
+        for (int i = split; i < n_list; i += p.splits) {
           for (int e = 0; e < rank_chunks * parts; e++, at.next()) {
             const int rc = e / parts;
-            if (!(ok = mbar_wait(full(at.s), at.phase, &dead) && mbar_wait(written(at.s), (written_phase >> at.s) & 1, &dead))) break;
+            mbar_wait(full(at.s), at.phase, dead_);
+            mbar_wait(written(at.s), (written_phase >> at.s) & 1, dead_);
             written_phase ^= 1u << at.s;
             tc_fence_after();
             const uint64_t off = (uint64_t)(at.s * stage_bytes >> 4);
             const int steps = (min(64, p.rank - rc * 64) + 15) >> 4;
-            for (int k = 0; k < steps; k++) product(z_desc + off + k * token_step, w_desc + off + k * weight_step, true);
-            if (paired)
-              for (int k = 0; k < steps; k++) product(z_desc + off + (k + 2) * token_step, w_desc + off + k * weight_step, true);
-            mma_commit<PAIR>(empty(at.s), mask);
+            if (elect_one()) {
+              for (int k = 0; k < steps; k++) product(z_desc + off + k * token_step, w_desc + off + k * weight_step, true);
+              if (paired)
+                for (int k = 0; k < steps; k++) product(z_desc + off + (k + 2) * token_step, w_desc + off + k * weight_step, true);
+              mma_commit<PAIR>(empty(at.s), mask);
+            }
+            __syncwarp();
           }
         }
-        if (!ok) break;
-        mma_commit<PAIR>(done(b), mask);
+        if (elect_one()) mma_commit<PAIR>(done(b), mask);
+        __syncwarp();
       }
     }
   } else {
@@ -238,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
       if (PAIR) cluster_arrive(cluster_addr(bar, leader));
       else mbar_arrive(bar);
     };
-    bool waited = false, ok = true;
+    bool waited = false;
     for (int tile = blockIdx.x / team; tile < tiles; tile += step, turn++) {
       int tt, wt;
       tile_at(p, tile, tt, wt);
@@ -275,18 +285,14 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
       const int n_list = __ldcg(list);
       if (n_list > split && paired) load(0, 0);
       int next = split < n_list ? __ldcg(list + 1 + split) : 0;
-      for (int i = split; ok && i < n_list; i += p.splits) {
+      for (int i = split; i < n_list; i += p.splits) {
         const int a = next;
         if (i + p.splits < n_list) next = __ldcg(list + 1 + i + p.splits);
         for (int x = 0; x < rank_chunks * parts; x++, ring.next()) {
           const int rc = x / parts, s = ring.s;
           if (!paired) load(rc, x & 1);
-          ok = mbar_wait(granted(s), (granted_phase >> s) & 1, &dead);
+          mbar_wait(granted(s), (granted_phase >> s) & 1, dead_);
           granted_phase ^= 1u << s;
-          if (!__all_sync(0xffffffffu, ok)) {
-            ok = false;
-            break;
-          }
           const int wide = ((min(64, p.rank - rc * 64) + 15) & ~15) >> 3;  // pieces of whole steps of K
 #pragma unroll
           for (int h = 0; h < kRows; h++) {
@@ -309,8 +315,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
       }
       // the accumulators of the tile
       const int b = p.accumulators == 2 ? turn & 1 : 0, use = p.accumulators == 2 ? turn >> 1 : turn;
-      ok = ok && mbar_wait(done(b), use & 1, &dead);
-      if (!__all_sync(0xffffffffu, ok)) break;
+      mbar_wait(done(b), use & 1, dead_);
       tc_fence_after();
       const uint32_t d = tmem + b * 256 + ((uint32_t)(quarter * 32) << 16);
       const int columns = TALL ? p.token_rows : 2 * p.weight_rows, at = quarter * 32 + lane;
@@ -361,13 +366,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
   }
   __syncwarp();
   __syncthreads();
-  if (dead && threadIdx.x == 0) {
-    // copies this thread block has issued may still be landing in its shared memory
-    const long long begin = clock64();
-    while (clock64() - begin < 4000000) {
-    }
-    atomicAdd(p.stalls, 1ull);
-  }
+  if (dead) settle(p.stalls);
   __syncwarp();
   if (team > 1) cluster_sync();  // no more arrivals from other blocks; their sums are in shared memory
   if (warp == 1) {
@@ -456,8 +455,10 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   p.token_rows = tall ? token_tile(q.T) : 128;
   p.weight_rows = 128;
   p.token_tiles = (int)((q.T + p.token_rows * blocks_of_tile - 1) / (p.token_rows * blocks_of_tile));
-  const bool two = tall && p.token_rows <= 64;  // thread blocks an SM
-  const int64_t slots = (int64_t)ctx->sm_count * (two ? 2 : 1) / blocks_of_tile;
+  // tall tiles: two thread blocks an SM, so that one loads while the other joins and stores, as long as the sums of a
+  // split tile fit into half of the shared memory
+  const bool two = tall && p.token_rows * kTallPitch * 4 <= kSmemLimitTwo - 1024;
+  const int64_t slots = tall ? (int64_t)ctx->sm_count * (two ? 2 : 1) : ctx->sm_count / 2;
   p.splits = 1;
   if (!tall) {
     // outputs of a tile: the width that takes the fewest rounds over the GPU, a chunk of K costing 600 + width (0.39 us at
@@ -487,7 +488,8 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   p.accumulators = !tall && p.splits == 1 ? 2 : 1;
   p.columns = tall ? (p.token_rows <= 32 ? 32 : p.token_rows <= 64 ? 64 : p.token_rows <= 128 ? 128 : 256) : 256 * p.accumulators;
   const int64_t blocks = (p.splits > 1 ? tiles * p.splits : std::min(tiles, slots)) * blocks_of_tile;
-  const int smem = 1024 + p.stages * stage;
+  const int sums = p.splits > 1 ? (tall ? p.token_rows * kTallPitch : 128 * kWidePitch) * 4 : 0;
+  const int smem = 1024 + std::max(p.stages * stage, sums);
 
   CUtensorMap z, w, pm;
   WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");

@@ -19,33 +19,52 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
 // Every wait of a kernel ends: after about two seconds, or as soon as another wait of its thread block has given up, it
-// returns false and raises *dead (shared memory); the caller leaves its loop.
+// raises *dead (a word of shared memory) and falls through.  The roles then run to their ends without issuing copies.
+//
+// The loop stays inside the asm block on purpose: a branch the compiler saw would make the control flow of the issuing
+// warps look divergent, and with it every operand of the tcgen05 and TMA instructions, which want uniform registers; a
+// product then took 70 cycles to issue, more than most of them run.
 constexpr long long kWaitCycles = 4000000000ll;
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
-  if (mbar_try(bar, parity)) return true;
-  const long long begin = clock64();
-  while (!mbar_try(bar, parity)) {
-    if (*dead) return false;
-    if (clock64() - begin > kWaitCycles) {
-      *dead = 1;
-      return false;
-    }
-  }
-  return true;
+__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, uint32_t dead) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .u64 begin, now;\n\t.reg .u32 d;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t"
+      "@p bra DONE;\n\t"
+      "mov.u64 begin, %%clock64;\n\t"
+      "AGAIN:\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t"
+      "@p bra DONE;\n\t"
+      "ld.volatile.shared.u32 d, [%2];\n\t"
+      "setp.ne.u32 p, d, 0;\n\t"
+      "@p bra DONE;\n\t"
+      "mov.u64 now, %%clock64;\n\t"
+      "sub.u64 now, now, begin;\n\t"
+      "setp.lt.u64 p, now, %3;\n\t"
+      "@p bra AGAIN;\n\t"
+      "st.volatile.shared.u32 [%2], 1;\n\t"
+      "DONE:\n\t}" ::"r"(bar),
+      "r"(parity), "r"(dead), "n"(kWaitCycles)
+      : "memory");
 }
+// After a wait has given up, by all threads of the block: lets copies and products that were issued come to their ends
+// before the memory they use is given back, and counts the block.
+__device__ __forceinline__ void settle(unsigned long long* stalls) {
+  const long long begin = clock64();
+  while (clock64() - begin < 4000000) {
+  }
+  if (threadIdx.x == 0) atomicAdd(stalls, 1ull);
+}
+// One lane of a converged warp, the same every time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t on;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(on));
+  return on != 0;
+}
+// The warp's index, and a value all lanes agree on, in a form the compiler knows to be uniform.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 // Tensor-map copies into this block's shared memory; `bar` may, with PAIR, be a barrier of the other block of the pair.
 template <bool PAIR>

@@ -108,7 +108,10 @@ SHAPES = [  # T, R, C, rank, adapters, kind
     (65, 384, 96, 128, 3, "mixed"), (100, 256, 256, 32, 100, "distinct"), (128, 264, 392, 16, 9, "mixed"), (129, 136, 512, 40, 3, "none"),
     (200, 264, 72, 72, 6, "mixed"), (255, 513, 128, 8, 2, "segments"), (256, 248, 456, 16, 64, "distinct"), (257, 96, 640, 24, 3, "mixed"),
     (300, 520, 648, 64, 40, "mixed"), (511, 40, 88, 16, 2, "segments"), (640, 777, 320, 120, 5, "segments"), (1025, 512, 1032, 16, 4, "invalid"),
-    (2100, 264, 520, 32, 3, "segments"), (48, 640, 4160, 16, 24, "mixed"), (203, 1200, 8192, 32, 48, "mixed"), (330, 520, 6000, 16, 30, "mixed"), (3000, 1288, 136, 8, 1, "one"),
+    (2100, 264, 520, 32, 3, "segments"), (48, 640, 4160, 16, 24, "mixed"), (203, 1200, 8192, 32, 48, "mixed"), (330, 520, 6000, 16, 30, "mixed"),
+    # tiles that are split along the reduction, at every height of a tile whose sums share its memory
+    (112, 200, 1096, 16, 3, "mixed"), (144, 1030, 2056, 48, 3, "segments"), (192, 2056, 1032, 8, 20, "mixed"), (208, 136, 4104, 32, 3, "mixed"),
+    (209, 2050, 2056, 64, 3, "segments"), (240, 1096, 1096, 24, 7, "mixed"), (256, 4104, 4104, 16, 5, "segments"), (258, 4100, 4104, 128, 3, "mixed"), (3000, 1288, 136, 8, 1, "one"),
 ]
 
 
