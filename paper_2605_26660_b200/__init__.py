@@ -965,42 +965,47 @@ def windq_scratch_bytes_lora_backward(T: int, R: int, C: int, n_adapters: int, r
     return int(_lib.windq_scratch_bytes_lora_backward(T, R, C, n_adapters, rank))
 
 
+def _raw_stream(ctx: Context, stream) -> int:
+    """The handle of ``stream``, or of the context's device's current one (without building a Stream object: the small
+    calls below are bound by what the host does)."""
+    return torch._C._cuda_getCurrentRawStream(ctx.device) if stream is None else stream.cuda_stream
+
+
 def _lora_args(X, W, A, B, scaling, adapter_of):
     """Checks the arguments the two adapter calls share; returns (dtype code, T, C, ldx, R, ldw, n_adapters, rank)."""
     dt = X.dtype
     if dt is not torch.float16 and dt is not torch.bfloat16:
         raise TypeError("X must be torch.float16 or torch.bfloat16, got %s" % dt)
-    if X.dim() != 2 or W.dim() != 2 or A.dim() != 3 or B.dim() != 3 or scaling.dim() != 1 or adapter_of.dim() != 1:
-        raise ValueError("X and W have 2 dimensions, A and B 3, scaling and adapter_of 1")
-    T, C = X.shape
-    R, n, rank = W.shape[0], A.shape[0], A.shape[1]
-    ldx, ldw = X.stride(0), W.stride(0)
-    if not (X.is_cuda and W.is_cuda and A.is_cuda and B.is_cuda and scaling.is_cuda and adapter_of.is_cuda):
-        raise TypeError("X, W, A, B, scaling and adapter_of must be CUDA tensors")
     if W.dtype is not dt or A.dtype is not dt or B.dtype is not dt:
         raise TypeError("W, A and B must have the type of X, %s" % dt)
     if scaling.dtype is not torch.float32 or adapter_of.dtype is not torch.int32:
         raise TypeError("scaling must be torch.float32 and adapter_of torch.int32")
-    if W.shape[1] != C or A.shape[2] != C or B.shape != (n, R, rank) or scaling.shape[0] != n or adapter_of.shape[0] != T:
+    if not (X.is_cuda and W.is_cuda and A.is_cuda and B.is_cuda and scaling.is_cuda and adapter_of.is_cuda):
+        raise TypeError("X, W, A, B, scaling and adapter_of must be CUDA tensors")
+    if X.dim() != 2 or W.dim() != 2 or A.dim() != 3 or B.dim() != 3 or scaling.dim() != 1 or adapter_of.dim() != 1:
+        raise ValueError("X and W have 2 dimensions, A and B 3, scaling and adapter_of 1")
+    T, C = X.shape
+    R, wide = W.shape
+    n, rank, deep = A.shape
+    if wide != C or deep != C or B.shape != (n, R, rank) or scaling.shape[0] != n or adapter_of.shape[0] != T:
         raise ValueError("shapes do not fit: X [T, C], W [R, C], A [n, rank, C], B [n, R, rank], scaling [n], adapter_of [T]")
-    if (X.stride(1) != 1 and C > 1) or (W.stride(1) != 1 and C > 1):
+    (ldx, x1), (ldw, w1) = X.stride(), W.stride()
+    if (x1 != 1 or w1 != 1) and C > 1:
         raise ValueError("X and W must be row-major (unit stride along columns)")
     if not (A.is_contiguous() and B.is_contiguous() and scaling.is_contiguous() and adapter_of.is_contiguous()):
         raise ValueError("A, B, scaling and adapter_of must be contiguous")
-    if T == 1:      # the stride of a single row means nothing, and torch may report any
-        ldx = max(ldx, C)
-        ldx += -ldx % 8
-    return _DTYPE_CODES[dt], T, C, ldx, R, (ldw if R > 1 else C), n, rank
+    # the stride of a single row means nothing, and torch may report any
+    return _DTYPE_CODES[dt], T, C, (ldx if T > 1 else C + -C % 8), R, (ldw if R > 1 else C + -C % 8), n, rank
 
 
-def _row_output(t, rows, cols, dtype, device, name):
+def _row_output(t, rows, cols, like, name):
     """A caller's [rows, cols] output, or a new one whose rows are padded to a multiple of 8 elements."""
     if t is None:
         if cols % 8 == 0:
-            return torch.empty((rows, cols), dtype=dtype, device=device), cols
+            return like.new_empty((rows, cols)), cols
         ld = cols + -cols % 8
-        return torch.empty((rows, ld), dtype=dtype, device=device)[:, :cols], ld
-    _need(t, dtype, name, 2)
+        return like.new_empty((rows, ld))[:, :cols], ld
+    _need(t, like.dtype, name, 2)
     if t.shape != (rows, cols) or (t.stride(1) != 1 and cols > 1):
         raise ValueError("%s must be a row-major [%d, %d] tensor" % (name, rows, cols))
     return t, (t.stride(0) if rows > 1 else cols + -cols % 8)
@@ -1014,10 +1019,10 @@ def windq_lora_forward(ctx: Context, X: torch.Tensor, W: torch.Tensor, A: torch.
     X [T, C], W [R, C] (as windq_apply_plan leaves it), A [n, rank, C], B [n, R, rank], all fp16 or all bf16;
     scaling fp32 [n]; adapter_of int32 [T].  Returns Y [T, R] of the same type (``out`` if given)."""
     code, T, C, ldx, R, ldw, n, rank = _lora_args(X, W, A, B, scaling, adapter_of)
-    out, ldy = _row_output(out, T, R, X.dtype, X.device, "out")
+    out, ldy = _row_output(out, T, R, X, "out")
     ctx._check(_lib.windq_lora_forward(ctx._h, code, X.data_ptr(), T, C, ldx, W.data_ptr(), R, ldw, A.data_ptr(), B.data_ptr(),
                                        n, rank, scaling.data_ptr(), adapter_of.data_ptr(), out.data_ptr(), ldy,
-                                       _stream(stream)))
+                                       _raw_stream(ctx, stream)))
     return out
 
 
@@ -1034,20 +1039,20 @@ def windq_lora_backward(ctx: Context, X: torch.Tensor, W: torch.Tensor, A: torch
         raise ValueError("dY must be a row-major [T, R] tensor")
     lddy = dY.stride(0) if T > 1 else R + -R % 8
     out = dict(out) if out else {}
-    dx, lddx = _row_output(out.get("dx"), T, C, X.dtype, X.device, "dx") if want_dx else (None, 0)
+    dx, lddx = _row_output(out.get("dx"), T, C, X, "dx") if want_dx else (None, 0)
     dA, dB = (out.get("dA"), out.get("dB")) if want_dab else (None, None)
     if want_dab:
         if dA is None:
-            dA = torch.empty((n, rank, C), dtype=torch.float32, device=X.device)
+            dA = X.new_empty((n, rank, C), dtype=torch.float32)
         if dB is None:
-            dB = torch.empty((n, R, rank), dtype=torch.float32, device=X.device)
+            dB = X.new_empty((n, R, rank), dtype=torch.float32)
         _need(dA, torch.float32, "dA", 3)
         _need(dB, torch.float32, "dB", 3)
         if dA.shape != A.shape or dB.shape != B.shape or not (dA.is_contiguous() and dB.is_contiguous()):
             raise ValueError("dA and dB must be contiguous and have the shapes of A and B")
     ctx._check(_lib.windq_lora_backward(ctx._h, code, X.data_ptr(), T, C, ldx, W.data_ptr(), R, ldw, A.data_ptr(), B.data_ptr(),
                                         n, rank, scaling.data_ptr(), adapter_of.data_ptr(), dY.data_ptr(), lddy, _ptr(dx), lddx,
-                                        _ptr(dA), _ptr(dB), _stream(stream)))
+                                        _ptr(dA), _ptr(dB), _raw_stream(ctx, stream)))
     return dict(dx=dx, dA=dA, dB=dB)
 
 
@@ -1105,6 +1110,7 @@ class AdamwTensors:
                                       *(None if t is None else t.data_ptr() for t in scales),
                                       None if copy is None else copy.data_ptr(), n)
         self._keep = (list(params), list(m), list(v), m_scale, r_scale, copies)
+        self._sizes = [p.numel() for p in params]
         self._codes = (_DTYPE_CODES[self.param_dtype], _DTYPE_CODES[self.grad_dtype], _DTYPE_CODES[self.copy_dtype], self.state_bits)
         self.set_grads(grads)
 
@@ -1137,24 +1143,27 @@ def windq_adamw_step(ctx: Context, tensors: AdamwTensors, *, step: int, lr: floa
         if grad_scale.numel() != 1:
             raise ValueError("grad_scale must hold one value")
     ctx._check(_lib.windq_adamw_step(ctx._h, tensors._jobs, len(tensors._jobs), *tensors._codes, int(step), lr, beta1, beta2, eps,
-                                     weight_decay, _ptr(grad_scale), _stream(stream)))
+                                     weight_decay, _ptr(grad_scale), _raw_stream(ctx, stream)))
 
 
 def windq_adamw_states(ctx: Context, tensors: AdamwTensors, m_out=None, v_out=None, *, stream=None):
     """The fp32 values that 8-bit states stand for: (list of m, list of v), written to the given tensors if any."""
     if tensors.state_bits != 8:
         raise ValueError("the states are not held in 8 bits")
-    params, k = tensors._keep[0], len(tensors)
+    sizes, k = tensors._sizes, len(tensors)
     outs, arrays = [], []
     for given, name in ((m_out, "m_out"), (v_out, "v_out")):
         if given is None:
-            given = [torch.empty(p.shape, dtype=torch.float32, device=p.device) for p in params]
+            given = [torch.empty(p.shape, dtype=torch.float32, device=p.device) for p in tensors._keep[0]]
         elif len(given) != k:
             raise ValueError("%s must have one entry per parameter" % name)
         else:
-            for t, p in zip(given, params):
-                AdamwTensors._flat(t, torch.float32, p.numel(), name)
+            # hundreds of tensors a call: the checks go over whole lists
+            if list(map(torch.Tensor.numel, given)) != sizes or not all(map(torch.Tensor.is_contiguous, given)):
+                raise ValueError("%s: a tensor is not contiguous or has not the size of its parameter" % name)
+            if {(t.dtype, t.is_cuda) for t in given} != {(torch.float32, True)}:
+                raise TypeError("%s must be torch.float32 CUDA tensors" % name)
         outs.append(given)
-        arrays.append((ctypes.c_void_p * k)(*[t.data_ptr() for t in given]))
-    ctx._check(_lib.windq_adamw_states(ctx._h, tensors._jobs, k, arrays[0], arrays[1], _stream(stream)))
+        arrays.append((ctypes.c_void_p * k)(*map(torch.Tensor.data_ptr, given)))
+    ctx._check(_lib.windq_adamw_states(ctx._h, tensors._jobs, k, arrays[0], arrays[1], _raw_stream(ctx, stream)))
     return tuple(outs)
