@@ -10,6 +10,7 @@ be built, importing this package raises.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 import torch
@@ -1056,6 +1057,7 @@ def windq_lora_backward(ctx: Context, X: torch.Tensor, W: torch.Tensor, A: torch
     return dict(dx=dx, dA=dA, dB=dB)
 
 
+_DTYPE_OF, _ON_CUDA = operator.attrgetter("dtype"), operator.attrgetter("is_cuda")
 ADAMW_BLOCK = 256   # elements of a tensor that share the scales of 8-bit states
 
 
@@ -1161,7 +1163,7 @@ def windq_adamw_states(ctx: Context, tensors: AdamwTensors, m_out=None, v_out=No
             # hundreds of tensors a call: the checks go over whole lists
             if list(map(torch.Tensor.numel, given)) != sizes or not all(map(torch.Tensor.is_contiguous, given)):
                 raise ValueError("%s: a tensor is not contiguous or has not the size of its parameter" % name)
-            if {(t.dtype, t.is_cuda) for t in given} != {(torch.float32, True)}:
+            if set(map(_DTYPE_OF, given)) != {torch.float32} or not all(map(_ON_CUDA, given)):
                 raise TypeError("%s must be torch.float32 CUDA tensors" % name)
         outs.append(given)
         arrays.append((ctypes.c_void_p * k)(*map(torch.Tensor.data_ptr, given)))

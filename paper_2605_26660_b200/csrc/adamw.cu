@@ -1,7 +1,9 @@
 // One AdamW step over many tensors, states in 32 or in 8 bits, and the values of 8-bit states.
 //
 // Every element is read once and written once, so the step is bound by HBM: 28 bytes an element with fp32 parameter,
-// gradient and states, 16 (12 + two codes read and written) with 8-bit states.
+// gradient and states, 16 (12 + two codes read and written) with 8-bit states.  At the measured copy rate that leaves an
+// SM about 90 instructions an element with 8-bit states, and a plain version of that kernel took 119 (three square roots
+// and a quotient among them), so its arithmetic is written for few instructions; see adamw8_kernel.
 //
 // A warp owns 256 consecutive elements of one tensor -- the block that shares the scales of 8-bit states, so that their
 // two maxima are warp reductions -- and a lane eight of them, loaded as 128-bit words.  A thread block takes eight such
@@ -9,6 +11,8 @@
 // a kernel parameter: any mix of tensor sizes is one launch, and nothing is copied to the device before it.
 #include <math.h>
 
+#include "fit_device.cuh"
+#include "tcgen05.cuh"
 #include "typed.cuh"
 
 namespace windq {
@@ -28,24 +32,22 @@ struct AdamwEntry {
   void* copy;
   int64_t n;
 };
-// Kernel parameters may hold 32764 bytes; the small table keeps the launches of a few tensors cheap.
-template <int N>
+// The tensors of one launch: as many as 4 KB of kernel parameters hold.  (Tables of 448 tensors in 32 KB gained nothing for
+// 448 tensors, whose 8 launches overlap, and cost the host 5 us more for 14 or 120.)
+constexpr int kTable = 56;
 struct AdamwTable {
-  AdamwEntry e[N];
-  int first[N];  // first chunk of every tensor
+  AdamwEntry e[kTable];
+  int first[kTable];  // first chunk of every tensor
   int count;
 };
-constexpr int kSmallTable = 32, kLargeTable = 448;
-static_assert(sizeof(AdamwTable<kLargeTable>) + 128 < 32764, "kernel parameters");
 
 struct AdamwFactors {
-  float beta1, one_minus_beta1, beta2, one_minus_beta2, keep, rate, unbias, eps;
+  float beta1, one_minus_beta1, beta2, one_minus_beta2, keep, rate, unbias, eps, one;
   const float* grad_scale;
   int param_dtype, grad_dtype, copy_dtype;
 };
 
-template <int N>
-__device__ __forceinline__ int find_entry(const AdamwTable<N>& tab, int chunk) {
+__device__ __forceinline__ int find_entry(const AdamwTable& tab, int chunk) {
   int lo = 0, hi = tab.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -53,12 +55,6 @@ __device__ __forceinline__ int find_entry(const AdamwTable<N>& tab, int chunk) {
     else hi = mid - 1;
   }
   return lo;
-}
-
-__device__ __forceinline__ float warp_max(float x) {
-#pragma unroll
-  for (int d = 16; d; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-  return x;
 }
 
 constexpr float kPerM = (float)(1.0 / 127), kPerR = (float)(1.0 / 255);
@@ -74,46 +70,26 @@ __device__ __forceinline__ float decode_r(int q, float scale) {
 }
 
 // The eight codes of a lane, little-endian in two words.
-__device__ __forceinline__ void split_bytes(uint2 w, int (&q)[8], bool is_signed) {
-#pragma unroll
-  for (int k = 0; k < 8; k++) {
-    const uint32_t b = ((k < 4 ? w.x : w.y) >> (8 * (k & 3))) & 0xffu;
-    q[k] = is_signed ? (int)(int8_t)b : (int)b;
-  }
-}
-__device__ __forceinline__ uint2 join_bytes(const int (&q)[8]) {
+__device__ __forceinline__ uint2 load_codes(const void* base, int64_t i, int live) {
+  const uint8_t* p = static_cast<const uint8_t*>(base) + i;
+  if (live == 8) return *reinterpret_cast<const uint2*>(p);
   uint2 w = make_uint2(0, 0);
 #pragma unroll
-  for (int k = 0; k < 8; k++) {
-    const uint32_t b = ((uint32_t)q[k] & 0xffu) << (8 * (k & 3));
-    if (k < 4) w.x |= b;
-    else w.y |= b;
-  }
+  for (int k = 0; k < 8; k++)
+    if (k < live) {
+      if (k < 4) w.x |= (uint32_t)p[k] << (8 * k);
+      else w.y |= (uint32_t)p[k] << (8 * (k - 4));
+    }
   return w;
 }
-__device__ __forceinline__ void load_codes(const void* base, int64_t i, int live, bool is_signed, int (&q)[8]) {
-  const uint8_t* p = static_cast<const uint8_t*>(base) + i;
-  uint2 w = make_uint2(0, 0);
-  if (live == 8) {
-    w = *reinterpret_cast<const uint2*>(p);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; k++)
-      if (k < live) {
-        if (k < 4) w.x |= (uint32_t)p[k] << (8 * k);
-        else w.y |= (uint32_t)p[k] << (8 * (k - 4));
-      }
-  }
-  split_bytes(w, q, is_signed);
-}
-__device__ __forceinline__ void store_codes(void* base, int64_t i, int live, const int (&q)[8]) {
+__device__ __forceinline__ void store_codes(void* base, int64_t i, int live, uint2 w) {
   uint8_t* p = static_cast<uint8_t*>(base) + i;
   if (live == 8) {
-    *reinterpret_cast<uint2*>(p) = join_bytes(q);
+    *reinterpret_cast<uint2*>(p) = w;
   } else {
 #pragma unroll
     for (int k = 0; k < 8; k++)
-      if (k < live) p[k] = (uint8_t)q[k];
+      if (k < live) p[k] = (uint8_t)((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
   }
 }
 __device__ __forceinline__ void load_any(const void* base, int64_t i, int dt, int live, float (&x)[8]) {
@@ -125,119 +101,200 @@ __device__ __forceinline__ void store_any(void* base, int64_t i, int dt, int liv
   else store_some(base, i, dt, live, x);
 }
 
-template <int N, bool BITS8>
-__global__ void __launch_bounds__(kWarps * 32) adamw_kernel(const __grid_constant__ AdamwTable<N> tab,
-                                                            const __grid_constant__ AdamwFactors f) {
+__global__ void __launch_bounds__(kWarps * 32) adamw32_kernel(const __grid_constant__ AdamwTable tab,
+                                                              const __grid_constant__ AdamwFactors f) {
+  launch_dependents();
+  const int j = find_entry(tab, blockIdx.x);
+  const AdamwEntry& e = tab.e[j];
+  const int64_t block = (int64_t)(blockIdx.x - tab.first[j]) * kWarps + (threadIdx.x >> 5);
+  const int64_t n = e.n, i = block * kBlock + (threadIdx.x & 31) * 8;
+  if (i >= n) return wait_for_predecessor();
+  const int live = i + 8 <= n ? 8 : (int)(n - i);
+  float p[8], g[8], m[8], v[8];
+  load_any(e.grad, i, f.grad_dtype, live, g);
+  load_any(e.param, i, f.param_dtype, live, p);
+  load_any(e.m, i, WINDQ_F32, live, m);
+  load_any(e.v, i, WINDQ_F32, live, v);
+  const float scale = f.grad_scale ? *f.grad_scale : 1.0f;  // a product with 1 is exact
+#pragma unroll
+  for (int k = 0; k < 8; k++) {
+    const float gk = g[k] * scale;
+    m[k] = m[k] * f.beta1 + gk * f.one_minus_beta1;
+    v[k] = v[k] * f.beta2 + (gk * gk) * f.one_minus_beta2;
+    p[k] = p[k] * f.keep - (m[k] * f.rate) / (sqrtf(v[k]) * f.unbias + f.eps);
+  }
+  store_any(e.param, i, f.param_dtype, live, p);
+  if (e.copy) store_any(e.copy, i, f.copy_dtype, live, p);
+  store_any(e.m, i, WINDQ_F32, live, m);
+  store_any(e.v, i, WINDQ_F32, live, v);
+  wait_for_predecessor();
+}
+
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// Byte k of a word of codes as a binary32 value, offset by 2^23: the byte becomes the low end of a significand.
+__device__ __forceinline__ float code_bits(uint32_t w, int k) { return __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7550 | k)); }
+constexpr float kShift = 8388608.0f;   // 2^23
+constexpr float kRound = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer (to nearest even), kept in the low bits
+
+// rint(sqrt(x) * levels) of eight values in [0, 1], plus kRound; values with their signs when `sign` is given.  The
+// hardware's square root is off by 2^-22 of itself at most, the product by another 2^-24: less than `guard` of a code.  Only
+// where that could cross a rounding boundary is the correctly rounded root taken.
+template <bool SIGNED>
+__device__ __forceinline__ void encode8(const float (&x)[8], const float (&sign)[8], float levels, float guard, float (&out)[8]) {
+  float worst = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) {
+    float2 y;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fabsf(x[k])));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fabsf(x[k + 1])));
+    y = mul2(y, both(levels));
+    const float2 r = add2(y, both(kRound)), off = fma2(add2(r, both(-kRound)), both(-1.0f), y);
+    worst = fmaxf(worst, fmaxf(fabsf(off.x), fabsf(off.y)));
+    if (SIGNED) {
+      // the same code with the sign of the value: kRound - code for a negative one
+      out[k] = sign[k] < 0.0f ? 2.0f * kRound - r.x : r.x;
+      out[k + 1] = sign[k + 1] < 0.0f ? 2.0f * kRound - r.y : r.y;
+    } else {
+      out[k] = r.x;
+      out[k + 1] = r.y;
+    }
+  }
+  if (worst > 0.5f - guard) {
+#pragma unroll
+    for (int k = 0; k < 8; k++) {
+      const float r = sqrtf(fabsf(x[k])) * levels + kRound;
+      out[k] = SIGNED && sign[k] < 0.0f ? 2.0f * kRound - r : r;
+    }
+  }
+}
+// The low bytes of eight such values.
+__device__ __forceinline__ uint2 low_bytes(const float (&x)[8]) {
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; h++) {
+    const uint32_t a = __byte_perm(__float_as_uint(x[4 * h]), __float_as_uint(x[4 * h + 1]), 0x0040);
+    const uint32_t b = __byte_perm(__float_as_uint(x[4 * h + 2]), __float_as_uint(x[4 * h + 3]), 0x0040);
+    w[h] = __byte_perm(a, b, 0x5410);
+  }
+  return make_uint2(w[0], w[1]);
+}
+
+// What keeps the instructions few: pairs of binary32 operations in one (each half rounded like the scalar one), codes turned
+// into values and back by adding constants instead of conversions, and square roots for codes taken from the approximate
+// instruction wherever that decides the code.  All results are those of the formulas, bit for bit.
+__global__ void __launch_bounds__(kWarps * 32) adamw8_kernel(const __grid_constant__ AdamwTable tab,
+                                                             const __grid_constant__ AdamwFactors f) {
+  launch_dependents();
   const int j = find_entry(tab, blockIdx.x);
   const AdamwEntry& e = tab.e[j];
   const int64_t block = (int64_t)(blockIdx.x - tab.first[j]) * kWarps + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   const int64_t n = e.n;
-  if (block * kBlock >= n) return;  // whole warps only
+  if (block * kBlock >= n) return wait_for_predecessor();  // whole warps only: the block's largest values are warp reductions
   const int64_t i = block * kBlock + lane * 8;
   const int live = i + 8 <= n ? 8 : i < n ? (int)(n - i) : 0;
 
   float p[8], g[8], m[8], r[8];
+  const uint2 qm = load_codes(e.m, i, live), qr = load_codes(e.v, i, live);
+  const float ms = e.m_scale[block], rs = e.r_scale[block];
   load_any(e.grad, i, f.grad_dtype, live, g);
   load_any(e.param, i, f.param_dtype, live, p);
-  if (BITS8) {
-    int q[8];
-    const float ms = e.m_scale[block], rs = e.r_scale[block];
-    load_codes(e.m, i, live, true, q);
-#pragma unroll
-    for (int k = 0; k < 8; k++) m[k] = decode_m(q[k], ms);
-    load_codes(e.v, i, live, false, q);
-#pragma unroll
-    for (int k = 0; k < 8; k++) {
-      r[k] = decode_r(q[k], rs);
-      r[k] = r[k] * r[k];
-    }
-  } else {
-    load_any(e.m, i, WINDQ_F32, live, m);
-    load_any(e.v, i, WINDQ_F32, live, r);
-  }
-  const float scale = f.grad_scale ? *f.grad_scale : 1.0f;  // a product with 1 is exact
+  const float2 scale = both(f.grad_scale ? *f.grad_scale : 1.0f);  // a product with 1 is exact
+  // The assembler joins a packed product and a packed sum into one rounding; a product with a one that it cannot see keeps
+  // both roundings of x + y.
+  const float2 one = both(f.one);
+  const uint32_t wm[2] = {qm.x ^ 0x80808080u, qm.y ^ 0x80808080u}, wr[2] = {qr.x, qr.y};
   float top_m = 0.0f, top_r = 0.0f;
 #pragma unroll
-  for (int k = 0; k < 8; k++) {
-    const float gk = g[k] * scale;
-    m[k] = m[k] * f.beta1 + gk * f.one_minus_beta1;
-    const float v = r[k] * f.beta2 + (gk * gk) * f.one_minus_beta2;
-    r[k] = sqrtf(v);
-    p[k] = p[k] * f.keep - (m[k] * f.rate) / (r[k] * f.unbias + f.eps);
-    if (BITS8) {
-      top_m = fmaxf(top_m, fabsf(m[k]));
-      top_r = fmaxf(top_r, r[k]);
-    } else {
-      r[k] = v;
-    }
+  for (int k = 0; k < 8; k += 2) {
+    float2 um = make_float2(code_bits(wm[k >> 2], k & 3), code_bits(wm[k >> 2], (k & 3) + 1));
+    float2 ur = make_float2(code_bits(wr[k >> 2], k & 3), code_bits(wr[k >> 2], (k & 3) + 1));
+    um = mul2(add2(um, both(-kShift - 128.0f)), both(kPerM));
+    ur = mul2(add2(ur, both(-kShift)), both(kPerR));
+    const float2 mk = mul2(make_float2(um.x * fabsf(um.x), um.y * fabsf(um.y)), both(ms));
+    const float2 rk = mul2(mul2(ur, ur), both(rs));
+    const float2 gk = mul2(make_float2(g[k], g[k + 1]), scale);
+    const float2 mn = fma2(mul2(mk, both(f.beta1)), one, mul2(gk, both(f.one_minus_beta1)));
+    const float2 v = fma2(mul2(mul2(rk, rk), both(f.beta2)), one, mul2(mul2(gk, gk), both(f.one_minus_beta2)));
+    const float2 rn = make_float2(sqrtf(v.x), sqrtf(v.y));
+    const float2 up = mul2(mn, both(f.rate)), down = fma2(mul2(rn, both(f.unbias)), one, both(f.eps));
+    const float2 pn = fma2(make_float2(up.x / down.x, up.y / down.y), both(-1.0f), mul2(make_float2(p[k], p[k + 1]), both(f.keep)));
+    p[k] = pn.x, p[k + 1] = pn.y;
+    m[k] = mn.x, m[k + 1] = mn.y;
+    r[k] = rn.x, r[k + 1] = rn.y;
+    top_m = fmaxf(top_m, fmaxf(fabsf(mn.x), fabsf(mn.y)));
+    top_r = fmaxf(top_r, fmaxf(rn.x, rn.y));
   }
   store_any(e.param, i, f.param_dtype, live, p);
   if (e.copy) store_any(e.copy, i, f.copy_dtype, live, p);
-  if (BITS8) {
-    top_m = warp_max(top_m);
-    top_r = warp_max(top_r);
-    top_m = top_m >= kTiny ? top_m : 0.0f;
-    top_r = top_r >= kTiny ? top_r : 0.0f;
-    const float inv_m = top_m > 0.0f ? 1.0f / top_m : 0.0f, inv_r = top_r > 0.0f ? 1.0f / top_r : 0.0f;
-    int q[8];
+  // values >= 0 order like their bit patterns
+  top_m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top_m)));
+  top_r = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top_r)));
+  top_m = top_m >= kTiny ? top_m : 0.0f;
+  top_r = top_r >= kTiny ? top_r : 0.0f;
+  const float inv_m = top_m > 0.0f ? 1.0f / top_m : 0.0f, inv_r = top_r > 0.0f ? 1.0f / top_r : 0.0f;
+  float x[8], c[8];
 #pragma unroll
-    for (int k = 0; k < 8; k++) {
-      const int c = min(__float2int_rn(sqrtf(fabsf(m[k]) * inv_m) * 127.0f), 127);
-      q[k] = m[k] < 0.0f ? -c : c;
-    }
-    store_codes(e.m, i, live, q);
-#pragma unroll
-    for (int k = 0; k < 8; k++) {
-      const int c = min(__float2int_rn(sqrtf(r[k] * inv_r) * 255.0f), 255);
-      q[k] = (r[k] > 0.0f && top_r > 0.0f) ? max(c, 1) : c;
-    }
-    store_codes(e.v, i, live, q);
-    if (lane == 0) {
-      e.m_scale[block] = top_m;
-      e.r_scale[block] = top_r;
-    }
-  } else {
-    store_any(e.m, i, WINDQ_F32, live, m);
-    store_any(e.v, i, WINDQ_F32, live, r);
+  for (int k = 0; k < 8; k += 2) {
+    const float2 y = mul2(make_float2(m[k], m[k + 1]), both(inv_m));
+    x[k] = y.x, x[k + 1] = y.y;
   }
+  encode8<true>(x, m, 127.0f, 0x1p-14f, c);
+  store_codes(e.m, i, live, low_bytes(c));
+  const float least = top_r > 0.0f ? kRound + 1.0f : kRound;  // the code an r above zero gets at least
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) {
+    const float2 y = mul2(make_float2(r[k], r[k + 1]), both(inv_r));
+    x[k] = y.x, x[k + 1] = y.y;
+  }
+  encode8<false>(x, r, 255.0f, 0x1p-13f, c);
+#pragma unroll
+  for (int k = 0; k < 8; k++) c[k] = r[k] > 0.0f ? fmaxf(c[k], least) : c[k];
+  store_codes(e.v, i, live, low_bytes(c));
+  if (lane == 0) {
+    e.m_scale[block] = top_m;
+    e.r_scale[block] = top_r;
+  }
+  wait_for_predecessor();
 }
 
 // param and copy of the table hold the two outputs.
-template <int N>
-__global__ void __launch_bounds__(kWarps * 32) adamw_states_kernel(const __grid_constant__ AdamwTable<N> tab) {
+__global__ void __launch_bounds__(kWarps * 32) adamw_states_kernel(const __grid_constant__ AdamwTable tab) {
+  launch_dependents();
   const int j = find_entry(tab, blockIdx.x);
   const AdamwEntry& e = tab.e[j];
   const int64_t block = (int64_t)(blockIdx.x - tab.first[j]) * kWarps + (threadIdx.x >> 5);
   const int64_t n = e.n;
-  if (block * kBlock >= n) return;
+  if (block * kBlock >= n) return wait_for_predecessor();
   const int64_t i = block * kBlock + (threadIdx.x & 31) * 8;
   const int live = i + 8 <= n ? 8 : i < n ? (int)(n - i) : 0;
-  int q[8];
-  float x[8];
+  const uint2 qm = load_codes(e.m, i, live), qr = load_codes(e.v, i, live);
   const float ms = e.m_scale[block], rs = e.r_scale[block];
-  load_codes(e.m, i, live, true, q);
+  float x[8];
 #pragma unroll
-  for (int k = 0; k < 8; k++) x[k] = decode_m(q[k], ms);
+  for (int k = 0; k < 8; k++) x[k] = decode_m((int)(int8_t)((k < 4 ? qm.x : qm.y) >> (8 * (k & 3))), ms);
   store_any(e.param, i, WINDQ_F32, live, x);
-  load_codes(e.v, i, live, false, q);
 #pragma unroll
   for (int k = 0; k < 8; k++) {
-    x[k] = decode_r(q[k], rs);
+    x[k] = decode_r((int)(uint8_t)((k < 4 ? qr.x : qr.y) >> (8 * (k & 3))), rs);
     x[k] = x[k] * x[k];
   }
   store_any(e.copy, i, WINDQ_F32, live, x);
+  wait_for_predecessor();
 }
 
-// Launches `go` over the entries in tables of at most kLargeTable tensors and 2^30 chunks.
-template <class Fill, class Small, class Large>
-windq_status over_tables(windq_ctx* ctx, int n_jobs, Fill fill, Small small, Large large) {
+// Launches `kernel` over the entries, kTable tensors and at most 2^30 chunks at a time.  The launches touch different
+// tensors: all but the first may start before their predecessor has ended, and end after it.
+template <class Fill, class... Kernel, class... More>
+windq_status over_tables(windq_ctx* ctx, int n_jobs, Fill fill, cudaStream_t st, void (*kernel)(Kernel...), const More&... more) {
   int j = 0;
+  bool first = true;
   while (j < n_jobs) {
-    AdamwTable<kLargeTable> tab;
+    AdamwTable tab;
     int64_t chunks = 0;
     tab.count = 0;
-    while (j < n_jobs && tab.count < kLargeTable) {
+    while (j < n_jobs && tab.count < kTable) {
       const AdamwEntry e = fill(j);
       const int64_t c = (e.n + kChunk - 1) / kChunk;
       if (c > 0) {
@@ -250,18 +307,17 @@ windq_status over_tables(windq_ctx* ctx, int n_jobs, Fill fill, Small small, Lar
       j++;
     }
     if (tab.count == 0) continue;
-    if (tab.count <= kSmallTable) {
-      AdamwTable<kSmallTable> less;
-      for (int k = 0; k < tab.count; k++) {
-        less.e[k] = tab.e[k];
-        less.first[k] = tab.first[k];
-      }
-      less.count = tab.count;
-      small(less, (unsigned)chunks);
-    } else {
-      large(tab, (unsigned)chunks);
-    }
-    WINDQ_CUDA(ctx, cudaGetLastError());
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)chunks);
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = first ? 0 : 1;
+    WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, tab, more...));
+    first = false;
   }
   return WINDQ_OK;
 }
@@ -327,27 +383,18 @@ windq_status windq_adamw_step(windq_ctx* ctx, const windq_adamw_job* jobs, int n
   f.rate = (float)(lr / (1.0 - pow(beta1, (double)step)));
   f.unbias = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step)));
   f.eps = (float)eps;
+  f.one = 1.0f;
   f.grad_scale = grad_scale;
   f.param_dtype = param_dtype;
   f.grad_dtype = grad_dtype;
   f.copy_dtype = copy_dtype;
   DeviceGuard guard(ctx->device);
   cudaStream_t st = (cudaStream_t)stream;
-  const int threads = kWarps * 32;
-  return over_tables(
-      ctx, n_jobs,
-      [&](int j) {
-        const windq_adamw_job& b = jobs[j];
-        return AdamwEntry{b.param, b.grad, b.m, b.v, b.m_scale, b.r_scale, b.copy, b.n};
-      },
-      [&](const AdamwTable<kSmallTable>& tab, unsigned chunks) {
-        if (state_bits == 8) adamw_kernel<kSmallTable, true><<<chunks, threads, 0, st>>>(tab, f);
-        else adamw_kernel<kSmallTable, false><<<chunks, threads, 0, st>>>(tab, f);
-      },
-      [&](const AdamwTable<kLargeTable>& tab, unsigned chunks) {
-        if (state_bits == 8) adamw_kernel<kLargeTable, true><<<chunks, threads, 0, st>>>(tab, f);
-        else adamw_kernel<kLargeTable, false><<<chunks, threads, 0, st>>>(tab, f);
-      });
+  auto fill = [&](int j) {
+    const windq_adamw_job& b = jobs[j];
+    return AdamwEntry{b.param, b.grad, b.m, b.v, b.m_scale, b.r_scale, b.copy, b.n};
+  };
+  return over_tables(ctx, n_jobs, fill, st, state_bits == 8 ? adamw8_kernel : adamw32_kernel, f);
 }
 
 windq_status windq_adamw_states(windq_ctx* ctx, const windq_adamw_job* jobs, int n_jobs, float* const* m_out,
@@ -367,18 +414,11 @@ windq_status windq_adamw_states(windq_ctx* ctx, const windq_adamw_job* jobs, int
   }
   DeviceGuard guard(ctx->device);
   cudaStream_t st = (cudaStream_t)stream;
-  return over_tables(
-      ctx, n_jobs,
-      [&](int j) {
-        const windq_adamw_job& b = jobs[j];
-        return AdamwEntry{m_out[j], nullptr, b.m, b.v, b.m_scale, b.r_scale, v_out[j], b.n};
-      },
-      [&](const AdamwTable<kSmallTable>& tab, unsigned chunks) {
-        adamw_states_kernel<kSmallTable><<<chunks, kWarps * 32, 0, st>>>(tab);
-      },
-      [&](const AdamwTable<kLargeTable>& tab, unsigned chunks) {
-        adamw_states_kernel<kLargeTable><<<chunks, kWarps * 32, 0, st>>>(tab);
-      });
+  auto fill = [&](int j) {
+    const windq_adamw_job& b = jobs[j];
+    return AdamwEntry{m_out[j], nullptr, b.m, b.v, b.m_scale, b.r_scale, v_out[j], b.n};
+  };
+  return over_tables(ctx, n_jobs, fill, st, adamw_states_kernel);
 }
 
 }  // extern "C"

@@ -67,6 +67,7 @@ struct Gradient {
 windq_status launch_gradients(windq_ctx* ctx, const Gradient* dA, const Gradient* dB, int dtype, int64_t T, int rank,
                               int64_t n_adapters, const int32_t* adapter_of, cudaStream_t st);
 
+constexpr int kProjectShare = 114 * 1024;  // shared memory of a thread block of the projection of few tokens, all told
 windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t st);
 
 }  // namespace windq

@@ -318,10 +318,11 @@ windq_status launch(windq_ctx* ctx, LowRankArgs p, cudaStream_t st) {
   }
   const int sums = p.rows * (p.rank + 4) * 4 + (kRows - p.rows) * 128;
   p.stage_bytes = p.rows * 128 + std::max(plain ? p.pack[0] * wide * 128 : 0, trans ? (p.rank > 64 ? 16384 : p.pack[1] * 8192) : 0);
-  // All blocks at once where they can be: an SM's share of its memory bounds the stages.  Up to 256 tokens half of it is
-  // left to the projection, whose blocks may start while this kernel runs.
-  const int64_t all = (int64_t)tiles * p.splits * (p.jobs * p.slots + 1), each = (all + ctx->sm_count - 1) / ctx->sm_count;
-  const int room = (int)((p.T <= 256 ? kLowSmem / 2 : kLowSmem) / std::min<int64_t>(each, 4));
+  // All blocks at once where they can be: an SM's share of its memory (228 KB, of which a block takes 1 KB and 2.4 KB beside
+  // the stages) bounds the stages.  Up to 256 tokens a block of the projection, which may start while this kernel runs,
+  // finds room beside them.
+  const int64_t all = (int64_t)tiles * p.splits * p.jobs * p.slots, each = (all + ctx->sm_count - 1) / ctx->sm_count;
+  const int room = (228 * 1024 - (p.T <= 256 ? kProjectShare : 0)) / (int)std::min<int64_t>(each, 4) - 3584;
   const int chunks = (std::max(p.job[0].K, p.job[p.jobs - 1].K) + 63) / 64;
   p.stages = std::max(2, std::min({kStages, (room - 1024 - sums) / p.stage_bytes, (chunks + p.splits - 1) / p.splits}));
   while (p.stages > 2 && 1024 + p.stages * p.stage_bytes + sums > kLowSmem) p.stages--;

@@ -7,6 +7,10 @@
 // over the output.  S enters as the sum of two 16-bit values (22 bits for fp16, 16 for bf16; written by the low-rank
 // kernel), which keeps the rounding of the low-rank term below that of the result.
 //
+// The low-rank stages come in the second half of a tile's reduction, one adapter after each chunk of K: their handshakes and
+// loads then hide behind the chunks' (at the end of 203 tokens with 48 adapters they took 14 us of 75), and the low-rank
+// kernel, which this one overlaps at its start, has long ended.
+//
 // Warps: one issues TMA copies, one issues matrix products, four write the S tiles and, after the tile, read the
 // accumulators and store.  Two layouts of a tile:
 //   wide  256 tokens x up to 256 outputs on a pair of thread blocks (cta_group::2: each holds half of either operand, so
@@ -29,6 +33,7 @@ constexpr int kMaxStages = 8;
 constexpr int kSmemLimit = 227 * 1024 - 2048;       // dynamic shared memory of one thread block per SM
 constexpr int kTallPitch = 132, kWidePitch = 260;    // binary32 sums of a split tile, rows free of bank conflicts
 constexpr int kSmemLimitTwo = 112 * 1024;           // of two
+static_assert(kSmemLimitTwo + 2048 <= kProjectShare, "what the low-rank kernel leaves");
 
 struct ProjectArgs {
   int T, N, chunks, rank, n_adapters, dtype;
@@ -65,6 +70,24 @@ struct Ring {
   }
 };
 
+// The adapters of a tile that are this split's, for a converged warp: 32 of them in its lanes at a time (one load from L2 an
+// adapter, even when issued one adapter ahead, took longer than the adapter's products).
+struct Adapters {
+  const int* list;
+  int first, step, lane, count = 0, held = 0;
+  __device__ Adapters(const int* list, int first, int step, int lane) : list(list + 1), first(first), step(step), lane(lane) {}
+  __device__ __forceinline__ void open() {
+    const int n = uniform(__ldcg(list - 1));
+    count = n > first ? (n - first + step - 1) / step : 0;
+    fetch(0);
+  }
+  __device__ __forceinline__ void fetch(int k) { held = k + lane < count ? __ldcg(list + first + (k + lane) * step) : 0; }
+  __device__ __forceinline__ int at(int k) {
+    if (k && (k & 31) == 0) fetch(k);
+    return __shfl_sync(0xffffffffu, held, k & 31);
+  }
+};
+
 // Tiles in an order that keeps a group of token tiles in L2 while the weight streams by.
 __device__ __forceinline__ void tile_at(const ProjectArgs& p, int tile, int& tt, int& wt) {
   const int per = p.group * p.weight_tiles, g = tile / per, rest = tile - g * per;
@@ -76,7 +99,8 @@ __device__ __forceinline__ void tile_at(const ProjectArgs& p, int tile, int& tt,
 template <bool TALL, bool TRANS>
 __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
     project_kernel(const __grid_constant__ CUtensorMap zmap, const __grid_constant__ CUtensorMap wmap,
-                   const __grid_constant__ CUtensorMap pmap, const __grid_constant__ ProjectArgs p) {
+                   const __grid_constant__ CUtensorMap pmap, const __grid_constant__ CUtensorMap omap,
+                   const __grid_constant__ ProjectArgs p) {
   extern __shared__ uint8_t raw[];
   __shared__ Barriers bars;
   __shared__ uint32_t tmem_slot;
@@ -126,6 +150,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
   const int team = kBlocks * p.splits;  // thread blocks of a tile
   const int split = (blockIdx.x % team) / kBlocks, step = gridDim.x / team, tiles = p.token_tiles * p.weight_tiles;
   const int c0 = (int)((int64_t)p.chunks * split / p.splits), c1 = (int)((int64_t)p.chunks * (split + 1) / p.splits);
+  const int middle = c0 + (c1 - c0) / 2;  // the chunk after which the first adapter comes
   const int rank_chunks = (p.rank + 63) >> 6;
   const bool paired = p.rank <= 32;  // both halves of S in one stage, at columns 0 and 32
   const int parts = paired ? 1 : 2;
@@ -133,35 +158,13 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
   if (warp == 0) {
     Ring at(p.stages);
     const uint32_t to = PAIR ? cluster_addr(full(0), leader) : full(0);  // barriers of the issuing block
-    bool waited = false;
     for (int tile = blockIdx.x / team; tile < tiles; tile += step) {
       int tt, wt;
       tile_at(p, tile, tt, wt);
       const int t0 = (tt * kBlocks + me) * p.token_rows, n0 = (wt * kBlocks + me) * p.weight_rows;
-      for (int c = c0; c < c1; c++, at.next()) {
-        mbar_wait(empty(at.s), at.phase ^ 1, dead_);
-        const uint32_t dst = base + at.s * stage_bytes, bar = to + at.s * 8;
-        if (elect_one() && !*(volatile int*)&dead) {
-          if (me == 0) mbar_expect(full(at.s), kBlocks * stage_bytes);
-          tma_load_2d<PAIR>(dst, &zmap, c * 64, t0, bar);
-          if (TRANS) {
-            for (int b = 0; b < weight_boxes; b++) tma_load_2d<PAIR>(dst + token_bytes + b * 8192, &wmap, n0 + b * 64, c * 64, bar);
-          } else {
-            tma_load_2d<PAIR>(dst + token_bytes, &wmap, c * 64, n0, bar);
-          }
-        }
-        __syncwarp();
-      }
-      if (!waited) {
-        wait_for_predecessor();
-        waited = true;
-      }
-      const int* list = p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1);
-      const int n_list = uniform(__ldcg(list));
-      int next = split < n_list ? __ldcg(list + 1 + split) : 0;
-      for (int i = split; i < n_list; i += p.splits) {
-        const int a = uniform(next);
-        if (i + p.splits < n_list) next = __ldcg(list + 1 + i + p.splits);
+      Adapters adapters(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1), split, p.splits, lane);
+      auto load_adapter = [&](int k) {
+        const int a = adapters.at(k);
         for (int e = 0; e < rank_chunks * parts; e++, at.next()) {
           const int rc = e / parts;
           mbar_wait(empty(at.s), at.phase ^ 1, dead_);
@@ -177,7 +180,29 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
           }
           __syncwarp();
         }
+      };
+      int k = 0;
+      for (int c = c0; c < c1; c++) {
+        mbar_wait(empty(at.s), at.phase ^ 1, dead_);
+        const uint32_t dst = base + at.s * stage_bytes, bar = to + at.s * 8;
+        if (elect_one() && !*(volatile int*)&dead) {
+          if (me == 0) mbar_expect(full(at.s), kBlocks * stage_bytes);
+          tma_load_2d<PAIR>(dst, &zmap, c * 64, t0, bar);
+          if (TRANS) {
+            for (int b = 0; b < weight_boxes; b++) tma_load_2d<PAIR>(dst + token_bytes + b * 8192, &wmap, n0 + b * 64, c * 64, bar);
+          } else {
+            tma_load_2d<PAIR>(dst + token_bytes, &wmap, c * 64, n0, bar);
+          }
+        }
+        __syncwarp();
+        at.next();
+        if (c == middle) {
+          wait_for_predecessor();
+          adapters.open();
+        }
+        if (k < adapters.count) load_adapter(k++);
       }
+      while (k < adapters.count) load_adapter(k++);
     }
   } else if (warp == 1) {
     if (me == 0) {
@@ -190,7 +215,6 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
       Ring at(p.stages);
       int turn = 0;
       uint32_t written_phase = 0;
-      bool waited = false;
       for (int tile = blockIdx.x / team; tile < tiles; tile += step, turn++) {
         int tt, wt;
         tile_at(p, tile, tt, wt);
@@ -199,23 +223,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
         tc_fence_after();
         const uint32_t d = tmem + b * 256;
         auto product = [&](uint64_t z, uint64_t w, bool accumulate) { mma_f16<PAIR>(d, TALL ? w : z, TALL ? z : w, idesc, accumulate); };
-        for (int c = c0; c < c1; c++, at.next()) {
-          mbar_wait(full(at.s), at.phase, dead_);
-          tc_fence_after();
-          const uint64_t off = (uint64_t)(at.s * stage_bytes >> 4);
-          if (elect_one()) {
-#pragma unroll
-            for (int k = 0; k < 4; k++) product(z_desc + off + k * token_step, w_desc + off + k * weight_step, c > c0 || k > 0);
-            mma_commit<PAIR>(empty(at.s), mask);
-          }
-          __syncwarp();
-        }
-        if (!waited) {
-          wait_for_predecessor();
-          waited = true;
-        }
-        const int n_list = uniform(__ldcg(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1)));
-        for (int i = split; i < n_list; i += p.splits) {
+        auto multiply_adapter = [&] {
           for (int e = 0; e < rank_chunks * parts; e++, at.next()) {
             const int rc = e / parts;
             mbar_wait(full(at.s), at.phase, dead_);
@@ -232,7 +240,30 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
             }
             __syncwarp();
           }
+        };
+        Adapters adapters(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1), split, p.splits, lane);
+        int k = 0;
+        for (int c = c0; c < c1; c++) {
+          mbar_wait(full(at.s), at.phase, dead_);
+          tc_fence_after();
+          const uint64_t off = (uint64_t)(at.s * stage_bytes >> 4);
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 4; k++) product(z_desc + off + k * token_step, w_desc + off + k * weight_step, c > c0 || k > 0);
+            mma_commit<PAIR>(empty(at.s), mask);
+          }
+          __syncwarp();
+          at.next();
+          if (c == middle) {
+            wait_for_predecessor();
+            adapters.open();
+          }
+          if (k < adapters.count) {
+            multiply_adapter();
+            k++;
+          }
         }
+        for (; k < adapters.count; k++) multiply_adapter();
         if (elect_one()) mma_commit<PAIR>(done(b), mask);
         __syncwarp();
       }
@@ -243,20 +274,18 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
     // warp, which follows every round, grants them the stage.
     Ring ring(p.stages);
     int turn = 0;
-    uint32_t granted_phase = 0;
+    uint32_t granted_phase = 0, buffer = 0;
+    const uint32_t staging = base + p.stages * stage_bytes;
     auto tell = [&](uint32_t bar) {  // the block that issues the products
       if (PAIR) cluster_arrive(cluster_addr(bar, leader));
       else mbar_arrive(bar);
     };
-    bool waited = false;
     for (int tile = blockIdx.x / team; tile < tiles; tile += step, turn++) {
       int tt, wt;
       tile_at(p, tile, tt, wt);
-      ring.skip(c1 - c0);
-      if (!waited) {
-        wait_for_predecessor();
-        waited = true;
-      }
+      int passed = middle - c0 + 1;  // chunks of K that the ring has seen
+      ring.skip(passed);
+      wait_for_predecessor();
       const int t0 = (tt * kBlocks + me) * p.token_rows;
       // S: a thread writes rows e and e + 128 of the token tile, 16-byte pieces of eight values
       constexpr int kRows = TALL ? 2 : 1;
@@ -281,13 +310,15 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
                                : make_uint4(0, 0, 0, 0);
           }
       };
-      const int* list = p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1);
-      const int n_list = __ldcg(list);
-      if (n_list > split && paired) load(0, 0);
-      int next = split < n_list ? __ldcg(list + 1 + split) : 0;
-      for (int i = split; i < n_list; i += p.splits) {
-        const int a = next;
-        if (i + p.splits < n_list) next = __ldcg(list + 1 + i + p.splits);
+      Adapters adapters(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1), split, p.splits, lane);
+      adapters.open();
+      if (adapters.count && paired) load(0, 0);
+      for (int k = 0; k < adapters.count; k++) {
+        const int a = adapters.at(k);
+        if (k && passed < c1 - c0) {
+          ring.next();
+          passed++;
+        }
         for (int x = 0; x < rank_chunks * parts; x++, ring.next()) {
           const int rc = x / parts, s = ring.s;
           if (!paired) load(rc, x & 1);
@@ -313,48 +344,93 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
           if (lane == 0) tell(written(s));
         }
       }
+      ring.skip(c1 - c0 - passed);
       // the accumulators of the tile
       const int b = p.accumulators == 2 ? turn & 1 : 0, use = p.accumulators == 2 ? turn >> 1 : turn;
       mbar_wait(done(b), use & 1, dead_);
       tc_fence_after();
       const uint32_t d = tmem + b * 256 + ((uint32_t)(quarter * 32) << 16);
       const int columns = TALL ? p.token_rows : 2 * p.weight_rows, at = quarter * 32 + lane;
-      for (int c = 0; c < columns; c += 16) {
-        uint32_t r[16];
-        tmem_load16(d + c, r);
-        tmem_load_wait();
-        if (p.splits > 1) {
-          // as the result lies: [token][output], the outputs of a tall tile being the lanes
-          if (TALL) {
+      if (!TALL && p.splits == 1) {
+        // 32 rows x 64 columns at a time through shared memory (128-byte swizzle, two buffers a warp) and out by TMA: rows
+        // are far apart, and 16-byte stores straight from the registers took as long as a third of the tile's products
+        for (int c = 0; c < columns; c += 64, buffer ^= 1) {
+          uint32_t r[4][16];
 #pragma unroll
-            for (int k = 0; k < 16; k++)
-              asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + ((c + k) * kTallPitch + at) * 4), "r"(r[k]) : "memory");
-          } else {
+          for (int h = 0; h < 4; h++)
+            if (c + h * 16 < columns) tmem_load16(d + c + h * 16, r[h]);
+          tmem_load_wait();
+          const uint32_t to = staging + ((quarter * 2 + buffer) * 32 + lane) * 128;
+          if (lane == 0) tma_store_wait<1>();
+          __syncwarp();
 #pragma unroll
-            for (int k = 0; k < 16; k += 4)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (at * kWidePitch + c + k) * 4), "r"(r[k]),
-                           "r"(r[k + 1]), "r"(r[k + 2]), "r"(r[k + 3])
-                           : "memory");
+          for (int h = 0; h < 4; h++)
+            if (c + h * 16 < columns) {
+#pragma unroll
+              for (int k = 0; k < 16; k += 8) {
+                uint32_t w[4];
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                  w[q] = pack2(__uint_as_float(r[h][k + 2 * q]), __uint_as_float(r[h][k + 2 * q + 1]), p.dtype);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((h * 2 + (k >> 3)) ^ (lane & 7)) << 4)), "r"(w[0]),
+                             "r"(w[1]), "r"(w[2]), "r"(w[3])
+                             : "memory");
+              }
+            }
+          fence_async_shared();
+          __syncwarp();
+          const int n = wt * 2 * p.weight_rows + c, t = t0 + quarter * 32;
+          // not by TMA: a box wider than what is left of the tile, whose other columns are the next tile's, and a box that
+          // ends in the middle of 16 bytes, which the copy would write whole
+          const bool whole = c + 64 <= columns && (n + 64 <= p.N || p.N % 8 == 0);
+          if (lane == 0) {
+            if (whole && t < p.T && n < p.N) tma_store_2d(&omap, n, t, staging + (quarter * 2 + buffer) * 4096);
+            tma_store_commit();
           }
-        } else if (TALL) {
-          const int n = wt * 128 + at;
-          if (n < p.N) {
-#pragma unroll
-            for (int k = 0; k < 16; k++) {
-              const int t = t0 + c + k;
-              if (t < p.T) store1(p.O, t * p.ldo + n, p.dtype, __uint_as_float(r[k]));
+          if (!whole && t0 + at < p.T) {
+            for (int g = 0; c + g * 8 < columns; g++) {
+              uint4 w;
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                           : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                           : "r"(to + ((g ^ (lane & 7)) << 4))
+                           : "memory");
+              uint16_t* out = static_cast<uint16_t*>(p.O) + (t0 + at) * p.ldo + n + g * 8;
+              if (n + g * 8 + 8 <= p.N) {
+                *reinterpret_cast<uint4*>(out) = w;
+              } else {
+                const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+                for (int k = 0; k < 8; k++)
+                  if (n + g * 8 + k < p.N) out[k] = (uint16_t)(v[k >> 1] >> (16 * (k & 1)));
+              }
             }
           }
-        } else {
-          const int t = t0 + at, n = wt * 2 * p.weight_rows + c;
-          if (t < p.T) {
+        }
+      } else {
+        for (int c = 0; c < columns; c += 16) {
+          uint32_t r[16];
+          tmem_load16(d + c, r);
+          tmem_load_wait();
+          if (p.splits > 1) {
+            // as the result lies: [token][output], the outputs of a tall tile being the lanes
+            if (TALL) {
 #pragma unroll
-            for (int k = 0; k < 16; k += 8) {
-              float x[8];
+              for (int k = 0; k < 16; k++)
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + ((c + k) * kTallPitch + at) * 4), "r"(r[k]) : "memory");
+            } else {
 #pragma unroll
-              for (int j = 0; j < 8; j++) x[j] = __uint_as_float(r[k + j]);
-              if (n + k + 8 <= p.N) store8(p.O, t * p.ldo + n + k, p.dtype, x);
-              else if (n + k < p.N) store_some(p.O, t * p.ldo + n + k, p.dtype, p.N - n - k, x);
+              for (int k = 0; k < 16; k += 4)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (at * kWidePitch + c + k) * 4), "r"(r[k]),
+                             "r"(r[k + 1]), "r"(r[k + 2]), "r"(r[k + 3])
+                             : "memory");
+            }
+          } else {
+            const int n = wt * 128 + at;
+            if (n < p.N) {
+#pragma unroll
+              for (int k = 0; k < 16; k++) {
+                const int t = t0 + c + k;
+                if (t < p.T) store1(p.O, t * p.ldo + n, p.dtype, __uint_as_float(r[k]));
+              }
             }
           }
         }
@@ -363,6 +439,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
       __syncwarp();
       if (lane == 0) tell(free_(b));
     }
+    if (!TALL && lane == 0) tma_store_wait<0>();
   }
   __syncwarp();
   __syncthreads();
@@ -411,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
 }
 
 template <bool TALL, bool TRANS>
-windq_status launch(windq_ctx* ctx, const CUtensorMap& z, const CUtensorMap& w, const CUtensorMap& pm, const ProjectArgs& p,
+windq_status launch(windq_ctx* ctx, const CUtensorMap& z, const CUtensorMap& w, const CUtensorMap& pm, const CUtensorMap& o, const ProjectArgs& p,
                     int blocks, int smem, cudaStream_t st) {
   const windq_status ready = prepare_kernel(ctx, kProject + 2 * TALL + TRANS, project_kernel<TALL, TRANS>, kThreads, kSmemLimit, false);
   if (ready != WINDQ_OK) return ready;
@@ -428,7 +505,7 @@ windq_status launch(windq_ctx* ctx, const CUtensorMap& z, const CUtensorMap& w, 
   attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
   cfg.attrs = attrs;
   cfg.numAttrs = attrs[1].val.clusterDim.x > 1 ? 2 : 1;
-  WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, project_kernel<TALL, TRANS>, z, w, pm, p));
+  WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, project_kernel<TALL, TRANS>, z, w, pm, o, p));
   return WINDQ_OK;
 }
 
@@ -481,7 +558,8 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.token_tiles, (48ll << 20) / (2 * q.K * p.token_rows * blocks_of_tile)));
   const int stage = p.token_rows * 128 + (q.transposed ? (p.weight_rows + 63) / 64 * 8192 : p.weight_rows * 128);
   const int limit = two ? kSmemLimitTwo : kSmemLimit;
-  p.stages = std::min(kMaxStages, (limit - 1024) / stage);
+  const int staging = tall || p.splits > 1 ? 0 : 4 * 2 * 4096;
+  p.stages = std::min(kMaxStages, (limit - 1024 - staging) / stage);
   const int64_t tiles = (int64_t)p.token_tiles * p.weight_tiles;
   if (tall)
     while (p.splits < 8 && tiles * p.splits * 2 <= slots && p.chunks >= p.splits * 2 * 4) p.splits *= 2;
@@ -489,9 +567,9 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   p.columns = tall ? (p.token_rows <= 32 ? 32 : p.token_rows <= 64 ? 64 : p.token_rows <= 128 ? 128 : 256) : 256 * p.accumulators;
   const int64_t blocks = (p.splits > 1 ? tiles * p.splits : std::min(tiles, slots)) * blocks_of_tile;
   const int sums = p.splits > 1 ? (tall ? p.token_rows * kTallPitch : 128 * kWidePitch) * 4 : 0;
-  const int smem = 1024 + std::max(p.stages * stage, sums);
+  const int smem = 1024 + std::max(p.stages * stage + staging, sums);
 
-  CUtensorMap z, w, pm;
+  CUtensorMap z, w, pm, o;
   WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
   bool ok = make_map(&z, q.dtype, q.Z, q.K, q.T, 0, q.ldz, 0, p.token_rows);
   if (q.transposed) {
@@ -501,11 +579,13 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
     ok = ok && make_map(&w, q.dtype, q.W, q.K, q.N, 0, q.ldw, 0, p.weight_rows);
     ok = ok && make_map(&pm, q.dtype, q.P, q.rank, q.N, q.n_adapters, q.rank, q.N * q.rank, p.weight_rows);
   }
+  if (tall) o = z;  // not used
+  else ok = ok && make_map(&o, q.dtype, q.O, q.N, q.T, 0, q.ldo, 0, 32);
   WINDQ_REQUIRE(ctx, ok, WINDQ_ERR_CUDA, "a tensor map could not be made");
-  if (tall) return q.transposed ? launch<true, true>(ctx, z, w, pm, p, (int)blocks, smem, st)
-                                : launch<true, false>(ctx, z, w, pm, p, (int)blocks, smem, st);
-  return q.transposed ? launch<false, true>(ctx, z, w, pm, p, (int)blocks, smem, st)
-                      : launch<false, false>(ctx, z, w, pm, p, (int)blocks, smem, st);
+  if (tall) return q.transposed ? launch<true, true>(ctx, z, w, pm, o, p, (int)blocks, smem, st)
+                                : launch<true, false>(ctx, z, w, pm, o, p, (int)blocks, smem, st);
+  return q.transposed ? launch<false, true>(ctx, z, w, pm, o, p, (int)blocks, smem, st)
+                      : launch<false, false>(ctx, z, w, pm, o, p, (int)blocks, smem, st);
 }
 
 }  // namespace windq

@@ -94,6 +94,16 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
+// A box from shared memory into the array; what lies outside the array is not written.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int y, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
+               : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N>  // all but the last N groups of this thread's stores have read their shared memory
+__device__ __forceinline__ void tma_store_wait() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -181,22 +191,34 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void cluster_arrive(uint32_t remote_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote_bar) : "memory");
 }
-// Distributed shared memory answers after the better part of a microsecond, so sums over a cluster's blocks have several
-// loads in flight: `U` of them, at base + offset[u] in each of the n blocks of ranks first, first + stride, ...
+// Sums over the blocks of a cluster, in the order of their ranks: `U` quads of binary32 values, at base + offset[u] in each
+// of n (a power of two, at most 8) blocks of ranks first, first + stride, ...  Distributed shared memory answers after the
+// better part of a microsecond, so the loads of several blocks are in flight together.
 template <int U>
 __device__ __forceinline__ void cluster_sum(uint32_t base, const uint32_t (&offset)[U], int n, int first, int stride, float4 (&x)[U]) {
+  constexpr int Q = U >= 4 ? 4 : 8;
 #pragma unroll
   for (int u = 0; u < U; u++) x[u] = make_float4(0, 0, 0, 0);
-  for (int q = 0; q < n; q++) {
-    const uint32_t from = cluster_addr(base, first + q * stride);
-    float4 y[U];
+  for (int q0 = 0; q0 < n; q0 += Q) {
+    float4 y[Q][U];
 #pragma unroll
-    for (int u = 0; u < U; u++)
-      asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                   : "=f"(y[u].x), "=f"(y[u].y), "=f"(y[u].z), "=f"(y[u].w)
-                   : "r"(from + offset[u]));
+    for (int q = 0; q < Q; q++) {
+      if (q0 + q < n) {
+        const uint32_t from = cluster_addr(base, first + (q0 + q) * stride);
 #pragma unroll
-    for (int u = 0; u < U; u++) x[u].x += y[u].x, x[u].y += y[u].y, x[u].z += y[u].z, x[u].w += y[u].w;
+        for (int u = 0; u < U; u++)
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(y[q][u].x), "=f"(y[q][u].y), "=f"(y[q][u].z), "=f"(y[q][u].w)
+                       : "r"(from + offset[u]));
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+      if (q0 + q < n) {
+#pragma unroll
+        for (int u = 0; u < U; u++) x[u].x += y[q][u].x, x[u].y += y[q][u].y, x[u].z += y[q][u].z, x[u].w += y[q][u].w;
+      }
+    }
   }
 }
 
