@@ -181,8 +181,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
           __syncwarp();
         }
       };
-      int k = 0;
-      for (int c = c0; c < c1; c++) {
+      auto load_chunk = [&](int c) {
         mbar_wait(empty(at.s), at.phase ^ 1, dead_);
         const uint32_t dst = base + at.s * stage_bytes, bar = to + at.s * 8;
         if (elect_one() && !*(volatile int*)&dead) {
@@ -196,13 +195,16 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
         }
         __syncwarp();
         at.next();
-        if (c == middle) {
-          wait_for_predecessor();
-          adapters.open();
-        }
-        if (k < adapters.count) load_adapter(k++);
+      };
+      for (int c = c0; c <= middle; c++) load_chunk(c);
+      wait_for_predecessor();
+      adapters.open();
+      int c = middle + 1;
+      for (int k = 0; k < adapters.count; k++) {
+        if (k && c < c1) load_chunk(c++);
+        load_adapter(k);
       }
-      while (k < adapters.count) load_adapter(k++);
+      for (; c < c1; c++) load_chunk(c);
     }
   } else if (warp == 1) {
     if (me == 0) {
@@ -241,29 +243,28 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
             __syncwarp();
           }
         };
-        Adapters adapters(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1), split, p.splits, lane);
-        int k = 0;
-        for (int c = c0; c < c1; c++) {
+        auto multiply_chunk = [&](bool accumulate) {
           mbar_wait(full(at.s), at.phase, dead_);
           tc_fence_after();
           const uint64_t off = (uint64_t)(at.s * stage_bytes >> 4);
           if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < 4; k++) product(z_desc + off + k * token_step, w_desc + off + k * weight_step, c > c0 || k > 0);
+            for (int k = 0; k < 4; k++) product(z_desc + off + k * token_step, w_desc + off + k * weight_step, accumulate || k > 0);
             mma_commit<PAIR>(empty(at.s), mask);
           }
           __syncwarp();
           at.next();
-          if (c == middle) {
-            wait_for_predecessor();
-            adapters.open();
-          }
-          if (k < adapters.count) {
-            multiply_adapter();
-            k++;
-          }
+        };
+        for (int c = c0; c <= middle; c++) multiply_chunk(c > c0);
+        wait_for_predecessor();
+        Adapters adapters(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1), split, p.splits, lane);
+        adapters.open();
+        int c = middle + 1;
+        for (int k = 0; k < adapters.count; k++) {
+          if (k && c < c1) multiply_chunk(true), c++;
+          multiply_adapter();
         }
-        for (; k < adapters.count; k++) multiply_adapter();
+        for (; c < c1; c++) multiply_chunk(true);
         if (elect_one()) mma_commit<PAIR>(done(b), mask);
         __syncwarp();
       }
