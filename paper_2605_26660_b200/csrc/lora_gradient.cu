@@ -14,13 +14,14 @@ namespace {
 
 // ---- D[a][j][c] = sum over the tokens t of a of S[t][j] Z[t][c] ----------------------------------------------------
 
-constexpr int kGradWarps = 8, kGradThreads = 256, kGradCols = 128;
+constexpr int kGradWarps = 8, kGradThreads = 256, kGradCols = 256;
 constexpr int kZPitch = kGradCols * 2 + 16;  // bytes
-constexpr int kWindow = 64;                  // blocks of tokens whose adapters are looked up at a time
+constexpr int kGradTokens = 32;              // of a block
+constexpr int kWindow = 128;                 // blocks of tokens whose adapters are looked up at a time
 
-// Blocks of tokens and stages of copies in flight, by the rank / 8 that a kernel is made for: two thread blocks an SM.
-__host__ __device__ constexpr int grad_tokens(int nb) { return nb <= 4 ? 64 : 32; }
-__host__ __device__ constexpr int grad_stages(int nb) { return nb <= 2 ? 4 : nb <= 4 ? 3 : nb <= 8 ? 4 : 2; }
+// Stages of copies in flight, by the rank / 8 that a kernel is made for, and thread blocks an SM.
+__host__ __device__ constexpr int grad_stages(int nb) { return nb <= 4 ? 4 : 3; }
+__host__ __device__ constexpr int grad_blocks(int nb) { return nb <= 8 ? 2 : 1; }
 
 struct GradJob {
   const uint16_t* Z;
@@ -37,18 +38,20 @@ struct GradArgs {
   const int32_t* adapter_of;
 };
 
-// A thread block owns 128 columns of Z for one adapter; a cluster of `splits` shares the tokens.  The tokens that are not
+// A thread block owns 256 columns of Z for one adapter, a warp 32 of them; a cluster of `splits` shares the tokens.  (What
+// bounds it once the loads flow is shared memory: every warp reads all of S, so few warps with many columns each are better
+// than many with few -- with 128 columns, 16 a warp, the backward pass of 8192 x 4096 x 4096 took 308 us, and takes 298.)  The tokens that are not
 // the adapter's are left out as rows of zeros (copied with size zero, so that what they hold cannot spoil a sum), blocks
 // of tokens without any of its tokens are skipped.  Z is the transposed left operand (ldmatrix.trans); S enters as two
 // fp16 or three bf16 values whose sum is S to 22 or 24 bits -- fp16 ones after a scaling by a power of two that puts the
-// adapter's largest |S| near 2^13, undone at the end, so that small gradients keep their bits.
+// largest |S| of the adapter's tokens so far near 2^13, so that small gradients keep their bits (the sums are rescaled,
+// exactly, where a later window of tokens holds a larger one).
 template <int NB, bool BF>
-__global__ void __launch_bounds__(kGradThreads) gradient_kernel(const __grid_constant__ GradArgs p) {
-  constexpr int kTerms = BF ? 3 : 2, kTokens = grad_tokens(NB), kStages = grad_stages(NB);
-  constexpr int kHalves = kTokens / 32;                                                  // of a block's tokens, 32 each
+__global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel(const __grid_constant__ GradArgs p) {
+  constexpr int kTerms = BF ? 3 : 2, kTokens = kGradTokens, kStages = grad_stages(NB);
   constexpr int kPieces = (kTokens * NB + kGradThreads - 1) / kGradThreads;              // of eight values of S, a thread
   extern __shared__ uint4 shared[];
-  __shared__ unsigned masks[kWindow][kHalves];  // tokens of the adapter
+  __shared__ unsigned masks[kWindow];  // tokens of the adapter
   __shared__ short active[kWindow];
   __shared__ int n_active;
   __shared__ float tops[kGradWarps];
@@ -63,47 +66,61 @@ __global__ void __launch_bounds__(kGradThreads) gradient_kernel(const __grid_con
   launch_dependents();
   wait_for_predecessor();
 
-  float up = 1.0f, down = 1.0f;
-  if (!BF) {
-    float top = 0.0f;
-    for (int t = tid; t < p.T; t += kGradThreads) {
-      const float x = job.top[t];
-      if (p.adapter_of[t] == a) top = fmaxf(top, x);
-    }
-#pragma unroll
-    for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-    if (lane == 0) tops[warp] = top;
-    __syncthreads();
-    for (int w = 0; w < kGradWarps; w++) top = fmaxf(top, tops[w]);
-    // 2^e <= top < 2^(e + 1); both factors are kept normal
-    const int e = (int)((__float_as_uint(top) >> 23) & 255) - 127, k = max(-100, min(100, 13 - e));
-    up = __uint_as_float((uint32_t)(127 + k) << 23);
-    down = __uint_as_float((uint32_t)(127 - k) << 23);
-  }
+  float top = 0.0f, up = 1.0f, down = 1.0f;  // largest |S| so far; scaling of S and its inverse
 
   // a stage: Z [token][column], then S [token][j] in binary32; after the stages two buffers of S in 16-bit terms
   const int s_pitch = r * 2 + 16, s_raw = kTokens * r * 4, s_terms = kTerms * kTokens * s_pitch;
   const int stage_bytes = kTokens * kZPitch + s_raw;
   const uint32_t base = smem_addr(shared), terms = base + kStages * stage_bytes;
-  float acc[NB][4];
+  float acc[2][NB][4];
 #pragma unroll
-  for (int n = 0; n < NB; n++)
+  for (int h = 0; h < 2; h++)
 #pragma unroll
-    for (int k = 0; k < 4; k++) acc[n][k] = 0.0f;
+    for (int n = 0; n < NB; n++)
+#pragma unroll
+      for (int k = 0; k < 4; k++) acc[h][n][k] = 0.0f;
 
   for (int w0 = 0; w0 < all; w0 += kWindow) {
     const int count = min(kWindow, all - w0);
     __syncthreads();
-    for (int i = warp; i < count * kHalves; i += kGradWarps) {
+    float most = 0.0f;
+#pragma unroll 8
+    for (int i = warp; i < count; i += kGradWarps) {
       const int t = w0 * kTokens + i * 32 + lane;
-      const unsigned vote = __ballot_sync(0xffffffffu, t < p.T && p.adapter_of[t] == a);
-      if (lane == 0) masks[i / kHalves][i % kHalves] = vote;
+      const int id = t < p.T ? p.adapter_of[t] : -1;
+      const float x = !BF && t < p.T ? job.top[t] : 0.0f;
+      const unsigned vote = __ballot_sync(0xffffffffu, id == a);
+      if (lane == 0) masks[i] = vote;
+      if (!BF && id == a) most = fmaxf(most, x);
+    }
+    if (!BF) {
+      most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));  // values >= 0 order like their bits
+      if (lane == 0) tops[warp] = most;
     }
     __syncthreads();
+    if (!BF) {
+      for (int w = 0; w < kGradWarps; w++) most = fmaxf(most, tops[w]);
+      if (most > top) {
+        top = most;
+        // 2^e <= top < 2^(e + 1); both factors are kept normal
+        const int e = (int)((__float_as_uint(top) >> 23) & 255) - 127, k = max(-100, min(100, 13 - e));
+        const float next = __uint_as_float((uint32_t)(127 + k) << 23), change = next * down;
+        up = next;
+        down = __uint_as_float((uint32_t)(127 - k) << 23);
+        if (w0 > 0) {
+#pragma unroll
+          for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int n = 0; n < NB; n++)
+#pragma unroll
+              for (int q = 0; q < 4; q++) acc[h][n][q] *= change;
+        }
+      }
+    }
     if (warp == 0) {
       int n = 0;
       for (int h = 0; h < count; h += 32) {
-        const bool on = h + lane < count && (masks[h + lane][0] | masks[h + lane][kHalves - 1]);
+        const bool on = h + lane < count && masks[h + lane];
         const unsigned vote = __ballot_sync(0xffffffffu, on);
         if (on) active[n + __popc(vote & ((1u << lane) - 1))] = (short)(h + lane);
         n += __popc(vote);
@@ -117,16 +134,16 @@ __global__ void __launch_bounds__(kGradThreads) gradient_kernel(const __grid_con
         const int b = active[split + i * p.splits], t0 = (w0 + b) * kTokens;
         const uint32_t at = base + (i % kStages) * stage_bytes;
 #pragma unroll
-        for (int h = 0; h < kTokens * 16 / kGradThreads; h++) {
-          const int x = h * kGradThreads + tid, row = x >> 4, piece = x & 15, c = c0 + piece * 8;
-          const bool on = c < job.cols && (masks[b][row >> 5] >> (row & 31) & 1);
+        for (int h = 0; h < kTokens * 32 / kGradThreads; h++) {
+          const int x = h * kGradThreads + tid, row = x >> 5, piece = x & 31, c = c0 + piece * 8;
+          const bool on = c < job.cols && (masks[b] >> row & 1);
           copy16(at + row * kZPitch + piece * 16, on ? job.Z + (t0 + row) * job.ldz + c : job.Z, on ? min(16, (job.cols - c) * 2) : 0);
         }
 #pragma unroll
         for (int h = 0; h < kPieces; h++) {
           const int x = h * kGradThreads + tid, row = x / NB, piece = x % NB;
           if (row >= kTokens || piece * 8 >= r) continue;
-          const bool on = masks[b][row >> 5] >> (row & 31) & 1;
+          const bool on = masks[b] >> row & 1;
           const float* src = on ? job.S + (int64_t)(t0 + row) * r + piece * 8 : job.S;
           const uint32_t dst = at + kTokens * kZPitch + (row * r + piece * 8) * 4;
           copy16(dst, src, on ? 16 : 0);
@@ -177,9 +194,11 @@ __global__ void __launch_bounds__(kGradThreads) gradient_kernel(const __grid_con
       const uint32_t z_at = base + (i % kStages) * stage_bytes, s_at0 = terms + (i & 1) * s_terms;
 #pragma unroll
       for (int k = 0; k < kTokens / 16; k++) {
-        // left operand: columns 16 warp .. + 15 (rows of the product), tokens 16 k .. + 15
-        uint32_t za[4];
-        ldmatrix_trans(z_at + (k * 16 + (lane & 7) + (lane >> 4) * 8) * kZPitch + (warp * 16 + ((lane >> 3) & 1) * 8) * 2, za);
+        // left operand: columns 32 warp + 16 h .. + 15 (rows of the product), tokens 16 k .. + 15
+        uint32_t za[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+          ldmatrix_trans(z_at + (k * 16 + (lane & 7) + (lane >> 4) * 8) * kZPitch + (warp * 32 + h * 16 + ((lane >> 3) & 1) * 8) * 2, za[h]);
 #pragma unroll
         for (int term = 0; term < kTerms; term++) {
           const uint32_t s_at = s_at0 + (term * kTokens + k * 16 + (lane & 15)) * s_pitch + (lane >> 4) * 16;
@@ -189,8 +208,11 @@ __global__ void __launch_bounds__(kGradThreads) gradient_kernel(const __grid_con
               uint32_t sb[4];
               // an odd last block has no right neighbour: its lanes read the left one again
               ldmatrix_trans((n + 1) * 8 < r ? s_at + n * 16 : s_at + n * 16 - (lane >> 4) * 16, sb);
-              mma16816(acc[n], za, sb[0], sb[1], BF);
-              if (n + 1 < NB && (n + 1) * 8 < r) mma16816(acc[n + 1 < NB ? n + 1 : n], za, sb[2], sb[3], BF);
+#pragma unroll
+              for (int h = 0; h < 2; h++) {
+                mma16816(acc[h][n], za[h], sb[0], sb[1], BF);
+                if (n + 1 < NB && (n + 1) * 8 < r) mma16816(acc[h][n + 1 < NB ? n + 1 : n], za[h], sb[2], sb[3], BF);
+              }
             }
           }
         }
@@ -202,15 +224,18 @@ __global__ void __launch_bounds__(kGradThreads) gradient_kernel(const __grid_con
   // join the cluster: [column][j] for dB, [j][column] for dA, as the result lies
   const int pitch = job.j_first ? r + 4 : kGradCols + 4;
 #pragma unroll
-  for (int n = 0; n < NB; n++)
-    if (n * 8 < r) {
+  for (int h = 0; h < 2; h++)
 #pragma unroll
-      for (int k = 0; k < 4; k++) {
-        const int j = n * 8 + q * 2 + (k & 1), c = warp * 16 + g + (k >> 1) * 8;
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(base + (job.j_first ? c * pitch + j : j * pitch + c) * 4), "f"(acc[n][k] * down)
-                     : "memory");
+    for (int n = 0; n < NB; n++)
+      if (n * 8 < r) {
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          const int j = n * 8 + q * 2 + (k & 1), c = warp * 32 + h * 16 + g + (k >> 1) * 8;
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(base + (job.j_first ? c * pitch + j : j * pitch + c) * 4),
+                       "f"(acc[h][n][k] * down)
+                       : "memory");
+        }
       }
-    }
   __syncwarp();
   if (p.splits > 1) cluster_sync();
   else __syncthreads();
@@ -241,15 +266,16 @@ __global__ void __launch_bounds__(kGradThreads) gradient_kernel(const __grid_con
 
 template <int NB, bool BF>
 windq_status launch_gradients(windq_ctx* ctx, int id, GradArgs p, cudaStream_t st) {
-  const int tiles = p.job[0].tiles + p.job[1].tiles, blocks = (p.T + grad_tokens(NB) - 1) / grad_tokens(NB);
-  // every token has one adapter, so the work of a column tile over all adapters is about one pass over the tokens
+  const int tiles = p.job[0].tiles + p.job[1].tiles, blocks = (p.T + kGradTokens - 1) / kGradTokens;
+  // every token has one adapter, so the work of a column tile over all adapters is about one pass over the tokens; as many
+  // thread blocks as fit, counting on two adapters with tokens where there are so many
   p.splits = 1;
-  while (p.splits < 8 && tiles * p.splits * 2 <= 3 * ctx->sm_count && blocks >= p.splits * 2 * 4) p.splits *= 2;
-  const int tokens = grad_tokens(NB), terms = BF ? 3 : 2;
-  const int loop = grad_stages(NB) * tokens * (kZPitch + p.rank * 4) + 2 * terms * tokens * (p.rank * 2 + 16);
+  while (p.splits < 8 && (int64_t)tiles * std::min(p.n_adapters, 2) * p.splits * 2 <= grad_blocks(NB) * ctx->sm_count && blocks >= p.splits * 2 * 4) p.splits *= 2;
+  const int loop = grad_stages(NB) * kGradTokens * (kZPitch + p.rank * 4) + 2 * (BF ? 3 : 2) * kGradTokens * (p.rank * 2 + 16);
   const int smem = std::max(loop, std::max(kGradCols * (p.rank + 4), p.rank * (kGradCols + 4)) * 4);
-  constexpr int kMost = 112 * 1024;
-  static_assert(grad_stages(NB) * grad_tokens(NB) * (kZPitch + NB * 32) + 6 * grad_tokens(NB) * (NB * 16 + 16) <= kMost, "two an SM");
+  constexpr int kMost = 224 * 1024 / grad_blocks(NB) - 2048;
+  static_assert(grad_stages(NB) * kGradTokens * (kZPitch + NB * 32) + 6 * kGradTokens * (NB * 16 + 16) <= kMost &&
+                    (kGradCols + 4) * (NB * 8 + 4) * 4 <= kMost, "grad_blocks an SM");
   const windq_status ready = prepare_kernel(ctx, id, gradient_kernel<NB, BF>, kGradThreads, kMost, false);
   if (ready != WINDQ_OK) return ready;
   cudaLaunchConfig_t cfg = {};
