@@ -111,7 +111,11 @@ SHAPES = [  # T, R, C, rank, adapters, kind
     (2100, 264, 520, 32, 3, "segments"), (48, 640, 4160, 16, 24, "mixed"), (203, 1200, 8192, 32, 48, "mixed"), (330, 520, 6000, 16, 30, "mixed"),
     # tiles that are split along the reduction, at every height of a tile whose sums share its memory
     (112, 200, 1096, 16, 3, "mixed"), (144, 1030, 2056, 48, 3, "segments"), (192, 2056, 1032, 8, 20, "mixed"), (208, 136, 4104, 32, 3, "mixed"),
-    (209, 2050, 2056, 64, 3, "segments"), (240, 1096, 1096, 24, 7, "mixed"), (256, 4104, 4104, 16, 5, "segments"), (258, 4100, 4104, 128, 3, "mixed"), (3000, 1288, 136, 8, 1, "one"),
+    (209, 2050, 2056, 64, 3, "segments"), (240, 1096, 1096, 24, 7, "mixed"), (256, 4104, 4104, 16, 5, "segments"), (258, 4100, 4104, 128, 3, "mixed"),
+    (300, 1096, 2056, 24, 5, "mixed"), (320, 264, 1096, 16, 2, "segments"),
+    # wide tiles: few and many, split along the reduction or not, of odd widths
+    (321, 200, 8200, 16, 3, "segments"), (700, 2600, 2056, 64, 3, "segments"), (777, 5120, 1032, 8, 6, "segments"), (1300, 3000, 1096, 40, 4, "mixed"),
+    (500, 9001, 520, 16, 3, "segments"), (2600, 4104, 1544, 32, 5, "segments"), (4100, 700, 4104, 16, 2, "segments"), (350, 40, 130 * 64, 8, 1, "one"), (3000, 1288, 136, 8, 1, "one"),
 ]
 
 
