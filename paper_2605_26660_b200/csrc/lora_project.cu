@@ -541,11 +541,19 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   p.token_rows = tall ? token_tile(q.T) : 128;
   p.weight_rows = 128;
   p.token_tiles = (int)((q.T + p.token_rows * blocks_of_tile - 1) / (p.token_rows * blocks_of_tile));
-  // tall tiles: two thread blocks an SM, so that one loads while the other joins and stores, as long as the sums of a
-  // split tile fit into half of the shared memory
-  const bool two = tall && p.token_rows * kTallPitch * 4 <= kSmemLimitTwo - 1024;
+  // Tall tiles: one thread block an SM, with many stages, where tiles split along K then fill most of the GPU (203 tokens x
+  // 8192 x 8192, 128 blocks: 64 against 72 us); otherwise two, if the sums of a split tile fit into half of the shared memory
+  // (150 tokens x 11008 x 4096, 86 blocks against 172: 52 against 46 us).  Up to 64 tokens two blocks have stages enough.
+  const int64_t tall_tiles = (int64_t)p.token_tiles * ((q.N + 127) / 128);
+  auto tall_splits = [&](int64_t slots) {
+    int splits = 1;
+    while (splits < 8 && tall_tiles * splits * 2 <= slots && p.chunks >= splits * 2 * 4) splits *= 2;
+    return splits;
+  };
+  const bool two = tall && p.token_rows * kTallPitch * 4 <= kSmemLimitTwo - 1024 &&
+                   (p.token_rows <= 64 || tall_tiles * tall_splits(ctx->sm_count) * 5 < ctx->sm_count * 4);
   const int64_t slots = tall ? (int64_t)ctx->sm_count * (two ? 2 : 1) : ctx->sm_count / 2;
-  p.splits = 1;
+  p.splits = tall ? tall_splits(slots) : 1;
   if (!tall) {
     // outputs of a tile: the width that takes the fewest rounds over the GPU, a chunk of K costing 600 + width (0.39 us at
     // 128, 0.42 at 192, 0.47 at 256).  Tiles that fill less than half of the GPU are split along K instead.
@@ -570,8 +578,6 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   const int staging = tall || p.splits > 1 ? 0 : 4 * 2 * 4096;
   p.stages = std::min(kMaxStages, (limit - 1024 - staging) / stage);
   const int64_t tiles = (int64_t)p.token_tiles * p.weight_tiles;
-  if (tall)
-    while (p.splits < 8 && tiles * p.splits * 2 <= slots && p.chunks >= p.splits * 2 * 4) p.splits *= 2;
   p.accumulators = !tall && p.splits == 1 ? 2 : 1;
   p.columns = tall ? (p.token_rows <= 32 ? 32 : p.token_rows <= 64 ? 64 : p.token_rows <= 128 ? 128 : 256) : 256 * p.accumulators;
   const int64_t blocks = (p.splits > 1 ? tiles * p.splits : std::min(tiles, slots)) * blocks_of_tile;
