@@ -544,10 +544,11 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   // Tall tiles: one thread block an SM, with many stages, where tiles split along K then fill most of the GPU (203 tokens x
   // 8192 x 8192, 128 blocks: 64 against 72 us); otherwise two, if the sums of a split tile fit into half of the shared memory
   // (150 tokens x 11008 x 4096, 86 blocks against 172: 52 against 46 us).  Up to 64 tokens two blocks have stages enough.
+  // Four splits at most: clusters of eight start and join slowly (192 tokens x 2048 x 8192: 42 us, with four 34).
   const int64_t tall_tiles = (int64_t)p.token_tiles * ((q.N + 127) / 128);
   auto tall_splits = [&](int64_t slots) {
     int splits = 1;
-    while (splits < 8 && tall_tiles * splits * 2 <= slots && p.chunks >= splits * 2 * 4) splits *= 2;
+    while (splits < 4 && tall_tiles * splits * 2 <= slots && p.chunks >= splits * 2 * 4) splits *= 2;
     return splits;
   };
   const bool two = tall && p.token_rows * kTallPitch * 4 <= kSmemLimitTwo - 1024 &&
