@@ -122,7 +122,7 @@ __device__ __forceinline__ void finish_tokens(const LowRankArgs& p, const LowJob
   }
 }
 
-constexpr int kStages = 8, kRows = 128;
+constexpr int kStages = 16, kRows = 128;
 constexpr int kLowSmem = 227 * 1024 - 3072;
 
 // Passes: `pack` adapters at a time, as many as 128 columns hold (transposed, where an adapter takes a block of 64 columns
@@ -149,8 +149,6 @@ __global__ void __launch_bounds__(kLowThreads)
   const bool other = blockIdx.y >= p.slots;
   const int slot = blockIdx.y - (other ? p.slots : 0);
   const LowJob& job = p.job[other];
-  const CUtensorMap* zmap = other ? &z1 : &z0;
-  const CUtensorMap* pmap = other ? &p1 : &p0;
   const bool trans = job.transposed;
   const int r = p.rank, wide = (r + 15) & ~15;
   const int pack = p.pack[trans];
@@ -166,8 +164,8 @@ __global__ void __launch_bounds__(kLowThreads)
   const int t0 = tile * p.rows;
 
   if (tid == 0) {
-    prefetch_map(zmap);
-    prefetch_map(pmap);
+    prefetch_map(other ? &z1 : &z0);
+    prefetch_map(other ? &p1 : &p0);
     for (int s = 0; s < p.stages; s++) {
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
@@ -193,29 +191,36 @@ __global__ void __launch_bounds__(kLowThreads)
   const int passes = (n_used + pack - 1) / pack;
 
   if (warp == 0) {
-    int s = 0;
-    uint32_t phase = 0;
-    for (int pass = slot; pass < passes; pass += p.slots) {
-      const int count = min(pack, n_used - pass * pack);
-      const uint32_t bytes = token_bytes + (trans ? (r > 64 ? 16384 : count * 8192) : count * wide * 128);
-      for (int c = c0; c < c1; c++) {
-        mbar_wait(empty(s), phase ^ 1, dead_);
-        const uint32_t at = base + s * stage_bytes;
-        if (elect_one() && !*(volatile int*)&dead) {
-          mbar_expect(full(s), bytes);
-          tma_load_2d<false>(at, zmap, c * 64, t0, full(s));
-          if (trans) {
-            for (int u = 0; u < count; u++) tma_load_3d<false>(at + token_bytes + u * 8192, pmap, 0, c * 64, used[pass * pack + u], full(s));
-            if (r > 64) tma_load_3d<false>(at + token_bytes + 8192, pmap, 64, c * 64, used[pass], full(s));
-          } else {
-            for (int u = 0; u < count; u++)
-              tma_load_3d<false>(at + token_bytes + u * wide * 128, pmap, c * 64, 0, used[pass * pack + u], full(s));
+    // (a copy of the loop for each job's maps: an address that is picked at run time takes three times as long to issue)
+    auto copy = [&](const CUtensorMap& zmap, const CUtensorMap& pmap) {
+      int s = 0;
+      uint32_t phase = 0;
+      for (int pass = slot; pass < passes; pass += p.slots) {
+        const int count = min(pack, n_used - pass * pack), first = uniform(used[pass * pack]);
+        const uint32_t bytes = token_bytes + (trans ? (r > 64 ? 16384 : count * 8192) : count * wide * 128);
+        for (int c = c0; c < c1; c++) {
+          mbar_wait(empty(s), phase ^ 1, dead_);
+          const uint32_t at = base + s * stage_bytes, bar = full(s);
+          if (elect_one() && !*(volatile int*)&dead) {
+            mbar_expect(bar, bytes);
+            tma_load_2d<false>(at, &zmap, c * 64, t0, bar);
+            if (trans) {
+              tma_load_3d<false>(at + token_bytes, &pmap, 0, c * 64, first, bar);
+              if (r > 64) tma_load_3d<false>(at + token_bytes + 8192, &pmap, 64, c * 64, first, bar);
+              else if (count > 1) tma_load_3d<false>(at + token_bytes + 8192, &pmap, 0, c * 64, used[pass * pack + 1], bar);
+            } else {
+              tma_load_3d<false>(at + token_bytes, &pmap, c * 64, 0, first, bar);
+              for (int u = 1; u < count; u++)
+                tma_load_3d<false>(at + token_bytes + u * wide * 128, &pmap, c * 64, 0, used[pass * pack + u], bar);
+            }
           }
+          __syncwarp();
+          if (++s == p.stages) s = 0, phase ^= 1;
         }
-        __syncwarp();
-        if (++s == p.stages) s = 0, phase ^= 1;
       }
-    }
+    };
+    if (other) copy(z1, p1);
+    else copy(z0, p0);
   } else if (warp == 1) {
     const uint64_t z_desc = smem_desc(base, 16), p_desc = smem_desc(base + token_bytes, trans ? 8192 : 16);
     const uint32_t p_step = trans ? 2048 >> 4 : 32 >> 4;
