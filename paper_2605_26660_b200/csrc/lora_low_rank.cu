@@ -140,9 +140,10 @@ __global__ void __launch_bounds__(kLowThreads)
   __shared__ int dead, ids[256], used[kRows], tops[kRows], taken[kLowWarps];
   __shared__ bool mine[kRows];
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
-  launch_dependents();
   const int split = blockIdx.x % p.splits, tile = blockIdx.x / p.splits;
   if (blockIdx.y == p.jobs * p.slots) {
+    wait_for_predecessor();
+    launch_dependents();
     if (split == 0 && tile < p.list_tiles) write_list(p, tile, ids, taken);
     return;  // of a whole cluster
   }
@@ -178,6 +179,10 @@ __global__ void __launch_bounds__(kLowThreads)
   }
   __syncwarp();
   if (warp == 1) tmem_alloc<false>(smem_addr(&tmem_slot), columns);
+  // Nothing of this call is read or written before the stream's earlier work has ended -- and the kernels that follow may
+  // not start before that either: the projection reads its operands without waiting for this kernel.
+  wait_for_predecessor();
+  launch_dependents();
   int n_used;
   const int id = tid < p.rows ? valid_id(p, t0 + tid) : -1, place = first_place(id, p.rows, ids, taken, &n_used);
   if (place >= 0) used[place] = id;
@@ -347,12 +352,14 @@ windq_status launch(windq_ctx* ctx, LowRankArgs p, cudaStream_t st) {
   cfg.blockDim = dim3(kLowThreads);
   cfg.dynamicSmemBytes = 1024 + p.stages * p.stage_bytes + sums;
   cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = p.splits;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = p.splits > 1 ? 1 : 0;
+  cudaLaunchAttribute attrs[2];
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = p.splits;
+  attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+  cfg.attrs = attrs;
+  cfg.numAttrs = p.splits > 1 ? 2 : 1;
   WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, low_rank_kernel, z[0], pm[0], z[1], pm[1], p));
   return WINDQ_OK;
 }

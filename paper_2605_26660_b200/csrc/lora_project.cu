@@ -145,6 +145,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
   __syncthreads();
   if (PAIR) cluster_sync();  // the other block's barriers are ready
   tc_fence_after();
+  launch_dependents();  // the next call's low-rank kernel may set itself up while the last tiles finish
   const uint32_t tmem = tmem_slot;
 
   const int team = kBlocks * p.splits;  // thread blocks of a tile
