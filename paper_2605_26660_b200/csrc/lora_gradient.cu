@@ -19,9 +19,13 @@ constexpr int kZPitch = kGradCols * 2 + 16;  // bytes
 constexpr int kGradTokens = 32;              // of a block
 constexpr int kWindow = 128;                 // blocks of tokens whose adapters are looked up at a time
 
-// Stages of copies in flight, by the rank / 8 that a kernel is made for, and thread blocks an SM.
-__host__ __device__ constexpr int grad_stages(int nb) { return nb <= 4 ? 4 : 3; }
-__host__ __device__ constexpr int grad_blocks(int nb) { return nb <= 8 ? 2 : 1; }
+// Values j of S that a thread block takes: all of rank 32, and blocks of 32 of a larger one (Z is then read again, from L2).
+constexpr int kGradRank = 32;
+constexpr int kGradStages = 4, kGradBlocks = 2;  // stages of copies in flight; thread blocks an SM
+// The products cut a sum off where they add to it: over 1024 tokens 1.2e-6 of a gradient with S in one term, and more with
+// the small second and third terms, where a plain binary32 product is 1e-6 off.  So the sums of four blocks of tokens (128)
+// are added, rounded, to a second set of registers, which is also why the rank is taken in blocks.
+constexpr int kFlush = 4;
 
 struct GradJob {
   const uint16_t* Z;
@@ -47,8 +51,8 @@ struct GradArgs {
 // largest |S| of the adapter's tokens so far near 2^13, so that small gradients keep their bits (the sums are rescaled,
 // exactly, where a later window of tokens holds a larger one).
 template <int NB, bool BF>
-__global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel(const __grid_constant__ GradArgs p) {
-  constexpr int kTerms = BF ? 3 : 2, kTokens = kGradTokens, kStages = grad_stages(NB);
+__global__ void __launch_bounds__(kGradThreads, kGradBlocks) gradient_kernel(const __grid_constant__ GradArgs p) {
+  constexpr int kTerms = BF ? 3 : 2, kTokens = kGradTokens, kStages = kGradStages;
   constexpr int kPieces = (kTokens * NB + kGradThreads - 1) / kGradThreads;              // of eight values of S, a thread
   extern __shared__ uint4 shared[];
   __shared__ unsigned masks[kWindow];  // tokens of the adapter
@@ -56,7 +60,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel
   __shared__ int n_active;
   __shared__ float tops[kGradWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
-  const int split = blockIdx.x % p.splits, a = blockIdx.y, r = p.rank;
+  const int split = blockIdx.x % p.splits, a = blockIdx.y, j0 = blockIdx.z * kGradRank, r = min(p.rank - j0, kGradRank);
   int tile = blockIdx.x / p.splits;
   const bool second = tile >= p.job[0].tiles;
   const GradJob& job = p.job[second];
@@ -79,6 +83,18 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel
     for (int n = 0; n < NB; n++)
 #pragma unroll
       for (int k = 0; k < 4; k++) acc[h][n][k] = 0.0f;
+  float kept[2][NB][4] = {};
+  auto flush = [&] {
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+      for (int n = 0; n < NB; n++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          kept[h][n][k] += acc[h][n][k];
+          acc[h][n][k] = 0.0f;
+        }
+  };
 
   for (int w0 = 0; w0 < all; w0 += kWindow) {
     const int count = min(kWindow, all - w0);
@@ -108,12 +124,13 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel
         up = next;
         down = __uint_as_float((uint32_t)(127 - k) << 23);
         if (w0 > 0) {
+          flush();
 #pragma unroll
           for (int h = 0; h < 2; h++)
 #pragma unroll
             for (int n = 0; n < NB; n++)
 #pragma unroll
-              for (int q = 0; q < 4; q++) acc[h][n][q] *= change;
+              for (int q = 0; q < 4; q++) kept[h][n][q] *= change;
         }
       }
     }
@@ -144,7 +161,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel
           const int x = h * kGradThreads + tid, row = x / NB, piece = x % NB;
           if (row >= kTokens || piece * 8 >= r) continue;
           const bool on = masks[b] >> row & 1;
-          const float* src = on ? job.S + (int64_t)(t0 + row) * r + piece * 8 : job.S;
+          const float* src = on ? job.S + (int64_t)(t0 + row) * p.rank + j0 + piece * 8 : job.S;
           const uint32_t dst = at + kTokens * kZPitch + (row * r + piece * 8) * 4;
           copy16(dst, src, on ? 16 : 0);
           copy16(dst + 16, src + 4, on ? 16 : 0);
@@ -187,6 +204,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel
 #pragma unroll
     for (int i = 0; i < kStages - 1; i++) copy_block(i);
     for (int i = 0; i < n_blocks; i++) {
+      if (i % kFlush == 0 && i) flush();
       copy_wait<kStages - 2>();
       split_s(i);
       __syncthreads();
@@ -221,6 +239,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel
     copy_wait<0>();
   }
   __syncthreads();
+  flush();
   // join the cluster: [column][j] for dB, [j][column] for dA, as the result lies
   const int pitch = job.j_first ? r + 4 : kGradCols + 4;
 #pragma unroll
@@ -232,7 +251,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel
         for (int k = 0; k < 4; k++) {
           const int j = n * 8 + q * 2 + (k & 1), c = warp * 32 + h * 16 + g + (k >> 1) * 8;
           asm volatile("st.shared.f32 [%0], %1;" ::"r"(base + (job.j_first ? c * pitch + j : j * pitch + c) * 4),
-                       "f"(acc[h][n][k] * down)
+                       "f"(kept[h][n][k] * down)
                        : "memory");
         }
       }
@@ -241,7 +260,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel
   else __syncthreads();
   const int cols = min(kGradCols, job.cols - c0);
   const int quads = (job.j_first ? r : cols) / 4, items = (job.j_first ? cols : r) * quads;  // four values each
-  float* D = job.D + (int64_t)a * r * job.cols;
+  float* D = job.D + (int64_t)a * p.rank * job.cols + (job.j_first ? j0 : (int64_t)j0 * job.cols);
   constexpr int U = 4;
   for (int i = split * kGradThreads + tid; i < items; i += U * p.splits * kGradThreads) {
     uint32_t offset[U];
@@ -257,7 +276,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_blocks(NB)) gradient_kernel
       const int e = i + u * p.splits * kGradThreads;
       if (e >= items) continue;
       const int row = e / quads, col = e % quads * 4;
-      *reinterpret_cast<float4*>(D + (job.j_first ? (int64_t)(c0 + row) * r + col : (int64_t)row * job.cols + c0 + col)) = x[u];
+      *reinterpret_cast<float4*>(D + (job.j_first ? (int64_t)(c0 + row) * p.rank + col : (int64_t)row * job.cols + c0 + col)) = x[u];
     }
   }
   __syncwarp();
@@ -269,17 +288,20 @@ windq_status launch_gradients(windq_ctx* ctx, int id, GradArgs p, cudaStream_t s
   const int tiles = p.job[0].tiles + p.job[1].tiles, blocks = (p.T + kGradTokens - 1) / kGradTokens;
   // every token has one adapter, so the work of a column tile over all adapters is about one pass over the tokens; as many
   // thread blocks as fit, counting on two adapters with tokens where there are so many
+  const int ranks = (p.rank + kGradRank - 1) / kGradRank, r = std::min(p.rank, kGradRank);
   p.splits = 1;
-  while (p.splits < 8 && (int64_t)tiles * std::min(p.n_adapters, 2) * p.splits * 2 <= grad_blocks(NB) * ctx->sm_count && blocks >= p.splits * 2 * 4) p.splits *= 2;
-  const int loop = grad_stages(NB) * kGradTokens * (kZPitch + p.rank * 4) + 2 * (BF ? 3 : 2) * kGradTokens * (p.rank * 2 + 16);
-  const int smem = std::max(loop, std::max(kGradCols * (p.rank + 4), p.rank * (kGradCols + 4)) * 4);
-  constexpr int kMost = 224 * 1024 / grad_blocks(NB) - 2048;
-  static_assert(grad_stages(NB) * kGradTokens * (kZPitch + NB * 32) + 6 * kGradTokens * (NB * 16 + 16) <= kMost &&
-                    (kGradCols + 4) * (NB * 8 + 4) * 4 <= kMost, "grad_blocks an SM");
+  while (p.splits < 8 && (int64_t)tiles * ranks * std::min(p.n_adapters, 2) * p.splits * 2 <= kGradBlocks * ctx->sm_count &&
+         blocks >= p.splits * 2 * 4)
+    p.splits *= 2;
+  const int loop = kGradStages * kGradTokens * (kZPitch + r * 4) + 2 * (BF ? 3 : 2) * kGradTokens * (r * 2 + 16);
+  const int smem = std::max(loop, std::max(kGradCols * (r + 4), r * (kGradCols + 4)) * 4);
+  constexpr int kMost = 224 * 1024 / kGradBlocks - 2048;
+  static_assert(kGradStages * kGradTokens * (kZPitch + NB * 32) + 6 * kGradTokens * (NB * 16 + 16) <= kMost &&
+                    (kGradCols + 4) * (NB * 8 + 4) * 4 <= kMost, "kGradBlocks an SM");
   const windq_status ready = prepare_kernel(ctx, id, gradient_kernel<NB, BF>, kGradThreads, kMost, false);
   if (ready != WINDQ_OK) return ready;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * p.splits), (unsigned)p.n_adapters);
+  cfg.gridDim = dim3((unsigned)(tiles * p.splits), (unsigned)p.n_adapters, (unsigned)ranks);
   cfg.blockDim = dim3(kGradThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -318,13 +340,11 @@ windq_status launch_gradients(windq_ctx* ctx, const Gradient* dA, const Gradient
   p.n_adapters = (int)n_adapters;
   p.adapter_of = adapter_of;
 #define WINDQ_GRAD(index, nb)                                                                     \
-  return dtype == WINDQ_BF16 ? launch_gradients<nb, true>(ctx, kGradient + 5 + (index), p, st)    \
+  return dtype == WINDQ_BF16 ? launch_gradients<nb, true>(ctx, kGradient + 3 + (index), p, st)    \
                              : launch_gradients<nb, false>(ctx, kGradient + (index), p, st)
   if (rank <= 8) WINDQ_GRAD(0, 1);
   if (rank <= 16) WINDQ_GRAD(1, 2);
-  if (rank <= 32) WINDQ_GRAD(2, 4);
-  if (rank <= 64) WINDQ_GRAD(3, 8);
-  WINDQ_GRAD(4, 16);
+  WINDQ_GRAD(2, 4);
 #undef WINDQ_GRAD
 }
 

@@ -123,6 +123,7 @@ __device__ __forceinline__ void finish_tokens(const LowRankArgs& p, const LowJob
 }
 
 constexpr int kStages = 16, kRows = 128;
+constexpr int kGroup = 4;  // chunks of K that one accumulator takes
 constexpr int kLowSmem = 227 * 1024 - 3072;
 
 // Passes: `pack` adapters at a time, as many as 128 columns hold (transposed, where an adapter takes a block of 64 columns
@@ -130,12 +131,16 @@ constexpr int kLowSmem = 227 * 1024 - 3072;
 // adapter a pass such tiles took twice as long and with them the whole kernel (41 against 22 us for 8192 tokens of 4096
 // values, rank 64).  `slots` blocks share the passes of a tile, `splits` blocks of a cluster K.  Warps: one issues TMA
 // copies, one the products, four take the rows of their own adapter out of tensor memory.
+//
+// The tensor cores cut a sum off where they add to an accumulator; over 256 steps of K that was 7e-6 of S, and of the
+// gradients S goes into (which are binary32; a plain binary32 product is 1e-6 off).  So an accumulator takes four chunks of
+// K (16 steps), then its values are added, rounded, to sums in shared memory while the other accumulator fills.
 __global__ void __launch_bounds__(kLowThreads)
     low_rank_kernel(const __grid_constant__ CUtensorMap z0, const __grid_constant__ CUtensorMap p0,
                        const __grid_constant__ CUtensorMap z1, const __grid_constant__ CUtensorMap p1,
                        const __grid_constant__ LowRankArgs p) {
   extern __shared__ uint8_t raw[];
-  __shared__ uint64_t full_[kStages], empty_[kStages], done_, free_;
+  __shared__ uint64_t full_[kStages], empty_[kStages], done_[2], free_[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int dead, ids[256], used[kRows], tops[kRows], taken[kLowWarps];
   __shared__ bool mine[kRows];
@@ -153,15 +158,15 @@ __global__ void __launch_bounds__(kLowThreads)
   const bool trans = job.transposed;
   const int r = p.rank, wide = (r + 15) & ~15;
   const int pack = p.pack[trans];
-  const int apart = trans ? 64 : wide;  // columns between the adapters of a pass
   const uint32_t token_bytes = p.rows * 128, stage_bytes = p.stage_bytes;
-  const uint32_t columns = max(32, trans ? (r > 64 ? 128 : 64 * pack) : pack * wide <= 32 ? 32 : pack * wide <= 64 ? 64 : 128);
+  const uint32_t columns = pack * wide <= 32 ? 32 : pack * wide <= 64 ? 64 : 128;  // of an accumulator
   // the product reads 128 rows whatever the tile holds; what follows a short tile gives rows that nobody keeps
   const uint32_t base = (smem_addr(raw) + 1023) & ~1023u, sums = base + p.stages * stage_bytes + (kRows - p.rows) * 128;
   auto full = [&](int s) { return smem_addr(&full_[s]); };
   auto empty = [&](int s) { return smem_addr(&empty_[s]); };
   const uint32_t dead_ = smem_addr(&dead);
-  const uint32_t done = smem_addr(&done_), free = smem_addr(&free_);
+  auto done = [&](int g) { return smem_addr(&done_[g & 1]); };  // of group g's accumulator
+  auto free = [&](int g) { return smem_addr(&free_[g & 1]); };
   const int t0 = tile * p.rows;
 
   if (tid == 0) {
@@ -171,14 +176,16 @@ __global__ void __launch_bounds__(kLowThreads)
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
     }
-    mbar_init(done, 1);
-    mbar_init(free, 4);
+    for (int g = 0; g < 2; g++) {
+      mbar_init(done(g), 1);
+      mbar_init(free(g), 4);
+    }
     dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
   }
   __syncwarp();
-  if (warp == 1) tmem_alloc<false>(smem_addr(&tmem_slot), columns);
+  if (warp == 1) tmem_alloc<false>(smem_addr(&tmem_slot), 2 * columns);
   // Nothing of this call is read or written before the stream's earlier work has ended -- and the kernels that follow may
   // not start before that either: the projection reads its operands without waiting for this kernel.
   wait_for_predecessor();
@@ -229,59 +236,71 @@ __global__ void __launch_bounds__(kLowThreads)
   } else if (warp == 1) {
     const uint64_t z_desc = smem_desc(base, 16), p_desc = smem_desc(base + token_bytes, trans ? 8192 : 16);
     const uint32_t p_step = trans ? 2048 >> 4 : 32 >> 4;
-    int s = 0, turn = 0;
+    int s = 0, g = 0;
     uint32_t phase = 0;
-    for (int pass = slot; pass < passes; pass += p.slots, turn++) {
+    for (int pass = slot; pass < passes; pass += p.slots) {
       const int count = min(pack, n_used - pass * pack);
       const uint32_t idesc = instr_desc(p.dtype, false, trans, 128, trans ? wide : count * wide);
-      mbar_wait(free, (turn & 1) ^ 1, dead_);
-      tc_fence_after();
-      for (int c = c0; c < c1; c++) {
-        mbar_wait(full(s), phase, dead_);
+      for (int c = c0; c < c1; g++) {
+        const uint32_t d = tmem + (g & 1) * columns;
+        mbar_wait(free(g), ((g >> 1) & 1) ^ 1, dead_);
         tc_fence_after();
-        const uint64_t off = (uint64_t)(s * stage_bytes >> 4);
-        if (elect_one()) {
-#pragma unroll
-          for (int k = 0; k < 4; k++)
-            mma_f16<false>(tmem, z_desc + off + k * (32 >> 4), p_desc + off + k * p_step, idesc, c > c0 || k > 0);
-          if (trans && count > 1) {
+        const int end = min(c + kGroup, c1);
+        for (const int begin = c; c < end; c++) {
+          mbar_wait(full(s), phase, dead_);
+          tc_fence_after();
+          const uint64_t off = (uint64_t)(s * stage_bytes >> 4);
+          if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < 4; k++)
-              mma_f16<false>(tmem + 64, z_desc + off + k * (32 >> 4), p_desc + off + (8192 >> 4) + k * p_step, idesc, c > c0 || k > 0);
+              mma_f16<false>(d, z_desc + off + k * (32 >> 4), p_desc + off + k * p_step, idesc, c > begin || k > 0);
+            if (trans && count > 1) {
+#pragma unroll
+              for (int k = 0; k < 4; k++)
+                mma_f16<false>(d + wide, z_desc + off + k * (32 >> 4), p_desc + off + (8192 >> 4) + k * p_step, idesc, c > begin || k > 0);
+            }
+            mma_commit<false>(empty(s), 0);
           }
-          mma_commit<false>(empty(s), 0);
+          __syncwarp();
+          if (++s == p.stages) s = 0, phase ^= 1;
         }
+        if (elect_one()) mma_commit<false>(done(g), 0);
         __syncwarp();
-        if (++s == p.stages) s = 0, phase ^= 1;
       }
-      if (elect_one()) mma_commit<false>(done, 0);
-      __syncwarp();
     }
   } else if (warp < 6) {
     const int quarter = warp & 3, row = quarter * 32 + lane, own = ids[row];
-    int turn = 0;
-    for (int pass = slot; pass < passes; pass += p.slots, turn++) {
-      mbar_wait(done, turn & 1, dead_);
-      tc_fence_after();
+    int g = 0;
+    for (int pass = slot; pass < passes; pass += p.slots) {
       const int count = min(pack, n_used - pass * pack);
-      for (int i = 0; i < count; i++) {
-        const bool keep = own == used[pass * pack + i];
-        if (!__any_sync(0xffffffffu, keep)) continue;
-        if (keep) mine[row] = true;
-        for (int c = 0; c < wide; c += 16) {
-          uint32_t x[16];
-          tmem_load16(tmem + ((uint32_t)(quarter * 32) << 16) + i * apart + c, x);
-          tmem_load_wait();
-          if (keep) {
+      for (int c = c0; c < c1; c += kGroup, g++) {
+        mbar_wait(done(g), (g >> 1) & 1, dead_);
+        tc_fence_after();
+        for (int i = 0; i < count; i++) {
+          const bool keep = own == used[pass * pack + i];
+          if (!__any_sync(0xffffffffu, keep)) continue;
+          if (keep) mine[row] = true;
+          for (int j = 0; j < wide; j += 16) {
+            uint32_t x[16];
+            tmem_load16(tmem + (g & 1) * columns + ((uint32_t)(quarter * 32) << 16) + i * wide + j, x);
+            tmem_load_wait();
+            if (keep) {
 #pragma unroll
-            for (int k = 0; k < 16; k++)
-              if (c + k < r) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sums + (row * (r + 4) + c + k) * 4), "r"(x[k]) : "memory");
+              for (int k = 0; k < 16; k += 4)
+                if (j + k < r) {
+                  const uint32_t at = sums + (row * (r + 4) + j + k) * 4;
+                  float4 y = make_float4(0, 0, 0, 0);
+                  if (c > c0) asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y.x), "=f"(y.y), "=f"(y.z), "=f"(y.w) : "r"(at) : "memory");
+                  y.x += __uint_as_float(x[k]), y.y += __uint_as_float(x[k + 1]), y.z += __uint_as_float(x[k + 2]), y.w += __uint_as_float(x[k + 3]);
+                  asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(y.x), "f"(y.y), "f"(y.z), "f"(y.w) : "memory");
+                }
+            }
           }
         }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(free(g));
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(free);
     }
   }
   __syncwarp();
@@ -291,7 +310,7 @@ __global__ void __launch_bounds__(kLowThreads)
   if (p.splits > 1) cluster_sync();
   if (warp == 1) {
     tc_fence_after();
-    tmem_free<false>(tmem, columns);
+    tmem_free<false>(tmem, 2 * columns);
   }
   finish_tokens(p, job, t0, p.rows, sums, r + 4, split, ids, tops, [&](int i) { return mine[i]; });
   __syncwarp();
