@@ -7,12 +7,39 @@
 
 #include "lora.cuh"
 #include "tcgen05.cuh"
-#include "warp_mma.cuh"
 
 namespace windq {
 namespace {
 
-// ---- D[a][j][c] = sum over the tokens t of a of S[t][j] Z[t][c] ----------------------------------------------------
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool bf) {
+  if (bf)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldmatrix_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+// 16 bytes of which the first `bytes` are read and the rest is zero.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// D[a][j][c] = sum over the tokens t of a of S[t][j] Z[t][c]
 
 constexpr int kGradWarps = 8, kGradThreads = 256, kGradCols = 256;
 constexpr int kZPitch = kGradCols * 2 + 16;  // bytes
@@ -42,14 +69,16 @@ struct GradArgs {
   const int32_t* adapter_of;
 };
 
-// A thread block owns 256 columns of Z for one adapter, a warp 32 of them; a cluster of `splits` shares the tokens.  (What
+// A thread block owns 256 columns of Z for one adapter, a warp 32 of them; a cluster of `splits` shares the tokens.  What
 // bounds it once the loads flow is shared memory: every warp reads all of S, so few warps with many columns each are better
-// than many with few -- with 128 columns, 16 a warp, the backward pass of 8192 x 4096 x 4096 took 308 us, and takes 298.)  The tokens that are not
-// the adapter's are left out as rows of zeros (copied with size zero, so that what they hold cannot spoil a sum), blocks
-// of tokens without any of its tokens are skipped.  Z is the transposed left operand (ldmatrix.trans); S enters as two
-// fp16 or three bf16 values whose sum is S to 22 or 24 bits -- fp16 ones after a scaling by a power of two that puts the
-// largest |S| of the adapter's tokens so far near 2^13, so that small gradients keep their bits (the sums are rescaled,
-// exactly, where a later window of tokens holds a larger one).
+// than many with few (with 128 columns a block and 16 a warp the backward pass of 8192 x 4096 x 4096 took 308 us, with these
+// 298; both with 23 us of products of S before and 205 of dX after).
+//
+// The tokens that are not the adapter's are left out as rows of zeros (copied with size zero, so that what they hold cannot
+// spoil a sum), blocks of tokens without any of its tokens are skipped.  Z is the transposed left operand (ldmatrix.trans);
+// S enters as two fp16 or three bf16 values whose sum is S to 22 or 24 bits -- fp16 ones after a scaling by a power of two
+// that puts the largest |S| of the adapter's tokens so far near 2^13, so that small gradients keep their bits (the sums are
+// rescaled, exactly, where a later window of tokens holds a larger one).
 template <int NB, bool BF>
 __global__ void __launch_bounds__(kGradThreads, kGradBlocks) gradient_kernel(const __grid_constant__ GradArgs p) {
   constexpr int kTerms = BF ? 3 : 2, kTokens = kGradTokens, kStages = kGradStages;
