@@ -9,6 +9,7 @@ be built, importing this package raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import operator
 import os
@@ -1166,6 +1167,6 @@ def windq_adamw_states(ctx: Context, tensors: AdamwTensors, m_out=None, v_out=No
             if set(map(_DTYPE_OF, given)) != {torch.float32} or not all(map(_ON_CUDA, given)):
                 raise TypeError("%s must be torch.float32 CUDA tensors" % name)
         outs.append(given)
-        arrays.append((ctypes.c_void_p * k)(*map(torch.Tensor.data_ptr, given)))
-    ctx._check(_lib.windq_adamw_states(ctx._h, tensors._jobs, k, arrays[0], arrays[1], _raw_stream(ctx, stream)))
+        arrays.append(array.array("Q", map(torch.Tensor.data_ptr, given)))   # pointers are 64 bits wide
+    ctx._check(_lib.windq_adamw_states(ctx._h, tensors._jobs, k, *(a.buffer_info()[0] for a in arrays), _raw_stream(ctx, stream)))
     return tuple(outs)

@@ -137,11 +137,15 @@ __device__ __forceinline__ float code_bits(uint32_t w, int k) { return __uint_as
 constexpr float kShift = 8388608.0f;   // 2^23
 constexpr float kRound = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer (to nearest even), kept in the low bits
 
-// rint(sqrt(x) * levels) of eight values in [0, 1], plus kRound; values with their signs when `sign` is given.  The
-// hardware's square root is off by 2^-22 of itself at most, the product by another 2^-24: less than `guard` of a code.  Only
-// where that could cross a rounding boundary is the correctly rounded root taken.
+// rint(sqrt(|x|) * levels) of eight values in [-1, 1], with the sign of x where SIGNED, plus kRound.  The hardware's square
+// root is off by 2^-22 of itself at most, the product by another 2^-24: less than `guard` of a code.  Only where that could
+// cross a rounding boundary is the correctly rounded root taken.
 template <bool SIGNED>
-__device__ __forceinline__ void encode8(const float (&x)[8], const float (&sign)[8], float levels, float guard, float (&out)[8]) {
+__device__ __forceinline__ float with_sign(float y, float x) {  // y >= 0
+  return SIGNED ? __uint_as_float(__float_as_uint(y) | (__float_as_uint(x) & 0x80000000u)) : y;
+}
+template <bool SIGNED>
+__device__ __forceinline__ void encode8(const float (&x)[8], float levels, float guard, float (&out)[8]) {
   float worst = 0.0f;
 #pragma unroll
   for (int k = 0; k < 8; k += 2) {
@@ -149,23 +153,15 @@ __device__ __forceinline__ void encode8(const float (&x)[8], const float (&sign)
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fabsf(x[k])));
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fabsf(x[k + 1])));
     y = mul2(y, both(levels));
+    y = make_float2(with_sign<SIGNED>(y.x, x[k]), with_sign<SIGNED>(y.y, x[k + 1]));
     const float2 r = add2(y, both(kRound)), off = fma2(add2(r, both(-kRound)), both(-1.0f), y);
     worst = fmaxf(worst, fmaxf(fabsf(off.x), fabsf(off.y)));
-    if (SIGNED) {
-      // the same code with the sign of the value: kRound - code for a negative one
-      out[k] = sign[k] < 0.0f ? 2.0f * kRound - r.x : r.x;
-      out[k + 1] = sign[k + 1] < 0.0f ? 2.0f * kRound - r.y : r.y;
-    } else {
-      out[k] = r.x;
-      out[k + 1] = r.y;
-    }
+    out[k] = r.x;
+    out[k + 1] = r.y;
   }
   if (worst > 0.5f - guard) {
 #pragma unroll
-    for (int k = 0; k < 8; k++) {
-      const float r = sqrtf(fabsf(x[k])) * levels + kRound;
-      out[k] = SIGNED && sign[k] < 0.0f ? 2.0f * kRound - r : r;
-    }
+    for (int k = 0; k < 8; k++) out[k] = with_sign<SIGNED>(sqrtf(fabsf(x[k])) * levels, x[k]) + kRound;
   }
 }
 // The low bytes of eight such values.
@@ -240,7 +236,7 @@ __global__ void __launch_bounds__(kWarps * 32) adamw8_kernel(const __grid_consta
     const float2 y = mul2(make_float2(m[k], m[k + 1]), both(inv_m));
     x[k] = y.x, x[k + 1] = y.y;
   }
-  encode8<true>(x, m, 127.0f, 0x1p-14f, c);
+  encode8<true>(x, 127.0f, 0x1p-14f, c);
   store_codes(e.m, i, live, low_bytes(c));
   const float least = top_r > 0.0f ? kRound + 1.0f : kRound;  // the code an r above zero gets at least
 #pragma unroll
@@ -248,7 +244,7 @@ __global__ void __launch_bounds__(kWarps * 32) adamw8_kernel(const __grid_consta
     const float2 y = mul2(make_float2(r[k], r[k + 1]), both(inv_r));
     x[k] = y.x, x[k + 1] = y.y;
   }
-  encode8<false>(x, r, 255.0f, 0x1p-13f, c);
+  encode8<false>(x, 255.0f, 0x1p-13f, c);
 #pragma unroll
   for (int k = 0; k < 8; k++) c[k] = r[k] > 0.0f ? fmaxf(c[k], least) : c[k];
   store_codes(e.v, i, live, low_bytes(c));
