@@ -186,8 +186,10 @@ __global__ void __launch_bounds__(kLowThreads)
   }
   __syncwarp();
   if (warp == 1) tmem_alloc<false>(smem_addr(&tmem_slot), 2 * columns);
+  __syncthreads();
   // Nothing of this call is read or written before the stream's earlier work has ended -- and the kernels that follow may
-  // not start before that either: the projection reads its operands without waiting for this kernel.
+  // not start before that either: the projection reads its operands without waiting for this kernel.  Nor may they start
+  // before this block has its tensor memory: the projection holds its own while it waits for this kernel.
   wait_for_predecessor();
   launch_dependents();
   int n_used;
@@ -355,6 +357,10 @@ windq_status launch(windq_ctx* ctx, LowRankArgs p, cudaStream_t st) {
   const int chunks = (std::max(p.job[0].K, p.job[p.jobs - 1].K) + 63) / 64;
   p.stages = std::max(2, std::min({kStages, (room - 1024 - sums) / p.stage_bytes, (chunks + p.splits - 1) / p.splits}));
   while (p.stages > 2 && 1024 + p.stages * p.stage_bytes + sums > kLowSmem) p.stages--;
+  // No more blocks an SM than its 512 columns of tensor memory serve: a block that waited for columns while the rest of its
+  // cluster holds some could wait for a block that waits for it.
+  const int columns = p.pack[0] * wide <= 32 ? 32 : p.pack[0] * wide <= 64 ? 64 : 128;  // at least those of the transposed job
+  const int smem = std::max(1024 + p.stages * p.stage_bytes + sums, 228 * 1024 / (512 / (2 * columns) + 1) + 1);
   const windq_status ready = prepare_kernel(ctx, kLowRank, low_rank_kernel, kLowThreads, kLowSmem, false);
   if (ready != WINDQ_OK) return ready;
   WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
@@ -369,7 +375,7 @@ windq_status launch(windq_ctx* ctx, LowRankArgs p, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * p.splits), (unsigned)(p.jobs * p.slots + (p.lists ? 1 : 0)));
   cfg.blockDim = dim3(kLowThreads);
-  cfg.dynamicSmemBytes = 1024 + p.stages * p.stage_bytes + sums;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attrs[2];
   attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
