@@ -557,15 +557,18 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   const int64_t slots = tall ? (int64_t)ctx->sm_count * (two ? 2 : 1) : ctx->sm_count / 2;
   p.splits = tall ? tall_splits(slots) : 1;
   if (!tall) {
-    // outputs of a tile: the width that takes the fewest rounds over the GPU, a chunk of K costing 600 + width (0.39 us at
-    // 128, 0.42 at 192, 0.47 at 256).  Tiles that fill less than half of the GPU are split along K instead.
+    // Outputs of a tile: the width that takes the least time in rounds over the GPU.  Measured, a chunk of K takes 0.23 us at
+    // width 128, 0.24 at 160, 0.27 at 192, 0.31 at 224 and 0.36 at 256 (max(210 + w / 5, 1.39 w) ns), a tile 2 us more, and 5
+    // where it is split along K; a narrow tile moves more bytes a product, which tells where power is the limit.  Tiles that
+    // fill less than half of the GPU are split.
     int64_t best = INT64_MAX;
     for (int rows = 128; rows >= 48; rows -= 16) {
       const int64_t tiles = p.token_tiles * ((q.N + 2 * rows - 1) / (2 * rows));
       int splits = 1;
       while (splits < 4 && tiles * splits * 2 <= slots && p.chunks >= splits * 2 * 4) splits *= 2;
       const int64_t waves = (tiles * splits + slots - 1) / slots;
-      const int64_t cost = waves * ((p.chunks + splits - 1) / splits * (600 + 2 * rows) + (splits > 1 ? 9000 : 4000));
+      const int width = 2 * rows, chunk = std::max(210 + width / 5, width * 139 / 100) * (1256 - width) / 1000;
+      const int64_t cost = waves * ((int64_t)(p.chunks + splits - 1) / splits * chunk + (splits > 1 ? 5000 : 2000));
       if (cost < best) {
         best = cost;
         p.weight_rows = rows;
