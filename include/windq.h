@@ -90,7 +90,9 @@ windq_status windq_fit_work(windq_ctx* ctx, int64_t* evaluated_out, int64_t* sea
 
 /* Thread blocks of windq_lora_forward / windq_lora_backward in which a wait on a copy or a matrix product gave up after
  * about two seconds: 0 unless the GPU or the library is broken; the results of a call that adds to it are invalid.  (Every
- * wait of a kernel is bounded, so that such a fault ends the kernel instead of hanging the GPU.)
+ * wait on a barrier of shared memory is bounded, so that such a fault ends the kernel instead of hanging the GPU.  What
+ * waits without a limit -- for tensor memory, for the other blocks of a cluster, for the kernel before -- waits for blocks
+ * that run to that point by themselves.)
  *   n_out: HOST pointer to one int64; reset != 0 puts the counter back to zero.  Synchronises the device. */
 windq_status windq_stalls(windq_ctx* ctx, int64_t* n_out, int reset);
 

@@ -309,11 +309,14 @@ __global__ void __launch_bounds__(kLowThreads)
   __syncthreads();
   if (dead) settle(p.stalls);
   __syncwarp();
-  if (p.splits > 1) cluster_sync();
+  // Before the cluster's barrier: a block that waits for its peers holds no tensor memory, so that whoever waits for columns
+  // (a peer's allocation behind a block of another stream, say) waits only for blocks that run to this point by themselves.
   if (warp == 1) {
     tc_fence_after();
     tmem_free<false>(tmem, 2 * columns);
   }
+  __syncwarp();
+  if (p.splits > 1) cluster_sync();
   finish_tokens(p, job, t0, p.rows, sums, r + 4, split, ids, tops, [&](int i) { return mine[i]; });
   __syncwarp();
   if (p.splits > 1) cluster_sync();
@@ -357,8 +360,7 @@ windq_status launch(windq_ctx* ctx, LowRankArgs p, cudaStream_t st) {
   const int chunks = (std::max(p.job[0].K, p.job[p.jobs - 1].K) + 63) / 64;
   p.stages = std::max(2, std::min({kStages, (room - 1024 - sums) / p.stage_bytes, (chunks + p.splits - 1) / p.splits}));
   while (p.stages > 2 && 1024 + p.stages * p.stage_bytes + sums > kLowSmem) p.stages--;
-  // No more blocks an SM than its 512 columns of tensor memory serve: a block that waited for columns while the rest of its
-  // cluster holds some could wait for a block that waits for it.
+  // No more blocks an SM than its 512 columns of tensor memory serve: another would hold shared memory only to wait.
   const int columns = p.pack[0] * wide <= 32 ? 32 : p.pack[0] * wide <= 64 ? 64 : 128;  // at least those of the transposed job
   const int smem = std::max(1024 + p.stages * p.stage_bytes + sums, 228 * 1024 / (512 / (2 * columns) + 1) + 1);
   const windq_status ready = prepare_kernel(ctx, kLowRank, low_rank_kernel, kLowThreads, kLowSmem, false);

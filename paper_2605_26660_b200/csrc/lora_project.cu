@@ -447,8 +447,16 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
   __syncthreads();
   if (dead) settle(p.stalls);
   __syncwarp();
+  // A block of its own gives its tensor memory back before it waits for the cluster (see low_rank_kernel).  A pair frees it
+  // together, when neither is at work any more; what may share an SM with a pair of split tiles (256 columns, at least 180 KB)
+  // is one low-rank block of at most 128 columns; beside a pair of whole tiles (512 columns, at least 202 KB) none fits.
+  if (!PAIR && warp == 1) {
+    tc_fence_after();
+    tmem_free<PAIR>(tmem, p.columns);
+  }
+  __syncwarp();
   if (team > 1) cluster_sync();  // no more arrivals from other blocks; their sums are in shared memory
-  if (warp == 1) {
+  if (PAIR && warp == 1) {
     tc_fence_after();
     tmem_free<PAIR>(tmem, p.columns);
   }

@@ -19,7 +19,7 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// Every wait of a kernel ends: after about two seconds, or as soon as another wait of its thread block has given up, it
+// Every wait on a barrier ends: after about two seconds, or as soon as another wait of its thread block has given up, it
 // raises *dead (a word of shared memory) and falls through.  The roles then run to their ends without issuing copies.
 //
 // The loop stays inside the asm block on purpose: a branch the compiler saw would make the control flow of the issuing
