@@ -1112,7 +1112,8 @@ class AdamwTensors:
             self._jobs[j] = _AdamwJob(params[j].data_ptr(), None, m[j].data_ptr(), v[j].data_ptr(),
                                       *(None if t is None else t.data_ptr() for t in scales),
                                       None if copy is None else copy.data_ptr(), n)
-        self._keep = (list(params), list(m), list(v), m_scale, r_scale, copies)
+        # aliases, not the caller's lists and tensor objects: either may come to hold other memory while the jobs keep the addresses
+        self._keep = [[None if t is None else t.detach() for t in ts] for ts in (params, m, v, m_scale, r_scale, copies) if ts is not None]
         self._sizes = [p.numel() for p in params]
         self._codes = (_DTYPE_CODES[self.param_dtype], _DTYPE_CODES[self.grad_dtype], _DTYPE_CODES[self.copy_dtype], self.state_bits)
         self.set_grads(grads)
@@ -1134,7 +1135,7 @@ class AdamwTensors:
             self._flat(g, self.grad_dtype, self._jobs[j].n, "grads")
         for j, g in enumerate(grads):
             self._jobs[j].grad = g.data_ptr()
-        self._grads = list(grads)
+        self._grads = [g.detach() for g in grads]
 
 
 def windq_adamw_step(ctx: Context, tensors: AdamwTensors, *, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
