@@ -21,8 +21,12 @@
  *     Nothing is retained after a call.  `stream` is a cudaStream_t passed as void* (NULL = the
  *     legacy default stream).  Calls only enqueue work on `stream`; outputs are valid once the
  *     stream has reached that point.  The library allocates no outputs.  It owns a scratch
- *     buffer inside the context, grown (cudaMalloc, which synchronises) only when a call needs
- *     more than it has; windq_reserve sizes it ahead of time.
+ *     buffer inside the context, grown (cudaMalloc, which may synchronise) only when a call needs
+ *     more than it has; windq_reserve sizes it ahead of time.  A buffer it has outgrown stays allocated
+ *     until windq_destroy (all of them together take no more than the one in use), so that a call captured
+ *     in a CUDA graph replays at any time before that, whatever the context did since.  Scratch cannot grow
+ *     while a stream is captured: make the call once before, or reserve.  A replay counts as a call for the
+ *     ordering below.
  *   - Errors: every argument check happens on the host before anything is launched; a failing
  *     call launches nothing and returns a status, and windq_last_error gives the reason.  There
  *     are no exceptions, aborts or device traps.  Inputs must be finite; NaN / Inf give
@@ -96,7 +100,7 @@ windq_status windq_fit_work(windq_ctx* ctx, int64_t* evaluated_out, int64_t* sea
  *   n_out: HOST pointer to one int64; reset != 0 puts the counter back to zero.  Synchronises the device. */
 windq_status windq_stalls(windq_ctx* ctx, int64_t* n_out, int reset);
 
-/* Grows the context's scratch buffer to at least `bytes` now (synchronises the device), so that
+/* Grows the context's scratch buffer to at least `bytes` now (may synchronise the device), so that
  * later calls do not allocate.  windq_scratch_bytes_* tell how much a call will need. */
 windq_status windq_reserve(windq_ctx* ctx, int64_t bytes);
 int64_t windq_scratch_bytes_act_stats(int64_t T, int64_t C);

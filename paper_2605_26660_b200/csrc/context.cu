@@ -29,17 +29,18 @@ windq_status fail(windq_ctx* ctx, windq_status st, const char* fmt, ...) {
 
 windq_status ensure_scratch(windq_ctx* ctx, int64_t bytes) {
   if (bytes <= ctx->scratch_bytes) return WINDQ_OK;
-  const int64_t want = round_up(bytes, 1 << 20);
+  // The old buffer stays: earlier calls may still be using it, and a captured call that is replayed later will.  Doubling
+  // bounds what all of them take by the size of the one in use (where the GPU has room for that).
+  const int64_t least = round_up(bytes, 1 << 20), twice = 2 * ctx->scratch_bytes;
+  int64_t want = least > twice ? least : twice;
+  const bool full = ctx->n_outgrown == (int)(sizeof(ctx->outgrown) / sizeof(ctx->outgrown[0]));
   void* p = nullptr;
-  if (cudaMalloc(&p, (size_t)want) != cudaSuccess) {
+  if (full || (cudaMalloc(&p, (size_t)want) != cudaSuccess && cudaMalloc(&p, (size_t)(want = least)) != cudaSuccess)) {
     cudaGetLastError();
-    return fail(ctx, WINDQ_ERR_SCRATCH, "cannot grow scratch to %lld bytes", (long long)want);
+    return fail(ctx, WINDQ_ERR_SCRATCH, "cannot grow scratch to %lld bytes", (long long)least);
   }
-  if (ctx->scratch) {
-    // earlier calls may still be using the old buffer on some stream
-    cudaDeviceSynchronize();
-    cudaFree(ctx->scratch);
-  }
+  cudaGetLastError();
+  if (ctx->scratch) ctx->outgrown[ctx->n_outgrown++] = ctx->scratch;
   ctx->scratch = p;
   ctx->scratch_bytes = want;
   return WINDQ_OK;
@@ -100,6 +101,7 @@ windq_status windq_create(windq_ctx** out, int device) {
   ctx->sm_count = prop.multiProcessorCount;
   ctx->scratch = nullptr;
   ctx->scratch_bytes = 0;
+  ctx->n_outgrown = 0;
   ctx->prepared[0] = ctx->prepared[1] = 0;
   memset(ctx->occupancy, 0, sizeof(ctx->occupancy));
   ctx->err[0] = 0;
@@ -113,6 +115,7 @@ void windq_destroy(windq_ctx* ctx) {
     windq::DeviceGuard guard(ctx->device);
     cudaDeviceSynchronize();
     if (ctx->scratch) cudaFree(ctx->scratch);
+    for (int k = 0; k < ctx->n_outgrown; k++) cudaFree(ctx->outgrown[k]);
     cudaFree(ctx->sync);
   }
   delete ctx;

@@ -14,6 +14,8 @@ struct windq_ctx {
   int sm_count;
   void* scratch;
   int64_t scratch_bytes;
+  void* outgrown[32];  // earlier scratch buffers, kept for what still uses them; each at least twice the one before (see ensure_scratch)
+  int n_outgrown;
   unsigned int* sync;  // kSyncCounters arrival counters, zero between launches; two 64-bit work counters and one of stalls follow them
   unsigned long long prepared[2];  // kernels whose attributes have been set on this context's device (bit per KernelId)
   int occupancy[128];              // resident blocks per SM of those kernels (0 where not asked)
