@@ -594,8 +594,10 @@ typedef enum { WINDQ_F16 = 0, WINDQ_BF16 = 1, WINDQ_F32 = 2 } windq_dtype;
  *                                            smaller rank are padded with zeros)
  *   scaling     fp32 [n_adapters];  adapter_of  i32 [T]
  * T = 0 is allowed and does nothing.  Y must not overlap an input.  Columns of Y at and beyond R are not written.
- * On WINDQ_F16, u_t is carried as the sum of two fp16 values and therefore saturates at +-131008; inputs must be finite
- * (an adapter with a non-finite weight spoils the rows of every token within 256 tokens of one of its own).
+ * On WINDQ_F16, u_t is carried as the sum of two fp16 values and therefore saturates at +-131008.  What is not finite shows:
+ * a token, or an adapter with its scaling, that is not finite gives rows that are not, where the formula has none.  Rows of
+ * others are not touched, but for one case: a weight of B[a] that is not finite (in windq_lora_backward's dX: of A[a]) may
+ * spoil the rows of every token within 256 tokens of one of a's.
  * Scratch: windq_scratch_bytes_lora_forward. */
 int64_t windq_scratch_bytes_lora_forward(int64_t T, int64_t R, int64_t C, int rank);
 windq_status windq_lora_forward(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx, const void* W,

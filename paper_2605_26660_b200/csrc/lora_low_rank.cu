@@ -74,6 +74,10 @@ __device__ void write_list(const LowRankArgs& p, int tile, int* ids, int* taken)
   if (threadIdx.x == 0) list[0] = all;
 }
 
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < __int_as_float(0x7f800000); }
+// x in [-most, most]; infinities and NaN as they are (fminf and fmaxf would make a number of NaN).
+__device__ __forceinline__ float clamp(float x, float most) { return finite(x) ? fminf(fmaxf(x, -most), most) : x; }
+
 // S of the tokens of this block from the sums of the cluster's blocks, [token][pitch] at `sums`: four values a thread.
 // kept(i) tells whether token t0 + i is to be written; tops: one word a token, zero.
 template <class Kept>
@@ -91,22 +95,29 @@ __device__ __forceinline__ void finish_tokens(const LowRankArgs& p, const LowJob
     float v[4] = {y[0].x * scale, y[0].y * scale, y[0].z * scale, y[0].w * scale};
     const int64_t at = (int64_t)(t0 + i) * p.rank + j;
     if (job.S) *reinterpret_cast<float4*>(job.S + at) = make_float4(v[0], v[1], v[2], v[3]);
-    if (job.top) atomicMax(&tops[i], __float_as_int(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])))));
+    if (job.top) {
+      // of the finite values: the others come through any scaling, and must not set it
+      float most = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 4; k++) most = fmaxf(most, finite(v[k]) ? fabsf(v[k]) : 0.0f);
+      atomicMax(&tops[i], __float_as_int(most));
+    }
     if (job.pair) {
-      // 22 bits of fp16 (saturating: the first value takes what it can, the second up to as much again), 16 of bf16
+      // 22 bits of fp16 (saturating: the first value takes what it can, the second up to as much again), 16 of bf16; what is
+      // not finite stays so, in the first value
       uint32_t hi[2], lo[2];
 #pragma unroll
       for (int k = 0; k < 2; k++) {
         float a = v[2 * k], b = v[2 * k + 1];
         if (p.dtype == WINDQ_F16) {
-          a = fminf(fmaxf(a, -131008.0f), 131008.0f);
-          b = fminf(fmaxf(b, -131008.0f), 131008.0f);
-          hi[k] = pack2(fminf(fmaxf(a, -65504.0f), 65504.0f), fminf(fmaxf(b, -65504.0f), 65504.0f), p.dtype);
+          a = clamp(a, 131008.0f);
+          b = clamp(b, 131008.0f);
+          hi[k] = pack2(clamp(a, 65504.0f), clamp(b, 65504.0f), p.dtype);
         } else {
           hi[k] = pack2(a, b, p.dtype);
         }
         const float2 back = unpack2(hi[k], p.dtype);
-        lo[k] = pack2(a - back.x, b - back.y, p.dtype);
+        lo[k] = pack2(finite(a) ? a - back.x : 0.0f, finite(b) ? b - back.y : 0.0f, p.dtype);
       }
       uint16_t* out = job.pair + (int64_t)(t0 + i) * 2 * p.rank + j;
       *reinterpret_cast<uint2*>(out) = make_uint2(hi[0], hi[1]);
