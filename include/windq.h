@@ -584,8 +584,9 @@ windq_status windq_fallback(windq_ctx* ctx, const float* err, const float* energ
 typedef enum { WINDQ_F16 = 0, WINDQ_BF16 = 1, WINDQ_F32 = 2 } windq_dtype;
 
 /* Shared projection with one low-rank adapter per token.  With a = adapter_of[t]:
- *   u_t = scaling[a] * A[a] x_t              (rank values, binary32)
+ *   u_t = scaling[a] * A[a] x_t              (rank values, summed in binary32)
  *   Y[t] = W x_t + B[a] u_t                  (binary32 accumulation, one rounding to the type of Y)
+ * The tensor cores cut a sum off, to binary32, where they add to it; Y and dX are one such sum over all of C (or R).
  * A token whose adapter_of is outside [0, n_adapters) has no adapter: Y[t] = W x_t.  Tokens may come in any order;
  * a batch in which neighbouring tokens share an adapter (prompts one after another) runs fastest.
  *   dtype       WINDQ_F16 or WINDQ_BF16, the type of X, W, A, B and Y
@@ -594,8 +595,9 @@ typedef enum { WINDQ_F16 = 0, WINDQ_BF16 = 1, WINDQ_F32 = 2 } windq_dtype;
  *                                            smaller rank are padded with zeros)
  *   scaling     fp32 [n_adapters];  adapter_of  i32 [T]
  * T = 0 is allowed and does nothing.  Y must not overlap an input.  Columns of Y at and beyond R are not written.
- * On WINDQ_F16, u_t is carried as the sum of two fp16 values and therefore saturates at +-131008.  What is not finite shows:
- * a token, or an adapter with its scaling, that is not finite gives rows that are not, where the formula has none.  Rows of
+ * Into Y, u_t goes as the sum of two values of the type of X: 16 bits of bf16; of fp16, scaled by a power of two where a
+ * token's are small or large, 22 bits of the token's largest |u|, or 16 where that is near 2^-9, for |u| below 2^57.  What is
+ * not finite shows: a token, or an adapter with its scaling, that is not finite gives rows that are not, where the formula has none.  Rows of
  * others are not touched, but for one case: a weight of B[a] that is not finite (in windq_lora_backward's dX: of A[a]) may
  * spoil the rows of every token within 256 tokens of one of a's.
  * Scratch: windq_scratch_bytes_lora_forward. */
@@ -609,6 +611,7 @@ windq_status windq_lora_forward(windq_ctx* ctx, int dtype, const void* X, int64_
  *   dX[t] = W^T dY[t] + A[a]^T v_t           type `dtype`, [T][lddx], nullable
  *   dA[a] = sum over the tokens t of a  of  v_t x_t^T      fp32 [n_adapters][rank][C], nullable
  *   dB[a] = sum over the tokens t of a  of  dY[t] u_t^T    fp32 [n_adapters][R][rank], nullable
+ * Into dX, v_t goes as u_t does into Y; dA and dB are sums of binary32 values to 22 bits of the largest (fp16) or 24 (bf16).
  * u_t is computed again from X; nothing has to be kept from the forward call.  The outputs are overwritten (an adapter
  * without tokens gets zeros).  Every sum is taken in an order fixed by the sizes: equal calls give equal bits.
  * Arguments as windq_lora_forward; lddy >= R, lddx >= C, multiples of 8.  With T = 0 dA and dB become zero.

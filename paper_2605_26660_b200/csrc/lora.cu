@@ -49,7 +49,7 @@ extern "C" {
 
 int64_t windq_scratch_bytes_lora_forward(int64_t T, int64_t R, int64_t C, int rank) {
   if (T < 0 || R <= 0 || C <= 0 || rank <= 0) return 0;
-  return windq::round_up(4 * T * rank, 256) + windq::list_bytes(T);
+  return windq::round_up(4 * T * rank, 256) + windq::round_up(T, 256) + windq::list_bytes(T);
 }
 
 windq_status windq_lora_forward(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx, const void* W,
@@ -69,16 +69,19 @@ windq_status windq_lora_forward(windq_ctx* ctx, int dtype, const void* X, int64_
   if (room != WINDQ_OK) return room;
   cudaStream_t st = (cudaStream_t)stream;
   void* U = ctx->scratch;
-  int* lists = (int*)((char*)ctx->scratch + round_up(4 * T * rank, 256));
+  int8_t* shift = (int8_t*)ctx->scratch + round_up(4 * T * rank, 256);
+  int* lists = (int*)(shift + round_up(T, 256));
+  if (dtype == WINDQ_BF16) shift = nullptr;
   const windq_status low = launch_low_rank(
-      ctx, LowRank{dtype, T, n_adapters, rank, scaling, adapter_of, lists, 1, {{false, X, C, ldx, A, nullptr, U, nullptr}}}, st);
+      ctx, LowRank{dtype, T, n_adapters, rank, scaling, adapter_of, lists, 1, {{false, X, C, ldx, A, nullptr, U, shift, nullptr}}}, st);
   if (low != WINDQ_OK) return low;
-  return launch_projection(ctx, Projection{dtype, false, X, T, C, R, ldx, W, ldw, B, n_adapters, rank, adapter_of, U, lists, Y, ldy}, st);
+  return launch_projection(
+      ctx, Projection{dtype, false, X, T, C, R, ldx, W, ldw, B, n_adapters, rank, adapter_of, U, shift, lists, Y, ldy}, st);
 }
 
 int64_t windq_scratch_bytes_lora_backward(int64_t T, int64_t R, int64_t C, int64_t n_adapters, int rank) {
   if (T < 0 || R <= 0 || C <= 0 || rank <= 0 || n_adapters <= 0) return 0;
-  return 3 * windq::round_up(4 * T * rank, 256) + 2 * windq::round_up(4 * T, 256) + windq::list_bytes(T);
+  return 3 * windq::round_up(4 * T * rank, 256) + 2 * windq::round_up(4 * T, 256) + windq::round_up(T, 256) + windq::list_bytes(T);
 }
 
 windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx, const void* W,
@@ -117,10 +120,13 @@ windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64
   void* V_pair = take(4 * T * rank);
   float* top_u = (float*)take(4 * T);
   float* top_v = (float*)take(4 * T);
+  int8_t* shift = (int8_t*)take(T);
   int* lists = (int*)at;
+  if (dtype == WINDQ_BF16) shift = nullptr;
   LowRank low = {dtype, T, n_adapters, rank, scaling, adapter_of, dX ? lists : nullptr, 0, {}};
-  if (dB) low.job[low.jobs++] = LowRankJob{false, X, C, ldx, A, U, nullptr, top_u};
-  if (dX || dA) low.job[low.jobs++] = LowRankJob{true, dY, R, lddy, B, dA ? V : nullptr, dX ? V_pair : nullptr, dA ? top_v : nullptr};
+  if (dB) low.job[low.jobs++] = LowRankJob{false, X, C, ldx, A, U, nullptr, nullptr, top_u};
+  if (dX || dA)
+    low.job[low.jobs++] = LowRankJob{true, dY, R, lddy, B, dA ? V : nullptr, dX ? V_pair : nullptr, dX ? shift : nullptr, dA ? top_v : nullptr};
   windq_status done = launch_low_rank(ctx, low, st);
   // the gradients before dX: the projection's first tiles then start while the last of them finish
   if (done == WINDQ_OK && (dA || dB)) {
@@ -129,7 +135,7 @@ windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64
   }
   if (done == WINDQ_OK && dX)
     done = launch_projection(
-        ctx, Projection{dtype, true, dY, T, R, C, lddy, W, ldw, A, n_adapters, rank, adapter_of, V_pair, lists, dX, lddx}, st);
+        ctx, Projection{dtype, true, dY, T, R, C, lddy, W, ldw, A, n_adapters, rank, adapter_of, V_pair, shift, lists, dX, lddx}, st);
   return done;
 }
 

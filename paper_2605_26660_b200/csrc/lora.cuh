@@ -20,6 +20,7 @@ struct Projection {
   int rank;
   const int32_t* adapter_of;
   const void* pair;  // S as launch_low_rank leaves it
+  const int8_t* shift;
   const int* lists;  // see token_tile
   void* O;
   int64_t ldo;
@@ -42,6 +43,8 @@ struct LowRankJob {
   const void* P;
   float* S;    // nullable
   void* pair;  // 16-bit [T][2][rank]: first and second term of S, for the projection; nullable
+  // With pair, fp16: [T rounded up to 256], S of a token is kept as S * 2^shift (see shift_of).  bf16: NULL.
+  int8_t* shift;
   float* top;  // fp32 [T], the largest |S[t][j]| of every token; nullable
 };
 struct LowRank {

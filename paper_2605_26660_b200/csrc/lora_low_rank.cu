@@ -24,6 +24,7 @@ struct LowJob {
   const uint16_t* P;  // [a][j][k], or transposed [a][k][j]
   float* S;        // binary32, or NULL
   uint16_t* pair;  // [t][2][j]: the two 16-bit values whose sum stands for S, or NULL
+  int8_t* shift;   // fp16 pairs: the power of two by which the token's are scaled
   float* top;      // largest |S[t][j]| of a token, or NULL
   int K, transposed;
 };
@@ -78,6 +79,39 @@ __device__ __forceinline__ bool finite(float x) { return fabsf(x) < __int_as_flo
 // x in [-most, most]; infinities and NaN as they are (fminf and fmaxf would make a number of NaN).
 __device__ __forceinline__ float clamp(float x, float most) { return finite(x) ? fminf(fmaxf(x, -most), most) : x; }
 
+// The power of two by which the fp16 pairs of a token are scaled, from its largest |S|.  Two fp16 values lie on the grid
+// 2^-24 of their type's smallest step, which leaves 22 bits of the largest |S| where that is 2^-3 or more and 16, as bf16
+// pairs have, at 2^-9; they hold up to 2 * 65504.  Within [2^-9, 2^16) nothing is scaled: the projection has less to do then (us
+// without and with scaled tokens: 48 single tokens with 32 adapters x 11008 x 4096 29.7 and 32.6, 203 with 48 x 8192 x 8192 67.6
+// and 74.3, the backward pass of 8192 x 4096 x 4096 303 and 310).  Outside, the largest goes to [2^12, 2^13), as far as 2^40
+// reaches: what lies below after that is less than any result of 16 bits, 128 products with values up to 65504 included, and
+// what lies above is more.
+__device__ __forceinline__ int shift_of(float top) {
+  const int e = (int)(__float_as_uint(top) >> 23) - 127;  // 2^e <= top < 2^(e + 1)
+  return top == 0.0f || (e >= -9 && e <= 15) ? 0 : max(-40, min(40, 12 - e));
+}
+
+// The two 16-bit values of four values of S: 22 bits of fp16, 16 of bf16.  What is not finite stays so, in the first.
+__device__ __forceinline__ void write_pair(const LowRankArgs& p, const LowJob& job, int t, int j, const float (&v)[4]) {
+  uint32_t hi[2], lo[2];
+#pragma unroll
+  for (int k = 0; k < 2; k++) {
+    float a = v[2 * k], b = v[2 * k + 1];
+    if (p.dtype == WINDQ_F16) {
+      a = clamp(a, 131008.0f);
+      b = clamp(b, 131008.0f);
+      hi[k] = pack2(clamp(a, 65504.0f), clamp(b, 65504.0f), p.dtype);
+    } else {
+      hi[k] = pack2(a, b, p.dtype);
+    }
+    const float2 back = unpack2(hi[k], p.dtype);
+    lo[k] = pack2(finite(a) ? a - back.x : 0.0f, finite(b) ? b - back.y : 0.0f, p.dtype);
+  }
+  uint16_t* out = job.pair + (int64_t)t * 2 * p.rank + j;
+  *reinterpret_cast<uint2*>(out) = make_uint2(hi[0], hi[1]);
+  *reinterpret_cast<uint2*>(out + p.rank) = make_uint2(lo[0], lo[1]);
+}
+
 // S of the tokens of this block from the sums of the cluster's blocks, [token][pitch] at `sums`: four values a thread.
 // kept(i) tells whether token t0 + i is to be written; tops: one word a token, zero.
 template <class Kept>
@@ -92,43 +126,40 @@ __device__ __forceinline__ void finish_tokens(const LowRankArgs& p, const LowJob
     if (p.splits > 1) cluster_sum<1>(sums, offset, p.splits, 0, 1, y);
     else asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y[0].x), "=f"(y[0].y), "=f"(y[0].z), "=f"(y[0].w) : "r"(sums + offset[0]) : "memory");
     const float scale = p.scaling[ids[i]];
-    float v[4] = {y[0].x * scale, y[0].y * scale, y[0].z * scale, y[0].w * scale};
-    const int64_t at = (int64_t)(t0 + i) * p.rank + j;
-    if (job.S) *reinterpret_cast<float4*>(job.S + at) = make_float4(v[0], v[1], v[2], v[3]);
-    if (job.top) {
+    const float v[4] = {y[0].x * scale, y[0].y * scale, y[0].z * scale, y[0].w * scale};
+    if (job.S) *reinterpret_cast<float4*>(job.S + (int64_t)(t0 + i) * p.rank + j) = make_float4(v[0], v[1], v[2], v[3]);
+    if (job.top || job.shift) {
       // of the finite values: the others come through any scaling, and must not set it
       float most = 0.0f;
 #pragma unroll
       for (int k = 0; k < 4; k++) most = fmaxf(most, finite(v[k]) ? fabsf(v[k]) : 0.0f);
       atomicMax(&tops[i], __float_as_int(most));
     }
-    if (job.pair) {
-      // 22 bits of fp16 (saturating: the first value takes what it can, the second up to as much again), 16 of bf16; what is
-      // not finite stays so, in the first value
-      uint32_t hi[2], lo[2];
-#pragma unroll
-      for (int k = 0; k < 2; k++) {
-        float a = v[2 * k], b = v[2 * k + 1];
-        if (p.dtype == WINDQ_F16) {
-          a = clamp(a, 131008.0f);
-          b = clamp(b, 131008.0f);
-          hi[k] = pack2(clamp(a, 65504.0f), clamp(b, 65504.0f), p.dtype);
-        } else {
-          hi[k] = pack2(a, b, p.dtype);
-        }
-        const float2 back = unpack2(hi[k], p.dtype);
-        lo[k] = pack2(finite(a) ? a - back.x : 0.0f, finite(b) ? b - back.y : 0.0f, p.dtype);
-      }
-      uint16_t* out = job.pair + (int64_t)(t0 + i) * 2 * p.rank + j;
-      *reinterpret_cast<uint2*>(out) = make_uint2(hi[0], hi[1]);
-      *reinterpret_cast<uint2*>(out + p.rank) = make_uint2(lo[0], lo[1]);
-    }
+    if (job.shift)  // in the place of the sums, which no other block reads in this one's rows
+      asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(sums + offset[0]), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
+    else if (job.pair)
+      write_pair(p, job, t0 + i, j, v);
   }
+  if (!job.top && !job.shift) return;
+  __syncthreads();
   if (job.top) {
-    __syncthreads();
     for (int x = threadIdx.x; x < share; x += kLowThreads) {
       const int i = split + x * p.splits;
       if (kept(i)) job.top[t0 + i] = __int_as_float(tops[i]);
+    }
+  }
+  if (job.shift) {
+    for (int x = threadIdx.x; x < share * quads; x += kLowThreads) {
+      const int i = split + x / quads * p.splits, j = x % quads * 4;
+      if (!kept(i)) continue;
+      float v[4];
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(sums + (uint32_t)(i * pitch + j) * 4) : "memory");
+      const int e = shift_of(__int_as_float(tops[i]));
+      const float up = __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+      for (int k = 0; k < 4; k++) v[k] *= up;
+      write_pair(p, job, t0 + i, j, v);
+      if (j == 0) job.shift[t0 + i] = (int8_t)e;
     }
   }
 }
@@ -206,6 +237,7 @@ __global__ void __launch_bounds__(kLowThreads)
   int n_used;
   const int id = tid < p.rows ? valid_id(p, t0 + tid) : -1, place = first_place(id, p.rows, ids, taken, &n_used);
   if (place >= 0) used[place] = id;
+  if (job.shift && slot == 0 && split == 0 && tid < p.rows && id < 0) job.shift[t0 + tid] = 0;  // nobody else's tokens
   if (tid < kRows) tops[tid] = 0, mine[tid] = false;
   tc_fence_before();
   __syncthreads();
@@ -408,7 +440,7 @@ windq_status launch_low_rank(windq_ctx* ctx, const LowRank& q, cudaStream_t st) 
   LowRankArgs p = {};
   for (int k = 0; k < q.jobs; k++) {
     const LowRankJob& j = q.job[k];
-    p.job[k] = LowJob{(const uint16_t*)j.Z, j.ldz, (const uint16_t*)j.P, j.S, (uint16_t*)j.pair, j.top, (int)j.K, j.transposed};
+    p.job[k] = LowJob{(const uint16_t*)j.Z, j.ldz, (const uint16_t*)j.P, j.S, (uint16_t*)j.pair, j.shift, j.top, (int)j.K, j.transposed};
   }
   p.jobs = q.jobs;
   p.T = (int)q.T;

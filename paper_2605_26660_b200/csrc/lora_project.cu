@@ -7,6 +7,10 @@
 // over the output.  S enters as the sum of two 16-bit values (22 bits for fp16, 16 for bf16; written by the low-rank
 // kernel), which keeps the rounding of the low-rank term below that of the result.
 //
+// fp16 pairs of tokens whose S is very small or large are scaled by a power of two (shift_of in the low-rank kernel).  In a
+// tile that has such tokens the adapters come after all of K, and between the two the accumulators are multiplied by the same
+// powers, token by token (exact, in tensor memory, by the warps that store); storing takes them off again.
+//
 // The low-rank stages come in the second half of a tile's reduction, one adapter after each chunk of K: their handshakes and
 // loads then hide behind the chunks' (at the end of 203 tokens with 48 adapters they took 14 us of 75), and the low-rank
 // kernel, which this one overlaps at its start, has long ended.
@@ -39,6 +43,7 @@ struct ProjectArgs {
   int T, N, chunks, rank, n_adapters, dtype;
   const int32_t* adapter_of;
   const uint16_t* pair;
+  const int8_t* shift;
   const int* lists;
   void* O;
   int64_t ldo;
@@ -48,7 +53,7 @@ struct ProjectArgs {
 };
 
 struct Barriers {
-  uint64_t full[kMaxStages], empty[kMaxStages], granted[kMaxStages], written[kMaxStages], done[2], free[2];
+  uint64_t full[kMaxStages], empty[kMaxStages], granted[kMaxStages], written[kMaxStages], done[2], free[2], whole, shifted;
 };
 
 // A place in the ring of stages.  The roles step through it thousands of times in one thread each, where a division by the
@@ -75,11 +80,27 @@ struct Ring {
 struct Adapters {
   const int* list;
   int first, step, lane, count = 0, held = 0;
+  bool late = false;  // some of the tile's tokens are scaled: the adapters come after all of K
+  unsigned shifts[2] = {};  // of four tokens each: 4 lane and 128 + 4 lane of the tile
   __device__ Adapters(const int* list, int first, int step, int lane) : list(list + 1), first(first), step(step), lane(lane) {}
-  __device__ __forceinline__ void open() {
+  __device__ __forceinline__ void open(const ProjectArgs& p, int t0, int rows) {  // the tile's tokens
+    if (p.shift) {
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        const int i = (h * 32 + lane) * 4;  // (the low-rank kernel fills the last four up with zeros)
+        shifts[h] = i < rows && t0 + i < p.T ? __ldcg(reinterpret_cast<const unsigned*>(p.shift + t0 + i)) : 0;
+      }
+    }
     const int n = uniform(__ldcg(list - 1));
     count = n > first ? (n - first + step - 1) / step : 0;
     fetch(0);
+    late = count > 0 && __any_sync(0xffffffffu, (shifts[0] | shifts[1]) != 0);
+  }
+  // 2^shift (or, with sign = -1, its inverse) of token `i` of the tile: of one that all lanes agree on, or of each lane's own.
+  __device__ __forceinline__ float power(int i, int sign) {
+    const int a = __shfl_sync(0xffffffffu, (int)shifts[0], (i >> 2) & 31), b = __shfl_sync(0xffffffffu, (int)shifts[1], (i >> 2) & 31);
+    const int shift = (int)(int8_t)((i < 128 ? a : b) >> (8 * (i & 3)));
+    return __uint_as_float((uint32_t)(127 + sign * shift) << 23);
   }
   __device__ __forceinline__ void fetch(int k) { held = k + lane < count ? __ldcg(list + first + (k + lane) * step) : 0; }
   __device__ __forceinline__ int at(int k) {
@@ -87,6 +108,24 @@ struct Adapters {
     return __shfl_sync(0xffffffffu, held, k & 31);
   }
 };
+
+// A warp's quarter of the accumulators times the powers of their tokens (sign = 1) or divided by them (-1).  The tokens are the
+// columns of a tall tile; of a wide one they are the rows, `token` this thread's.  Out of line, away from what tiles without
+// scaled tokens run (in line it cost 48 single tokens with 32 adapters 0.9 us of 29).
+template <bool TALL>
+__device__ __noinline__ void rescale(Adapters adapters, uint32_t d, int columns, int token, int sign) {
+  const float row = adapters.power(token, sign);
+#pragma unroll 1
+  for (int c = 0; c < columns; c += 16) {
+    uint32_t r[16];
+    tmem_load16(d + c, r);
+    tmem_load_wait();
+#pragma unroll
+    for (int k = 0; k < 16; k++) r[k] = __float_as_uint(__uint_as_float(r[k]) * (TALL ? adapters.power(c + k, sign) : row));
+    tmem_store16(d + c, r);
+  }
+  tmem_store_wait();
+}
 
 // Tiles in an order that keeps a group of token tiles in L2 while the weight streams by.
 __device__ __forceinline__ void tile_at(const ProjectArgs& p, int tile, int& tt, int& wt) {
@@ -120,6 +159,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
   auto written = [&](int s) { return smem_addr(&bars.written[s]); };
   auto done = [&](int b) { return smem_addr(&bars.done[b]); };
   auto free_ = [&](int b) { return smem_addr(&bars.free[b]); };
+  const uint32_t whole = smem_addr(&bars.whole), shifted = smem_addr(&bars.shifted);
 
   if (threadIdx.x == 0) {
     prefetch_map(&zmap);
@@ -135,6 +175,8 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
       mbar_init(done(b), 1);
       mbar_init(free_(b), 4 * kBlocks);
     }
+    mbar_init(whole, 1);
+    mbar_init(shifted, 4 * kBlocks);
     dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
@@ -199,8 +241,12 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
       };
       for (int c = c0; c <= middle; c++) load_chunk(c);
       wait_for_predecessor();
-      adapters.open();
+      adapters.open(p, tt * kBlocks * p.token_rows, kBlocks * p.token_rows);
       int c = middle + 1;
+      if (adapters.late) {
+#pragma unroll 1
+        for (; c < c1; c++) load_chunk(c);
+      }
       for (int k = 0; k < adapters.count; k++) {
         if (k && c < c1) load_chunk(c++);
         load_adapter(k);
@@ -217,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
       const uint64_t z_desc = smem_desc(base, 16), w_desc = smem_desc(base + token_bytes, TRANS ? 8192 : 16);
       Ring at(p.stages);
       int turn = 0;
-      uint32_t written_phase = 0;
+      uint32_t written_phase = 0, shifted_phase = 0;
       for (int tile = blockIdx.x / team; tile < tiles; tile += step, turn++) {
         int tt, wt;
         tile_at(p, tile, tt, wt);
@@ -259,8 +305,17 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
         for (int c = c0; c <= middle; c++) multiply_chunk(c > c0);
         wait_for_predecessor();
         Adapters adapters(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1), split, p.splits, lane);
-        adapters.open();
+        adapters.open(p, tt * kBlocks * p.token_rows, kBlocks * p.token_rows);
         int c = middle + 1;
+        if (adapters.late) {
+#pragma unroll 1
+          for (; c < c1; c++) multiply_chunk(true);
+          if (elect_one()) mma_commit<PAIR>(whole, mask);
+          __syncwarp();
+          mbar_wait(shifted, shifted_phase, dead_);
+          shifted_phase ^= 1;
+          tc_fence_after();
+        }
         for (int k = 0; k < adapters.count; k++) {
           if (k && c < c1) multiply_chunk(true), c++;
           multiply_adapter();
@@ -276,7 +331,7 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
     // warp, which follows every round, grants them the stage.
     Ring ring(p.stages);
     int turn = 0;
-    uint32_t granted_phase = 0, buffer = 0;
+    uint32_t granted_phase = 0, whole_phase = 0, buffer = 0;
     const uint32_t staging = base + p.stages * stage_bytes;
     auto tell = [&](uint32_t bar) {  // the block that issues the products
       if (PAIR) cluster_arrive(cluster_addr(bar, leader));
@@ -313,8 +368,22 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
           }
       };
       Adapters adapters(p.lists + (int64_t)tt * (kBlocks * p.token_rows + 1), split, p.splits, lane);
-      adapters.open();
+      adapters.open(p, tt * kBlocks * p.token_rows, kBlocks * p.token_rows);
       if (adapters.count && paired) load(0, 0);
+      const int b = p.accumulators == 2 ? turn & 1 : 0, use = p.accumulators == 2 ? turn >> 1 : turn;
+      const uint32_t d = tmem + b * 256 + ((uint32_t)(quarter * 32) << 16);
+      const int columns = TALL ? p.token_rows : 2 * p.weight_rows, at = quarter * 32 + lane;
+      if (adapters.late) {
+        ring.skip(c1 - c0 - passed);
+        passed = c1 - c0;
+        mbar_wait(whole, whole_phase, dead_);
+        whole_phase ^= 1;
+        tc_fence_after();
+        rescale<TALL>(adapters, d, columns, me * 128 + at, 1);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tell(shifted);
+      }
       for (int k = 0; k < adapters.count; k++) {
         const int a = adapters.at(k);
         if (k && passed < c1 - c0) {
@@ -348,11 +417,9 @@ __global__ void __launch_bounds__(kThreads, TALL ? 2 : 1)
       }
       ring.skip(c1 - c0 - passed);
       // the accumulators of the tile
-      const int b = p.accumulators == 2 ? turn & 1 : 0, use = p.accumulators == 2 ? turn >> 1 : turn;
       mbar_wait(done(b), use & 1, dead_);
       tc_fence_after();
-      const uint32_t d = tmem + b * 256 + ((uint32_t)(quarter * 32) << 16);
-      const int columns = TALL ? p.token_rows : 2 * p.weight_rows, at = quarter * 32 + lane;
+      if (adapters.late) rescale<TALL>(adapters, d, columns, me * 128 + at, -1);
       if (!TALL && p.splits == 1) {
         // 32 rows x 64 columns at a time through shared memory (128-byte swizzle, two buffers a warp) and out by TMA: rows
         // are far apart, and 16-byte stores straight from the registers took as long as a third of the tile's products
@@ -542,6 +609,7 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   p.dtype = q.dtype;
   p.adapter_of = q.adapter_of;
   p.pair = (const uint16_t*)q.pair;
+  p.shift = q.shift;
   p.lists = q.lists;
   p.O = q.O;
   p.ldo = q.ldo;
