@@ -89,7 +89,7 @@ windq_status windq_selfcheck(windq_ctx* ctx, int64_t* n_failures_out, void* stre
  * data.  Every fit kernel of the context adds to two counters: the clip candidates of its searches, counted once
  * per warp pass (a pass covers the 1024 weights a warp holds), and those of them it evaluated in full.
  *   evaluated_out, searched_out: HOST pointers to one int64 each; reset != 0 puts both counters back to zero.
- * Synchronises the device (a blocking copy). */
+ * Synchronises the device first: every call issued before it, on whatever stream, is counted. */
 windq_status windq_fit_work(windq_ctx* ctx, int64_t* evaluated_out, int64_t* searched_out, int reset);
 
 /* Thread blocks of windq_lora_forward / windq_lora_backward in which a wait on a copy or a matrix product gave up after
@@ -97,7 +97,8 @@ windq_status windq_fit_work(windq_ctx* ctx, int64_t* evaluated_out, int64_t* sea
  * wait on a barrier of shared memory is bounded, so that such a fault ends the kernel instead of hanging the GPU.  What
  * waits without a limit -- for tensor memory, for the other blocks of a cluster, for the kernel before -- waits for blocks
  * that run to that point by themselves.)
- *   n_out: HOST pointer to one int64; reset != 0 puts the counter back to zero.  Synchronises the device. */
+ *   n_out: HOST pointer to one int64; reset != 0 puts the counter back to zero.  Synchronises the device first: every
+ *   call issued before it, on whatever stream, is counted. */
 windq_status windq_stalls(windq_ctx* ctx, int64_t* n_out, int reset);
 
 /* Grows the context's scratch buffer to at least `bytes` now (may synchronise the device), so that

@@ -142,6 +142,7 @@ windq_status windq_fit_work(windq_ctx* ctx, int64_t* evaluated_out, int64_t* sea
   WINDQ_REQUIRE(ctx, evaluated_out && searched_out, WINDQ_ERR_NULL, "windq_fit_work: evaluated_out or searched_out is NULL");
   DeviceGuard guard(ctx->device);
   unsigned long long host[2] = {0, 0};
+  WINDQ_CUDA(ctx, cudaDeviceSynchronize());  // the copy below waits for blocking streams only
   WINDQ_CUDA(ctx, cudaMemcpy(host, fit_work_counters(ctx), sizeof(host), cudaMemcpyDeviceToHost));
   if (reset) WINDQ_CUDA(ctx, cudaMemset(fit_work_counters(ctx), 0, sizeof(host)));
   *evaluated_out = (int64_t)host[0];
@@ -155,6 +156,7 @@ windq_status windq_stalls(windq_ctx* ctx, int64_t* n_out, int reset) {
   WINDQ_REQUIRE(ctx, n_out, WINDQ_ERR_NULL, "windq_stalls: n_out is NULL");
   DeviceGuard guard(ctx->device);
   unsigned long long host = 0;
+  WINDQ_CUDA(ctx, cudaDeviceSynchronize());  // the copy below waits for blocking streams only
   WINDQ_CUDA(ctx, cudaMemcpy(&host, stall_counter(ctx), sizeof(host), cudaMemcpyDeviceToHost));
   if (reset) WINDQ_CUDA(ctx, cudaMemset(stall_counter(ctx), 0, sizeof(host)));
   *n_out = (int64_t)host;
