@@ -21,32 +21,40 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 }
 // Every wait on a barrier ends: after about two seconds, or as soon as another wait of its thread block has given up, it
 // raises *dead (a word of shared memory) and falls through.  The roles then run to their ends without issuing copies.
+// Between two looks at most kLookCycles count: a context that is switched out, for however long, comes back with the time
+// that it had left, and looks again first.
 //
 // The loop stays inside the asm block on purpose: a branch the compiler saw would make the control flow of the issuing
 // warps look divergent, and with it every operand of the tcgen05 and TMA instructions, which want uniform registers; a
-// product then took 70 cycles to issue, more than most of them run.
-constexpr long long kWaitCycles = 4000000000ll;
+// product then took 70 cycles to issue, more than most of them run.  It is in line a dozen times, so it is kept short: six
+// instructions more cost 48 single tokens with 32 adapters 0.9 us of 29.
+constexpr unsigned kWaitCycles = 4000000000u, kLookCycles = 1u << 26;
 __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, uint32_t dead) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .u64 begin, now;\n\t.reg .u32 d;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .u32 spent, last, now, d;\n\t"
       "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t"
       "@p bra DONE;\n\t"
-      "mov.u64 begin, %%clock64;\n\t"
+      "mov.u32 spent, 0;\n\t"
+      "mov.u32 last, %%clock;\n\t"
       "AGAIN:\n\t"
       "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t"
       "@p bra DONE;\n\t"
       "ld.volatile.shared.u32 d, [%2];\n\t"
       "setp.ne.u32 p, d, 0;\n\t"
       "@p bra DONE;\n\t"
-      "mov.u64 now, %%clock64;\n\t"
-      "sub.u64 now, now, begin;\n\t"
-      "setp.lt.u64 p, now, %3;\n\t"
+      "mov.u32 now, %%clock;\n\t"
+      "sub.u32 d, now, last;\n\t"
+      "mov.u32 last, now;\n\t"
+      "min.u32 d, d, %4;\n\t"
+      "add.u32 spent, spent, d;\n\t"
+      "setp.lt.u32 p, spent, %3;\n\t"
       "@p bra AGAIN;\n\t"
       "st.volatile.shared.u32 [%2], 1;\n\t"
       "DONE:\n\t}" ::"r"(bar),
-      "r"(parity), "r"(dead), "n"(kWaitCycles)
+      "r"(parity), "r"(dead), "n"(kWaitCycles), "n"(kLookCycles)
       : "memory");
 }
+static_assert(kWaitCycles + (uint64_t)kLookCycles < 1ull << 32, "32-bit sums");
 // After a wait has given up, by all threads of the block: lets copies and products that were issued come to their ends
 // before the memory they use is given back, and counts the block.
 __device__ __forceinline__ void settle(unsigned long long* stalls) {
