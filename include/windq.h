@@ -93,10 +93,11 @@ windq_status windq_selfcheck(windq_ctx* ctx, int64_t* n_failures_out, void* stre
 windq_status windq_fit_work(windq_ctx* ctx, int64_t* evaluated_out, int64_t* searched_out, int reset);
 
 /* Thread blocks of windq_lora_forward / windq_lora_backward in which a wait on a copy or a matrix product gave up after
- * about two seconds: 0 unless the GPU or the library is broken; the results of a call that adds to it are invalid.  (Every
- * wait on a barrier of shared memory is bounded, so that such a fault ends the kernel instead of hanging the GPU.  What
- * waits without a limit -- for tensor memory, for the other blocks of a cluster, for the kernel before -- waits for blocks
- * that run to that point by themselves.)
+ * about two seconds: 0 unless the GPU or the library is broken; the results of a call that adds to it are invalid.  Once
+ * one did, the two calls refuse to run (WINDQ_ERR_CUDA) until the counter is put back; the replay of a captured call does
+ * not look.  (Every wait on a barrier of shared memory is bounded, so that such a fault ends the kernel instead of hanging
+ * the GPU.  What waits without a limit -- for tensor memory, for the other blocks of a cluster, for the kernel before --
+ * waits for blocks that run to that point by themselves.)
  *   n_out: HOST pointer to one int64; reset != 0 puts the counter back to zero.  Synchronises the device first: every
  *   call issued before it, on whatever stream, is counted. */
 windq_status windq_stalls(windq_ctx* ctx, int64_t* n_out, int reset);

@@ -86,10 +86,11 @@ windq_status windq_create(windq_ctx** out, int device) {
   if (prop.major != 10)
     return windq::fail(nullptr, WINDQ_ERR_UNSUPPORTED, "windq_create: device %d is sm_%d%d, this library is built for sm_100a",
                        device, prop.major, prop.minor);
-  unsigned int* sync = nullptr;
+  unsigned int *sync = nullptr, *gave_up = nullptr;
   {
     windq::DeviceGuard guard(device);
-    if (cudaMalloc(&sync, windq::kSyncBytes) != cudaSuccess || cudaMemset(sync, 0, windq::kSyncBytes) != cudaSuccess) {
+    if (cudaMalloc(&sync, windq::kSyncBytes) != cudaSuccess || cudaMemset(sync, 0, windq::kSyncBytes) != cudaSuccess ||
+        cudaHostAlloc(&gave_up, sizeof(*gave_up), cudaHostAllocPortable | cudaHostAllocMapped) != cudaSuccess) {
       cudaGetLastError();
       if (sync) cudaFree(sync);
       return windq::fail(nullptr, WINDQ_ERR_CUDA, "windq_create: cannot allocate the arrival counters on device %d", device);
@@ -98,6 +99,8 @@ windq_status windq_create(windq_ctx** out, int device) {
   windq_ctx* ctx = new windq_ctx;
   ctx->device = device;
   ctx->sync = sync;
+  *gave_up = 0;
+  ctx->gave_up = gave_up;
   ctx->sm_count = prop.multiProcessorCount;
   ctx->scratch = nullptr;
   ctx->scratch_bytes = 0;
@@ -117,6 +120,7 @@ void windq_destroy(windq_ctx* ctx) {
     if (ctx->scratch) cudaFree(ctx->scratch);
     for (int k = 0; k < ctx->n_outgrown; k++) cudaFree(ctx->outgrown[k]);
     cudaFree(ctx->sync);
+    cudaFreeHost((void*)ctx->gave_up);
   }
   delete ctx;
 }
@@ -157,8 +161,12 @@ windq_status windq_stalls(windq_ctx* ctx, int64_t* n_out, int reset) {
   DeviceGuard guard(ctx->device);
   unsigned long long host = 0;
   WINDQ_CUDA(ctx, cudaDeviceSynchronize());  // the copy below waits for blocking streams only
-  WINDQ_CUDA(ctx, cudaMemcpy(&host, stall_counter(ctx), sizeof(host), cudaMemcpyDeviceToHost));
-  if (reset) WINDQ_CUDA(ctx, cudaMemset(stall_counter(ctx), 0, sizeof(host)));
+  const Stalls stalls = stalls_of(ctx);
+  WINDQ_CUDA(ctx, cudaMemcpy(&host, stalls.blocks, sizeof(host), cudaMemcpyDeviceToHost));
+  if (reset) {
+    WINDQ_CUDA(ctx, cudaMemset(stalls.blocks, 0, sizeof(host)));
+    *stalls.gave_up = 0;
+  }
   *n_out = (int64_t)host;
   return WINDQ_OK;
 }

@@ -20,6 +20,7 @@ struct LoraArgs {
 
 windq_status check_lora(windq_ctx* ctx, const LoraArgs& q) {
   const char* who = q.who;
+  WINDQ_REQUIRE(ctx, !*ctx->gave_up, WINDQ_ERR_CUDA, "%s: a wait of an earlier call gave up, its results are invalid (windq_stalls)", who);
   WINDQ_REQUIRE(ctx, q.dtype == WINDQ_F16 || q.dtype == WINDQ_BF16, WINDQ_ERR_ARG, "%s: dtype = %d is neither fp16 nor bf16", who,
                 q.dtype);
   WINDQ_REQUIRE(ctx, q.W && q.A && q.B && q.scaling, WINDQ_ERR_NULL, "%s: W, A, B or scaling is NULL", who);

@@ -36,7 +36,7 @@ struct LowRankArgs {
   const int32_t* adapter_of;
   int* lists;  // adapters of the projection's token tiles, or NULL
   int list_rows, list_tiles;
-  unsigned long long* stalls;
+  Stalls stalls;
 };
 
 // Thread i's id of `count` (at most 256, one a thread): its place among the different ids in the order of their first
@@ -452,7 +452,7 @@ windq_status launch_low_rank(windq_ctx* ctx, const LowRank& q, cudaStream_t st) 
   p.lists = q.lists;
   p.list_rows = token_tile(q.T);
   p.list_tiles = (int)((q.T + p.list_rows - 1) / p.list_rows);
-  p.stalls = stall_counter(ctx);
+  p.stalls = stalls_of(ctx);
   return launch(ctx, p, st);
 }
 

@@ -49,7 +49,7 @@ struct ProjectArgs {
   int64_t ldo;
   int token_rows, weight_rows, token_tiles, weight_tiles, group;
   int splits, stages, accumulators, columns;  // columns: of tensor memory
-  unsigned long long* stalls;
+  Stalls stalls;
 };
 
 struct Barriers {
@@ -613,7 +613,7 @@ windq_status launch_projection(windq_ctx* ctx, const Projection& q, cudaStream_t
   p.lists = q.lists;
   p.O = q.O;
   p.ldo = q.ldo;
-  p.stalls = stall_counter(ctx);
+  p.stalls = stalls_of(ctx);
   const int blocks_of_tile = tall ? 1 : 2;
   p.token_rows = tall ? token_tile(q.T) : 128;
   p.weight_rows = 128;

@@ -56,12 +56,16 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, uint32_
 }
 static_assert(kWaitCycles + (uint64_t)kLookCycles < 1ull << 32, "32-bit sums");
 // After a wait has given up, by all threads of the block: lets copies and products that were issued come to their ends
-// before the memory they use is given back, and counts the block.
-__device__ __forceinline__ void settle(unsigned long long* stalls) {
+// before the memory they use is given back, counts the block and tells the host.
+__device__ __forceinline__ void settle(const Stalls& stalls) {
   const long long begin = clock64();
   while (clock64() - begin < 4000000) {
   }
-  if (threadIdx.x == 0) atomicAdd(stalls, 1ull);
+  if (threadIdx.x == 0) {
+    atomicAdd(stalls.blocks, 1ull);
+    *stalls.gave_up = 1;
+    __threadfence_system();
+  }
 }
 // One lane of a converged warp, the same every time.
 __device__ __forceinline__ bool elect_one() {

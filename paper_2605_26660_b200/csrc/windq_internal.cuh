@@ -12,6 +12,7 @@
 struct windq_ctx {
   int device;
   int sm_count;
+  volatile unsigned int* gave_up;  // page-locked host memory the GPU can write: not zero once a bounded wait gave up
   void* scratch;
   int64_t scratch_bytes;
   void* outgrown[32];  // earlier scratch buffers, kept for what still uses them; each at least twice the one before (see ensure_scratch)
@@ -32,8 +33,12 @@ windq_status fail(windq_ctx* ctx, windq_status st, const char* fmt, ...);
 inline unsigned long long* fit_work_counters(windq_ctx* ctx) {
   return reinterpret_cast<unsigned long long*>(ctx->sync + kSyncCounters);
 }
-// Thread blocks whose bounded waits gave up (see windq_stalls).
-inline unsigned long long* stall_counter(windq_ctx* ctx) { return fit_work_counters(ctx) + 2; }
+// Where a kernel tells that a bounded wait of one of its thread blocks gave up (see windq_stalls).
+struct Stalls {
+  unsigned long long* blocks;
+  volatile unsigned int* gave_up;
+};
+inline Stalls stalls_of(windq_ctx* ctx) { return Stalls{fit_work_counters(ctx) + 2, ctx->gave_up}; }
 // Makes the context's scratch at least `bytes` large (may cudaMalloc).
 windq_status ensure_scratch(windq_ctx* ctx, int64_t bytes);
 
