@@ -595,7 +595,7 @@ typedef enum { WINDQ_F16 = 0, WINDQ_BF16 = 1, WINDQ_F32 = 2 } windq_dtype;
  *   X [T][ldx], W [R][ldw], Y [T][ldy]       row-major; ldx, ldw >= C, ldy >= R, all multiples of 8; C % 8 == 0
  *   A [n_adapters][rank][C], B [n_adapters][R][rank]   contiguous; rank a multiple of 8 in [8, 128] (adapters of
  *                                            smaller rank are padded with zeros)
- *   scaling     fp32 [n_adapters];  adapter_of  i32 [T]
+ *   scaling     fp32 [n_adapters];  adapter_of  i32 [T]; of any 4-byte alignment (a part of a longer batch, say)
  * T = 0 is allowed and does nothing.  Y must not overlap an input.  Columns of Y at and beyond R are not written.
  * Into Y, u_t goes as the sum of two values of the type of X: 16 bits of bf16; of fp16, scaled by a power of two where a
  * token's are small or large, 22 bits of the token's largest |u|, or 16 where that is near 2^-9, for |u| below 2^57.  What is

@@ -37,9 +37,10 @@ windq_status check_lora(windq_ctx* ctx, const LoraArgs& q) {
                 (long long)q.ldx, (long long)q.ldw, (long long)q.C);
   WINDQ_REQUIRE(ctx, q.ldx % 8 == 0 && q.ldw % 8 == 0, WINDQ_ERR_ALIGN, "%s: ldx = %lld or ldw = %lld is not a multiple of 8", who,
                 (long long)q.ldx, (long long)q.ldw);
-  WINDQ_REQUIRE(ctx, aligned16(q.X) && aligned16(q.W) && aligned16(q.A) && aligned16(q.B) && aligned16(q.scaling) &&
-                         aligned16(q.adapter_of),
-                WINDQ_ERR_ALIGN, "%s: X, W, A, B, scaling or adapter_of is not 16-byte aligned", who);
+  WINDQ_REQUIRE(ctx, aligned16(q.X) && aligned16(q.W) && aligned16(q.A) && aligned16(q.B), WINDQ_ERR_ALIGN,
+                "%s: X, W, A or B is not 16-byte aligned", who);
+  WINDQ_REQUIRE(ctx, (((uintptr_t)q.scaling | (uintptr_t)q.adapter_of) & 3) == 0, WINDQ_ERR_ALIGN,
+                "%s: scaling or adapter_of is misaligned", who);
   return WINDQ_OK;
 }
 
