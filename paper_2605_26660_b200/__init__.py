@@ -973,7 +973,13 @@ def _raw_stream(ctx: Context, stream) -> int:
     return torch._C._cuda_getCurrentRawStream(ctx.device) if stream is None else stream.cuda_stream
 
 
-def _lora_args(X, W, A, B, scaling, adapter_of):
+def _on_device(t, device, name):
+    if t.get_device() != device:
+        raise ValueError("%s is on device %d, not on device %d" % (name, t.get_device(), device))
+    return t
+
+
+def _lora_args(ctx, X, W, A, B, scaling, adapter_of):
     """Checks the arguments the two adapter calls share; returns (dtype code, T, C, ldx, R, ldw, n_adapters, rank)."""
     dt = X.dtype
     if dt is not torch.float16 and dt is not torch.bfloat16:
@@ -982,8 +988,11 @@ def _lora_args(X, W, A, B, scaling, adapter_of):
         raise TypeError("W, A and B must have the type of X, %s" % dt)
     if scaling.dtype is not torch.float32 or adapter_of.dtype is not torch.int32:
         raise TypeError("scaling must be torch.float32 and adapter_of torch.int32")
-    if not (X.is_cuda and W.is_cuda and A.is_cuda and B.is_cuda and scaling.is_cuda and adapter_of.is_cuda):
-        raise TypeError("X, W, A, B, scaling and adapter_of must be CUDA tensors")
+    if not (X.get_device() == W.get_device() == A.get_device() == B.get_device() == scaling.get_device() == adapter_of.get_device()
+            == ctx.device):
+        if not (X.is_cuda and W.is_cuda and A.is_cuda and B.is_cuda and scaling.is_cuda and adapter_of.is_cuda):
+            raise TypeError("X, W, A, B, scaling and adapter_of must be CUDA tensors")
+        raise ValueError("X, W, A, B, scaling and adapter_of must be on the context's device, %d" % ctx.device)
     if X.dim() != 2 or W.dim() != 2 or A.dim() != 3 or B.dim() != 3 or scaling.dim() != 1 or adapter_of.dim() != 1:
         raise ValueError("X and W have 2 dimensions, A and B 3, scaling and adapter_of 1")
     T, C = X.shape
@@ -1000,14 +1009,14 @@ def _lora_args(X, W, A, B, scaling, adapter_of):
     return _DTYPE_CODES[dt], T, C, (ldx if T > 1 else C + -C % 8), R, (ldw if R > 1 else C + -C % 8), n, rank
 
 
-def _row_output(t, rows, cols, like, name):
+def _row_output(t, rows, cols, like, name):   # like: a tensor on the context's device
     """A caller's [rows, cols] output, or a new one whose rows are padded to a multiple of 8 elements."""
     if t is None:
         if cols % 8 == 0:
             return like.new_empty((rows, cols)), cols
         ld = cols + -cols % 8
         return like.new_empty((rows, ld))[:, :cols], ld
-    _need(t, like.dtype, name, 2)
+    _on_device(_need(t, like.dtype, name, 2), like.get_device(), name)
     if t.shape != (rows, cols) or (t.stride(1) != 1 and cols > 1):
         raise ValueError("%s must be a row-major [%d, %d] tensor" % (name, rows, cols))
     return t, (t.stride(0) if rows > 1 else cols + -cols % 8)
@@ -1020,7 +1029,7 @@ def windq_lora_forward(ctx: Context, X: torch.Tensor, W: torch.Tensor, A: torch.
 
     X [T, C], W [R, C] (as windq_apply_plan leaves it), A [n, rank, C], B [n, R, rank], all fp16 or all bf16;
     scaling fp32 [n]; adapter_of int32 [T].  Returns Y [T, R] of the same type (``out`` if given)."""
-    code, T, C, ldx, R, ldw, n, rank = _lora_args(X, W, A, B, scaling, adapter_of)
+    code, T, C, ldx, R, ldw, n, rank = _lora_args(ctx, X, W, A, B, scaling, adapter_of)
     out, ldy = _row_output(out, T, R, X, "out")
     ctx._check(_lib.windq_lora_forward(ctx._h, code, X.data_ptr(), T, C, ldx, W.data_ptr(), R, ldw, A.data_ptr(), B.data_ptr(),
                                        n, rank, scaling.data_ptr(), adapter_of.data_ptr(), out.data_ptr(), ldy,
@@ -1035,8 +1044,8 @@ def windq_lora_backward(ctx: Context, X: torch.Tensor, W: torch.Tensor, A: torch
 
     Returns dict(dx [T, C] of X's type | None, dA fp32 [n, rank, C] | None, dB fp32 [n, R, rank] | None), overwritten,
     not added to.  ``out`` may hold preallocated tensors under the same keys."""
-    code, T, C, ldx, R, ldw, n, rank = _lora_args(X, W, A, B, scaling, adapter_of)
-    _need(dY, X.dtype, "dY", 2)
+    code, T, C, ldx, R, ldw, n, rank = _lora_args(ctx, X, W, A, B, scaling, adapter_of)
+    _on_device(_need(dY, X.dtype, "dY", 2), ctx.device, "dY")
     if dY.shape != (T, R) or (dY.stride(1) != 1 and R > 1):
         raise ValueError("dY must be a row-major [T, R] tensor")
     lddy = dY.stride(0) if T > 1 else R + -R % 8
@@ -1048,8 +1057,8 @@ def windq_lora_backward(ctx: Context, X: torch.Tensor, W: torch.Tensor, A: torch
             dA = X.new_empty((n, rank, C), dtype=torch.float32)
         if dB is None:
             dB = X.new_empty((n, R, rank), dtype=torch.float32)
-        _need(dA, torch.float32, "dA", 3)
-        _need(dB, torch.float32, "dB", 3)
+        _on_device(_need(dA, torch.float32, "dA", 3), ctx.device, "dA")
+        _on_device(_need(dB, torch.float32, "dB", 3), ctx.device, "dB")
         if dA.shape != A.shape or dB.shape != B.shape or not (dA.is_contiguous() and dB.is_contiguous()):
             raise ValueError("dA and dB must be contiguous and have the shapes of A and B")
     ctx._check(_lib.windq_lora_backward(ctx._h, code, X.data_ptr(), T, C, ldx, W.data_ptr(), R, ldw, A.data_ptr(), B.data_ptr(),
@@ -1058,7 +1067,7 @@ def windq_lora_backward(ctx: Context, X: torch.Tensor, W: torch.Tensor, A: torch
     return dict(dx=dx, dA=dA, dB=dB)
 
 
-_DTYPE_OF, _ON_CUDA = operator.attrgetter("dtype"), operator.attrgetter("is_cuda")
+_DTYPE_OF = operator.attrgetter("dtype")
 ADAMW_BLOCK = 256   # elements of a tensor that share the scales of 8-bit states
 
 
@@ -1094,6 +1103,7 @@ class AdamwTensors:
         self.copy_dtype = next((c.dtype for c in copies or [] if c is not None), torch.float16)
         if self.copy_dtype not in (torch.float16, torch.bfloat16):
             raise TypeError("copies must be fp16 or bf16")
+        self.device = params[0].get_device()
         state = (torch.int8, torch.uint8) if self.state_bits == 8 else (torch.float32, torch.float32)
         self._jobs = (_AdamwJob * k)()
         for j in range(k):
@@ -1118,11 +1128,15 @@ class AdamwTensors:
         self._codes = (_DTYPE_CODES[self.param_dtype], _DTYPE_CODES[self.grad_dtype], _DTYPE_CODES[self.copy_dtype], self.state_bits)
         self.set_grads(grads)
 
-    @staticmethod
-    def _flat(t, dtype, n, name):
-        _need(t, dtype, name)
+    def _flat(self, t, dtype, n, name):
+        _on_device(_need(t, dtype, name), self.device, name)
         if t.numel() != n or not t.is_contiguous():
             raise ValueError("%s: a tensor is not contiguous or has %d elements where %d are needed" % (name, t.numel(), n))
+
+    def _for(self, ctx):
+        if self.device != ctx.device:
+            raise ValueError("the tensors are on device %d, the context on device %d" % (self.device, ctx.device))
+        return self
 
     def __len__(self):
         return len(self._jobs)
@@ -1142,8 +1156,9 @@ def windq_adamw_step(ctx: Context, tensors: AdamwTensors, *, step: int, lr: floa
                      eps: float = 1e-8, weight_decay: float = 0.0, grad_scale: torch.Tensor | None = None, stream=None) -> None:
     """One AdamW step over all tensors, in place.  ``step`` counts from one; ``grad_scale`` (fp32 [1] on the device)
     multiplies every gradient first."""
+    tensors._for(ctx)
     if grad_scale is not None:
-        _need(grad_scale, torch.float32, "grad_scale")
+        _on_device(_need(grad_scale, torch.float32, "grad_scale"), ctx.device, "grad_scale")
         if grad_scale.numel() != 1:
             raise ValueError("grad_scale must hold one value")
     ctx._check(_lib.windq_adamw_step(ctx._h, tensors._jobs, len(tensors._jobs), *tensors._codes, int(step), lr, beta1, beta2, eps,
@@ -1154,7 +1169,7 @@ def windq_adamw_states(ctx: Context, tensors: AdamwTensors, m_out=None, v_out=No
     """The fp32 values that 8-bit states stand for: (list of m, list of v), written to the given tensors if any."""
     if tensors.state_bits != 8:
         raise ValueError("the states are not held in 8 bits")
-    sizes, k = tensors._sizes, len(tensors)
+    sizes, k = tensors._for(ctx)._sizes, len(tensors)
     outs, arrays = [], []
     for given, name in ((m_out, "m_out"), (v_out, "v_out")):
         if given is None:
@@ -1165,8 +1180,11 @@ def windq_adamw_states(ctx: Context, tensors: AdamwTensors, m_out=None, v_out=No
             # hundreds of tensors a call: the checks go over whole lists
             if list(map(torch.Tensor.numel, given)) != sizes or not all(map(torch.Tensor.is_contiguous, given)):
                 raise ValueError("%s: a tensor is not contiguous or has not the size of its parameter" % name)
-            if set(map(_DTYPE_OF, given)) != {torch.float32} or not all(map(_ON_CUDA, given)):
+            devices = set(map(torch.Tensor.get_device, given))   # -1: not a GPU
+            if set(map(_DTYPE_OF, given)) != {torch.float32} or -1 in devices:
                 raise TypeError("%s must be torch.float32 CUDA tensors" % name)
+            if devices != {ctx.device}:
+                raise ValueError("%s must be on the context's device, %d" % (name, ctx.device))
         outs.append(given)
         arrays.append(array.array("Q", map(torch.Tensor.data_ptr, given)))   # pointers are 64 bits wide
     ctx._check(_lib.windq_adamw_states(ctx._h, tensors._jobs, k, *(a.buffer_info()[0] for a in arrays), _raw_stream(ctx, stream)))
