@@ -641,7 +641,9 @@ windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64
  *                   scales are the block's largest |m| and r (0, with codes 0, where that is below 2^-100); codes are
  *                   rounded to nearest in the square-root domain, and an r above zero in such a block never gets code 0
  *                   (its element would divide by eps).  The step itself uses m and r before they are rounded to codes.
- *                   All-zero codes and scales are the empty state.
+ *                   All-zero codes and scales are the empty state, which an element whose r is not finite goes back to (its
+ *                   gradient was not, or its square overflowed): the others of its block keep theirs.  With 32-bit states
+ *                   such an r stays.  The parameter takes the step as written in either case.
  *   step >= 1 counts from one;  lr >= 0, 0 <= beta1, beta2 < 1, eps > 0, weight_decay >= 0, all finite;
  *   grad_scale  fp32 [1] on the device, or NULL: an unscaling and / or clipping factor formed there */
 typedef struct {

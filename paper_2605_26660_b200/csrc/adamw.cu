@@ -201,7 +201,8 @@ __global__ void __launch_bounds__(kWarps * 32) adamw8_kernel(const __grid_consta
   // both roundings of x + y.
   const float2 one = both(f.one);
   const uint32_t wm[2] = {qm.x ^ 0x80808080u, qm.y ^ 0x80808080u}, wr[2] = {qr.x, qr.y};
-  float top_m = 0.0f, top_r = 0.0f;
+  float top_m = 0.0f;
+  uint32_t top_r_bits = 0;  // values >= 0 order like their bit patterns, and NaN comes out largest
 #pragma unroll
   for (int k = 0; k < 8; k += 2) {
     float2 um = make_float2(code_bits(wm[k >> 2], k & 3), code_bits(wm[k >> 2], (k & 3) + 1));
@@ -220,13 +221,25 @@ __global__ void __launch_bounds__(kWarps * 32) adamw8_kernel(const __grid_consta
     m[k] = mn.x, m[k + 1] = mn.y;
     r[k] = rn.x, r[k + 1] = rn.y;
     top_m = fmaxf(top_m, fmaxf(fabsf(mn.x), fabsf(mn.y)));
-    top_r = fmaxf(top_r, fmaxf(rn.x, rn.y));
+    top_r_bits = max(top_r_bits, max(__float_as_uint(rn.x), __float_as_uint(rn.y)));
   }
   store_any(e.param, i, f.param_dtype, live, p);
   if (e.copy) store_any(e.copy, i, f.copy_dtype, live, p);
-  // values >= 0 order like their bit patterns
+  top_r_bits = __reduce_max_sync(0xffffffffu, top_r_bits);
+  if (top_r_bits >= 0x7f800000u) {
+    // Some r is not finite (m is wherever r is): its element starts anew, so that the scales stay those of the others.
+    top_m = 0.0f;
+    top_r_bits = 0;
+#pragma unroll
+    for (int k = 0; k < 8; k++) {
+      if (__float_as_uint(r[k]) >= 0x7f800000u) m[k] = r[k] = 0.0f;
+      top_m = fmaxf(top_m, fabsf(m[k]));
+      top_r_bits = max(top_r_bits, __float_as_uint(r[k]));
+    }
+    top_r_bits = __reduce_max_sync(0xffffffffu, top_r_bits);
+  }
   top_m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top_m)));
-  top_r = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top_r)));
+  float top_r = __uint_as_float(top_r_bits);
   top_m = top_m >= kTiny ? top_m : 0.0f;
   top_r = top_r >= kTiny ? top_r : 0.0f;
   const float inv_m = top_m > 0.0f ? 1.0f / top_m : 0.0f, inv_r = top_r > 0.0f ? 1.0f / top_r : 0.0f;
