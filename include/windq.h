@@ -629,8 +629,10 @@ windq_status windq_lora_backward(windq_ctx* ctx, int dtype, const void* X, int64
  *   g = grad * grad_scale[0]                      (no product when grad_scale is NULL)
  *   m = m * beta1 + g * (1 - beta1);   v = v * beta2 + (g * g) * (1 - beta2);   r = sqrt(v)
  *   param = param * (1 - lr * weight_decay) - (m * (lr / (1 - beta1^step))) / (r * (1 / sqrt(1 - beta2^step)) + eps)
- *   copy = param rounded to the copy's type       (e.g. the 16-bit adapters windq_lora_forward reads)
- * The factors of the hyperparameters are formed in double and rounded to binary32 once.
+ *   copy = that binary32 value rounded to the copy's type   (e.g. the 16-bit adapters windq_lora_forward reads; of a 16-bit
+ *                                                 param too, whose own rounding does not go into it)
+ * The factors of the hyperparameters are formed in double, on the host, and rounded to binary32 once: the replay of a
+ * captured step takes the step number and the learning rate that were captured.
  *   jobs: HOST array of n_jobs descriptors (n_jobs >= 1, no upper limit), read during the call only; all jobs share the
  *         types.  Tensors are flat, 16-byte aligned, of any length n >= 0 (0 does nothing); none may overlap.
  *   param_dtype WINDQ_F32, _F16 or _BF16 (16-bit parameters are rounded once per step);  grad_dtype likewise
