@@ -1028,7 +1028,8 @@ def windq_lora_forward(ctx: Context, X: torch.Tensor, W: torch.Tensor, A: torch.
     """Y[t] = W x_t + B[a] (scaling[a] A[a] x_t) with a = adapter_of[t] (outside [0, n): no adapter).
 
     X [T, C], W [R, C] (as windq_apply_plan leaves it), A [n, rank, C], B [n, R, rank], all fp16 or all bf16;
-    scaling fp32 [n]; adapter_of int32 [T].  Returns Y [T, R] of the same type (``out`` if given)."""
+    scaling fp32 [n]; adapter_of int32 [T].  Returns Y [T, R] of the same type (``out`` if given).  As with every call here,
+    autograd records nothing: the gradients are windq_lora_backward's."""
     code, T, C, ldx, R, ldw, n, rank = _lora_args(ctx, X, W, A, B, scaling, adapter_of)
     out, ldy = _row_output(out, T, R, X, "out")
     ctx._check(_lib.windq_lora_forward(ctx._h, code, X.data_ptr(), T, C, ldx, W.data_ptr(), R, ldw, A.data_ptr(), B.data_ptr(),
@@ -1122,14 +1123,16 @@ class AdamwTensors:
             self._jobs[j] = _AdamwJob(params[j].data_ptr(), None, m[j].data_ptr(), v[j].data_ptr(),
                                       *(None if t is None else t.data_ptr() for t in scales),
                                       None if copy is None else copy.data_ptr(), n)
-        # aliases, not the caller's lists and tensor objects: either may come to hold other memory while the jobs keep the addresses
-        self._keep = [[None if t is None else t.detach() for t in ts] for ts in (params, m, v, m_scale, r_scale, copies) if ts is not None]
-        self._sizes = [p.numel() for p in params]
+        # the memory, not the caller's lists and tensor objects: either may come to hold other memory while the jobs keep the addresses
+        self._keep = [t.untyped_storage() for ts in (params, m, v, m_scale, r_scale, copies) if ts is not None for t in ts if t is not None]
+        self._shapes, self._sizes = [p.shape for p in params], [p.numel() for p in params]
         self._codes = (_DTYPE_CODES[self.param_dtype], _DTYPE_CODES[self.grad_dtype], _DTYPE_CODES[self.copy_dtype], self.state_bits)
         self.set_grads(grads)
 
     def _flat(self, t, dtype, n, name):
-        _on_device(_need(t, dtype, name), self.device, name)
+        _need(t, dtype, name)
+        if t.get_device() != self.device:
+            _on_device(t, self.device, name)
         if t.numel() != n or not t.is_contiguous():
             raise ValueError("%s: a tensor is not contiguous or has %d elements where %d are needed" % (name, t.numel(), n))
 
@@ -1149,7 +1152,7 @@ class AdamwTensors:
             self._flat(g, self.grad_dtype, self._jobs[j].n, "grads")
         for j, g in enumerate(grads):
             self._jobs[j].grad = g.data_ptr()
-        self._grads = [g.detach() for g in grads]
+        self._grads = [g.untyped_storage() for g in grads]
 
 
 def windq_adamw_step(ctx: Context, tensors: AdamwTensors, *, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
@@ -1173,7 +1176,7 @@ def windq_adamw_states(ctx: Context, tensors: AdamwTensors, m_out=None, v_out=No
     outs, arrays = [], []
     for given, name in ((m_out, "m_out"), (v_out, "v_out")):
         if given is None:
-            given = [torch.empty(p.shape, dtype=torch.float32, device=p.device) for p in tensors._keep[0]]
+            given = [torch.empty(shape, dtype=torch.float32, device=torch.device("cuda", ctx.device)) for shape in tensors._shapes]
         elif len(given) != k:
             raise ValueError("%s must have one entry per parameter" % name)
         else:
