@@ -397,7 +397,7 @@ windq_status launch(windq_ctx* ctx, LowRankArgs p, cudaStream_t st) {
   p.stage_bytes = p.rows * 128 + std::max(plain ? p.pack[0] * wide * 128 : 0, trans ? (p.rank > 64 ? 16384 : p.pack[1] * 8192) : 0);
   // All blocks at once where they can be: an SM's share of its memory (228 KB, of which a block takes 1 KB and 2.4 KB beside
   // the stages) bounds the stages.  Up to 256 tokens a block of the projection, which may start while this kernel runs,
-  // finds room beside them.
+  // finds room beside them where it takes half of an SM's (not where launch_projection gives it the whole, see `two` there).
   const int64_t all = (int64_t)tiles * p.splits * p.jobs * p.slots, each = (all + ctx->sm_count - 1) / ctx->sm_count;
   const int room = (228 * 1024 - (p.T <= 256 ? kProjectShare : 0)) / (int)std::min<int64_t>(each, 4) - 3584;
   const int chunks = (std::max(p.job[0].K, p.job[p.jobs - 1].K) + 63) / 64;
