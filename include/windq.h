@@ -598,10 +598,10 @@ typedef enum { WINDQ_F16 = 0, WINDQ_BF16 = 1, WINDQ_F32 = 2 } windq_dtype;
  *   scaling     fp32 [n_adapters];  adapter_of  i32 [T]; of any 4-byte alignment (a part of a longer batch, say)
  * T = 0 is allowed and does nothing.  Y must not overlap an input.  Columns of Y at and beyond R are not written.
  * Into Y, u_t goes as the sum of two values of the type of X: 16 bits of bf16; of fp16, scaled by a power of two where a
- * token's are small or large, 22 bits of the token's largest |u|, or 16 where that is near 2^-9, for |u| below 2^57.  What is
- * not finite shows: a token, or an adapter with its scaling, that is not finite gives rows that are not, where the formula has none.  Rows of
- * others are not touched, but for one case: a weight of B[a] that is not finite (in windq_lora_backward's dX: of A[a]) may
- * spoil the rows of every token within 256 tokens of one of a's.
+ * token's are small or large, 22 bits of the token's largest |u|, or 16 where that is near 2^-9, for |u| below 2^57.
+ * What is not finite shows: where a token's X, its adapter or its scaling leave the formula without a finite value, Y has
+ * none.  Rows of other tokens are not touched, but for one case: a weight of B[a] that is not finite (in windq_lora_backward's
+ * dX: of A[a]) may spoil the rows of every token within 256 tokens of one of a's.
  * Scratch: windq_scratch_bytes_lora_forward. */
 int64_t windq_scratch_bytes_lora_forward(int64_t T, int64_t R, int64_t C, int rank);
 windq_status windq_lora_forward(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx, const void* W,
