@@ -668,6 +668,77 @@ windq_status windq_adamw_step(windq_ctx* ctx, const windq_adamw_job* jobs, int n
 windq_status windq_adamw_states(windq_ctx* ctx, const windq_adamw_job* jobs, int n_jobs, float* const* m_out,
                                 float* const* v_out, void* stream);
 
+/* ---- the feed-forward block: trained in 16 bits, served in 8 ------------------------------------------
+ *
+ * A decoder block's gate and up projections are used together, h = act(Wg x) * (Wu x).  (The paper has no counterpart: its
+ * plans quantise these matrices like any other.)  windq_gated_forward computes both and h in one kernel, windq_gated_backward
+ * their gradients, for a consumer that trains on after a plan; windq_quantize_rows turns a weight's rows, when a model is
+ * loaded, and every batch of tokens into 8-bit codes with one scale each, and windq_int8_forward (any projection) and
+ * windq_gated_int8_forward multiply codes with codes.  None of the four forward calls uses the context's scratch. */
+
+/* Rows of 16-bit values (tokens, or a weight's output channels) as 8-bit codes with one scale a row.  With a = max_j |X[t][j]|:
+ *   q[t][j] = 127 X[t][j] / a, the exact quotient rounded to nearest (ties to even), in [-127, 127]
+ *   scale[t] = a / 127       (binary32);   a row of zeros: codes and scale 0
+ * A row with an infinity or a NaN gets codes 0 and scale NaN, so that what is computed from it is NaN, too.
+ *   dtype       WINDQ_F16 or WINDQ_BF16, the type of X and values_out
+ *   X [T][ldx], ldx >= C a multiple of 8;  codes_out i8 [T][ldq], ldq >= C a multiple of 16;  scale_out fp32 [T]
+ *   values_out  [T][ldv], nullable: the values the codes stand for, q * scale, rounded to the type of X; ldv >= C, a multiple of 8
+ * Any C >= 1 and T >= 0; columns at and beyond C are neither read nor written.  scale_out may start at any 4-byte address. */
+windq_status windq_quantize_rows(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx,
+                                 int8_t* codes_out, int64_t ldq, float* scale_out, void* values_out, int64_t ldv, void* stream);
+
+/* Product of codes with a scale for each token and each output channel:
+ *   Y[t][r] = (sum_j X[t][j] W[r][j]) * x_scale[t] * w_scale[r]
+ * The sum is exact (32-bit integers); it is rounded to binary32, multiplied from left to right there and rounded to Y's type.
+ *   X i8 [T][ldx], W i8 [R][ldw]: ldx, ldw >= C, multiples of 16; any codes, -128 among them; 1 <= C <= 131071
+ *   x_scale fp32 [T], w_scale fp32 [R]: of any 4-byte alignment
+ *   Y [T][ldy] of type dtype (WINDQ_F16 or WINDQ_BF16), ldy >= R, a multiple of 8; columns at and beyond R are not written
+ * T = 0 is allowed and does nothing.  Y must not overlap an input.  Columns at and beyond C are not read into a sum. */
+windq_status windq_int8_forward(windq_ctx* ctx, const int8_t* X, int64_t T, int64_t C, int64_t ldx, const float* x_scale,
+                                const int8_t* W, int64_t R, int64_t ldw, const float* w_scale, int dtype, void* Y, int64_t ldy,
+                                void* stream);
+
+/* The activation of the gate: g s(y), s(y) = 1 / (1 + exp(-y)), with
+ *   WINDQ_SILU       y = g
+ *   WINDQ_GELU_TANH  y = 2 sqrt(2 / pi) (g + 0.044715 g^3)     (the tanh form of gelu) */
+typedef enum { WINDQ_SILU = 0, WINDQ_GELU_TANH = 1 } windq_activation;
+
+/* Gate and up projection, activation and product in one kernel:
+ *   g = Wg x_t,  u = Wu x_t  (binary32 accumulation in the tensor cores, which cut a sum off where they add to it)
+ *   H[t] = act(g) * u        (from the binary32 sums, rounded once)
+ *   dtype       WINDQ_F16 or WINDQ_BF16, the type of everything
+ *   X [T][ldx], Wg [F][ldwg], Wu [F][ldwu]: leading dimensions >= C, multiples of 8; any C, F >= 1 (the two weights may be
+ *               parts of one matrix)
+ *   H [T][ldh], ldh >= F, a multiple of 8
+ *   gate_out, up_out  [T][ldg], both or neither: g and u, rounded, for windq_gated_backward
+ * T = 0 is allowed and does nothing.  Outputs must not overlap one another or an input; columns at and beyond F are not
+ * written.  In fp16 a sum beyond 65504 becomes infinite, as in any conversion. */
+windq_status windq_gated_forward(windq_ctx* ctx, int dtype, int activation, const void* X, int64_t T, int64_t C, int64_t ldx,
+                                 const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, int64_t F, void* H, int64_t ldh,
+                                 void* gate_out, void* up_out, int64_t ldg, void* stream);
+
+/* windq_gated_forward from 8-bit codes: g and u as windq_int8_forward forms them (before its rounding to 16 bits). */
+windq_status windq_gated_int8_forward(windq_ctx* ctx, int activation, const int8_t* X, int64_t T, int64_t C, int64_t ldx,
+                                      const float* x_scale, const int8_t* Wg, int64_t ldwg, const float* wg_scale, const int8_t* Wu,
+                                      int64_t ldwu, const float* wu_scale, int64_t F, int dtype, void* H, int64_t ldh, void* stream);
+
+/* Gradients of windq_gated_forward, given dH = the gradient of H:
+ *   dU = dH act(g),  dG = dH u act'(g)           (binary32, rounded to `dtype` for the tensor cores)
+ *   dX = dG Wg + dU Wu     [T][lddx], nullable
+ *   dWg = dG^T X, dWu = dU^T X   [F][lddw], both or neither
+ *   gate, up    [T][ldg], both or neither: what the forward call left.  Without them it is computed again, from X, and rounded
+ *               as the forward call rounds it.
+ *   dH [T][lddh];  lddh, ldg >= F, lddx, lddw >= C, multiples of 8
+ * In fp16 dG and dU are kept times one power of two a call, which puts their largest near 2^15, and the products are
+ * divided by it: small gradients lose nothing to fp16's range before they are rounded to the type of the result.
+ * The outputs are overwritten, in an order of sums fixed by the sizes: equal calls give equal bits.  With T = 0 dWg and dWu
+ * become zero.  Scratch: windq_scratch_bytes_gated_backward (recompute: 1 without gate and up). */
+int64_t windq_scratch_bytes_gated_backward(int64_t T, int64_t C, int64_t F, int recompute);
+windq_status windq_gated_backward(windq_ctx* ctx, int dtype, int activation, const void* X, int64_t T, int64_t C, int64_t ldx,
+                                  const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, int64_t F, const void* gate,
+                                  const void* up, int64_t ldg, const void* dH, int64_t lddh, void* dX, int64_t lddx, void* dWg,
+                                  void* dWu, int64_t lddw, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

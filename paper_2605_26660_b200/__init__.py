@@ -108,6 +108,14 @@ def _load() -> ctypes.CDLL:
     lib.windq_scratch_bytes_lora_backward.restype = i64
     lib.windq_adamw_step.argtypes = [vp, vp, i32, i32, i32, i32, i32, i64, f64, f64, f64, f64, f64, vp, vp]
     lib.windq_adamw_states.argtypes = [vp, vp, i32, vp, vp, vp]
+    lib.windq_quantize_rows.argtypes = [vp, i32, vp, i64, i64, i64, vp, i64, vp, vp, i64, vp]
+    lib.windq_int8_forward.argtypes = [vp, vp, i64, i64, i64, vp, vp, i64, i64, vp, i32, vp, i64, vp]
+    lib.windq_gated_forward.argtypes = [vp, i32, i32, vp, i64, i64, i64, vp, i64, vp, i64, i64, vp, i64, vp, vp, i64, vp]
+    lib.windq_gated_int8_forward.argtypes = [vp, i32, vp, i64, i64, i64, vp, vp, i64, vp, vp, i64, vp, i64, i32, vp, i64, vp]
+    lib.windq_gated_backward.argtypes = [vp, i32, i32, vp, i64, i64, i64, vp, i64, vp, i64, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, i64,
+                                         vp]
+    lib.windq_scratch_bytes_gated_backward.argtypes = [i64, i64, i64, i32]
+    lib.windq_scratch_bytes_gated_backward.restype = i64
     lib.windq_fit_ternary_search.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
     lib.windq_scratch_bytes_fit_ternary_search.argtypes = [i64, i64, i32]
     lib.windq_scratch_bytes_fit_ternary_search.restype = i64
@@ -1192,3 +1200,200 @@ def windq_adamw_states(ctx: Context, tensors: AdamwTensors, m_out=None, v_out=No
         arrays.append(array.array("Q", map(torch.Tensor.data_ptr, given)))   # pointers are 64 bits wide
     ctx._check(_lib.windq_adamw_states(ctx._h, tensors._jobs, k, *(a.buffer_info()[0] for a in arrays), _raw_stream(ctx, stream)))
     return tuple(outs)
+
+
+# ---- the feed-forward block: trained in 16 bits, served in 8 ----
+
+ACTIVATIONS = {"silu": 0, "gelu": 1}   # windq_activation of the header; gelu is its tanh form
+
+
+def _activation(name):
+    code = ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError("activation must be one of %s, got %r" % (", ".join(map(repr, ACTIVATIONS)), name))
+    return code
+
+
+def _rows_of(t, dtype, device, step, name):
+    """(rows, columns, leading dimension) of a row-major matrix on the context's device."""
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.get_device() != device:
+        if not t.is_cuda:
+            raise TypeError("%s must be a CUDA tensor" % name)
+        raise ValueError("%s is on device %d, not on the context's, %d" % (name, t.get_device(), device))
+    if t.dim() != 2:
+        raise ValueError("%s must have 2 dimensions" % name)
+    rows, cols = t.shape
+    ld, unit = t.stride()
+    if unit != 1 and cols > 1:
+        raise ValueError("%s must be row-major (unit stride along columns)" % name)
+    # the stride of a single row means nothing, and torch may report any
+    return rows, cols, (ld if rows > 1 else cols + -cols % step)
+
+
+def _scales_of(t, n, device, name):
+    if t.dtype is not torch.float32:
+        raise TypeError("%s must be torch.float32, got %s" % (name, t.dtype))
+    if t.get_device() != device:
+        raise ValueError("%s is on device %d, not on the context's, %d" % (name, t.get_device(), device))
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous [%d] tensor" % (name, n))
+    return t.data_ptr()
+
+
+def _rows_out(t, rows, cols, dtype, device, step, name, like):
+    """A caller's [rows, cols] output, or a new one whose rows are padded to a multiple of ``step`` elements."""
+    if t is None:
+        ld = cols + -cols % step
+        t = like.new_empty((rows, ld), dtype=dtype)
+        return (t if ld == cols else t[:, :cols]), ld
+    r, c, ld = _rows_of(t, dtype, device, step, name)
+    if r != rows or c != cols:
+        raise ValueError("%s must be a [%d, %d] tensor" % (name, rows, cols))
+    return t, ld
+
+
+def windq_quantize_rows(ctx: Context, X: torch.Tensor, *, want_values: bool = False, out: dict | None = None, stream=None) -> dict:
+    """8-bit codes of every row of X [T, C] (fp16 or bf16) with one scale a row: codes = round(127 X / a), scale = a / 127,
+    a the row's largest magnitude.
+
+    Returns dict(codes int8 [T, C], whose rows are a multiple of 16 bytes apart, scale fp32 [T], values [T, C] of X's type
+    | None: what the codes stand for).  ``out`` may hold preallocated tensors under the same keys."""
+    dt, device = X.dtype, ctx.device
+    if dt is not torch.float16 and dt is not torch.bfloat16:
+        raise TypeError("X must be torch.float16 or torch.bfloat16, got %s" % dt)
+    T, C, ldx = _rows_of(X, dt, device, 8, "X")
+    given = out or {}
+    codes, ldq = _rows_out(given.get("codes"), T, C, torch.int8, device, 16, "codes", X)
+    scale = given.get("scale")
+    if scale is None:
+        scale = X.new_empty(T, dtype=torch.float32)
+    values, ldv = _rows_out(given.get("values"), T, C, dt, device, 8, "values", X) if want_values else (None, 0)
+    ctx._check(_lib.windq_quantize_rows(ctx._h, _DTYPE_CODES[dt], X.data_ptr(), T, C, ldx, codes.data_ptr(), ldq,
+                                        _scales_of(scale, T, device, "scale"), _ptr(values), ldv, _raw_stream(ctx, stream)))
+    return dict(codes=codes, scale=scale, values=values)
+
+
+def _out_dtype(dtype, out):
+    if out is not None:
+        dtype = out.dtype
+    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+        raise TypeError("the output must be torch.float16 or torch.bfloat16, got %s" % dtype)
+    return dtype
+
+
+def windq_int8_forward(ctx: Context, codes: torch.Tensor, scale: torch.Tensor, w_codes: torch.Tensor, w_scale: torch.Tensor, *,
+                       dtype: torch.dtype = torch.float16, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Y[t, r] = (sum_j codes[t, j] w_codes[r, j]) scale[t] w_scale[r], the sum exact.
+
+    codes int8 [T, C], w_codes int8 [R, C] (rows a multiple of 16 bytes apart, as windq_quantize_rows leaves them); scale
+    fp32 [T], w_scale fp32 [R].  Returns Y [T, R] of ``dtype``, fp16 or bf16 (``out`` if given)."""
+    device = ctx.device
+    T, C, ldx = _rows_of(codes, torch.int8, device, 16, "codes")
+    R, wide, ldw = _rows_of(w_codes, torch.int8, device, 16, "w_codes")
+    if wide != C:
+        raise ValueError("codes have %d columns, w_codes %d" % (C, wide))
+    dtype = _out_dtype(dtype, out)
+    out, ldy = _rows_out(out, T, R, dtype, device, 8, "out", codes)
+    ctx._check(_lib.windq_int8_forward(ctx._h, codes.data_ptr(), T, C, ldx, _scales_of(scale, T, device, "scale"), w_codes.data_ptr(),
+                                       R, ldw, _scales_of(w_scale, R, device, "w_scale"), _DTYPE_CODES[dtype], out.data_ptr(), ldy,
+                                       _raw_stream(ctx, stream)))
+    return out
+
+
+def windq_gated_int8_forward(ctx: Context, codes: torch.Tensor, scale: torch.Tensor, wg_codes: torch.Tensor, wg_scale: torch.Tensor,
+                             wu_codes: torch.Tensor, wu_scale: torch.Tensor, *, activation: str = "silu",
+                             dtype: torch.dtype = torch.float16, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """H = act(g) u with g and u as windq_int8_forward forms them from the two weights [F, C], before its rounding to 16
+    bits.  Returns H [T, F] of ``dtype``, fp16 or bf16 (``out`` if given)."""
+    device, act = ctx.device, _activation(activation)
+    T, C, ldx = _rows_of(codes, torch.int8, device, 16, "codes")
+    F, wide, ldwg = _rows_of(wg_codes, torch.int8, device, 16, "wg_codes")
+    F_up, wide_up, ldwu = _rows_of(wu_codes, torch.int8, device, 16, "wu_codes")
+    if wide != C or wide_up != C or F_up != F:
+        raise ValueError("shapes do not fit: codes [T, C], wg_codes and wu_codes [F, C]")
+    dtype = _out_dtype(dtype, out)
+    out, ldh = _rows_out(out, T, F, dtype, device, 8, "out", codes)
+    ctx._check(_lib.windq_gated_int8_forward(ctx._h, act, codes.data_ptr(), T, C, ldx, _scales_of(scale, T, device, "scale"),
+                                             wg_codes.data_ptr(), ldwg, _scales_of(wg_scale, F, device, "wg_scale"),
+                                             wu_codes.data_ptr(), ldwu, _scales_of(wu_scale, F, device, "wu_scale"), F,
+                                             _DTYPE_CODES[dtype], out.data_ptr(), ldh, _raw_stream(ctx, stream)))
+    return out
+
+
+def _gated_args(ctx, X, Wg, Wu):
+    """Checks the arguments the two gated calls share; returns (type, T, C, ldx, ldwg, ldwu, F)."""
+    dt, device = X.dtype, ctx.device
+    if dt is not torch.float16 and dt is not torch.bfloat16:
+        raise TypeError("X must be torch.float16 or torch.bfloat16, got %s" % dt)
+    T, C, ldx = _rows_of(X, dt, device, 8, "X")
+    F, wide, ldwg = _rows_of(Wg, dt, device, 8, "Wg")
+    F_up, wide_up, ldwu = _rows_of(Wu, dt, device, 8, "Wu")
+    if wide != C or wide_up != C or F_up != F:
+        raise ValueError("shapes do not fit: X [T, C], Wg and Wu [F, C]")
+    return dt, T, C, ldx, ldwg, ldwu, F
+
+
+def windq_gated_forward(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, *, activation: str = "silu",
+                        want_saved: bool = False, out: dict | None = None, stream=None) -> dict:
+    """H = act(X Wg^T) * (X Wu^T) in one kernel.  X [T, C], Wg and Wu [F, C], all fp16 or all bf16; activation "silu" or "gelu"
+    (the tanh form).
+
+    Returns dict(h [T, F], gate, up [T, F] | None: both products, rounded, for windq_gated_backward).  ``out`` may hold
+    preallocated tensors under the same keys.  Autograd records nothing: the gradients are windq_gated_backward's."""
+    act = _activation(activation)
+    dt, T, C, ldx, ldwg, ldwu, F = _gated_args(ctx, X, Wg, Wu)
+    given, device = out or {}, ctx.device
+    h, ldh = _rows_out(given.get("h"), T, F, dt, device, 8, "h", X)
+    gate = up = None
+    ldg = 0
+    if want_saved:
+        gate, ldg = _rows_out(given.get("gate"), T, F, dt, device, 8, "gate", X)
+        up, ldu = _rows_out(given.get("up"), T, F, dt, device, 8, "up", X)
+        if ldu != ldg:
+            raise ValueError("gate and up must have the same stride between rows")
+    ctx._check(_lib.windq_gated_forward(ctx._h, _DTYPE_CODES[dt], act, X.data_ptr(), T, C, ldx, Wg.data_ptr(), ldwg, Wu.data_ptr(),
+                                        ldwu, F, h.data_ptr(), ldh, _ptr(gate), _ptr(up), ldg, _raw_stream(ctx, stream)))
+    return dict(h=h, gate=gate, up=up)
+
+
+def windq_scratch_bytes_gated_backward(T: int, C: int, F: int, recompute: bool = False) -> int:
+    return int(_lib.windq_scratch_bytes_gated_backward(T, C, F, 1 if recompute else 0))
+
+
+def windq_gated_backward(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, dH: torch.Tensor, *,
+                         gate: torch.Tensor | None = None, up: torch.Tensor | None = None, activation: str = "silu",
+                         want_dx: bool = True, want_dw: bool = True, out: dict | None = None, stream=None) -> dict:
+    """Gradients of windq_gated_forward, from dH [T, F] (the gradient of H) and the gate and up that the forward call left;
+    without them they are computed again.
+
+    Returns dict(dx [T, C] | None, dWg, dWu [F, C] | None), of X's type, overwritten, not added to.  ``out`` may hold
+    preallocated tensors under the same keys."""
+    act = _activation(activation)
+    dt, T, C, ldx, ldwg, ldwu, F = _gated_args(ctx, X, Wg, Wu)
+    given, device = out or {}, ctx.device
+    if (gate is None) != (up is None):
+        raise ValueError("gate and up must be given together")
+    ldg = 0
+    if gate is not None:
+        for t, name in ((gate, "gate"), (up, "up")):
+            rows, cols, ld = _rows_of(t, dt, device, 8, name)
+            if rows != T or cols != F or (name == "up" and ld != ldg):
+                raise ValueError("gate and up must be [%d, %d] tensors with the same stride between rows" % (T, F))
+            ldg = ld
+    rows, cols, lddh = _rows_of(dH, dt, device, 8, "dH")
+    if rows != T or cols != F:
+        raise ValueError("dH must be a [%d, %d] tensor" % (T, F))
+    dx, lddx = _rows_out(given.get("dx"), T, C, dt, device, 8, "dx", X) if want_dx else (None, 0)
+    dWg = dWu = None
+    lddw = 0
+    if want_dw:
+        dWg, lddw = _rows_out(given.get("dWg"), F, C, dt, device, 8, "dWg", X)
+        dWu, other = _rows_out(given.get("dWu"), F, C, dt, device, 8, "dWu", X)
+        if other != lddw:
+            raise ValueError("dWg and dWu must have the same stride between rows")
+    ctx._check(_lib.windq_gated_backward(ctx._h, _DTYPE_CODES[dt], act, X.data_ptr(), T, C, ldx, Wg.data_ptr(), ldwg, Wu.data_ptr(),
+                                         ldwu, F, _ptr(gate), _ptr(up), ldg, dH.data_ptr(), lddh, _ptr(dx), lddx, _ptr(dWg),
+                                         _ptr(dWu), lddw, _raw_stream(ctx, stream)))
+    return dict(dx=dx, dWg=dWg, dWu=dWu)

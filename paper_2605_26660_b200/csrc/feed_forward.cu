@@ -1,0 +1,267 @@
+// The feed-forward block of a quantised model: checks, the gradients of its two products, and the order of the kernels.
+#include <algorithm>
+
+#include "feed_forward.cuh"
+
+namespace windq {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct GateArgs {
+  const void *gate, *up, *dH;
+  int64_t T, ldg, lddh, half;
+  int F, dtype, act;
+  uint16_t* D;     // [T][2 * half]: dG, dU; columns of a half behind F are zeros
+  uint32_t* top;   // fp16: bits of the largest |dG|, |dU|; bf16: NULL
+};
+
+// dU = dH g s, dG = dH u (s + g s (1 - s) y'(g)): see act.
+__device__ __forceinline__ void gate_gradient(float g, float u, float dh, int act, float& dg, float& du) {
+  const float s = logistic(gate_exponent(g, act)), t = s * (1.0f - s);
+  // a gate far out has no slope, and the polynomial of its exponent may have left binary32
+  const float slope = act == WINDQ_SILU ? g : g * (kGeluA * fmaf(3.0f * kGeluB * g, g, 1.0f));
+  du = dh * (g * s);
+  dg = dh * u * (t == 0.0f ? s : fmaf(slope, t, s));
+}
+
+// Eight columns a thread, rows of blocks one after another.  TOP: only the largest magnitude is found (fp16, whose range does
+// not hold what small losses leave: the values are stored times a power of two, see gradient_power).
+template <bool TOP>
+__global__ void __launch_bounds__(kThreads) gate_gradient_kernel(const GateArgs p) {
+  const int groups = (int)(p.half / 8);
+  const int64_t items = p.T * groups;
+  const float power = !TOP && p.top ? gradient_power(*p.top, 1) : 1.0f;
+  uint32_t top = 0;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < items; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t t = i / groups;
+    const int f = (int)(i - t * groups) * 8;
+    float g[8], u[8], dh[8], dg[8], du[8];
+    const int live = min(8, p.F - f);
+    if (live == 8) {
+      load8(p.gate, t * p.ldg + f, p.dtype, g);
+      load8(p.up, t * p.ldg + f, p.dtype, u);
+      load8(p.dH, t * p.lddh + f, p.dtype, dh);
+    } else {
+      load_some(p.gate, t * p.ldg + f, p.dtype, live, g);
+      load_some(p.up, t * p.ldg + f, p.dtype, live, u);
+      load_some(p.dH, t * p.lddh + f, p.dtype, live, dh);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; k++) {
+      gate_gradient(g[k], u[k], dh[k], p.act, dg[k], du[k]);
+      if (TOP) {
+        top = max(top, max(__float_as_uint(dg[k]) & 0x7fffffffu, __float_as_uint(du[k]) & 0x7fffffffu));
+      } else {
+        dg[k] *= power;
+        du[k] *= power;
+      }
+    }
+    if (!TOP) {
+      store8(p.D, t * 2 * p.half + f, p.dtype, dg);
+      store8(p.D, t * 2 * p.half + p.half + f, p.dtype, du);
+    }
+  }
+  if (TOP) {
+    top = __reduce_max_sync(0xffffffffu, top);
+    if ((threadIdx.x & 31) == 0 && top) atomicMax(p.top, top);
+  }
+}
+
+
+windq_status check_common(windq_ctx* ctx, const char* who, const void* X, int64_t T, int64_t C, int64_t ldx, int64_t R, int step) {
+  WINDQ_REQUIRE(ctx, !*ctx->gave_up, WINDQ_ERR_CUDA, "%s: a wait of an earlier call gave up, its results are invalid (windq_stalls)", who);
+  WINDQ_REQUIRE(ctx, T >= 0 && T < (1ll << 31) - 256, WINDQ_ERR_SHAPE, "%s: T = %lld", who, (long long)T);
+  WINDQ_REQUIRE(ctx, R > 0 && C > 0 && R < (1ll << 30) && C < (1ll << 30), WINDQ_ERR_SHAPE, "%s: %lld outputs of %lld channels", who,
+                (long long)R, (long long)C);
+  WINDQ_REQUIRE(ctx, T == 0 || X, WINDQ_ERR_NULL, "%s: the tokens are NULL", who);
+  WINDQ_REQUIRE(ctx, ldx >= C, WINDQ_ERR_SHAPE, "%s: ldx = %lld is below C = %lld", who, (long long)ldx, (long long)C);
+  WINDQ_REQUIRE(ctx, ldx % step == 0 && aligned16(X), WINDQ_ERR_ALIGN, "%s: the tokens are not 16-byte aligned or ldx = %lld is no multiple of %d",
+                who, (long long)ldx, step);
+  return WINDQ_OK;
+}
+windq_status check_weight(windq_ctx* ctx, const char* who, const char* name, const void* W, int64_t ldw, int64_t C, int step) {
+  WINDQ_REQUIRE(ctx, W, WINDQ_ERR_NULL, "%s: %s is NULL", who, name);
+  WINDQ_REQUIRE(ctx, ldw >= C, WINDQ_ERR_SHAPE, "%s: the leading dimension %lld of %s is below C = %lld", who, (long long)ldw, name, (long long)C);
+  WINDQ_REQUIRE(ctx, ldw % step == 0 && aligned16(W), WINDQ_ERR_ALIGN,
+                "%s: %s is not 16-byte aligned or its leading dimension %lld no multiple of %d", who, name, (long long)ldw, step);
+  return WINDQ_OK;
+}
+windq_status check_rows(windq_ctx* ctx, const char* who, const char* name, const void* O, int64_t ld, int64_t width) {
+  WINDQ_REQUIRE(ctx, ld >= width, WINDQ_ERR_SHAPE, "%s: the leading dimension %lld of %s is below %lld", who, (long long)ld, name, (long long)width);
+  WINDQ_REQUIRE(ctx, ld % 8 == 0 && aligned16(O), WINDQ_ERR_ALIGN, "%s: %s is not 16-byte aligned or its leading dimension %lld no multiple of 8",
+                who, name, (long long)ld);
+  return WINDQ_OK;
+}
+windq_status check_scale(windq_ctx* ctx, const char* who, const char* name, const float* s) {
+  WINDQ_REQUIRE(ctx, s, WINDQ_ERR_NULL, "%s: %s is NULL", who, name);
+  WINDQ_REQUIRE(ctx, ((uintptr_t)s & 3) == 0, WINDQ_ERR_ALIGN, "%s: %s is misaligned", who, name);
+  return WINDQ_OK;
+}
+windq_status check_16bit(windq_ctx* ctx, const char* who, int dtype) {
+  WINDQ_REQUIRE(ctx, dtype == WINDQ_F16 || dtype == WINDQ_BF16, WINDQ_ERR_ARG, "%s: dtype = %d is neither fp16 nor bf16", who, dtype);
+  return WINDQ_OK;
+}
+windq_status check_act(windq_ctx* ctx, const char* who, int act) {
+  WINDQ_REQUIRE(ctx, act == WINDQ_SILU || act == WINDQ_GELU_TANH, WINDQ_ERR_ARG, "%s: activation = %d", who, act);
+  return WINDQ_OK;
+}
+#define WINDQ_TRY(call)                    \
+  do {                                     \
+    const windq_status s_ = (call);        \
+    if (s_ != WINDQ_OK) return s_;         \
+  } while (0)
+
+// Sums of products of two codes stay in 32-bit integers up to here.
+constexpr int64_t kMaxCodes = 131071;
+
+}  // namespace
+}  // namespace windq
+
+extern "C" {
+
+windq_status windq_int8_forward(windq_ctx* ctx, const int8_t* X, int64_t T, int64_t C, int64_t ldx, const float* x_scale,
+                                const int8_t* W, int64_t R, int64_t ldw, const float* w_scale, int dtype, void* Y, int64_t ldy,
+                                void* stream) {
+  using namespace windq;
+  const char* who = "windq_int8_forward";
+  if (!ctx) return fail(nullptr, WINDQ_ERR_NULL, "%s: ctx is NULL", who);
+  WINDQ_TRY(check_common(ctx, who, X, T, C, ldx, R, 16));
+  WINDQ_REQUIRE(ctx, C <= kMaxCodes, WINDQ_ERR_SHAPE, "%s: C = %lld is above %lld", who, (long long)C, (long long)kMaxCodes);
+  WINDQ_TRY(check_16bit(ctx, who, dtype));
+  WINDQ_TRY(check_weight(ctx, who, "W", W, ldw, C, 16));
+  WINDQ_TRY(check_scale(ctx, who, "w_scale", w_scale));
+  WINDQ_TRY(check_rows(ctx, who, "Y", Y, ldy, R));
+  if (T == 0) return WINDQ_OK;
+  WINDQ_TRY(check_scale(ctx, who, "x_scale", x_scale));
+  WINDQ_REQUIRE(ctx, Y, WINDQ_ERR_NULL, "%s: Y is NULL", who);
+  DeviceGuard guard(ctx->device);
+  Product q = {kInt8, dtype, 0, T, R, C, X, ldx, {W, nullptr}, {ldw, 0}, 0, x_scale, {w_scale, nullptr}, nullptr, {Y, nullptr, nullptr}, {ldy, 0, 0}};
+  return launch_product(ctx, q, (cudaStream_t)stream);
+}
+
+windq_status windq_gated_int8_forward(windq_ctx* ctx, int activation, const int8_t* X, int64_t T, int64_t C, int64_t ldx,
+                                      const float* x_scale, const int8_t* Wg, int64_t ldwg, const float* wg_scale, const int8_t* Wu,
+                                      int64_t ldwu, const float* wu_scale, int64_t F, int dtype, void* H, int64_t ldh, void* stream) {
+  using namespace windq;
+  const char* who = "windq_gated_int8_forward";
+  if (!ctx) return fail(nullptr, WINDQ_ERR_NULL, "%s: ctx is NULL", who);
+  WINDQ_TRY(check_common(ctx, who, X, T, C, ldx, F, 16));
+  WINDQ_REQUIRE(ctx, C <= kMaxCodes, WINDQ_ERR_SHAPE, "%s: C = %lld is above %lld", who, (long long)C, (long long)kMaxCodes);
+  WINDQ_TRY(check_act(ctx, who, activation));
+  WINDQ_TRY(check_16bit(ctx, who, dtype));
+  WINDQ_TRY(check_weight(ctx, who, "Wg", Wg, ldwg, C, 16));
+  WINDQ_TRY(check_weight(ctx, who, "Wu", Wu, ldwu, C, 16));
+  WINDQ_TRY(check_scale(ctx, who, "wg_scale", wg_scale));
+  WINDQ_TRY(check_scale(ctx, who, "wu_scale", wu_scale));
+  WINDQ_TRY(check_rows(ctx, who, "H", H, ldh, F));
+  if (T == 0) return WINDQ_OK;
+  WINDQ_TRY(check_scale(ctx, who, "x_scale", x_scale));
+  WINDQ_REQUIRE(ctx, H, WINDQ_ERR_NULL, "%s: H is NULL", who);
+  DeviceGuard guard(ctx->device);
+  Product q = {kInt8Gated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, x_scale, {wg_scale, wu_scale}, nullptr,
+               {H, nullptr, nullptr}, {ldh, 0, 0}};
+  return launch_product(ctx, q, (cudaStream_t)stream);
+}
+
+windq_status windq_gated_forward(windq_ctx* ctx, int dtype, int activation, const void* X, int64_t T, int64_t C, int64_t ldx,
+                                 const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, int64_t F, void* H, int64_t ldh,
+                                 void* gate_out, void* up_out, int64_t ldg, void* stream) {
+  using namespace windq;
+  const char* who = "windq_gated_forward";
+  if (!ctx) return fail(nullptr, WINDQ_ERR_NULL, "%s: ctx is NULL", who);
+  WINDQ_TRY(check_common(ctx, who, X, T, C, ldx, F, 8));
+  WINDQ_TRY(check_16bit(ctx, who, dtype));
+  WINDQ_TRY(check_act(ctx, who, activation));
+  WINDQ_TRY(check_weight(ctx, who, "Wg", Wg, ldwg, C, 8));
+  WINDQ_TRY(check_weight(ctx, who, "Wu", Wu, ldwu, C, 8));
+  WINDQ_TRY(check_rows(ctx, who, "H", H, ldh, F));
+  WINDQ_REQUIRE(ctx, !gate_out == !up_out, WINDQ_ERR_NULL, "%s: one of gate_out and up_out is NULL", who);
+  if (gate_out) {
+    WINDQ_TRY(check_rows(ctx, who, "gate_out", gate_out, ldg, F));
+    WINDQ_TRY(check_rows(ctx, who, "up_out", up_out, ldg, F));
+  }
+  if (T == 0) return WINDQ_OK;
+  WINDQ_REQUIRE(ctx, H, WINDQ_ERR_NULL, "%s: H is NULL", who);
+  DeviceGuard guard(ctx->device);
+  Product q = {kGated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, nullptr, {nullptr, nullptr}, nullptr,
+               {H, gate_out, up_out}, {ldh, ldg, ldg}};
+  return launch_product(ctx, q, (cudaStream_t)stream);
+}
+
+int64_t windq_scratch_bytes_gated_backward(int64_t T, int64_t C, int64_t F, int recompute) {
+  if (T < 0 || C <= 0 || F <= 0) return 0;
+  const int64_t half = windq::round_up(F, 64);
+  return 256 + windq::round_up(4 * T * half, 256) * (recompute ? 2 : 1);
+}
+
+windq_status windq_gated_backward(windq_ctx* ctx, int dtype, int activation, const void* X, int64_t T, int64_t C, int64_t ldx,
+                                  const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, int64_t F, const void* gate,
+                                  const void* up, int64_t ldg, const void* dH, int64_t lddh, void* dX, int64_t lddx, void* dWg,
+                                  void* dWu, int64_t lddw, void* stream) {
+  using namespace windq;
+  const char* who = "windq_gated_backward";
+  if (!ctx) return fail(nullptr, WINDQ_ERR_NULL, "%s: ctx is NULL", who);
+  WINDQ_TRY(check_common(ctx, who, X, T, C, ldx, F, 8));
+  WINDQ_TRY(check_16bit(ctx, who, dtype));
+  WINDQ_TRY(check_act(ctx, who, activation));
+  WINDQ_TRY(check_weight(ctx, who, "Wg", Wg, ldwg, C, 8));
+  WINDQ_TRY(check_weight(ctx, who, "Wu", Wu, ldwu, C, 8));
+  WINDQ_REQUIRE(ctx, !gate == !up, WINDQ_ERR_NULL, "%s: one of gate and up is NULL", who);
+  if (gate) {
+    WINDQ_TRY(check_rows(ctx, who, "gate", gate, ldg, F));
+    WINDQ_TRY(check_rows(ctx, who, "up", up, ldg, F));
+  }
+  WINDQ_TRY(check_rows(ctx, who, "dH", dH, lddh, F));
+  WINDQ_REQUIRE(ctx, !dWg == !dWu, WINDQ_ERR_NULL, "%s: one of dWg and dWu is NULL", who);
+  WINDQ_REQUIRE(ctx, dX || dWg, WINDQ_ERR_NULL, "%s: dX, dWg and dWu are all NULL", who);
+  if (dX) WINDQ_TRY(check_rows(ctx, who, "dX", dX, lddx, C));
+  if (dWg) {
+    WINDQ_TRY(check_rows(ctx, who, "dWg", dWg, lddw, C));
+    WINDQ_TRY(check_rows(ctx, who, "dWu", dWu, lddw, C));
+  }
+  DeviceGuard guard(ctx->device);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (T == 0) {
+    if (dWg) WINDQ_CUDA(ctx, cudaMemset2DAsync(dWg, 2 * lddw, 0, 2 * C, F, st));
+    if (dWg) WINDQ_CUDA(ctx, cudaMemset2DAsync(dWu, 2 * lddw, 0, 2 * C, F, st));
+    return WINDQ_OK;
+  }
+  WINDQ_REQUIRE(ctx, dH, WINDQ_ERR_NULL, "%s: dH is NULL", who);
+  WINDQ_TRY(ensure_scratch(ctx, windq_scratch_bytes_gated_backward(T, C, F, !gate)));
+  const int64_t half = round_up(F, 64);
+  uint32_t* top = (uint32_t*)ctx->scratch;
+  uint16_t* D = (uint16_t*)((char*)ctx->scratch + 256);
+  if (!gate) {
+    uint16_t* kept = (uint16_t*)((char*)D + round_up(4 * T * half, 256));
+    gate = kept;
+    up = kept + T * half;
+    ldg = half;
+    Product q = {kGated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, nullptr, {nullptr, nullptr}, nullptr,
+                 {nullptr, kept, kept + T * half}, {0, half, half}};
+    WINDQ_TRY(launch_product(ctx, q, st));
+  }
+  GateArgs a = {gate, up, dH, T, ldg, lddh, half, (int)F, dtype, activation, D, dtype == WINDQ_F16 ? top : nullptr};
+  const int64_t items = T * (half / 8);
+  const unsigned blocks = (unsigned)std::min<int64_t>((items + kThreads - 1) / kThreads, (int64_t)ctx->sm_count * 16);
+  if (a.top) {
+    WINDQ_CUDA(ctx, cudaMemsetAsync(top, 0, 4, st));
+    gate_gradient_kernel<true><<<blocks, kThreads, 0, st>>>(a);
+    WINDQ_CUDA(ctx, cudaGetLastError());
+  }
+  gate_gradient_kernel<false><<<blocks, kThreads, 0, st>>>(a);
+  WINDQ_CUDA(ctx, cudaGetLastError());
+  if (dX) {
+    Product q = {kInputGrad, dtype, 0, T, C, F, D, 2 * half, {Wg, Wu}, {ldwg, ldwu}, half, nullptr, {nullptr, nullptr}, a.top,
+                 {dX, nullptr, nullptr}, {lddx, 0, 0}};
+    WINDQ_TRY(launch_product(ctx, q, st));
+  }
+  if (dWg) {
+    Product q = {kWeightGrad, dtype, 0, F, C, T, D, 2 * half, {X, nullptr}, {ldx, 0}, half, nullptr, {nullptr, nullptr}, a.top,
+                 {dWg, dWu, nullptr}, {lddw, lddw, 0}};
+    WINDQ_TRY(launch_product(ctx, q, st));
+  }
+  return WINDQ_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,53 @@
+// Declarations shared by the translation units of the feed-forward calls.
+#pragma once
+
+#include "typed.cuh"
+
+namespace windq {
+
+// act(g) = g s(y(g)) with the logistic function s; y(g) = g (silu) or 2 sqrt(2 / pi) (g + 0.044715 g^3), the tanh form of gelu.
+constexpr float kGeluA = 1.5957691216057308f, kGeluB = 0.044715f;
+__device__ __forceinline__ float gate_exponent(float g, int act) {
+  return act == WINDQ_SILU ? g : kGeluA * fmaf(kGeluB * g * g, g, g);
+}
+// 1 / (1 + exp(-y)) from exp(-|y|), which cannot overflow.  Relative to the result the two fast functions are off by a few 2^-23
+// and by |y| 2^-24 through the exponent's argument, far below the rounding to 16 bits that follows.
+__device__ __forceinline__ float logistic(float y) {
+  const float e = __expf(-fabsf(y));
+  return __fdividef(y < 0.0f ? e : 1.0f, 1.0f + e);
+}
+
+// The power of two that the gradients of the two products are multiplied with before they are rounded to fp16 (and its
+// inverse, for the products formed from them): their largest then is in [2^14, 2^15).  `top`: bits of the largest |value|.
+__device__ __forceinline__ float gradient_power(uint32_t top, int sign) {
+  const int e = (int)(top >> 23);
+  if (top == 0 || e == 255) return 1.0f;
+  const int shift = min(max(14 + 127 - e, -112), 112);
+  return __uint_as_float((uint32_t)(127 + sign * shift) << 23);
+}
+
+// The products of the feed-forward calls.  D(m, n) = sum_k A(m, k) B(n, k), operands by what they are:
+//   kInt8        codes of tokens x codes of a weight: O = D * row_scale[m] * col_scale[n]
+//   kInt8Gated   two weights: O = act(g) u with g, u as above
+//   kGated       the same of 16-bit tokens and weights; optionally g and u are stored too
+//   kInputGrad   dX: tokens' [dG | dU] x the two weights, transposed
+//   kWeightGrad  dWg, dWu: [dG | dU], transposed, x tokens, transposed
+enum ProductKind { kInt8, kInt8Gated, kGated, kInputGrad, kWeightGrad };
+
+struct Product {
+  int kind, dtype, act;
+  int64_t M, N, K;        // rows and columns of an output, and the sum; kInputGrad: K of each of its two halves
+  const void* A;          // tokens (kWeightGrad: [K][2 * half])
+  int64_t lda;
+  const void* B[2];       // weights (kWeightGrad: tokens [K][N])
+  int64_t ldb[2];
+  int64_t half;           // columns of each half of [dG | dU], a multiple of 64
+  const float* row_scale;
+  const float* col_scale[2];
+  const uint32_t* top;    // fp16 gradients: see gradient_power; nullable
+  void* O[3];             // the output (kWeightGrad: two); kGated: also g and u, nullable
+  int64_t ldo[3];
+};
+windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st);
+
+}  // namespace windq

@@ -56,25 +56,6 @@ struct Barriers {
   uint64_t full[kMaxStages], empty[kMaxStages], granted[kMaxStages], written[kMaxStages], done[2], free[2], whole, shifted;
 };
 
-// A place in the ring of stages.  The roles step through it thousands of times in one thread each, where a division by the
-// number of stages would be most of the time (measured: 0.52 us a chunk of K with it).
-struct Ring {
-  int s = 0, n;
-  uint32_t phase = 0;
-  __device__ explicit Ring(int stages) : n(stages) {}
-  __device__ __forceinline__ void next() {
-    if (++s == n) {
-      s = 0;
-      phase ^= 1;
-    }
-  }
-  __device__ __forceinline__ void skip(int k) {
-    k += s;
-    phase ^= (k / n) & 1;
-    s = k % n;
-  }
-};
-
 // The adapters of a tile that are this split's, for a converged warp: 32 of them in its lanes at a time (one load from L2 an
 // adapter, even when issued one adapter ahead, took longer than the adapter's products).
 struct Adapters {

@@ -1,0 +1,170 @@
+// Rows of 16-bit values as 8-bit codes with one scale a row.
+//
+//   q = round(127 x / a), ties to even, of the exact quotient;  a = max |x| of the row;  scale = a / 127
+// One pass: a row is held in registers between its maximum and its codes (up to 16384 values; of a longer one the rest is
+// read again, from L2).  Bound by memory: 2 bytes read, 1 written a value.  W warps share a row: as few as hold it where there
+// are many rows, more where there are few and the time is one row's latency.
+#include <algorithm>
+
+#include "typed.cuh"
+
+namespace windq {
+namespace {
+
+constexpr int kThreads = 256, kHeld = 8;  // 16-byte pieces of a row in a lane's registers
+
+struct QuantizeArgs {
+  const uint16_t* X;
+  int64_t T, ldx;
+  int C;
+  int8_t* q;
+  int64_t ldq;
+  float* scale;
+  uint16_t* values;
+  int64_t ldv;
+};
+
+// Eight values of a row as they are stored; what lies behind its end reads as zero and is not touched.
+__device__ __forceinline__ uint4 load_piece(const uint16_t* row, int i, int C) {
+  if (i * 8 + 8 <= C) return __ldg(reinterpret_cast<const uint4*>(row) + i);
+  uint32_t w[4] = {0, 0, 0, 0};
+  for (int k = 0; i * 8 + k < C; k++) w[k >> 1] |= (uint32_t)row[i * 8 + k] << (16 * (k & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The largest magnitudes as bit patterns, two to a word: they order as the numbers do, infinities and then NaN above them all.
+__device__ __forceinline__ uint32_t top_of(uint32_t top, const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int k = 0; k < 4; k++) top = __vmaxu2(top, w[k] & 0x7fff7fffu);
+  return top;
+}
+
+// Codes of eight values.  x * inv is within 2^-23 of 127 x / a.  That quotient either is a border between two codes (8 bits) or
+// is at least 2^-18 of itself away from one (127 x has 18 bits, or 15), so rounding the product to 20 bits first puts both on
+// their side.  `lift` (1, or 2^60 for rows of tiny values, whose 127 / a would overflow) is a power of two.
+template <int DT, bool VALUES>
+__device__ __forceinline__ void encode(const uint4& v, float lift, float inv, float scale, uint2& codes, uint4& values) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  float t[8];
+#pragma unroll
+  for (int k = 0; k < 4; k++) {
+    const float2 x = unpack2(w[k], DT);
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const float y = (h ? x.y : x.x) * lift * inv, c = y * 17.0f;
+      t[2 * k + h] = (c - (c - y)) + 12582912.0f;  // 1.5 * 2^23: the integer, rounded, in the low bits
+    }
+  }
+  uint32_t b[8];
+#pragma unroll
+  for (int k = 0; k < 8; k++) b[k] = __float_as_uint(t[k]);
+  codes.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  codes.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+  if (VALUES) {
+    uint32_t o[4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) o[k] = pack2((t[2 * k] - 12582912.0f) * scale, (t[2 * k + 1] - 12582912.0f) * scale, DT);
+    values = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+}
+
+template <int DT, int W, bool VALUES>
+__global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeArgs p) {
+  __shared__ uint32_t tops[kThreads / 32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % W;
+  const int64_t t = (int64_t)blockIdx.x * (kThreads / 32 / W) + warp / W;
+  const bool live = t < p.T;
+  const uint16_t* row = p.X + (live ? t : 0) * p.ldx;
+  const int pieces = live ? (p.C + 7) / 8 : 0, first = part * 32 + lane, step = W * 32;
+  uint4 held[kHeld];
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < kHeld; k++) held[k] = first + k * step < pieces ? load_piece(row, first + k * step, p.C) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int k = 0; k < kHeld; k++) top = top_of(top, held[k]);
+  for (int i = first + kHeld * step; i < pieces; i += step) top = top_of(top, load_piece(row, i, p.C));
+  top = __reduce_max_sync(0xffffffffu, max(top & 0xffff, top >> 16));
+  if (W > 1) {
+    if (lane == 0) tops[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < W; k++) top = max(top, tops[warp / W * W + k]);
+  }
+  if (!live) return;
+  // a row with an infinity or a NaN: codes of zero and a scale of NaN, which spoil its row of every product
+  const bool finite = top < (DT == WINDQ_F16 ? 0x7c00u : 0x7f80u);
+  const float a = finite ? unpack2(top, DT).x : 0.0f, lift = a < 0x1p-60f ? 0x1p60f : 1.0f;
+  const float scale = finite ? __fdiv_rn(a, 127.0f) : __uint_as_float(0x7fffffffu);
+  const float inv = a > 0.0f ? __fdiv_rn(127.0f, a * lift) : 0.0f;
+  if (first == 0) p.scale[t] = scale;
+  int8_t* q = p.q + t * p.ldq;
+  uint16_t* out = VALUES ? p.values + t * p.ldv : nullptr;
+  auto write = [&](int i, uint4 v) {
+    uint2 codes;
+    uint4 values = make_uint4(0, 0, 0, 0);
+    if (!finite) v = make_uint4(0, 0, 0, 0);
+    encode<DT, VALUES>(v, lift, inv, scale, codes, values);
+    if (i * 8 + 8 <= p.C) {
+      reinterpret_cast<uint2*>(q)[i] = codes;
+      if (VALUES) reinterpret_cast<uint4*>(out)[i] = values;
+    } else {
+      const uint32_t o[4] = {values.x, values.y, values.z, values.w};
+      for (int k = 0; i * 8 + k < p.C; k++) {
+        q[i * 8 + k] = (int8_t)((k < 4 ? codes.x : codes.y) >> (8 * (k & 3)));
+        if (VALUES) out[i * 8 + k] = (uint16_t)(o[k >> 1] >> (16 * (k & 1)));
+      }
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < kHeld; k++)
+    if (first + k * step < pieces) write(first + k * step, held[k]);
+  for (int i = first + kHeld * step; i < pieces; i += step) write(i, load_piece(row, i, p.C));
+}
+
+template <int DT, int W>
+void launch(const QuantizeArgs& p, cudaStream_t st) {
+  const int64_t rows = kThreads / 32 / W;
+  const unsigned blocks = (unsigned)((p.T + rows - 1) / rows);
+  if (p.values) quantize_kernel<DT, W, true><<<blocks, kThreads, 0, st>>>(p);
+  else quantize_kernel<DT, W, false><<<blocks, kThreads, 0, st>>>(p);
+}
+template <int DT>
+void launch(const QuantizeArgs& p, int warps, cudaStream_t st) {
+  switch (warps) {
+    case 1: return launch<DT, 1>(p, st);
+    case 2: return launch<DT, 2>(p, st);
+    case 4: return launch<DT, 4>(p, st);
+    default: return launch<DT, 8>(p, st);
+  }
+}
+
+}  // namespace
+}  // namespace windq
+
+extern "C" windq_status windq_quantize_rows(windq_ctx* ctx, int dtype, const void* X, int64_t T, int64_t C, int64_t ldx,
+                                            int8_t* codes_out, int64_t ldq, float* scale_out, void* values_out, int64_t ldv,
+                                            void* stream) {
+  using namespace windq;
+  const char* who = "windq_quantize_rows";
+  if (!ctx) return fail(nullptr, WINDQ_ERR_NULL, "%s: ctx is NULL", who);
+  WINDQ_REQUIRE(ctx, dtype == WINDQ_F16 || dtype == WINDQ_BF16, WINDQ_ERR_ARG, "%s: dtype = %d is neither fp16 nor bf16", who, dtype);
+  WINDQ_REQUIRE(ctx, T >= 0 && T < (1ll << 31) - 256, WINDQ_ERR_SHAPE, "%s: T = %lld", who, (long long)T);
+  WINDQ_REQUIRE(ctx, C > 0 && C < (1ll << 31) - (1 << 20), WINDQ_ERR_SHAPE, "%s: C = %lld", who, (long long)C);
+  WINDQ_REQUIRE(ctx, T == 0 || (X && codes_out && scale_out), WINDQ_ERR_NULL, "%s: X, codes_out or scale_out is NULL", who);
+  WINDQ_REQUIRE(ctx, ldx >= C && ldq >= C && (!values_out || ldv >= C), WINDQ_ERR_SHAPE, "%s: ldx = %lld, ldq = %lld or ldv = %lld is below C = %lld",
+                who, (long long)ldx, (long long)ldq, (long long)ldv, (long long)C);
+  WINDQ_REQUIRE(ctx, ldx % 8 == 0 && ldq % 16 == 0 && (!values_out || ldv % 8 == 0), WINDQ_ERR_ALIGN,
+                "%s: ldx = %lld or ldv = %lld is not a multiple of 8, or ldq = %lld of 16", who, (long long)ldx, (long long)ldv, (long long)ldq);
+  WINDQ_REQUIRE(ctx, aligned16(X) && aligned16(codes_out) && aligned16(values_out), WINDQ_ERR_ALIGN,
+                "%s: X, codes_out or values_out is not 16-byte aligned", who);
+  WINDQ_REQUIRE(ctx, ((uintptr_t)scale_out & 3) == 0, WINDQ_ERR_ALIGN, "%s: scale_out is misaligned", who);
+  if (T == 0) return WINDQ_OK;
+  DeviceGuard guard(ctx->device);
+  QuantizeArgs p = {(const uint16_t*)X, T, ldx, (int)C, codes_out, ldq, scale_out, (uint16_t*)values_out, ldv};
+  int warps = 1;
+  while (warps < 8 && (C > warps * 32 * 8 * kHeld || (T * warps < ctx->sm_count * 16 && C > warps * 32 * 8))) warps *= 2;
+  if (dtype == WINDQ_F16) launch<WINDQ_F16>(p, warps, (cudaStream_t)stream);
+  else launch<WINDQ_BF16>(p, warps, (cudaStream_t)stream);
+  WINDQ_CUDA(ctx, cudaGetLastError());
+  return WINDQ_OK;
+}

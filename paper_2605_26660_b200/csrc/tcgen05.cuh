@@ -1,4 +1,4 @@
-// Thin wrappers around the sm_100a instructions the projection kernel is built from: mbarriers, tensor-map copies,
+// Thin wrappers around the sm_100a instructions the matrix products are built from: mbarriers, tensor-map copies,
 // tcgen05 matrix products with accumulators in tensor memory, clusters, and launches that overlap their predecessor.
 #pragma once
 
@@ -120,6 +120,25 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
+// A place in the ring of stages.  The roles step through it thousands of times in one thread each, where a division by the
+// number of stages would be most of the time (measured: 0.52 us a chunk of K with it).
+struct Ring {
+  int s = 0, n;
+  uint32_t phase = 0;
+  __device__ explicit Ring(int stages) : n(stages) {}
+  __device__ __forceinline__ void next() {
+    if (++s == n) {
+      s = 0;
+      phase ^= 1;
+    }
+  }
+  __device__ __forceinline__ void skip(int k) {
+    k += s;
+    phase ^= (k / n) & 1;
+    s = k % n;
+  }
+};
+
 // Shared-memory matrix descriptor, 128-byte swizzle.  K-major: rows of 64 16-bit values (128 bytes), groups of 8 rows
 // 1024 bytes apart.  MN-major: blocks of 64 values along M or N, `block` bytes apart, each [k][64], 8 k 1024 bytes.
 __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t block) {
@@ -160,6 +179,25 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// The same of signed 8-bit integers, 32 of K a product; the accumulators are 32-bit integers.
+__host__ __device__ inline uint32_t instr_desc_i8(int m, int n) {
+  return 2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
+}
+template <bool PAIR>
+__device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
         : "memory");
 }
@@ -275,6 +313,19 @@ inline bool make_map(CUtensorMap* map, int dtype, const void* base, int64_t inne
   const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, ones[3] = {1, 1, 1};
   return encode_tiled()(map, dtype == WINDQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
                         planes > 0 ? 3 : 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A row-major array [rows][inner] of 16-bit values, or of bytes (dtype < 0), its rows `row_bytes` apart, in boxes of
+// box_rows x 128 bytes.
+inline bool make_map_2d(CUtensorMap* map, int dtype, const void* base, int64_t inner, int64_t rows, int64_t row_bytes, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)row_bytes};
+  const cuuint32_t box[2] = {dtype < 0 ? 128u : 64u, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+  const CUtensorMapDataType type = dtype < 0              ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                   : dtype == WINDQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                        : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return encode_tiled()(map, type, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
