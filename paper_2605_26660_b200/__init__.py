@@ -3,7 +3,8 @@
 Every function below has the name of the C-ABI entry point it calls
 (``include/windq.h``) and does nothing but check tensor types, allocate output
 tensors with torch, pass raw device pointers and the current CUDA stream, and
-turn a non-zero status into ``WindqError``.  All arithmetic happens in the CUDA
+turn a non-zero status into ``WindqError`` (for the feed-forward calls most of
+that is compiled: ``csrc/binding.cpp``).  All arithmetic happens in the CUDA
 kernels.  There is no CPU fallback: if the shared library is missing and cannot
 be built, importing this package raises.
 """
@@ -11,6 +12,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import importlib
 import operator
 import os
 
@@ -122,7 +124,18 @@ def _load() -> ctypes.CDLL:
     return lib
 
 
+def _load_binding():
+    """The compiled marshalling of the feed-forward calls (csrc/binding.cpp)."""
+    try:
+        _build.build_binding()
+    except Exception as exc:  # no compiler, or a compile error
+        if not os.path.exists(_build.BINDING):
+            raise ImportError("the compiled binding is not built and cannot be built here: %s" % exc) from exc
+    return importlib.import_module("._binding", __name__)
+
+
 _lib = _load()
+_binding = _load_binding()
 LIBRARY_PATH = _build.LIB
 
 
@@ -1214,44 +1227,9 @@ def _activation(name):
     return code
 
 
-def _rows_of(t, dtype, device, step, name):
-    """(rows, columns, leading dimension) of a row-major matrix on the context's device."""
-    if t.dtype is not dtype:
-        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if t.get_device() != device:
-        if not t.is_cuda:
-            raise TypeError("%s must be a CUDA tensor" % name)
-        raise ValueError("%s is on device %d, not on the context's, %d" % (name, t.get_device(), device))
-    if t.dim() != 2:
-        raise ValueError("%s must have 2 dimensions" % name)
-    rows, cols = t.shape
-    ld, unit = t.stride()
-    if unit != 1 and cols > 1:
-        raise ValueError("%s must be row-major (unit stride along columns)" % name)
-    # the stride of a single row means nothing, and torch may report any
-    return rows, cols, (ld if rows > 1 else cols + -cols % step)
-
-
-def _scales_of(t, n, device, name):
-    if t.dtype is not torch.float32:
-        raise TypeError("%s must be torch.float32, got %s" % (name, t.dtype))
-    if t.get_device() != device:
-        raise ValueError("%s is on device %d, not on the context's, %d" % (name, t.get_device(), device))
-    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous [%d] tensor" % (name, n))
-    return t.data_ptr()
-
-
-def _rows_out(t, rows, cols, dtype, device, step, name, like):
-    """A caller's [rows, cols] output, or a new one whose rows are padded to a multiple of ``step`` elements."""
-    if t is None:
-        ld = cols + -cols % step
-        t = like.new_empty((rows, ld), dtype=dtype)
-        return (t if ld == cols else t[:, :cols]), ld
-    r, c, ld = _rows_of(t, dtype, device, step, name)
-    if r != rows or c != cols:
-        raise ValueError("%s must be a [%d, %d] tensor" % (name, rows, cols))
-    return t, ld
+def _handles(ctx, stream):
+    """What every function of the compiled binding takes first."""
+    return ctx._h.value, ctx.device, None if stream is None else stream.cuda_stream
 
 
 def windq_quantize_rows(ctx: Context, X: torch.Tensor, *, want_values: bool = False, out: dict | None = None, stream=None) -> dict:
@@ -1260,27 +1238,11 @@ def windq_quantize_rows(ctx: Context, X: torch.Tensor, *, want_values: bool = Fa
 
     Returns dict(codes int8 [T, C], whose rows are a multiple of 16 bytes apart, scale fp32 [T], values [T, C] of X's type
     | None: what the codes stand for).  ``out`` may hold preallocated tensors under the same keys."""
-    dt, device = X.dtype, ctx.device
-    if dt is not torch.float16 and dt is not torch.bfloat16:
-        raise TypeError("X must be torch.float16 or torch.bfloat16, got %s" % dt)
-    T, C, ldx = _rows_of(X, dt, device, 8, "X")
     given = out or {}
-    codes, ldq = _rows_out(given.get("codes"), T, C, torch.int8, device, 16, "codes", X)
-    scale = given.get("scale")
-    if scale is None:
-        scale = X.new_empty(T, dtype=torch.float32)
-    values, ldv = _rows_out(given.get("values"), T, C, dt, device, 8, "values", X) if want_values else (None, 0)
-    ctx._check(_lib.windq_quantize_rows(ctx._h, _DTYPE_CODES[dt], X.data_ptr(), T, C, ldx, codes.data_ptr(), ldq,
-                                        _scales_of(scale, T, device, "scale"), _ptr(values), ldv, _raw_stream(ctx, stream)))
-    return dict(codes=codes, scale=scale, values=values)
-
-
-def _out_dtype(dtype, out):
-    if out is not None:
-        dtype = out.dtype
-    if dtype is not torch.float16 and dtype is not torch.bfloat16:
-        raise TypeError("the output must be torch.float16 or torch.bfloat16, got %s" % dtype)
-    return dtype
+    st, codes, scale, values = _binding.quantize_rows(*_handles(ctx, stream), X, want_values, given.get("codes"), given.get("scale"),
+                                                      given.get("values"))
+    ctx._check(st)
+    return {"codes": codes, "scale": scale, "values": values}
 
 
 def windq_int8_forward(ctx: Context, codes: torch.Tensor, scale: torch.Tensor, w_codes: torch.Tensor, w_scale: torch.Tensor, *,
@@ -1288,17 +1250,9 @@ def windq_int8_forward(ctx: Context, codes: torch.Tensor, scale: torch.Tensor, w
     """Y[t, r] = (sum_j codes[t, j] w_codes[r, j]) scale[t] w_scale[r], the sum exact.
 
     codes int8 [T, C], w_codes int8 [R, C] (rows a multiple of 16 bytes apart, as windq_quantize_rows leaves them); scale
-    fp32 [T], w_scale fp32 [R].  Returns Y [T, R] of ``dtype``, fp16 or bf16 (``out`` if given)."""
-    device = ctx.device
-    T, C, ldx = _rows_of(codes, torch.int8, device, 16, "codes")
-    R, wide, ldw = _rows_of(w_codes, torch.int8, device, 16, "w_codes")
-    if wide != C:
-        raise ValueError("codes have %d columns, w_codes %d" % (C, wide))
-    dtype = _out_dtype(dtype, out)
-    out, ldy = _rows_out(out, T, R, dtype, device, 8, "out", codes)
-    ctx._check(_lib.windq_int8_forward(ctx._h, codes.data_ptr(), T, C, ldx, _scales_of(scale, T, device, "scale"), w_codes.data_ptr(),
-                                       R, ldw, _scales_of(w_scale, R, device, "w_scale"), _DTYPE_CODES[dtype], out.data_ptr(), ldy,
-                                       _raw_stream(ctx, stream)))
+    fp32 [T], w_scale fp32 [R].  Returns Y [T, R] of ``dtype``, fp16 or bf16 (``out`` if given, whose type counts)."""
+    st, out = _binding.int8_forward(*_handles(ctx, stream), codes, scale, w_codes, w_scale, dtype, out)
+    ctx._check(st)
     return out
 
 
@@ -1306,33 +1260,11 @@ def windq_gated_int8_forward(ctx: Context, codes: torch.Tensor, scale: torch.Ten
                              wu_codes: torch.Tensor, wu_scale: torch.Tensor, *, activation: str = "silu",
                              dtype: torch.dtype = torch.float16, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """H = act(g) u with g and u as windq_int8_forward forms them from the two weights [F, C], before its rounding to 16
-    bits.  Returns H [T, F] of ``dtype``, fp16 or bf16 (``out`` if given)."""
-    device, act = ctx.device, _activation(activation)
-    T, C, ldx = _rows_of(codes, torch.int8, device, 16, "codes")
-    F, wide, ldwg = _rows_of(wg_codes, torch.int8, device, 16, "wg_codes")
-    F_up, wide_up, ldwu = _rows_of(wu_codes, torch.int8, device, 16, "wu_codes")
-    if wide != C or wide_up != C or F_up != F:
-        raise ValueError("shapes do not fit: codes [T, C], wg_codes and wu_codes [F, C]")
-    dtype = _out_dtype(dtype, out)
-    out, ldh = _rows_out(out, T, F, dtype, device, 8, "out", codes)
-    ctx._check(_lib.windq_gated_int8_forward(ctx._h, act, codes.data_ptr(), T, C, ldx, _scales_of(scale, T, device, "scale"),
-                                             wg_codes.data_ptr(), ldwg, _scales_of(wg_scale, F, device, "wg_scale"),
-                                             wu_codes.data_ptr(), ldwu, _scales_of(wu_scale, F, device, "wu_scale"), F,
-                                             _DTYPE_CODES[dtype], out.data_ptr(), ldh, _raw_stream(ctx, stream)))
+    bits.  Returns H [T, F] of ``dtype``, fp16 or bf16 (``out`` if given, whose type counts)."""
+    st, out = _binding.gated_int8_forward(*_handles(ctx, stream), codes, scale, wg_codes, wg_scale, wu_codes, wu_scale,
+                                          _activation(activation), dtype, out)
+    ctx._check(st)
     return out
-
-
-def _gated_args(ctx, X, Wg, Wu):
-    """Checks the arguments the two gated calls share; returns (type, T, C, ldx, ldwg, ldwu, F)."""
-    dt, device = X.dtype, ctx.device
-    if dt is not torch.float16 and dt is not torch.bfloat16:
-        raise TypeError("X must be torch.float16 or torch.bfloat16, got %s" % dt)
-    T, C, ldx = _rows_of(X, dt, device, 8, "X")
-    F, wide, ldwg = _rows_of(Wg, dt, device, 8, "Wg")
-    F_up, wide_up, ldwu = _rows_of(Wu, dt, device, 8, "Wu")
-    if wide != C or wide_up != C or F_up != F:
-        raise ValueError("shapes do not fit: X [T, C], Wg and Wu [F, C]")
-    return dt, T, C, ldx, ldwg, ldwu, F
 
 
 def windq_gated_forward(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, *, activation: str = "silu",
@@ -1342,20 +1274,11 @@ def windq_gated_forward(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: tor
 
     Returns dict(h [T, F], gate, up [T, F] | None: both products, rounded, for windq_gated_backward).  ``out`` may hold
     preallocated tensors under the same keys.  Autograd records nothing: the gradients are windq_gated_backward's."""
-    act = _activation(activation)
-    dt, T, C, ldx, ldwg, ldwu, F = _gated_args(ctx, X, Wg, Wu)
-    given, device = out or {}, ctx.device
-    h, ldh = _rows_out(given.get("h"), T, F, dt, device, 8, "h", X)
-    gate = up = None
-    ldg = 0
-    if want_saved:
-        gate, ldg = _rows_out(given.get("gate"), T, F, dt, device, 8, "gate", X)
-        up, ldu = _rows_out(given.get("up"), T, F, dt, device, 8, "up", X)
-        if ldu != ldg:
-            raise ValueError("gate and up must have the same stride between rows")
-    ctx._check(_lib.windq_gated_forward(ctx._h, _DTYPE_CODES[dt], act, X.data_ptr(), T, C, ldx, Wg.data_ptr(), ldwg, Wu.data_ptr(),
-                                        ldwu, F, h.data_ptr(), ldh, _ptr(gate), _ptr(up), ldg, _raw_stream(ctx, stream)))
-    return dict(h=h, gate=gate, up=up)
+    given = out or {}
+    st, h, gate, up = _binding.gated_forward(*_handles(ctx, stream), X, Wg, Wu, _activation(activation), want_saved, given.get("h"),
+                                             given.get("gate"), given.get("up"))
+    ctx._check(st)
+    return {"h": h, "gate": gate, "up": up}
 
 
 def windq_scratch_bytes_gated_backward(T: int, C: int, F: int, recompute: bool = False) -> int:
@@ -1370,30 +1293,8 @@ def windq_gated_backward(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: to
 
     Returns dict(dx [T, C] | None, dWg, dWu [F, C] | None), of X's type, overwritten, not added to.  ``out`` may hold
     preallocated tensors under the same keys."""
-    act = _activation(activation)
-    dt, T, C, ldx, ldwg, ldwu, F = _gated_args(ctx, X, Wg, Wu)
-    given, device = out or {}, ctx.device
-    if (gate is None) != (up is None):
-        raise ValueError("gate and up must be given together")
-    ldg = 0
-    if gate is not None:
-        for t, name in ((gate, "gate"), (up, "up")):
-            rows, cols, ld = _rows_of(t, dt, device, 8, name)
-            if rows != T or cols != F or (name == "up" and ld != ldg):
-                raise ValueError("gate and up must be [%d, %d] tensors with the same stride between rows" % (T, F))
-            ldg = ld
-    rows, cols, lddh = _rows_of(dH, dt, device, 8, "dH")
-    if rows != T or cols != F:
-        raise ValueError("dH must be a [%d, %d] tensor" % (T, F))
-    dx, lddx = _rows_out(given.get("dx"), T, C, dt, device, 8, "dx", X) if want_dx else (None, 0)
-    dWg = dWu = None
-    lddw = 0
-    if want_dw:
-        dWg, lddw = _rows_out(given.get("dWg"), F, C, dt, device, 8, "dWg", X)
-        dWu, other = _rows_out(given.get("dWu"), F, C, dt, device, 8, "dWu", X)
-        if other != lddw:
-            raise ValueError("dWg and dWu must have the same stride between rows")
-    ctx._check(_lib.windq_gated_backward(ctx._h, _DTYPE_CODES[dt], act, X.data_ptr(), T, C, ldx, Wg.data_ptr(), ldwg, Wu.data_ptr(),
-                                         ldwu, F, _ptr(gate), _ptr(up), ldg, dH.data_ptr(), lddh, _ptr(dx), lddx, _ptr(dWg),
-                                         _ptr(dWu), lddw, _raw_stream(ctx, stream)))
-    return dict(dx=dx, dWg=dWg, dWu=dWu)
+    given = out or {}
+    st, dx, dWg, dWu = _binding.gated_backward(*_handles(ctx, stream), X, Wg, Wu, _activation(activation), dH, gate, up, want_dx, want_dw,
+                                               given.get("dx"), given.get("dWg"), given.get("dWu"))
+    ctx._check(st)
+    return {"dx": dx, "dWg": dWg, "dWu": dWu}

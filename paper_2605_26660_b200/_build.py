@@ -1,4 +1,4 @@
-"""In-tree build of the CUDA library (nvcc, sm_100a only)."""
+"""In-tree build of the CUDA library (nvcc, sm_100a only) and of the compiled part of its Python binding (g++)."""
 from __future__ import annotations
 
 import hashlib
@@ -12,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libwindq.so")
 STAMP = LIB + ".srchash"
+BINDING = os.path.join(HERE, "_binding.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -65,5 +66,46 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+# ---- the compiled binding: csrc/binding.cpp against torch's headers, linked to the library beside it ----
+
+def binding_command(out: str):
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    include = os.path.join(base, "include")
+    return [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+            "-I", INCLUDE, "-I", include, "-I", os.path.join(include, "torch", "csrc", "api", "include"),
+            "-I", os.path.join(os.path.dirname(os.path.dirname(nvcc_path())), "include"), "-I", sysconfig.get_paths()["include"],
+            os.path.join(CSRC, "binding.cpp"), "-o", out, "-L", HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN",
+            "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+
+
+def binding_hash() -> str:
+    import torch
+    h = hashlib.sha256((torch.__version__ + " ".join(binding_command("")[1:6])).encode())
+    for f in (os.path.join(CSRC, "binding.cpp"), os.path.join(INCLUDE, "windq.h")):
+        with open(f, "rb") as fh:
+            h.update(fh.read())
+    return h.hexdigest()
+
+
+def build_binding(force: bool = False) -> str:
+    """Builds _binding.so unless it is current.  The library has to be there."""
+    stamp = BINDING + ".srchash"
+    if not force and os.path.exists(BINDING) and os.path.exists(stamp):
+        with open(stamp) as fh:
+            if fh.read().strip() == binding_hash():
+                return BINDING
+    tmp = BINDING + ".tmp.%d" % os.getpid()
+    subprocess.run(binding_command(tmp), check=True)
+    os.replace(tmp, BINDING)
+    with open(stamp, "w") as fh:
+        fh.write(binding_hash())
+    return BINDING
+
+
 if __name__ == "__main__":
     print(build(force=True, verbose=True))
+    print(build_binding(force=True))

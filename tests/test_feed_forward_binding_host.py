@@ -1,0 +1,42 @@
+"""What the compiled marshalling of the feed-forward calls refuses, before the library is reached.  Needs no GPU: every tensor
+here is a host one, and a context without a library handle stands for the device."""
+import types
+
+import pytest
+import torch
+
+import paper_2605_26660_b200 as wq
+
+CTX = types.SimpleNamespace(device=0, _h=types.SimpleNamespace(value=None), _check=None)
+STREAM = types.SimpleNamespace(cuda_stream=0)
+X, W = torch.zeros(4, 64, dtype=torch.float16), torch.zeros(8, 64, dtype=torch.float16)
+Q, P = torch.zeros(4, 64, dtype=torch.int8), torch.zeros(8, 64, dtype=torch.int8)
+S, R = torch.zeros(4), torch.zeros(8)
+CALLS = {
+    "quantize": lambda **k: wq.windq_quantize_rows(CTX, k.get("X", X), stream=STREAM),
+    "int8": lambda **k: wq.windq_int8_forward(CTX, k.get("X", Q), S, P, R, dtype=k.get("dtype", torch.float16), stream=STREAM),
+    "gated": lambda **k: wq.windq_gated_forward(CTX, k.get("X", X), W, W, activation=k.get("activation", "silu"), stream=STREAM),
+    "gated_int8": lambda **k: wq.windq_gated_int8_forward(CTX, k.get("X", Q), S, P, R, P, R, activation=k.get("activation", "silu"), stream=STREAM),
+    "backward": lambda **k: wq.windq_gated_backward(CTX, k.get("X", X), W, W, X, activation=k.get("activation", "gelu"), stream=STREAM),
+}
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_host_tensors_and_other_types_are_refused(call):
+    with pytest.raises(TypeError, match="must be a CUDA tensor"):
+        CALLS[call]()
+    with pytest.raises(TypeError, match="must be"):
+        CALLS[call](X=X.double())
+    with pytest.raises(TypeError, match="must be a tensor"):
+        CALLS[call](X=[1.0])
+
+
+@pytest.mark.parametrize("call", ["gated", "gated_int8", "backward"])
+def test_unknown_activations_are_refused(call):
+    with pytest.raises(ValueError, match="activation"):
+        CALLS[call](activation="tanh")
+
+
+def test_functions_count_their_arguments():
+    with pytest.raises(TypeError, match="arguments"):
+        wq._binding.quantize_rows(None, 0, 0, X)
