@@ -674,7 +674,7 @@ windq_status windq_adamw_states(windq_ctx* ctx, const windq_adamw_job* jobs, int
  * plans quantise these matrices like any other.)  windq_gated_forward computes both and h in one kernel, windq_gated_backward
  * their gradients, for a consumer that trains on after a plan; windq_quantize_rows turns a weight's rows, when a model is
  * loaded, and every batch of tokens into 8-bit codes with one scale each, and windq_int8_forward (any projection) and
- * windq_gated_int8_forward multiply codes with codes.  None of the four forward calls uses the context's scratch. */
+ * windq_gated_int8_forward multiply codes with codes. */
 
 /* Rows of 16-bit values (tokens, or a weight's output channels) as 8-bit codes with one scale a row.  With a = max_j |X[t][j]|:
  *   q[t][j] = 127 X[t][j] / a, the exact quotient rounded to nearest (ties to even), in [-127, 127]
@@ -693,7 +693,9 @@ windq_status windq_quantize_rows(windq_ctx* ctx, int dtype, const void* X, int64
  *   X i8 [T][ldx], W i8 [R][ldw]: ldx, ldw >= C, multiples of 16; any codes, -128 among them; 1 <= C <= 131071
  *   x_scale fp32 [T], w_scale fp32 [R]: of any 4-byte alignment
  *   Y [T][ldy] of type dtype (WINDQ_F16 or WINDQ_BF16), ldy >= R, a multiple of 8; columns at and beyond R are not written
- * T = 0 is allowed and does nothing.  Y must not overlap an input.  Columns at and beyond C are not read into a sum. */
+ * T = 0 is allowed and does nothing.  Y must not overlap an input.  Columns at and beyond C are not read into a sum.
+ * Scratch: windq_scratch_bytes_int8_forward. */
+int64_t windq_scratch_bytes_int8_forward(int64_t T, int64_t R, int64_t C);
 windq_status windq_int8_forward(windq_ctx* ctx, const int8_t* X, int64_t T, int64_t C, int64_t ldx, const float* x_scale,
                                 const int8_t* W, int64_t R, int64_t ldw, const float* w_scale, int dtype, void* Y, int64_t ldy,
                                 void* stream);
@@ -712,7 +714,9 @@ typedef enum { WINDQ_SILU = 0, WINDQ_GELU_TANH = 1 } windq_activation;
  *   H [T][ldh], ldh >= F, a multiple of 8
  *   gate_out, up_out  [T][ldg], both or neither: g and u, rounded, for windq_gated_backward
  * T = 0 is allowed and does nothing.  Outputs must not overlap one another or an input; columns at and beyond F are not
- * written.  In fp16 a sum beyond 65504 becomes infinite, as in any conversion. */
+ * written.  In fp16 a sum beyond 65504 becomes infinite, as in any conversion.  Equal calls give equal bits.
+ * Scratch, here and of windq_gated_int8_forward: windq_scratch_bytes_gated_forward. */
+int64_t windq_scratch_bytes_gated_forward(int64_t T, int64_t C, int64_t F);
 windq_status windq_gated_forward(windq_ctx* ctx, int dtype, int activation, const void* X, int64_t T, int64_t C, int64_t ldx,
                                  const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, int64_t F, void* H, int64_t ldh,
                                  void* gate_out, void* up_out, int64_t ldg, void* stream);

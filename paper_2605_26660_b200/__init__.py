@@ -116,6 +116,9 @@ def _load() -> ctypes.CDLL:
     lib.windq_gated_int8_forward.argtypes = [vp, i32, vp, i64, i64, i64, vp, vp, i64, vp, vp, i64, vp, i64, i32, vp, i64, vp]
     lib.windq_gated_backward.argtypes = [vp, i32, i32, vp, i64, i64, i64, vp, i64, vp, i64, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, i64,
                                          vp]
+    for name in ("windq_scratch_bytes_int8_forward", "windq_scratch_bytes_gated_forward"):
+        getattr(lib, name).argtypes = [i64, i64, i64]
+        getattr(lib, name).restype = i64
     lib.windq_scratch_bytes_gated_backward.argtypes = [i64, i64, i64, i32]
     lib.windq_scratch_bytes_gated_backward.restype = i64
     lib.windq_fit_ternary_search.argtypes = [vp, vp, i64, i64, i64, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
@@ -1279,6 +1282,14 @@ def windq_gated_forward(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: tor
                                              given.get("gate"), given.get("up"))
     ctx._check(st)
     return {"h": h, "gate": gate, "up": up}
+
+
+def windq_scratch_bytes_int8_forward(T: int, R: int, C: int) -> int:
+    return int(_lib.windq_scratch_bytes_int8_forward(T, R, C))
+
+
+def windq_scratch_bytes_gated_forward(T: int, C: int, F: int) -> int:
+    return int(_lib.windq_scratch_bytes_gated_forward(T, C, F))
 
 
 def windq_scratch_bytes_gated_backward(T: int, C: int, F: int, recompute: bool = False) -> int:

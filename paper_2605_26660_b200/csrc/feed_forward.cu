@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "feed_forward.cuh"
+#include "tcgen05.cuh"
 
 namespace windq {
 namespace {
@@ -14,6 +15,7 @@ struct GateArgs {
   int F, dtype, act;
   uint16_t* D;     // [T][2 * half]: dG, dU; columns of a half behind F are zeros
   uint32_t* top;   // fp16: bits of the largest |dG|, |dU|; bf16: NULL
+  uint32_t* tops;  // of every block, before that
 };
 
 // dU = dH g s, dG = dH u (s + g s (1 - s) y'(g)): see act.
@@ -25,54 +27,86 @@ __device__ __forceinline__ void gate_gradient(float g, float u, float dh, int ac
   dg = dh * u * (t == 0.0f ? s : fmaf(slope, t, s));
 }
 
-// Eight columns a thread, rows of blocks one after another.  TOP: only the largest magnitude is found (fp16, whose range does
-// not hold what small losses leave: the values are stored times a power of two, see gradient_power).
+// Eight columns a thread, rows gridDim.y apart.  Bound by memory: 6 bytes read and 4 written a value.  fp16's range does not hold
+// what small losses leave, so its values are stored times a power of two (see gradient_power) that a launch with TOP finds
+// first: another 6 bytes read, 4 % of a long backward pass.
 template <bool TOP>
 __global__ void __launch_bounds__(kThreads) gate_gradient_kernel(const GateArgs p) {
-  const int groups = (int)(p.half / 8);
-  const int64_t items = p.T * groups;
-  const float power = !TOP && p.top ? gradient_power(*p.top, 1) : 1.0f;
-  uint32_t top = 0;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < items; i += (int64_t)gridDim.x * kThreads) {
-    const int64_t t = i / groups;
-    const int f = (int)(i - t * groups) * 8;
-    float g[8], u[8], dh[8], dg[8], du[8];
-    const int live = min(8, p.F - f);
-    if (live == 8) {
-      load8(p.gate, t * p.ldg + f, p.dtype, g);
-      load8(p.up, t * p.ldg + f, p.dtype, u);
-      load8(p.dH, t * p.lddh + f, p.dtype, dh);
-    } else {
-      load_some(p.gate, t * p.ldg + f, p.dtype, live, g);
-      load_some(p.up, t * p.ldg + f, p.dtype, live, u);
-      load_some(p.dH, t * p.lddh + f, p.dtype, live, dh);
-    }
+  __shared__ uint32_t warps[kThreads / 32];
+  auto most = [&](uint32_t x) {  // of the block, in every thread
+    x = __reduce_max_sync(0xffffffffu, x);
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = x;
+    __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 8; k++) {
-      gate_gradient(g[k], u[k], dh[k], p.act, dg[k], du[k]);
-      if (TOP) {
-        top = max(top, max(__float_as_uint(dg[k]) & 0x7fffffffu, __float_as_uint(du[k]) & 0x7fffffffu));
+    for (int k = 0; k < kThreads / 32; k++) x = max(x, warps[k]);
+    return x;
+  };
+  launch_dependents();
+  wait_for_predecessor();
+  uint32_t top = 0;
+  float power = 1.0f;
+  if (!TOP && p.top) {
+    const int blocks = gridDim.x * gridDim.y;
+    for (int i = threadIdx.x; i < blocks; i += kThreads) top = max(top, __ldcg(p.tops + i));
+    top = most(top);
+    if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) *p.top = top;
+    power = gradient_power(top, 1);
+    top = 0;
+  }
+  const int f = (blockIdx.x * kThreads + threadIdx.x) * 8;
+  if (f < p.half) {
+    const int live = min(8, p.F - f);
+    for (int64_t t = blockIdx.y; t < p.T; t += gridDim.y) {
+      float g[8], u[8], dh[8], dg[8], du[8];
+      if (live == 8) {
+        load8(p.gate, t * p.ldg + f, p.dtype, g);
+        load8(p.up, t * p.ldg + f, p.dtype, u);
+        load8(p.dH, t * p.lddh + f, p.dtype, dh);
       } else {
-        dg[k] *= power;
-        du[k] *= power;
+        load_some(p.gate, t * p.ldg + f, p.dtype, live, g);
+        load_some(p.up, t * p.ldg + f, p.dtype, live, u);
+        load_some(p.dH, t * p.lddh + f, p.dtype, live, dh);
       }
-    }
-    if (!TOP) {
-      store8(p.D, t * 2 * p.half + f, p.dtype, dg);
-      store8(p.D, t * 2 * p.half + p.half + f, p.dtype, du);
+#pragma unroll
+      for (int k = 0; k < 8; k++) {
+        gate_gradient(g[k], u[k], dh[k], p.act, dg[k], du[k]);
+        if (TOP) {
+          top = max(top, max(__float_as_uint(dg[k]) & 0x7fffffffu, __float_as_uint(du[k]) & 0x7fffffffu));
+        } else {
+          dg[k] *= power;
+          du[k] *= power;
+        }
+      }
+      if (!TOP) {
+        store8(p.D, t * 2 * p.half + f, p.dtype, dg);
+        store8(p.D, t * 2 * p.half + p.half + f, p.dtype, du);
+      }
     }
   }
   if (TOP) {
-    top = __reduce_max_sync(0xffffffffu, top);
-    if ((threadIdx.x & 31) == 0 && top) atomicMax(p.top, top);
+    top = most(top);
+    if (threadIdx.x == 0) p.tops[blockIdx.y * gridDim.x + blockIdx.x] = top;
   }
 }
 
+constexpr int kMostBlocks = 2048;  // of the kernel above
+constexpr int64_t kTopBytes = 256 + 4 * kMostBlocks;
+template <bool TOP>
+windq_status launch_gate_gradient(windq_ctx* ctx, const GateArgs& a, cudaStream_t st) {
+  const int64_t across = (a.half + 8 * kThreads - 1) / (8 * kThreads);
+  const int64_t down = std::max<int64_t>(1, std::min<int64_t>({a.T, ctx->sm_count * 8 / across, kMostBlocks / across}));
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attrs[2];
+  overlapped_launch(cfg, attrs, 1, kThreads, 1, 0, st);
+  cfg.gridDim = dim3((unsigned)across, (unsigned)down);
+  WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, gate_gradient_kernel<TOP>, a));
+  return WINDQ_OK;
+}
 
 windq_status check_common(windq_ctx* ctx, const char* who, const void* X, int64_t T, int64_t C, int64_t ldx, int64_t R, int step) {
   WINDQ_REQUIRE(ctx, !*ctx->gave_up, WINDQ_ERR_CUDA, "%s: a wait of an earlier call gave up, its results are invalid (windq_stalls)", who);
   WINDQ_REQUIRE(ctx, T >= 0 && T < (1ll << 31) - 256, WINDQ_ERR_SHAPE, "%s: T = %lld", who, (long long)T);
-  WINDQ_REQUIRE(ctx, R > 0 && C > 0 && R < (1ll << 30) && C < (1ll << 30), WINDQ_ERR_SHAPE, "%s: %lld outputs of %lld channels", who,
+  WINDQ_REQUIRE(ctx, R > 0 && C > 0 && R < (1ll << 28) && C < (1ll << 28), WINDQ_ERR_SHAPE, "%s: %lld outputs of %lld channels", who,
                 (long long)R, (long long)C);
   WINDQ_REQUIRE(ctx, T == 0 || X, WINDQ_ERR_NULL, "%s: the tokens are NULL", who);
   WINDQ_REQUIRE(ctx, ldx >= C, WINDQ_ERR_SHAPE, "%s: ldx = %lld is below C = %lld", who, (long long)ldx, (long long)C);
@@ -120,6 +154,9 @@ constexpr int64_t kMaxCodes = 131071;
 
 extern "C" {
 
+int64_t windq_scratch_bytes_int8_forward(int64_t T, int64_t R, int64_t C) { return T < 0 || R <= 0 || C <= 0 ? 0 : windq::product_scratch(T); }
+int64_t windq_scratch_bytes_gated_forward(int64_t T, int64_t C, int64_t F) { return T < 0 || C <= 0 || F <= 0 ? 0 : windq::product_scratch(T); }
+
 windq_status windq_int8_forward(windq_ctx* ctx, const int8_t* X, int64_t T, int64_t C, int64_t ldx, const float* x_scale,
                                 const int8_t* W, int64_t R, int64_t ldw, const float* w_scale, int dtype, void* Y, int64_t ldy,
                                 void* stream) {
@@ -136,7 +173,9 @@ windq_status windq_int8_forward(windq_ctx* ctx, const int8_t* X, int64_t T, int6
   WINDQ_TRY(check_scale(ctx, who, "x_scale", x_scale));
   WINDQ_REQUIRE(ctx, Y, WINDQ_ERR_NULL, "%s: Y is NULL", who);
   DeviceGuard guard(ctx->device);
-  Product q = {kInt8, dtype, 0, T, R, C, X, ldx, {W, nullptr}, {ldw, 0}, 0, x_scale, {w_scale, nullptr}, nullptr, {Y, nullptr, nullptr}, {ldy, 0, 0}};
+  WINDQ_TRY(ensure_scratch(ctx, product_scratch(T)));
+  Product q = {kInt8, dtype, 0, T, R, C, X, ldx, {W, nullptr}, {ldw, 0}, 0, x_scale, {w_scale, nullptr}, nullptr, {Y, nullptr, nullptr}, {ldy, 0, 0},
+               ctx->scratch};
   return launch_product(ctx, q, (cudaStream_t)stream);
 }
 
@@ -159,8 +198,9 @@ windq_status windq_gated_int8_forward(windq_ctx* ctx, int activation, const int8
   WINDQ_TRY(check_scale(ctx, who, "x_scale", x_scale));
   WINDQ_REQUIRE(ctx, H, WINDQ_ERR_NULL, "%s: H is NULL", who);
   DeviceGuard guard(ctx->device);
+  WINDQ_TRY(ensure_scratch(ctx, product_scratch(T)));
   Product q = {kInt8Gated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, x_scale, {wg_scale, wu_scale}, nullptr,
-               {H, nullptr, nullptr}, {ldh, 0, 0}};
+               {H, nullptr, nullptr}, {ldh, 0, 0}, ctx->scratch};
   return launch_product(ctx, q, (cudaStream_t)stream);
 }
 
@@ -184,15 +224,16 @@ windq_status windq_gated_forward(windq_ctx* ctx, int dtype, int activation, cons
   if (T == 0) return WINDQ_OK;
   WINDQ_REQUIRE(ctx, H, WINDQ_ERR_NULL, "%s: H is NULL", who);
   DeviceGuard guard(ctx->device);
+  WINDQ_TRY(ensure_scratch(ctx, product_scratch(T)));
   Product q = {kGated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, nullptr, {nullptr, nullptr}, nullptr,
-               {H, gate_out, up_out}, {ldh, ldg, ldg}};
+               {H, gate_out, up_out}, {ldh, ldg, ldg}, ctx->scratch};
   return launch_product(ctx, q, (cudaStream_t)stream);
 }
 
 int64_t windq_scratch_bytes_gated_backward(int64_t T, int64_t C, int64_t F, int recompute) {
   if (T < 0 || C <= 0 || F <= 0) return 0;
   const int64_t half = windq::round_up(F, 64);
-  return 256 + windq::round_up(4 * T * half, 256) * (recompute ? 2 : 1);
+  return windq::kTopBytes + windq::round_up(4 * T * half, 256) * (recompute ? 2 : 1) + windq::product_scratch(T);
 }
 
 windq_status windq_gated_backward(windq_ctx* ctx, int dtype, int activation, const void* X, int64_t T, int64_t C, int64_t ldx,
@@ -230,37 +271,33 @@ windq_status windq_gated_backward(windq_ctx* ctx, int dtype, int activation, con
   WINDQ_REQUIRE(ctx, dH, WINDQ_ERR_NULL, "%s: dH is NULL", who);
   WINDQ_TRY(ensure_scratch(ctx, windq_scratch_bytes_gated_backward(T, C, F, !gate)));
   const int64_t half = round_up(F, 64);
-  uint32_t* top = (uint32_t*)ctx->scratch;
-  uint16_t* D = (uint16_t*)((char*)ctx->scratch + 256);
+  char* at = (char*)ctx->scratch;
+  auto take = [&](int64_t bytes) {
+    char* p = at;
+    at += round_up(bytes, 256);
+    return p;
+  };
+  uint32_t* top = (uint32_t*)take(kTopBytes);
+  uint16_t* D = (uint16_t*)take(4 * T * half);
+  uint16_t* kept = gate ? nullptr : (uint16_t*)take(4 * T * half);
+  void* partials = at;
   if (!gate) {
-    uint16_t* kept = (uint16_t*)((char*)D + round_up(4 * T * half, 256));
     gate = kept;
     up = kept + T * half;
     ldg = half;
     Product q = {kGated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, nullptr, {nullptr, nullptr}, nullptr,
-                 {nullptr, kept, kept + T * half}, {0, half, half}};
+                 {nullptr, kept, kept + T * half}, {0, half, half}, partials};
     WINDQ_TRY(launch_product(ctx, q, st));
   }
-  GateArgs a = {gate, up, dH, T, ldg, lddh, half, (int)F, dtype, activation, D, dtype == WINDQ_F16 ? top : nullptr};
-  const int64_t items = T * (half / 8);
-  const unsigned blocks = (unsigned)std::min<int64_t>((items + kThreads - 1) / kThreads, (int64_t)ctx->sm_count * 16);
-  if (a.top) {
-    WINDQ_CUDA(ctx, cudaMemsetAsync(top, 0, 4, st));
-    gate_gradient_kernel<true><<<blocks, kThreads, 0, st>>>(a);
-    WINDQ_CUDA(ctx, cudaGetLastError());
-  }
-  gate_gradient_kernel<false><<<blocks, kThreads, 0, st>>>(a);
-  WINDQ_CUDA(ctx, cudaGetLastError());
+  GateArgs a = {gate, up, dH, T, ldg, lddh, half, (int)F, dtype, activation, D, dtype == WINDQ_F16 ? top : nullptr, top + 64};
+  if (a.top) WINDQ_TRY(launch_gate_gradient<true>(ctx, a, st));
+  WINDQ_TRY(launch_gate_gradient<false>(ctx, a, st));
   if (dX) {
     Product q = {kInputGrad, dtype, 0, T, C, F, D, 2 * half, {Wg, Wu}, {ldwg, ldwu}, half, nullptr, {nullptr, nullptr}, a.top,
-                 {dX, nullptr, nullptr}, {lddx, 0, 0}};
+                 {dX, nullptr, nullptr}, {lddx, 0, 0}, partials};
     WINDQ_TRY(launch_product(ctx, q, st));
   }
-  if (dWg) {
-    Product q = {kWeightGrad, dtype, 0, F, C, T, D, 2 * half, {X, nullptr}, {ldx, 0}, half, nullptr, {nullptr, nullptr}, a.top,
-                 {dWg, dWu, nullptr}, {lddw, lddw, 0}};
-    WINDQ_TRY(launch_product(ctx, q, st));
-  }
+  if (dWg) WINDQ_TRY(launch_weight_gradient(ctx, WeightGradient{dtype, T, F, C, half, D, X, ldx, a.top, dWg, dWu, lddw}, st));
   return WINDQ_OK;
 }
 

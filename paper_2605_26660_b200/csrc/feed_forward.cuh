@@ -26,28 +26,45 @@ __device__ __forceinline__ float gradient_power(uint32_t top, int sign) {
   return __uint_as_float((uint32_t)(127 + sign * shift) << 23);
 }
 
-// The products of the feed-forward calls.  D(m, n) = sum_k A(m, k) B(n, k), operands by what they are:
-//   kInt8        codes of tokens x codes of a weight: O = D * row_scale[m] * col_scale[n]
-//   kInt8Gated   two weights: O = act(g) u with g, u as above
+// Tokens times weights, D(t, n) = sum_k X[t][k] W(n, k), and what follows:
+//   kInt8        codes of tokens x codes of a weight: O = D * row_scale[t] * col_scale[n]
+//   kInt8Gated   two weights: O = act(g) u, with g and u such products
 //   kGated       the same of 16-bit tokens and weights; optionally g and u are stored too
-//   kInputGrad   dX: tokens' [dG | dU] x the two weights, transposed
-//   kWeightGrad  dWg, dWu: [dG | dU], transposed, x tokens, transposed
-enum ProductKind { kInt8, kInt8Gated, kGated, kInputGrad, kWeightGrad };
+//   kInputGrad   dX: [dG | dU] of the tokens x the two weights, transposed: W(n, k) = W[k][n]
+enum ProductKind { kInt8, kInt8Gated, kGated, kInputGrad };
 
 struct Product {
   int kind, dtype, act;
-  int64_t M, N, K;        // rows and columns of an output, and the sum; kInputGrad: K of each of its two halves
-  const void* A;          // tokens (kWeightGrad: [K][2 * half])
-  int64_t lda;
-  const void* B[2];       // weights (kWeightGrad: tokens [K][N])
-  int64_t ldb[2];
-  int64_t half;           // columns of each half of [dG | dU], a multiple of 64
+  int64_t T, N, K;        // tokens, outputs, length of the sum (kInputGrad: of each of its two halves)
+  const void* X;
+  int64_t ldx;
+  const void* W[2];
+  int64_t ldw[2];
+  int64_t half;           // kInputGrad: columns of each half of [dG | dU], a multiple of 64
   const float* row_scale;
   const float* col_scale[2];
   const uint32_t* top;    // fp16 gradients: see gradient_power; nullable
-  void* O[3];             // the output (kWeightGrad: two); kGated: also g and u, nullable
+  void* O[3];             // the output; kGated: nullable, and g and u, nullable
   int64_t ldo[3];
+  void* partials;         // product_scratch(T) bytes
 };
 windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st);
+int64_t product_scratch(int64_t T);
+// The same for up to so many tokens: see product_few.cu.
+constexpr int64_t kFewTokensMost = 64;
+windq_status launch_few_tokens(windq_ctx* ctx, const Product& q, cudaStream_t st);
+
+// dWg = dG^T X, dWu = dU^T X from D = [dG | dU], [T][2 * half].
+struct WeightGradient {
+  int dtype;
+  int64_t T, F, C, half;
+  const void* D;
+  const void* X;
+  int64_t ldx;
+  const uint32_t* top;
+  void *dWg, *dWu;
+  int64_t ldw;
+};
+windq_status launch_weight_gradient(windq_ctx* ctx, const WeightGradient& q, cudaStream_t st);
 
 }  // namespace windq

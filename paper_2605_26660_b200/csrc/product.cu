@@ -1,18 +1,22 @@
-// The matrix products of the feed-forward calls on the tensor cores (tcgen05, accumulators in tensor memory, operands by
+// Tokens times the weights of a feed-forward block on the tensor cores (tcgen05, accumulators in tensor memory, operands by
 // TMA), with what follows a product done on its accumulators: scales of codes, the gate, the rounding.
 //
-// Warps: one issues TMA copies, one issues matrix products, four read the accumulators and store.  Two layouts of a tile:
-//   wide  256 rows x up to 256 columns on a pair of thread blocks (cta_group::2: each holds half of either operand, so that a
-//         block's shared memory feeds a product twice as large); persistent over tiles with two accumulators, so that storing
-//         a tile overlaps the next
-//   tall  (few tokens) 128 outputs x up to 256 tokens: the weight is read once and the tokens cost little -- the shape of
-//         decoding, bound by the bytes of the weight
-// A gated tile has both products of the same outputs: half of its weight rows are the gate's, half the other's.  In a wide
-// tile the two blocks of a pair hold one each, and a row's two accumulators are columns c and c + block_cols; in a tall one
-// they are lanes n and n + 64.
+// A tile is 256 rows of weights x up to 256 tokens on a pair of thread blocks (cta_group::2: each holds half of either operand, so
+// that a block's shared memory feeds a product twice as large).  The weights are the rows of the accumulators and the tokens their
+// columns because the tokens are what is ragged: a tile takes as many as there are, in steps of 32, where rows come in 256.  A gated tile has both products of the same 128
+// outputs, 16 rows of one weight and 16 of the other in turns: a storing warp's 32 lanes hold g and u of 16 outputs, and read as
+// 16 x 8 fragments a thread has both in its registers.
 //
-// Where the tiles do not fill the GPU, `splits` thread blocks (a cluster) share a tile along K and add their accumulators
-// through distributed shared memory, in rank order: equal calls give equal bits.
+// Outputs leave transposed, [token][output]: fragments go to shared memory by stmatrix.trans and on by TMA.
+//
+// Persistent over tiles with two accumulators, so that storing a tile overlaps the next.  What does not come out even -- the last
+// one to two rounds of tiles over the GPU, or all of them where they do not fill it -- is cut along K into equal shares, one a pair,
+// where that saves more than it costs.  The pieces of a tile then go to scratch memory, and a second kernel adds them, in order, and
+// finishes the tile: nobody waits for another, and equal calls give equal bits.  (Tiles shared by a cluster, with sums through
+// distributed shared memory, came out slower: clusters of eight whole SMs fill few of a GPC's; one block adding all of a tile's
+// pieces, too: 100 tokens x 1024 x 4096 codes 19.5 us.)
+//
+// Warps: one issues TMA copies, one issues matrix products, four read the accumulators and store.
 #include <algorithm>
 
 #include "feed_forward.cuh"
@@ -22,25 +26,30 @@ namespace windq {
 namespace {
 
 constexpr int kThreads = 192;
-constexpr int kMaxStages = 8;
-constexpr int kSmemLimit = 227 * 1024 - 2048;      // dynamic shared memory of one thread block per SM
-constexpr int kSmemLimitTwo = 112 * 1024;          // of two
-constexpr int kTallPitch = 132, kWidePitch = 260;  // sums of a tile, 32 bits each, rows free of bank conflicts
-constexpr int kStaging = 4 * 2 * 4096;             // of the four storing warps of a wide tile
-constexpr int kChunkBytes = 128;                   // of K: 64 16-bit values or 128 codes
+constexpr int kMaxStages = 12;
+constexpr int kSmemLimit = 227 * 1024 - 2048;  // dynamic shared memory of one thread block per SM
+constexpr int kChunkBytes = 128;               // of K: 64 16-bit values or 128 codes
+constexpr int kWeightBytes = 128 * kChunkBytes;
+constexpr int kBoxBytes = 64 * 128;            // of a store: up to 64 tokens x 64 outputs
+constexpr int kBoxes = 4;                      // two turns of two (gated and stored g, u: two turns of three)
+constexpr int kBoxesSaved = 6;
+constexpr int kMaxPairs = 74;
+constexpr int kLeastShare = 4;                 // chunks of K a pair, where tiles are cut
 
 struct Args {
-  int M, N, dtype, act;
-  int chunks, half_chunks;         // of K; of the first weight (kInputGrad)
-  int block_rows, block_cols;      // of a thread block: wide 128 rows x half of the columns; tall tokens x weight rows of a box
-  int row_tiles, col_tiles, group;
-  int half_tiles, half;            // kWeightGrad: row tiles of the first output, columns of each half of A
-  int splits, stages, accumulators, columns;  // columns: of tensor memory
+  int T, N, dtype, act;
+  int chunks, half_chunks;      // of K; of the first weight (kInputGrad)
+  int tokens;                   // of a tile
+  int token_tiles, weight_tiles, group;
+  int whole_tiles;              // dealt out; the tiles after them are cut
+  int pairs;                    // that the cut ones are cut for
+  int stages;
   const float* row_scale;
   const float* col_scale[2];
   const uint32_t* top;
   void* O[3];
   int64_t ldo[3];
+  uint32_t* partials;
   Stalls stalls;
 };
 
@@ -51,19 +60,58 @@ struct Barriers {
 template <int KIND>
 struct Kind {
   static constexpr bool kCodes = KIND == kInt8 || KIND == kInt8Gated, kGate = KIND == kInt8Gated || KIND == kGated;
-  static constexpr bool kTransA = KIND == kWeightGrad, kTransB = KIND == kInputGrad || KIND == kWeightGrad;
+  static constexpr bool kTransposed = KIND == kInputGrad;
   static constexpr int kStepK = kCodes ? 128 : 64;  // values of a chunk
 };
 
-// Tiles in an order that keeps a group of row tiles in L2 while the columns stream by.
-__device__ __forceinline__ void tile_at(const Args& p, int tile, int& rt, int& ct) {
-  const int per = p.group * p.col_tiles, g = tile / per, rest = tile - g * per;
-  const int rows = min(p.group, p.row_tiles - g * p.group);
-  ct = rest / rows;
-  rt = g * p.group + rest - ct * rows;
+// Tiles in an order that keeps a group of token tiles in L2 while the weights stream by.
+__device__ __forceinline__ void tile_at(const Args& p, int tile, int& tt, int& wt) {
+  const int per = p.group * p.weight_tiles, g = tile / per, rest = tile - g * per;
+  const int rows = min(p.group, p.token_tiles - g * p.group);
+  wt = rest / rows;
+  tt = g * p.group + rest - wt * rows;
 }
 
-__device__ __forceinline__ float scale_of(const float* s, int i, int n) { return i < n ? __ldg(s + i) : 0.0f; }
+// The cut tiles as units of a chunk of a tile, tile by tile: where the share of pair i begins.
+__device__ __forceinline__ int share(const Args& p, int i) {
+  return (int)((int64_t)(p.token_tiles * p.weight_tiles - p.whole_tiles) * p.chunks * i / p.pairs);
+}
+// Where a pair's piece lies: its share has at most two, the first, and one that begins a tile later.  As the threads hold it: 32
+// tokens as eight times 16 bytes a lane of the accumulators.
+__device__ __forceinline__ uint32_t* piece_of(const Args& p, int pair, int later, int me) {
+  return p.partials + ((int64_t)(2 * pair + later) * 2 + me) * p.tokens * 128;
+}
+
+// What a pair does, in order; every warp walks through the same.
+struct Walk {
+  const Args& p;
+  const int pair, pairs;
+  int begin, at, end, next_tile;  // of its share of units; the next of its whole tiles
+  int tile, c0, c1;               // now
+  __device__ explicit Walk(const Args& p) : p(p), pair(blockIdx.x >> 1), pairs(gridDim.x >> 1) {
+    next_tile = pair;
+    at = begin = share(p, min(pair, p.pairs));
+    end = share(p, min(pair + 1, p.pairs));
+  }
+  __device__ __forceinline__ bool next() {
+    if (next_tile < p.whole_tiles) {
+      tile = next_tile;
+      next_tile += pairs;
+      c0 = 0;
+      c1 = p.chunks;
+      return true;
+    }
+    if (at >= end) return false;
+    const int k = at / p.chunks;
+    tile = p.whole_tiles + k;
+    c0 = at - k * p.chunks;
+    c1 = min(p.chunks, end - k * p.chunks);
+    at += c1 - c0;
+    return true;
+  }
+  __device__ __forceinline__ bool later() const { return (tile - p.whole_tiles) * p.chunks + c0 != begin; }
+};
+
 // What an accumulator stands for.
 template <bool CODES>
 __device__ __forceinline__ float value_of(uint32_t acc, float row, float col) {
@@ -71,116 +119,149 @@ __device__ __forceinline__ float value_of(uint32_t acc, float row, float col) {
   return __uint_as_float(acc) * row;
 }
 __device__ __forceinline__ float gated(float g, float u, int act) { return g * logistic(gate_exponent(g, act)) * u; }
+// The four storing warps.
+__device__ __forceinline__ void barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-// Sums over the n blocks of ranks first, first + stride, ... of U quads at base + offset[u] in each, in that order.  Distributed
-// shared memory answers after the better part of a microsecond: the loads of up to four blocks are in flight together.
-template <int U, bool CODES>
-__device__ __forceinline__ void sum_quads(uint32_t base, const uint32_t (&offset)[U], int n, int first, int stride, uint32_t (&x)[U][4]) {
-  if (n == 1) {
+// 16 lanes x 32 columns of accumulators: of every 8 columns a thread has lanes t / 4 and t / 4 + 8, columns 2 (t % 4) and the next.
+__device__ __forceinline__ void tmem_load_fragments(uint32_t addr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+}
+// 16 outputs x 32 tokens as fragments x to a box in shared memory, [token][64 outputs] with the 128-byte swizzle: tokens from c
+// on, outputs from 8 * chunk on.
+__device__ __forceinline__ void put_fragments(uint32_t box, int c, int chunk, int lane, int dtype, const float (&x)[16]) {
 #pragma unroll
-    for (int u = 0; u < U; u++)
-      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(x[u][0]), "=r"(x[u][1]), "=r"(x[u][2]), "=r"(x[u][3])
-                   : "r"(base + offset[u])
-                   : "memory");
+  for (int h = 0; h < 2; h++) {
+    uint32_t w[4];
+#pragma unroll
+    for (int m = 0; m < 4; m++) w[m] = pack2(x[8 * h + 2 * m], x[8 * h + 2 * m + 1], dtype);
+    const int token = c + 16 * h + 8 * (lane >> 4) + (lane & 7), at = chunk + ((lane >> 3) & 1);
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(box + token * 128 + ((at ^ (token & 7)) << 4)),
+                 "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                 : "memory");
+  }
+}
+// A box of finished values to O: outputs n0 .. n0 + 63, tokens t0 .. t0 + live - 1; by the storing threads, of whom the first issues.
+__device__ __forceinline__ void send_box(const Args& p, uint32_t box, int k, const CUtensorMap* map, int n0, int t0, int live, int thread) {
+  if (n0 + 64 <= p.N || p.N % 8 == 0) {
+    if (thread == 0 && n0 < p.N) {
+      tma_store_2d(map, n0, t0, box);
+      if (live > 32) tma_store_2d(map, n0, t0 + 32, box + 32 * 128);
+    }
     return;
   }
-  uint32_t y[4][U][4];
-#pragma unroll
-  for (int q = 0; q < 4; q++) {
-    if (q < n) {
-      const uint32_t from = cluster_addr(base, first + q * stride);
-#pragma unroll
-      for (int u = 0; u < U; u++)
-        asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(y[q][u][0]), "=r"(y[q][u][1]), "=r"(y[q][u][2]), "=r"(y[q][u][3])
-                     : "r"(from + offset[u])
-                     : "memory");
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < U; u++)
-#pragma unroll
-    for (int k = 0; k < 4; k++) {
-      x[u][k] = y[0][u][k];
-#pragma unroll
-      for (int q = 1; q < 4; q++)
-        if (q < n) x[u][k] = CODES ? x[u][k] + y[q][u][k] : __float_as_uint(__uint_as_float(x[u][k]) + __uint_as_float(y[q][u][k]));
-    }
-}
-
-// Four neighbouring values of an output row, the last of which may lie beyond its end.
-__device__ __forceinline__ void store_quad(void* O, int64_t ldo, int64_t m, int n, int N, int dtype, const float (&v)[4]) {
-  uint16_t* out = static_cast<uint16_t*>(O) + m * ldo + n;
-  if (n + 4 <= N) {
-    *reinterpret_cast<uint2*>(out) = make_uint2(pack2(v[0], v[1], dtype), pack2(v[2], v[3], dtype));
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; k++)
-      if (n + k < N) store1(out, k, dtype, v[k]);
+  // not by TMA: a box that ends in the middle of 16 bytes, which the copy would write whole
+  const int n = n0 + (thread & 63);
+  for (int i = thread >> 6; i < min(live, 64); i += 2) {
+    uint16_t v;
+    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(box + i * 128 + ((((thread & 63) >> 3) ^ (i & 7)) << 4) + (thread & 7) * 2) : "memory");
+    if (n < p.N) static_cast<uint16_t*>(p.O[k])[(t0 + i) * p.ldo[k] + n] = v;
   }
 }
 
-// Adds the sums of a tile's splits, which lie as [row][column] in the shared memory of their blocks, and stores this block's
-// share of the rows: those of local index split, split + splits, ...
-template <int KIND, bool TALL>
-__device__ __forceinline__ void join(const Args& p, uint32_t base, int rt, int ct, int split, int me) {
+// 32 tokens of a warp's accumulators, from column d on: 16 lanes, and the 16 others.
+__device__ __forceinline__ void load_unit(uint32_t d, uint32_t (&r)[2][16]) {
+  tmem_load_fragments(d, r[0]);
+  tmem_load_fragments(d + (16u << 16), r[1]);
+}
+template <bool CODES>
+__device__ __forceinline__ void add_quad(uint32_t* x, const uint4& y) {
+  const uint32_t v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+  for (int e = 0; e < 4; e++) x[e] = CODES ? x[e] + v[e] : __float_as_uint(__uint_as_float(x[e]) + __uint_as_float(v[e]));
+}
+
+// What is done with whole sums, by the four storing warps.
+template <int KIND>
+struct Finish {
   using K = Kind<KIND>;
-  constexpr int pitch = TALL ? kTallPitch : kWidePitch, U = K::kGate ? 2 : 4;
-  const int outputs = TALL ? (K::kGate ? 64 : 128) : (K::kGate ? 1 : 2) * p.block_cols, quads = outputs / 4;
-  const bool second = KIND == kWeightGrad && rt >= p.half_tiles;
-  if (second) rt -= p.half_tiles;
-  const int m0 = TALL ? rt * p.block_rows : (rt * 2 + me) * 128, n0 = ct * outputs;
-  const int rows = min(TALL ? p.block_rows : 128, p.M - m0);
-  const int items = max(0, (rows - split + p.splits - 1) / p.splits) * quads;
-  const int shift = (TALL ? 64 : p.block_cols) * 4;  // bytes from g to u
-  const float unscale = p.top ? gradient_power(*p.top, -1) : 1.0f;
-  for (int i = threadIdx.x; i < items; i += U * kThreads) {
-    uint32_t offset[U], x[U][4], y[U][4];
+  const Args& p;
+  const CUtensorMap *omap0, *omap1, *omap2;
+  const uint32_t boxes;
+  const int thread, lane, quarter;
+  const bool saved, wanted;
+  const float unscale;
+  uint32_t phase = 0;  // which half of the boxes
+  int n0, t0, tokens;  // of the tile
+  float col[2][2];
+  __device__ Finish(const Args& p, const CUtensorMap* o0, const CUtensorMap* o1, const CUtensorMap* o2, uint32_t boxes, int first)
+      : p(p), omap0(o0), omap1(o1), omap2(o2), boxes(boxes), thread(threadIdx.x - first), lane(threadIdx.x & 31), quarter((threadIdx.x >> 5) & 3),
+        saved(KIND == kGated && p.O[1]), wanted(KIND != kGated || p.O[0]), unscale(p.top ? gradient_power(*p.top, -1) : 1.0f) {}
+  __device__ __forceinline__ void open(int tile, int me) {
+    int tt, wt;
+    tile_at(p, tile, tt, wt);
+    t0 = tt * p.tokens;
+    tokens = min(p.tokens, p.T - t0);
+    n0 = (2 * wt + me) * (K::kGate ? 64 : 128);
+    // the thread's rows: two of each half of the warp's lanes, outputs 8 apart; gated, the halves are the two weights' same outputs
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int q = min(i + u * kThreads, items - 1);
-      offset[u] = (uint32_t)((split + q / quads * p.splits) * pitch + q % quads * 4) * 4;
-    }
-    sum_quads<U, K::kCodes>(base, offset, p.splits, me, TALL ? 1 : 2, x);
-    if (K::kGate) {
+    for (int h = 0; h < 2; h++)
 #pragma unroll
-      for (int u = 0; u < U; u++) offset[u] += shift;
-      sum_quads<U, K::kCodes>(base, offset, p.splits, me, TALL ? 1 : 2, y);
-    }
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int q = i + u * kThreads, m = m0 + split + q / quads * p.splits, n = n0 + q % quads * 4;
-      if (q >= items || n >= p.N) continue;
-      const float row = K::kCodes ? __ldg(p.row_scale + m) : unscale;
-      float a[4], b[4], h[4];
-#pragma unroll
-      for (int k = 0; k < 4; k++) {
-        a[k] = value_of<K::kCodes>(x[u][k], row, K::kCodes ? scale_of(p.col_scale[0], n + k, p.N) : 1.0f);
-        if (K::kGate) {
-          b[k] = value_of<K::kCodes>(y[u][k], row, K::kCodes ? scale_of(p.col_scale[1], n + k, p.N) : 1.0f);
-          h[k] = gated(a[k], b[k], p.act);
-        }
+      for (int e = 0; e < 2; e++) {
+        const int n = n0 + (K::kGate ? quarter * 16 : quarter * 32 + h * 16) + e * 8 + (lane >> 2);
+        col[h][e] = K::kCodes && n < p.N ? __ldg(p.col_scale[K::kGate ? h : 0] + n) : 0.0f;
       }
+  }
+  // `units` times 32 tokens of the tile from c on.
+  template <int UNITS>
+  __device__ __forceinline__ void put(const uint32_t (&r)[UNITS][2][16], int c, int units) {
+    const uint32_t turn = boxes + phase * (saved ? 3 : 2) * kBoxBytes;
+    phase ^= 1;
+#pragma unroll
+    for (int u = 0; u < UNITS; u++) {
+      if (u >= units) break;
+      float row[8], x[2][16];
+#pragma unroll
+      for (int k = 0; k < 8; k++) {
+        const int t = t0 + c + u * 32 + (k >> 1) * 8 + (lane & 3) * 2 + (k & 1);
+        row[k] = K::kCodes ? (t < p.T ? __ldg(p.row_scale + t) : 0.0f) : unscale;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int k = 0; k < 16; k++) x[h][k] = value_of<K::kCodes>(r[u][h][k], row[(k >> 2) * 2 + (k & 1)], col[h][(k >> 1) & 1]);
       if (K::kGate) {
-        if (KIND != kGated || p.O[0]) store_quad(p.O[0], p.ldo[0], m, n, p.N, p.dtype, h);
-        if (KIND == kGated && p.O[1]) {
-          store_quad(p.O[1], p.ldo[1], m, n, p.N, p.dtype, a);
-          store_quad(p.O[2], p.ldo[2], m, n, p.N, p.dtype, b);
+        if (saved) {
+          put_fragments(turn + kBoxBytes, u * 32, quarter * 2, lane, p.dtype, x[0]);
+          put_fragments(turn + 2 * kBoxBytes, u * 32, quarter * 2, lane, p.dtype, x[1]);
+        }
+        if (wanted) {
+#pragma unroll
+          for (int k = 0; k < 16; k++) x[0][k] = gated(x[0][k], x[1][k], p.act);
+          put_fragments(turn, u * 32, quarter * 2, lane, p.dtype, x[0]);
         }
       } else {
-        store_quad(p.O[second], p.ldo[second], m, n, p.N, p.dtype, a);
+#pragma unroll
+        for (int h = 0; h < 2; h++) put_fragments(turn + (quarter >> 1) * kBoxBytes, u * 32, (quarter & 1) * 4 + h * 2, lane, p.dtype, x[h]);
       }
     }
+    fence_async_shared();
+    if (thread == 0) tma_store_wait<0>();  // of the boxes of the turn before, which the next one writes
+    barrier();
+    const int t = t0 + c, live = min(tokens - c, units * 32);
+    if (K::kGate) {
+      if (wanted) send_box(p, turn, 0, omap0, n0, t, live, thread);
+      if (saved) {
+        send_box(p, turn + kBoxBytes, 1, omap1, n0, t, live, thread);
+        send_box(p, turn + 2 * kBoxBytes, 2, omap2, n0, t, live, thread);
+      }
+    } else {
+      send_box(p, turn, 0, omap0, n0, t, live, thread);
+      send_box(p, turn + kBoxBytes, 0, omap0, n0 + 64, t, live, thread);
+    }
+    if (thread == 0) tma_store_commit();
   }
-}
+};
 
 template <int KIND>
 __global__ void __launch_bounds__(kThreads, 1)
-    wide_kernel(const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap0,
-                const __grid_constant__ CUtensorMap bmap1, const __grid_constant__ CUtensorMap omap0,
-                const __grid_constant__ CUtensorMap omap1, const __grid_constant__ CUtensorMap omap2,
-                const __grid_constant__ Args p) {
+    product_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap0,
+                   const __grid_constant__ CUtensorMap wmap1, const __grid_constant__ CUtensorMap omap0,
+                   const __grid_constant__ CUtensorMap omap1, const __grid_constant__ CUtensorMap omap2,
+                   const __grid_constant__ Args p) {
   using K = Kind<KIND>;
   extern __shared__ uint8_t raw[];
   __shared__ Barriers bars;
@@ -188,10 +269,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ int dead;
   const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
   const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_rank(), me = rank & 1, leader = rank & ~1u;
-  constexpr uint32_t a_bytes = 128 * kChunkBytes;
-  const int b_boxes = (p.block_cols + 63) / 64;  // of a transposed weight
-  const uint32_t b_bytes = K::kTransB ? b_boxes * 8192 : p.block_cols * kChunkBytes, stage_bytes = a_bytes + b_bytes;
+  const uint32_t me = cluster_rank();
+  const uint32_t stage_bytes = kWeightBytes + p.tokens / 2 * kChunkBytes;
   const uint32_t dead_ = smem_addr(&dead);
   auto full = [&](int s) { return smem_addr(&bars.full[s]); };
   auto empty = [&](int s) { return smem_addr(&bars.empty[s]); };
@@ -199,9 +278,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto free_ = [&](int b) { return smem_addr(&bars.free[b]); };
 
   if (threadIdx.x == 0) {
-    prefetch_map(&amap);
-    prefetch_map(&bmap0);
-    prefetch_map(&bmap1);
+    prefetch_map(&xmap);
+    prefetch_map(&wmap0);
+    prefetch_map(&wmap1);
     for (int s = 0; s < p.stages; s++) {
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
@@ -215,47 +294,41 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_async_shared();
   }
   __syncwarp();
-  if (warp == 1) tmem_alloc<true>(smem_addr(&tmem_slot), p.columns);
+  if (warp == 1) tmem_alloc<true>(smem_addr(&tmem_slot), 512);
   tc_fence_before();
   __syncthreads();
   cluster_sync();  // the other block's barriers are ready
   tc_fence_after();
   launch_dependents();  // tensor memory is in hand
   wait_for_predecessor();
-  const uint32_t tmem = tmem_slot;
-
-  const int team = 2 * p.splits;  // thread blocks of a tile
-  const int split = (blockIdx.x % team) / 2, step = gridDim.x / team, tiles = p.row_tiles * p.col_tiles;
-  const int c0 = (int)((int64_t)p.chunks * split / p.splits), c1 = (int)((int64_t)p.chunks * (split + 1) / p.splits);
+  const uint32_t tmem = tmem_slot, boxes = base + p.stages * stage_bytes;
 
   if (warp == 0) {
     Ring at(p.stages);
-    const uint32_t to = cluster_addr(full(0), leader);  // barriers of the issuing block
-    for (int tile = blockIdx.x / team; tile < tiles; tile += step) {
-      int rt, ct;
-      tile_at(p, tile, rt, ct);
-      const bool second = KIND == kWeightGrad && rt >= p.half_tiles;
-      const int m0 = (second ? p.half + (rt - p.half_tiles) * 256 : rt * 256) + me * 128;
-      const int n0 = K::kGate ? ct * p.block_cols : (ct * 2 + me) * p.block_cols;
-      for (int c = c0; c < c1; c++) {
+    const uint32_t to = cluster_addr(full(0), 0);  // barriers of the issuing block
+    for (Walk walk(p); walk.next();) {
+      int tt, wt;
+      tile_at(p, walk.tile, tt, wt);
+      const int t0 = tt * p.tokens + me * (p.tokens / 2), n0 = (2 * wt + me) * (K::kGate ? 64 : 128);
+      for (int c = walk.c0; c < walk.c1; c++) {
         mbar_wait(empty(at.s), at.phase ^ 1, dead_);
         const uint32_t dst = base + at.s * stage_bytes, bar = to + at.s * 8;
         if (elect_one() && !*(volatile int*)&dead) {
           if (me == 0) mbar_expect(full(at.s), 2 * stage_bytes);
-          if (K::kTransA) {
-            tma_load_2d<true>(dst, &amap, m0, c * 64, bar);
-            tma_load_2d<true>(dst + 8192, &amap, m0 + 64, c * 64, bar);
-          } else {
-            tma_load_2d<true>(dst, &amap, c * K::kStepK, m0, bar);
-          }
-          if (K::kTransB) {
-            const bool other = KIND == kInputGrad && c >= p.half_chunks;
+          if (K::kTransposed) {
+            const bool other = c >= p.half_chunks;
             const int k0 = (other ? c - p.half_chunks : c) * 64;
-            for (int b = 0; b < b_boxes; b++)
-              tma_load_2d<true>(dst + a_bytes + b * 8192, other ? &bmap1 : &bmap0, n0 + b * 64, k0, bar);
+            for (int b = 0; b < 2; b++) tma_load_2d<true>(dst + b * 8192, other ? &wmap1 : &wmap0, n0 + b * 64, k0, bar);
+          } else if (K::kGate) {
+#pragma unroll
+            for (int b = 0; b < 4; b++) {
+              tma_load_2d<true>(dst + b * 4096, &wmap0, c * K::kStepK, n0 + b * 16, bar);
+              tma_load_2d<true>(dst + b * 4096 + 2048, &wmap1, c * K::kStepK, n0 + b * 16, bar);
+            }
           } else {
-            tma_load_2d<true>(dst + a_bytes, K::kGate && me ? &bmap1 : &bmap0, c * K::kStepK, n0, bar);
+            tma_load_2d<true>(dst, &wmap0, c * K::kStepK, n0, bar);
           }
+          tma_load_2d<true>(dst + kWeightBytes, &xmap, c * K::kStepK, t0, bar);
         }
         __syncwarp();
         at.next();
@@ -263,434 +336,220 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == 1) {
     if (me == 0) {
-      const uint32_t idesc = K::kCodes ? instr_desc_i8(256, 2 * p.block_cols)
-                                       : instr_desc(p.dtype, K::kTransA, K::kTransB, 256, 2 * p.block_cols);
-      const uint32_t mask = 3u << leader;
+      const uint32_t idesc = K::kCodes ? instr_desc_i8(256, p.tokens) : instr_desc(p.dtype, K::kTransposed, false, 256, p.tokens);
       // a step of K further: 32 bytes in a K-major tile, two groups of 8 rows in an MN-major one
-      constexpr uint32_t a_step = (K::kTransA ? 2048 : 32) >> 4, b_step = (K::kTransB ? 2048 : 32) >> 4;
-      const uint64_t a_desc = smem_desc(base, K::kTransA ? 8192 : 16), b_desc = smem_desc(base + a_bytes, K::kTransB ? 8192 : 16);
+      constexpr uint32_t w_step = (K::kTransposed ? 2048 : 32) >> 4, x_step = 32 >> 4;
+      const uint64_t w_desc = smem_desc(base, K::kTransposed ? 8192 : 16), x_desc = smem_desc(base + kWeightBytes, 16);
       Ring at(p.stages);
       int turn = 0;
-      for (int tile = blockIdx.x / team; tile < tiles; tile += step, turn++) {
-        const int b = p.accumulators == 2 ? turn & 1 : 0, use = p.accumulators == 2 ? turn >> 1 : turn;
-        mbar_wait(free_(b), (use & 1) ^ 1, dead_);
+      for (Walk walk(p); walk.next(); turn++) {
+        const int b = turn & 1;
+        mbar_wait(free_(b), ((turn >> 1) & 1) ^ 1, dead_);
         tc_fence_after();
         const uint32_t d = tmem + b * 256;
-        for (int c = c0; c < c1; c++) {
+        for (int c = walk.c0; c < walk.c1; c++) {
           mbar_wait(full(at.s), at.phase, dead_);
           tc_fence_after();
           const uint64_t off = (uint64_t)(at.s * stage_bytes >> 4);
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < 4; k++) {
-              if (K::kCodes) mma_i8<true>(d, a_desc + off + k * a_step, b_desc + off + k * b_step, idesc, c > c0 || k > 0);
-              else mma_f16<true>(d, a_desc + off + k * a_step, b_desc + off + k * b_step, idesc, c > c0 || k > 0);
+              if (K::kCodes) mma_i8<true>(d, w_desc + off + k * w_step, x_desc + off + k * x_step, idesc, c > walk.c0 || k > 0);
+              else mma_f16<true>(d, w_desc + off + k * w_step, x_desc + off + k * x_step, idesc, c > walk.c0 || k > 0);
             }
-            mma_commit<true>(empty(at.s), mask);
+            mma_commit<true>(empty(at.s), 3);
           }
           __syncwarp();
           at.next();
         }
-        if (elect_one()) mma_commit<true>(done(b), mask);
+        if (elect_one()) mma_commit<true>(done(b), 3);
         __syncwarp();
       }
     }
   } else {
-    const int quarter = warp & 3, at = quarter * 32 + lane;
-    const uint32_t staging = base + p.stages * stage_bytes;
-    const float unscale = p.top ? gradient_power(*p.top, -1) : 1.0f;
-    uint32_t buffer = 0;
+    Finish<KIND> out(p, &omap0, &omap1, &omap2, boxes, 64);
     int turn = 0;
-    for (int tile = blockIdx.x / team; tile < tiles; tile += step, turn++) {
-      int rt, ct;
-      tile_at(p, tile, rt, ct);
-      const bool second = KIND == kWeightGrad && rt >= p.half_tiles;
-      if (second) rt -= p.half_tiles;
-      const int m0 = (rt * 2 + me) * 128, m = m0 + at, n0 = ct * (K::kGate ? 1 : 2) * p.block_cols;
-      const float row = K::kCodes ? scale_of(p.row_scale, m, p.M) : unscale;
-      const int b = p.accumulators == 2 ? turn & 1 : 0, use = p.accumulators == 2 ? turn >> 1 : turn;
-      const uint32_t d = tmem + b * 256 + ((uint32_t)(quarter * 32) << 16);
-      mbar_wait(done(b), use & 1, dead_);
+    for (Walk walk(p); walk.next(); turn++) {
+      const int b = turn & 1;
+      const uint32_t d = tmem + b * 256 + ((uint32_t)(out.quarter * 32) << 16);
+      out.open(walk.tile, me);
+      mbar_wait(done(b), (turn >> 1) & 1, dead_);
       tc_fence_after();
-      if (p.splits == 1) {
-        // 32 rows x 64 columns at a time through shared memory (128-byte swizzle, two buffers a warp) and out by TMA
-        const int outputs = (K::kGate ? 1 : 2) * p.block_cols;
-        // output 0 (h), 1 (g) or 2 (u); the plain kinds have one, of the accumulators at c
-        auto box = [&](int o, int c, void* O, int64_t ldo, const CUtensorMap* map) {
-          const uint32_t to = staging + ((quarter * 2 + buffer) * 32 + lane) * 128;
-          if (lane == 0) tma_store_wait<1>();
-          __syncwarp();
+      if (walk.c1 - walk.c0 == p.chunks) {
+        for (int c = 0; c < out.tokens; c += 64) {
+          const int units = c + 32 < out.tokens ? 2 : 1;
+          uint32_t r[2][2][16];
 #pragma unroll
-          for (int h = 0; h < 4; h++) {
-            uint32_t r[16], s[16], w[8];
-            if (!K::kGate || o != 2) tmem_load16(d + c + h * 16, r);
-            if (K::kGate && o != 1) tmem_load16(d + p.block_cols + c + h * 16, s);
-            tmem_load_wait();
-            float x[16];
-#pragma unroll
-            for (int k = 0; k < 16; k++) {
-              const int n = n0 + c + h * 16 + k;
-              if (!K::kGate) {
-                x[k] = value_of<K::kCodes>(r[k], row, K::kCodes ? scale_of(p.col_scale[0], n, p.N) : 1.0f);
-              } else {
-                const float g = o == 2 ? 0.0f : value_of<K::kCodes>(r[k], row, K::kCodes ? scale_of(p.col_scale[0], n, p.N) : 1.0f);
-                const float u = o == 1 ? 0.0f : value_of<K::kCodes>(s[k], row, K::kCodes ? scale_of(p.col_scale[1], n, p.N) : 1.0f);
-                x[k] = o == 1 ? g : o == 2 ? u : gated(g, u, p.act);
-              }
-            }
-#pragma unroll
-            for (int q = 0; q < 8; q++) w[q] = pack2(x[2 * q], x[2 * q + 1], p.dtype);
-#pragma unroll
-            for (int q = 0; q < 2; q++)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((h * 2 + q) ^ (lane & 7)) << 4)), "r"(w[4 * q]),
-                           "r"(w[4 * q + 1]), "r"(w[4 * q + 2]), "r"(w[4 * q + 3])
-                           : "memory");
-          }
-          fence_async_shared();
-          __syncwarp();
-          const int n = n0 + c;
-          // not by TMA: a box that ends in the middle of 16 bytes, which the copy would write whole
-          const bool whole = n + 64 <= p.N || p.N % 8 == 0;
-          if (lane == 0) {
-            if (whole && m0 + quarter * 32 < p.M && n < p.N) tma_store_2d(map, n, m0 + quarter * 32, staging + (quarter * 2 + buffer) * 4096);
-            tma_store_commit();
-          }
-          if (!whole && m < p.M) {
-            for (int g = 0; g < 8; g++) {
-              uint32_t v[4];
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                           : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                           : "r"(to + ((g ^ (lane & 7)) << 4))
-                           : "memory");
-              uint16_t* out = static_cast<uint16_t*>(O) + (int64_t)m * ldo + n + g * 8;
-              if (n + g * 8 + 8 <= p.N) {
-                *reinterpret_cast<uint4*>(out) = make_uint4(v[0], v[1], v[2], v[3]);
-              } else {
-                for (int k = 0; k < 8; k++)
-                  if (n + g * 8 + k < p.N) out[k] = (uint16_t)(v[k >> 1] >> (16 * (k & 1)));
-              }
-            }
-          }
-          buffer ^= 1;
-        };
-        for (int c = 0; c < outputs; c += 64) {
-          if (KIND == kGated) {
-            if (p.O[0]) box(0, c, p.O[0], p.ldo[0], &omap0);
-            if (p.O[1]) {
-              box(1, c, p.O[1], p.ldo[1], &omap1);
-              box(2, c, p.O[2], p.ldo[2], &omap2);
-            }
-          } else if (KIND == kWeightGrad) {
-            box(0, c, second ? p.O[1] : p.O[0], second ? p.ldo[1] : p.ldo[0], second ? &omap1 : &omap0);
-          } else {
-            box(0, c, p.O[0], p.ldo[0], &omap0);
-          }
+          for (int u = 0; u < 2; u++)
+            if (u < units) load_unit(d + c + u * 32, r[u]);
+          tmem_load_wait();
+          out.put(r, c, units);
         }
       } else {
-        for (int c = 0; c < 2 * p.block_cols; c += 16) {
-          uint32_t r[16];
-          tmem_load16(d + c, r);
+        uint32_t* piece = piece_of(p, walk.pair, walk.later(), me) + (out.quarter * 32 + lane) * 4;
+        for (int c = 0; c < out.tokens; c += 32) {
+          uint32_t r[2][16];
+          load_unit(d + c, r);
           tmem_load_wait();
 #pragma unroll
-          for (int k = 0; k < 16; k += 4)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + (at * kWidePitch + c + k) * 4), "r"(r[k]),
-                         "r"(r[k + 1]), "r"(r[k + 2]), "r"(r[k + 3])
-                         : "memory");
+          for (int k = 0; k < 8; k++) {
+            const uint32_t* x = &r[k >> 2][(k & 3) * 4];
+            __stcg(reinterpret_cast<uint4*>(piece + c * 128 + k * 512), make_uint4(x[0], x[1], x[2], x[3]));
+          }
         }
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) cluster_arrive(cluster_addr(free_(b), leader));
+      if (lane == 0) cluster_arrive(cluster_addr(free_(b), 0));
     }
-    if (lane == 0) tma_store_wait<0>();
+    if (out.thread == 0) tma_store_wait<0>();
   }
   __syncwarp();
   __syncthreads();
   if (dead) settle(p.stalls);
   __syncwarp();
-  cluster_sync();  // no more arrivals from other blocks; their sums are in shared memory
+  cluster_sync();  // no more arrivals from the other block
   if (warp == 1) {
     tc_fence_after();
-    tmem_free<true>(tmem, p.columns);
-  }
-  if (p.splits > 1) {
-    int rt, ct;
-    tile_at(p, blockIdx.x / team, rt, ct);  // one tile a team
-    join<KIND, false>(p, base, rt, ct, split, me);
-    __syncwarp();
-    cluster_sync();  // no block leaves while another reads its shared memory
+    tmem_free<true>(tmem, 512);
   }
 }
 
-// One tile (or, split, a part of its K) a thread block.
+// Adds the pieces of the cut tiles and finishes them: one block for 32 tokens of a block's half of a tile.
 template <int KIND>
-__global__ void __launch_bounds__(kThreads, 2)
-    tall_kernel(const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap0,
-                const __grid_constant__ CUtensorMap bmap1, const __grid_constant__ Args p) {
-  using K = Kind<KIND>;
-  extern __shared__ uint8_t raw[];
-  __shared__ Barriers bars;
-  __shared__ uint32_t tmem_slot;
-  __shared__ int dead;
-  const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
-  const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const uint32_t a_bytes = p.block_rows * kChunkBytes;
-  constexpr uint32_t b_bytes = 128 * kChunkBytes;
-  const uint32_t stage_bytes = a_bytes + b_bytes, dead_ = smem_addr(&dead), done = smem_addr(&bars.done[0]);
-  auto full = [&](int s) { return smem_addr(&bars.full[s]); };
-  auto empty = [&](int s) { return smem_addr(&bars.empty[s]); };
-
-  if (threadIdx.x == 0) {
-    prefetch_map(&amap);
-    prefetch_map(&bmap0);
-    prefetch_map(&bmap1);
-    for (int s = 0; s < p.stages; s++) {
-      mbar_init(full(s), 1);
-      mbar_init(empty(s), 1);
-    }
-    mbar_init(done, 1);
-    dead = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    fence_async_shared();
-  }
-  __syncwarp();
-  if (warp == 1) tmem_alloc<false>(smem_addr(&tmem_slot), p.columns);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  launch_dependents();  // tensor memory is in hand
+__global__ void __launch_bounds__(128)
+    combine_kernel(const __grid_constant__ CUtensorMap omap0, const __grid_constant__ CUtensorMap omap1,
+                   const __grid_constant__ CUtensorMap omap2, const __grid_constant__ Args p) {
+  __shared__ __align__(1024) uint8_t boxes[3 * kBoxBytes];
+  const int me = blockIdx.x & 1, cut = blockIdx.x >> 1, c = blockIdx.y * 32, s = cut * p.chunks;
+  launch_dependents();
   wait_for_predecessor();
-  const uint32_t tmem = tmem_slot;
-
-  const int split = blockIdx.x % p.splits;
-  const int c0 = (int)((int64_t)p.chunks * split / p.splits), c1 = (int)((int64_t)p.chunks * (split + 1) / p.splits);
-  int rt, ct;
-  tile_at(p, blockIdx.x / p.splits, rt, ct);
-
-  if (warp == 0) {
-    Ring at(p.stages);
-    const int m0 = rt * p.block_rows, n0 = ct * (K::kGate ? 64 : 128);
-    for (int c = c0; c < c1; c++) {
-      mbar_wait(empty(at.s), at.phase ^ 1, dead_);
-      const uint32_t dst = base + at.s * stage_bytes, bar = full(at.s);
-      if (elect_one() && !*(volatile int*)&dead) {
-        mbar_expect(bar, stage_bytes);
-        if (K::kTransB) {
-          const bool other = c >= p.half_chunks;
-          const int k0 = (other ? c - p.half_chunks : c) * 64;
-          tma_load_2d<false>(dst, other ? &bmap1 : &bmap0, n0, k0, bar);
-          tma_load_2d<false>(dst + 8192, other ? &bmap1 : &bmap0, n0 + 64, k0, bar);
-        } else {
-          tma_load_2d<false>(dst, &bmap0, c * K::kStepK, n0, bar);
-          tma_load_2d<false>(dst + 8192, K::kGate ? &bmap1 : &bmap0, c * K::kStepK, K::kGate ? n0 : n0 + 64, bar);
-        }
-        tma_load_2d<false>(dst + b_bytes, &amap, c * K::kStepK, m0, bar);
-      }
-      __syncwarp();
-      at.next();
-    }
-  } else if (warp == 1) {
-    const uint32_t idesc = K::kCodes ? instr_desc_i8(128, p.block_rows) : instr_desc(p.dtype, K::kTransB, false, 128, p.block_rows);
-    constexpr uint32_t w_step = (K::kTransB ? 2048 : 32) >> 4, t_step = 32 >> 4;
-    const uint64_t w_desc = smem_desc(base, K::kTransB ? 8192 : 16), t_desc = smem_desc(base + b_bytes, 16);
-    Ring at(p.stages);
-    for (int c = c0; c < c1; c++) {
-      mbar_wait(full(at.s), at.phase, dead_);
-      tc_fence_after();
-      const uint64_t off = (uint64_t)(at.s * stage_bytes >> 4);
-      if (elect_one()) {
+  Finish<KIND> out(p, &omap0, &omap1, &omap2, smem_addr(boxes), 0);
+  out.open(p.whole_tiles + cut, me);
+  int q = (int)((int64_t)p.pairs * cut / (p.token_tiles * p.weight_tiles - p.whole_tiles));  // near the pair that holds the first unit
+  while (share(p, q + 1) <= s) q++;
+  while (share(p, q) > s) q--;
+  if (share(p, q + 1) >= s + p.chunks || c >= out.tokens) return;  // one pair had all of it; or no such tokens
+  uint32_t r[1][2][16];
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
-          if (K::kCodes) mma_i8<false>(tmem, w_desc + off + k * w_step, t_desc + off + k * t_step, idesc, c > c0 || k > 0);
-          else mma_f16<false>(tmem, w_desc + off + k * w_step, t_desc + off + k * t_step, idesc, c > c0 || k > 0);
-        }
-        mma_commit<false>(empty(at.s), 0);
-      }
-      __syncwarp();
-      at.next();
-    }
-    if (elect_one()) mma_commit<false>(done, 0);
-    __syncwarp();
-  } else {
-    const int quarter = warp & 3, n = quarter * 32 + lane;
-    mbar_wait(done, 0, dead_);
-    tc_fence_after();
-    // as the result lies: [token][output], the outputs being the lanes; the copies and products of all stages have ended
-    for (int c = 0; c < p.block_rows; c += 16) {
-      uint32_t r[16];
-      tmem_load16(tmem + c + ((uint32_t)(quarter * 32) << 16), r);
-      tmem_load_wait();
+  for (int k = 0; k < 32; k++) r[0][k >> 4][k & 15] = 0;
+  bool more = true;
+  while (more) {
+    uint4 y[4][8];
+    int n = 0;
 #pragma unroll
-      for (int k = 0; k < 16; k++)
-        asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + ((c + k) * kTallPitch + n) * 4), "r"(r[k]) : "memory");
+    for (int i = 0; i < 4; i++) {
+      if (!more) break;
+      const int begin = share(p, q);
+      const uint4* from = reinterpret_cast<const uint4*>(piece_of(p, q, begin < s, me) + c * 128 + threadIdx.x * 4);
+#pragma unroll
+      for (int k = 0; k < 8; k++) y[i][k] = __ldcg(from + k * 128);
+      q++;
+      n++;
+      more = share(p, q) < s + p.chunks;
     }
-    tc_fence_before();
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      if (i < n) {
+#pragma unroll
+        for (int k = 0; k < 8; k++) add_quad<Kind<KIND>::kCodes>(&r[0][k >> 2][(k & 3) * 4], y[i][k]);
+      }
   }
-  __syncwarp();
-  __syncthreads();
-  if (dead) settle(p.stalls);
-  __syncwarp();
-  if (warp == 1) {  // given back before this block waits for its cluster
-    tc_fence_after();
-    tmem_free<false>(tmem, p.columns);
-  }
-  __syncwarp();
-  if (p.splits > 1) cluster_sync();
-  join<KIND, true>(p, base, rt, ct, split, 0);
-  if (p.splits > 1) {
-    __syncwarp();
-    cluster_sync();  // no block leaves while another reads its shared memory
-  }
+  out.put(r, c, 1);
+  if (out.thread == 0) tma_store_wait<0>();
 }
 
-void configure(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attrs)[2], int blocks, int cluster, int smem, cudaStream_t st) {
-  cfg.gridDim = dim3((unsigned)blocks);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attrs[0].val.programmaticStreamSerializationAllowed = 1;
-  attrs[1].id = cudaLaunchAttributeClusterDimension;
-  attrs[1].val.clusterDim.x = cluster;
-  attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
-  cfg.attrs = attrs;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
+// Tokens of a tile: as few tiles as there can be, of equal size.
+int tile_tokens(int64_t T) {
+  const int64_t tiles = std::max<int64_t>(1, (T + 255) / 256);
+  return (int)std::max<int64_t>(round_up((T + tiles - 1) / tiles, 32), 32);
 }
 
 template <int KIND>
-windq_status launch_wide(windq_ctx* ctx, const CUtensorMap& a, const CUtensorMap (&b)[2], const CUtensorMap (&o)[3], const Args& p,
-                         int blocks, int smem, cudaStream_t st) {
-  const windq_status ready = prepare_kernel(ctx, kProductWide + KIND, wide_kernel<KIND>, kThreads, kSmemLimit, false);
+windq_status launch(windq_ctx* ctx, const CUtensorMap& x, const CUtensorMap (&w)[2], const CUtensorMap (&o)[3], const Args& p, int blocks,
+                    int smem, cudaStream_t st) {
+  const windq_status ready = prepare_kernel(ctx, kProduct + KIND, product_kernel<KIND>, kThreads, kSmemLimit, false);
   if (ready != WINDQ_OK) return ready;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attrs[2];
-  configure(cfg, attrs, blocks, 2 * p.splits, smem, st);
-  WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, wide_kernel<KIND>, a, b[0], b[1], o[0], o[1], o[2], p));
-  return WINDQ_OK;
-}
-template <int KIND>
-windq_status launch_tall(windq_ctx* ctx, const CUtensorMap& a, const CUtensorMap (&b)[2], const Args& p, int blocks, int smem,
-                         cudaStream_t st) {
-  const windq_status ready = prepare_kernel(ctx, kProductTall + KIND, tall_kernel<KIND>, kThreads, kSmemLimit, false);
-  if (ready != WINDQ_OK) return ready;
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attrs[2];
-  configure(cfg, attrs, blocks, p.splits, smem, st);
-  WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, tall_kernel<KIND>, a, b[0], b[1], p));
+  overlapped_launch(cfg, attrs, blocks, kThreads, 2, smem, st);
+  WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, product_kernel<KIND>, x, w[0], w[1], o[0], o[1], o[2], p));
+  const int cut = p.token_tiles * p.weight_tiles - p.whole_tiles;
+  if (cut) {
+    cudaLaunchConfig_t second = {};
+    overlapped_launch(second, attrs, cut * 2, 128, 1, 0, st);
+    second.gridDim.y = (p.tokens + 31) / 32;
+    WINDQ_CUDA(ctx, cudaLaunchKernelEx(&second, combine_kernel<KIND>, o[0], o[1], o[2], p));
+  }
   return WINDQ_OK;
 }
 
 }  // namespace
 
+int64_t product_scratch(int64_t T) { return round_up((int64_t)kMaxPairs * 2 * 2 * tile_tokens(T) * 128 * 4, 256); }
+
 windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
+  if (q.T <= kFewTokensMost) return launch_few_tokens(ctx, q, st);
   const bool codes = q.kind == kInt8 || q.kind == kInt8Gated, gate = q.kind == kInt8Gated || q.kind == kGated;
-  const bool grad_w = q.kind == kWeightGrad, trans_b = q.kind == kInputGrad || grad_w;
-  const bool tall = !grad_w && q.M <= 320;
+  const bool transposed = q.kind == kInputGrad;
   const int step = codes ? 128 : 64;
   Args p = {};
-  p.M = (int)q.M;
+  p.T = (int)q.T;
   p.N = (int)q.N;
   p.dtype = q.dtype;
   p.act = q.act;
   p.half_chunks = (int)((q.K + step - 1) / step);
-  p.chunks = q.kind == kInputGrad ? 2 * p.half_chunks : p.half_chunks;
-  p.half = (int)q.half;
+  p.chunks = transposed ? 2 * p.half_chunks : p.half_chunks;
+  p.tokens = tile_tokens(q.T);
+  p.token_tiles = (int)((q.T + p.tokens - 1) / p.tokens);
+  const int outputs = gate ? 128 : 256;
+  p.weight_tiles = (int)((q.N + outputs - 1) / outputs);
+  p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.token_tiles, (48ll << 20) / ((int64_t)p.chunks * kChunkBytes * p.tokens)));
   p.row_scale = q.row_scale;
   p.top = q.top;
   for (int k = 0; k < 2; k++) p.col_scale[k] = q.col_scale[k];
   for (int k = 0; k < 3; k++) p.O[k] = q.O[k], p.ldo[k] = q.ldo[k];
+  p.partials = (uint32_t*)q.partials;
   p.stalls = stalls_of(ctx);
 
-  int smem, blocks;
-  if (tall) {
-    const int64_t tiles_of = std::max<int64_t>(1, (q.M + 255) / 256);
-    p.block_rows = (int)round_up((q.M + tiles_of - 1) / tiles_of, 16);
-    p.block_cols = 64;
-    p.row_tiles = (int)((q.M + p.block_rows - 1) / p.block_rows);
-    const int outputs = gate ? 64 : 128;
-    p.col_tiles = (int)((q.N + outputs - 1) / outputs);
-    const int64_t tiles = (int64_t)p.row_tiles * p.col_tiles;
-    auto splits_for = [&](int64_t slots) {
-      int splits = 1;
-      while (splits < 4 && tiles * splits * 2 <= slots && p.chunks >= splits * 2 * 4) splits *= 2;
-      return splits;
-    };
-    const bool two = p.block_rows * kTallPitch * 4 <= kSmemLimitTwo - 1024 &&
-                     (p.block_rows <= 64 || tiles * splits_for(ctx->sm_count) * 5 < ctx->sm_count * 4);
-    p.splits = splits_for((int64_t)ctx->sm_count * (two ? 2 : 1));
-    const int stage = (p.block_rows + 128) * kChunkBytes, limit = two ? kSmemLimitTwo : kSmemLimit;
-    p.stages = std::min(kMaxStages, (limit - 1024) / stage);
-    p.columns = p.block_rows <= 32 ? 32 : p.block_rows <= 64 ? 64 : p.block_rows <= 128 ? 128 : 256;
-    p.group = p.row_tiles;
-    blocks = (int)(tiles * p.splits);
-    smem = 1024 + std::max(p.stages * stage, p.block_rows * kTallPitch * 4);
-  } else {
-    p.block_rows = 128;
-    p.half_tiles = (int)((q.M + 255) / 256);
-    p.row_tiles = (grad_w ? 2 : 1) * p.half_tiles;
-    const int64_t slots = ctx->sm_count / 2;
-    // The width that takes the least time in rounds over the GPU (a chunk of K: 0.23 us at width 128, 0.27 at 192, 0.36 at 256;
-    // a tile 2 us more, 5 where it is split along K).  Tiles that fill less than half of the GPU are split.
-    int64_t best = INT64_MAX;
-    for (int cols = 128; cols >= 64; cols -= gate ? 64 : 32) {
-      const int64_t outputs = gate ? cols : 2 * cols, tiles = p.row_tiles * ((q.N + outputs - 1) / outputs);
-      int splits = 1;
-      while (splits < 4 && tiles * splits * 2 <= slots && p.chunks >= splits * 2 * 4) splits *= 2;
-      const int64_t waves = (tiles * splits + slots - 1) / slots;
-      const int width = 2 * cols, chunk = std::max(210 + width / 5, width * 139 / 100) * (1256 - width) / 1000;
-      const int64_t cost = waves * ((int64_t)(p.chunks + splits - 1) / splits * chunk + (splits > 1 ? 5000 : 2000));
-      if (cost < best) {
-        best = cost;
-        p.block_cols = cols;
-        p.splits = splits;
-      }
-    }
-    const int outputs = (gate ? 1 : 2) * p.block_cols;
-    p.col_tiles = (int)((q.N + outputs - 1) / outputs);
-    p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.row_tiles, (48ll << 20) / ((int64_t)p.chunks * kChunkBytes * 256)));
-    const int stage = 128 * kChunkBytes + (trans_b ? (p.block_cols + 63) / 64 * 8192 : p.block_cols * kChunkBytes);
-    const int staging = p.splits > 1 ? 0 : kStaging;
-    p.stages = std::min(kMaxStages, (kSmemLimit - 1024 - staging) / stage);
-    p.accumulators = p.splits == 1 ? 2 : 1;
-    p.columns = 256 * p.accumulators;
-    const int64_t tiles = (int64_t)p.row_tiles * p.col_tiles;
-    blocks = (int)(p.splits > 1 ? tiles * p.splits : std::min(tiles, slots)) * 2;
-    smem = 1024 + std::max(p.stages * stage + staging, p.splits > 1 ? 128 * kWidePitch * 4 : 0);
+  const int64_t tiles = (int64_t)p.token_tiles * p.weight_tiles, slots = std::min(ctx->sm_count / 2, kMaxPairs);
+  p.whole_tiles = (int)tiles;
+  p.pairs = (int)slots;
+  const int64_t pairs = std::min(tiles, slots), idle = (slots - tiles % slots) % slots;
+  int64_t blocks = pairs;
+  // Cutting saves the idle pairs' part of a tile and costs another kernel, about 4 us and 12 ns a token (a chunk of K takes 0.2 us
+  // for 32 tokens, 0.36 for 256).
+  if (idle * p.chunks * (170 + p.tokens * 3 / 4) > (4000 + 12 * p.tokens) * slots) {
+    p.whole_tiles = (int)(tiles > slots ? (tiles / slots - 1) * slots : 0);
+    p.pairs = (int)std::min(slots, std::max(pairs, tiles * p.chunks / kLeastShare));
+    blocks = p.pairs;
   }
+  const int stage = kWeightBytes + p.tokens / 2 * kChunkBytes, extra = (q.kind == kGated && q.O[1] ? kBoxesSaved : kBoxes) * kBoxBytes;
+  p.stages = std::min(kMaxStages, (kSmemLimit - 1024 - extra) / stage);
+  const int smem = kSmemLimit;  // all of it, whatever is used: no block that wants tensor memory fits beside this one
 
-  CUtensorMap a, b[2], o[3];
+  CUtensorMap x, w[2], o[3];
   WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
   const int type = codes ? -1 : q.dtype, bytes = codes ? 1 : 2;
-  bool ok;
-  if (grad_w) {
-    ok = make_map_2d(&a, type, q.A, 2 * q.half, q.K, q.lda * 2, 64) && make_map_2d(&b[0], type, q.B[0], q.N, q.K, q.ldb[0] * 2, 64);
-    b[1] = b[0];
-  } else {
-    const int b_rows = trans_b ? 64 : p.block_cols;
-    ok = make_map_2d(&a, type, q.A, q.kind == kInputGrad ? 2 * q.half : q.K, q.M, q.lda * bytes, p.block_rows);
-    for (int k = 0; ok && k < (q.B[1] ? 2 : 1); k++)
-      ok = make_map_2d(&b[k], type, q.B[k], trans_b ? q.N : q.K, trans_b ? q.K : q.N, q.ldb[k] * bytes, b_rows);
-    if (!q.B[1]) b[1] = b[0];
-  }
-  if (!tall) {
-    const CUtensorMap* any = nullptr;
-    for (int k = 0; ok && k < 3; k++) {
-      if (!q.O[k]) continue;
-      ok = make_map_2d(&o[k], q.dtype, q.O[k], q.N, q.M, q.ldo[k] * 2, 32);
-      any = &o[k];
-    }
-    for (int k = 0; ok && k < 3; k++)
-      if (!q.O[k]) o[k] = *any;  // not used
+  bool ok = make_map_2d(&x, type, q.X, transposed ? 2 * q.half : q.K, q.T, q.ldx * bytes, step, p.tokens / 2);
+  for (int k = 0; ok && k < (q.W[1] ? 2 : 1); k++)
+    ok = transposed ? make_map_2d(&w[k], type, q.W[k], q.N, q.K, q.ldw[k] * bytes, 64, 64)
+                    : make_map_2d(&w[k], type, q.W[k], q.K, q.N, q.ldw[k] * bytes, step, gate ? 16 : 128);
+  if (!q.W[1]) w[1] = w[0];
+  const CUtensorMap* any = nullptr;
+  for (int k = 0; ok && k < 3; k++) {
+    if (!q.O[k]) continue;
+    ok = make_map_2d(&o[k], q.dtype, q.O[k], q.N, q.T, q.ldo[k] * 2, 64, 32);
+    any = &o[k];
   }
   WINDQ_REQUIRE(ctx, ok, WINDQ_ERR_CUDA, "a tensor map could not be made");
+  for (int k = 0; k < 3; k++)
+    if (!q.O[k]) o[k] = *any;  // not used
   switch (q.kind) {
-    case kInt8: return tall ? launch_tall<kInt8>(ctx, a, b, p, blocks, smem, st) : launch_wide<kInt8>(ctx, a, b, o, p, blocks, smem, st);
-    case kInt8Gated:
-      return tall ? launch_tall<kInt8Gated>(ctx, a, b, p, blocks, smem, st) : launch_wide<kInt8Gated>(ctx, a, b, o, p, blocks, smem, st);
-    case kGated: return tall ? launch_tall<kGated>(ctx, a, b, p, blocks, smem, st) : launch_wide<kGated>(ctx, a, b, o, p, blocks, smem, st);
-    case kInputGrad:
-      return tall ? launch_tall<kInputGrad>(ctx, a, b, p, blocks, smem, st) : launch_wide<kInputGrad>(ctx, a, b, o, p, blocks, smem, st);
-    default: return launch_wide<kWeightGrad>(ctx, a, b, o, p, blocks, smem, st);
+    case kInt8: return launch<kInt8>(ctx, x, w, o, p, (int)blocks * 2, smem, st);
+    case kInt8Gated: return launch<kInt8Gated>(ctx, x, w, o, p, (int)blocks * 2, smem, st);
+    case kGated: return launch<kGated>(ctx, x, w, o, p, (int)blocks * 2, smem, st);
+    default: return launch<kInputGrad>(ctx, x, w, o, p, (int)blocks * 2, smem, st);
   }
 }
 
