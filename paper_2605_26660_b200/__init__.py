@@ -1230,11 +1230,6 @@ def _activation(name):
     return code
 
 
-def _handles(ctx, stream):
-    """What every function of the compiled binding takes first."""
-    return ctx._h.value, ctx.device, None if stream is None else stream.cuda_stream
-
-
 def windq_quantize_rows(ctx: Context, X: torch.Tensor, *, want_values: bool = False, out: dict | None = None, stream=None) -> dict:
     """8-bit codes of every row of X [T, C] (fp16 or bf16) with one scale a row: codes = round(127 X / a), scale = a / 127,
     a the row's largest magnitude.
@@ -1242,9 +1237,10 @@ def windq_quantize_rows(ctx: Context, X: torch.Tensor, *, want_values: bool = Fa
     Returns dict(codes int8 [T, C], whose rows are a multiple of 16 bytes apart, scale fp32 [T], values [T, C] of X's type
     | None: what the codes stand for).  ``out`` may hold preallocated tensors under the same keys."""
     given = out or {}
-    st, codes, scale, values = _binding.quantize_rows(*_handles(ctx, stream), X, want_values, given.get("codes"), given.get("scale"),
-                                                      given.get("values"))
-    ctx._check(st)
+    st, codes, scale, values = _binding.quantize_rows(ctx._h.value, ctx.device, stream, X, want_values, given.get("codes"),
+                                                      given.get("scale"), given.get("values"))
+    if st:
+        ctx._check(st)
     return {"codes": codes, "scale": scale, "values": values}
 
 
@@ -1254,8 +1250,9 @@ def windq_int8_forward(ctx: Context, codes: torch.Tensor, scale: torch.Tensor, w
 
     codes int8 [T, C], w_codes int8 [R, C] (rows a multiple of 16 bytes apart, as windq_quantize_rows leaves them); scale
     fp32 [T], w_scale fp32 [R].  Returns Y [T, R] of ``dtype``, fp16 or bf16 (``out`` if given, whose type counts)."""
-    st, out = _binding.int8_forward(*_handles(ctx, stream), codes, scale, w_codes, w_scale, dtype, out)
-    ctx._check(st)
+    st, out = _binding.int8_forward(ctx._h.value, ctx.device, stream, codes, scale, w_codes, w_scale, dtype, out)
+    if st:
+        ctx._check(st)
     return out
 
 
@@ -1264,9 +1261,10 @@ def windq_gated_int8_forward(ctx: Context, codes: torch.Tensor, scale: torch.Ten
                              dtype: torch.dtype = torch.float16, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """H = act(g) u with g and u as windq_int8_forward forms them from the two weights [F, C], before its rounding to 16
     bits.  Returns H [T, F] of ``dtype``, fp16 or bf16 (``out`` if given, whose type counts)."""
-    st, out = _binding.gated_int8_forward(*_handles(ctx, stream), codes, scale, wg_codes, wg_scale, wu_codes, wu_scale,
-                                          _activation(activation), dtype, out)
-    ctx._check(st)
+    st, out = _binding.gated_int8_forward(ctx._h.value, ctx.device, stream, codes, scale, wg_codes, wg_scale, wu_codes,
+                                          wu_scale, _activation(activation), dtype, out)
+    if st:
+        ctx._check(st)
     return out
 
 
@@ -1278,9 +1276,10 @@ def windq_gated_forward(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: tor
     Returns dict(h [T, F], gate, up [T, F] | None: both products, rounded, for windq_gated_backward).  ``out`` may hold
     preallocated tensors under the same keys.  Autograd records nothing: the gradients are windq_gated_backward's."""
     given = out or {}
-    st, h, gate, up = _binding.gated_forward(*_handles(ctx, stream), X, Wg, Wu, _activation(activation), want_saved, given.get("h"),
-                                             given.get("gate"), given.get("up"))
-    ctx._check(st)
+    st, h, gate, up = _binding.gated_forward(ctx._h.value, ctx.device, stream, X, Wg, Wu, _activation(activation), want_saved,
+                                             given.get("h"), given.get("gate"), given.get("up"))
+    if st:
+        ctx._check(st)
     return {"h": h, "gate": gate, "up": up}
 
 
@@ -1305,7 +1304,8 @@ def windq_gated_backward(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: to
     Returns dict(dx [T, C] | None, dWg, dWu [F, C] | None), of X's type, overwritten, not added to.  ``out`` may hold
     preallocated tensors under the same keys."""
     given = out or {}
-    st, dx, dWg, dWu = _binding.gated_backward(*_handles(ctx, stream), X, Wg, Wu, _activation(activation), dH, gate, up, want_dx, want_dw,
-                                               given.get("dx"), given.get("dWg"), given.get("dWu"))
-    ctx._check(st)
+    st, dx, dWg, dWu = _binding.gated_backward(ctx._h.value, ctx.device, stream, X, Wg, Wu, _activation(activation), dH, gate, up,
+                                               want_dx, want_dw, given.get("dx"), given.get("dWg"), given.get("dWu"))
+    if st:
+        ctx._check(st)
     return {"dx": dx, "dWg": dWg, "dWu": dWu}

@@ -90,8 +90,11 @@ struct Call {
       : ctx(reinterpret_cast<windq_ctx*>(a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]))), device((int)PyLong_AsLong(a[1])) {
     if (a[2] == Py_None) {
       stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
-    } else {
-      stream = PyLong_AsVoidPtr(a[2]);
+    } else {  // a torch.cuda.Stream
+      PyObject* handle = PyObject_GetAttrString(a[2], "cuda_stream");
+      if (!handle) throw python_error();
+      stream = PyLong_AsVoidPtr(handle);
+      Py_DECREF(handle);
     }
     if (PyErr_Occurred()) throw python_error();
   }

@@ -12,7 +12,7 @@ constexpr int kThreads = 256;
 struct GateArgs {
   const void *gate, *up, *dH;
   int64_t T, ldg, lddh, half;
-  int F, dtype, act;
+  int F, act;
   uint16_t* D;     // [T][2 * half]: dG, dU; columns of a half behind F are zeros
   uint32_t* top;   // fp16: bits of the largest |dG|, |dU|; bf16: NULL
   uint32_t* tops;  // of every block, before that
@@ -30,7 +30,7 @@ __device__ __forceinline__ void gate_gradient(float g, float u, float dh, int ac
 // Eight columns a thread, rows gridDim.y apart.  Bound by memory: 6 bytes read and 4 written a value.  fp16's range does not hold
 // what small losses leave, so its values are stored times a power of two (see gradient_power) that a launch with TOP finds
 // first: another 6 bytes read, 4 % of a long backward pass.
-template <bool TOP>
+template <int DT, bool TOP>
 __global__ void __launch_bounds__(kThreads) gate_gradient_kernel(const GateArgs p) {
   __shared__ uint32_t warps[kThreads / 32];
   auto most = [&](uint32_t x) {  // of the block, in every thread
@@ -59,13 +59,13 @@ __global__ void __launch_bounds__(kThreads) gate_gradient_kernel(const GateArgs 
     for (int64_t t = blockIdx.y; t < p.T; t += gridDim.y) {
       float g[8], u[8], dh[8], dg[8], du[8];
       if (live == 8) {
-        load8(p.gate, t * p.ldg + f, p.dtype, g);
-        load8(p.up, t * p.ldg + f, p.dtype, u);
-        load8(p.dH, t * p.lddh + f, p.dtype, dh);
+        load8(p.gate, t * p.ldg + f, DT, g);
+        load8(p.up, t * p.ldg + f, DT, u);
+        load8(p.dH, t * p.lddh + f, DT, dh);
       } else {
-        load_some(p.gate, t * p.ldg + f, p.dtype, live, g);
-        load_some(p.up, t * p.ldg + f, p.dtype, live, u);
-        load_some(p.dH, t * p.lddh + f, p.dtype, live, dh);
+        load_some(p.gate, t * p.ldg + f, DT, live, g);
+        load_some(p.up, t * p.ldg + f, DT, live, u);
+        load_some(p.dH, t * p.lddh + f, DT, live, dh);
       }
 #pragma unroll
       for (int k = 0; k < 8; k++) {
@@ -78,8 +78,8 @@ __global__ void __launch_bounds__(kThreads) gate_gradient_kernel(const GateArgs 
         }
       }
       if (!TOP) {
-        store8(p.D, t * 2 * p.half + f, p.dtype, dg);
-        store8(p.D, t * 2 * p.half + p.half + f, p.dtype, du);
+        store8(p.D, t * 2 * p.half + f, DT, dg);
+        store8(p.D, t * 2 * p.half + p.half + f, DT, du);
       }
     }
   }
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kThreads) gate_gradient_kernel(const GateArgs 
 
 constexpr int kMostBlocks = 2048;  // of the kernel above
 constexpr int64_t kTopBytes = 256 + 4 * kMostBlocks;
-template <bool TOP>
+template <int DT, bool TOP>
 windq_status launch_gate_gradient(windq_ctx* ctx, const GateArgs& a, cudaStream_t st) {
   const int64_t across = (a.half + 8 * kThreads - 1) / (8 * kThreads);
   const int64_t down = std::max<int64_t>(1, std::min<int64_t>({a.T, ctx->sm_count * 8 / across, kMostBlocks / across}));
@@ -99,7 +99,7 @@ windq_status launch_gate_gradient(windq_ctx* ctx, const GateArgs& a, cudaStream_
   cudaLaunchAttribute attrs[2];
   overlapped_launch(cfg, attrs, 1, kThreads, 1, 0, st);
   cfg.gridDim = dim3((unsigned)across, (unsigned)down);
-  WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, gate_gradient_kernel<TOP>, a));
+  WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, gate_gradient_kernel<DT, TOP>, a));
   return WINDQ_OK;
 }
 
@@ -289,9 +289,13 @@ windq_status windq_gated_backward(windq_ctx* ctx, int dtype, int activation, con
                  {nullptr, kept, kept + T * half}, {0, half, half}, partials};
     WINDQ_TRY(launch_product(ctx, q, st));
   }
-  GateArgs a = {gate, up, dH, T, ldg, lddh, half, (int)F, dtype, activation, D, dtype == WINDQ_F16 ? top : nullptr, top + 64};
-  if (a.top) WINDQ_TRY(launch_gate_gradient<true>(ctx, a, st));
-  WINDQ_TRY(launch_gate_gradient<false>(ctx, a, st));
+  GateArgs a = {gate, up, dH, T, ldg, lddh, half, (int)F, activation, D, dtype == WINDQ_F16 ? top : nullptr, top + 64};
+  if (a.top) {
+    WINDQ_TRY((launch_gate_gradient<WINDQ_F16, true>(ctx, a, st)));
+    WINDQ_TRY((launch_gate_gradient<WINDQ_F16, false>(ctx, a, st)));
+  } else {
+    WINDQ_TRY((launch_gate_gradient<WINDQ_BF16, false>(ctx, a, st)));
+  }
   if (dX) {
     Product q = {kInputGrad, dtype, 0, T, C, F, D, 2 * half, {Wg, Wu}, {ldwg, ldwu}, half, nullptr, {nullptr, nullptr}, a.top,
                  {dX, nullptr, nullptr}, {lddx, 0, 0}, partials};

@@ -9,10 +9,9 @@
 //
 // Outputs leave transposed, [token][output]: fragments go to shared memory by stmatrix.trans and on by TMA.
 //
-// Persistent over tiles with two accumulators, so that storing a tile overlaps the next.  What does not come out even -- the last
-// one to two rounds of tiles over the GPU, or all of them where they do not fill it -- is cut along K into equal shares, one a pair,
-// where that saves more than it costs.  The pieces of a tile then go to scratch memory, and a second kernel adds them, in order, and
-// finishes the tile: nobody waits for another, and equal calls give equal bits.  (Tiles shared by a cluster, with sums through
+// Persistent over tiles with two accumulators, so that storing a tile overlaps the next.  Tiles that do not fill the GPU are cut along
+// K into equal shares, one a pair, where that saves more than it costs.  The pieces of a tile then go to scratch memory, and a second
+// kernel adds them, in order, and finishes the tile: nobody waits for another, and equal calls give equal bits.  (Tiles shared by a cluster, with sums through
 // distributed shared memory, came out slower: clusters of eight whole SMs fill few of a GPC's; one block adding all of a tile's
 // pieces, too: 100 tokens x 1024 x 4096 codes 19.5 us.)
 //
@@ -514,16 +513,16 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
 
   const int64_t tiles = (int64_t)p.token_tiles * p.weight_tiles, slots = std::min(ctx->sm_count / 2, kMaxPairs);
   p.whole_tiles = (int)tiles;
-  p.pairs = (int)slots;
-  const int64_t pairs = std::min(tiles, slots), idle = (slots - tiles % slots) % slots;
-  int64_t blocks = pairs;
-  // Cutting saves the idle pairs' part of a tile and costs another kernel, about 4 us and 12 ns a token (a chunk of K takes 0.2 us
-  // for 32 tokens, 0.36 for 256).
-  if (idle * p.chunks * (170 + p.tokens * 3 / 4) > (4000 + 12 * p.tokens) * slots) {
-    p.whole_tiles = (int)(tiles > slots ? (tiles / slots - 1) * slots : 0);
-    p.pairs = (int)std::min(slots, std::max(pairs, tiles * p.chunks / kLeastShare));
-    blocks = p.pairs;
+  int64_t pairs = std::min(tiles, slots);
+  // Cutting saves the idle pairs' part of a tile (a chunk of K takes 0.2 us for 32 tokens, 0.36 for 256) and costs another kernel, 4
+  // us, and the pieces' way to memory and back, two for a pair at most.  333 tokens x 2048 x 16382: 32 + 9 us instead of 70.  Never
+  // with a whole round and more: pairs at different places of K no longer meet in L2 (8192 x 14336 x 4096 codes: 356 instead of 339
+  // us; 256 tokens x 2 x 11008 x 4096: 63 instead of 55).
+  if (tiles < slots && (slots - tiles) * p.chunks * (170 + p.tokens * 3 / 4) > (4000 + (slots + tiles) * p.tokens / 2) * slots) {
+    p.whole_tiles = 0;
+    pairs = std::min(slots, std::max(pairs, tiles * p.chunks / kLeastShare));
   }
+  p.pairs = (int)pairs;
   const int stage = kWeightBytes + p.tokens / 2 * kChunkBytes, extra = (q.kind == kGated && q.O[1] ? kBoxesSaved : kBoxes) * kBoxBytes;
   p.stages = std::min(kMaxStages, (kSmemLimit - 1024 - extra) / stage);
   const int smem = kSmemLimit;  // all of it, whatever is used: no block that wants tensor memory fits beside this one
@@ -546,10 +545,10 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   for (int k = 0; k < 3; k++)
     if (!q.O[k]) o[k] = *any;  // not used
   switch (q.kind) {
-    case kInt8: return launch<kInt8>(ctx, x, w, o, p, (int)blocks * 2, smem, st);
-    case kInt8Gated: return launch<kInt8Gated>(ctx, x, w, o, p, (int)blocks * 2, smem, st);
-    case kGated: return launch<kGated>(ctx, x, w, o, p, (int)blocks * 2, smem, st);
-    default: return launch<kInputGrad>(ctx, x, w, o, p, (int)blocks * 2, smem, st);
+    case kInt8: return launch<kInt8>(ctx, x, w, o, p, (int)pairs * 2, smem, st);
+    case kInt8Gated: return launch<kInt8Gated>(ctx, x, w, o, p, (int)pairs * 2, smem, st);
+    case kGated: return launch<kGated>(ctx, x, w, o, p, (int)pairs * 2, smem, st);
+    default: return launch<kInputGrad>(ctx, x, w, o, p, (int)pairs * 2, smem, st);
   }
 }
 

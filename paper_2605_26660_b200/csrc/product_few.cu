@@ -7,6 +7,8 @@
 // shared memory, where they lie as the result does; where the tiles do not fill the GPU, `splits` blocks (a cluster) share a tile
 // along K and add their sums through distributed shared memory, in rank order: equal calls give equal bits.
 //
+// A block starts while the stream's kernel before ends and first brings its first weights into L2.
+//
 // Warps: one issues TMA copies, one issues matrix products, four read the accumulators; all of them finish the tile.
 #include <algorithm>
 
@@ -188,7 +190,6 @@ __global__ void __launch_bounds__(kThreads, 2)
   __syncthreads();
   tc_fence_after();
   launch_dependents();  // tensor memory is in hand
-  wait_for_predecessor();
   const uint32_t tmem = tmem_slot;
 
   const int split = blockIdx.x % p.splits;
@@ -196,28 +197,38 @@ __global__ void __launch_bounds__(kThreads, 2)
   const int wt = blockIdx.x / p.splits;
 
   if (warp == 0) {
-    Ring at(p.stages);
     const int n0 = wt * (K::kGate ? 64 : 128);
+    auto weights = [&](int c, auto take) {  // the two boxes of a chunk
+      const bool other = K::kTransposed && c >= p.half_chunks;
+      const CUtensorMap *first = other ? &wmap1 : &wmap0, *second = K::kGate || other ? &wmap1 : &wmap0;
+      if (K::kTransposed) {
+        const int k0 = (other ? c - p.half_chunks : c) * 64;
+        take(0, first, n0, k0);
+        take(1, second, n0 + 64, k0);
+      } else {
+        take(0, first, c * K::kStepK, n0);
+        take(1, second, c * K::kStepK, K::kGate ? n0 : n0 + 64);
+      }
+    };
+    if (elect_one())
+      for (int c = c0; c < min(c1, c0 + p.stages); c++)
+        weights(c, [&](int, const CUtensorMap* map, int x, int y) { tma_prefetch_2d(map, x, y); });
+    __syncwarp();
+    wait_for_predecessor();
+    Ring at(p.stages);
     for (int c = c0; c < c1; c++) {
       mbar_wait(empty(at.s), at.phase ^ 1, dead_);
       const uint32_t dst = base + at.s * stage_bytes, bar = full(at.s);
       if (elect_one() && !*(volatile int*)&dead) {
         mbar_expect(bar, stage_bytes);
-        if (K::kTransposed) {
-          const bool other = c >= p.half_chunks;
-          const int k0 = (other ? c - p.half_chunks : c) * 64;
-          tma_load_2d<false>(dst, other ? &wmap1 : &wmap0, n0, k0, bar);
-          tma_load_2d<false>(dst + 8192, other ? &wmap1 : &wmap0, n0 + 64, k0, bar);
-        } else {
-          tma_load_2d<false>(dst, &wmap0, c * K::kStepK, n0, bar);
-          tma_load_2d<false>(dst + 8192, K::kGate ? &wmap1 : &wmap0, c * K::kStepK, K::kGate ? n0 : n0 + 64, bar);
-        }
+        weights(c, [&](int k, const CUtensorMap* map, int x, int y) { tma_load_2d<false>(dst + k * 8192, map, x, y, bar); });
         tma_load_2d<false>(dst + kWeightBytes, &xmap, c * K::kStepK, 0, bar);
       }
       __syncwarp();
       at.next();
     }
   } else if (warp == 1) {
+    wait_for_predecessor();
     const uint32_t idesc = K::kCodes ? instr_desc_i8(128, p.tokens) : instr_desc(p.dtype, K::kTransposed, false, 128, p.tokens);
     constexpr uint32_t w_step = (K::kTransposed ? 2048 : 32) >> 4, t_step = 32 >> 4;
     const uint64_t w_desc = smem_desc(base, K::kTransposed ? 8192 : 16), t_desc = smem_desc(base + kWeightBytes, 16);
@@ -240,6 +251,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (elect_one()) mma_commit<false>(done, 0);
     __syncwarp();
   } else {
+    wait_for_predecessor();
     const int quarter = warp & 3, n = quarter * 32 + lane;
     mbar_wait(done, 0, dead_);
     tc_fence_after();

@@ -6,6 +6,7 @@
 // are many rows, more where there are few and the time is one row's latency.
 #include <algorithm>
 
+#include "tcgen05.cuh"
 #include "typed.cuh"
 
 namespace windq {
@@ -74,6 +75,8 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeArgs p
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % W;
   const int64_t t = (int64_t)blockIdx.x * (kThreads / 32 / W) + warp / W;
   const bool live = t < p.T;
+  launch_dependents();
+  wait_for_predecessor();
   const uint16_t* row = p.X + (live ? t : 0) * p.ldx;
   const int pieces = live ? (p.C + 7) / 8 : 0, first = part * 32 + lane, step = W * 32;
   uint4 held[kHeld];
@@ -122,14 +125,15 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeArgs p
 }
 
 template <int DT, int W>
-void launch(const QuantizeArgs& p, cudaStream_t st) {
+cudaError_t launch(const QuantizeArgs& p, cudaStream_t st) {
   const int64_t rows = kThreads / 32 / W;
-  const unsigned blocks = (unsigned)((p.T + rows - 1) / rows);
-  if (p.values) quantize_kernel<DT, W, true><<<blocks, kThreads, 0, st>>>(p);
-  else quantize_kernel<DT, W, false><<<blocks, kThreads, 0, st>>>(p);
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attrs[2];
+  overlapped_launch(cfg, attrs, (int)((p.T + rows - 1) / rows), kThreads, 1, 0, st);
+  return p.values ? cudaLaunchKernelEx(&cfg, quantize_kernel<DT, W, true>, p) : cudaLaunchKernelEx(&cfg, quantize_kernel<DT, W, false>, p);
 }
 template <int DT>
-void launch(const QuantizeArgs& p, int warps, cudaStream_t st) {
+cudaError_t launch(const QuantizeArgs& p, int warps, cudaStream_t st) {
   switch (warps) {
     case 1: return launch<DT, 1>(p, st);
     case 2: return launch<DT, 2>(p, st);
@@ -163,8 +167,6 @@ extern "C" windq_status windq_quantize_rows(windq_ctx* ctx, int dtype, const voi
   QuantizeArgs p = {(const uint16_t*)X, T, ldx, (int)C, codes_out, ldq, scale_out, (uint16_t*)values_out, ldv};
   int warps = 1;
   while (warps < 8 && (C > warps * 32 * 8 * kHeld || (T * warps < ctx->sm_count * 16 && C > warps * 32 * 8))) warps *= 2;
-  if (dtype == WINDQ_F16) launch<WINDQ_F16>(p, warps, (cudaStream_t)stream);
-  else launch<WINDQ_BF16>(p, warps, (cudaStream_t)stream);
-  WINDQ_CUDA(ctx, cudaGetLastError());
+  WINDQ_CUDA(ctx, dtype == WINDQ_F16 ? launch<WINDQ_F16>(p, warps, (cudaStream_t)stream) : launch<WINDQ_BF16>(p, warps, (cudaStream_t)stream));
   return WINDQ_OK;
 }

@@ -3,7 +3,8 @@
 //
 // A tile is 256 rows (outputs of the block) x up to 256 columns (channels) on a pair of thread blocks (cta_group::2: each holds half
 // of either operand); persistent over tiles with two accumulators, so that storing a tile overlaps the next.  Warps: one issues TMA
-// copies, one issues matrix products, four read the accumulators and store.
+// copies, one issues matrix products, eight read the accumulators and store (with four, storing took longer than the products of a short K:
+// 333 tokens x 8191 x 2048 30 us).
 //
 // Where the tiles do not fill the GPU, `splits` pairs (a cluster) share a tile along K and add their accumulators through
 // distributed shared memory, in rank order: equal calls give equal bits.
@@ -15,11 +16,12 @@
 namespace windq {
 namespace {
 
-constexpr int kThreads = 192;
+constexpr int kStorers = 8;  // warps
+constexpr int kThreads = 64 + 32 * kStorers;
 constexpr int kMaxStages = 8;
 constexpr int kSmemLimit = 227 * 1024 - 2048;  // dynamic shared memory of one thread block per SM
 constexpr int kPitch = 260;                    // sums of a split tile, 32 bits each, rows free of bank conflicts
-constexpr int kStaging = 4 * 2 * 4096;         // of the four storing warps
+constexpr int kStaging = kStorers * 4096;      // a box of 32 rows x 64 columns each
 constexpr int kABytes = 2 * 8192;              // of a stage: 128 rows x 64 tokens
 
 struct Args {
@@ -110,7 +112,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int b = 0; b < 2; b++) {
       mbar_init(done(b), 1);
-      mbar_init(free_(b), 8);
+      mbar_init(free_(b), 2 * kStorers);
     }
     dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -178,10 +180,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   } else {
-    const int quarter = warp & 3, at = quarter * 32 + lane;
+    const int quarter = warp & 3, group = (warp - 2) >> 2, at = quarter * 32 + lane;
     const uint32_t staging = base + p.stages * stage_bytes;
     const float unscale = p.top ? gradient_power(*p.top, -1) : 1.0f;
-    uint32_t buffer = 0;
     int turn = 0;
     for (int tile = blockIdx.x / team; tile < tiles; tile += step, turn++) {
       int rt, ct;
@@ -194,13 +195,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_wait(done(b), use & 1, dead_);
       tc_fence_after();
       if (p.splits == 1) {
-        // 32 rows x 64 columns at a time through shared memory (128-byte swizzle, two buffers a warp) and out by TMA
-        for (int c = 0; c < 2 * p.block_cols; c += 64, buffer ^= 1) {
-          const uint32_t to = staging + ((quarter * 2 + buffer) * 32 + lane) * 128;
+        // 32 rows x 64 columns at a time through shared memory (128-byte swizzle) and out by TMA
+        for (int c = group * 64; c < 2 * p.block_cols; c += 128) {
+          const uint32_t to = staging + ((warp - 2) * 32 + lane) * 128;
           uint32_t r[4][16];
 #pragma unroll
           for (int h = 0; h < 4; h++) tmem_load16(d + c + h * 16, r[h]);
-          if (lane == 0) tma_store_wait<1>();
+          if (lane == 0) tma_store_wait<0>();
           tmem_load_wait();
           __syncwarp();
 #pragma unroll
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const bool whole = n + 64 <= p.N || p.N % 8 == 0;
           if (lane == 0) {
             if (whole && m0 + quarter * 32 < p.F && n < p.N)
-              tma_store_2d(second ? &omap1 : &omap0, n, m0 + quarter * 32, staging + (quarter * 2 + buffer) * 4096);
+              tma_store_2d(second ? &omap1 : &omap0, n, m0 + quarter * 32, staging + (warp - 2) * 4096);
             tma_store_commit();
           }
           if (!whole && m < p.F) {
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       } else {
-        for (int c = 0; c < 2 * p.block_cols; c += 16) {
+        for (int c = group * 16; c < 2 * p.block_cols; c += 32) {
           uint32_t r[16];
           tmem_load16(d + c, r);
           tmem_load_wait();

@@ -39,4 +39,4 @@ def test_unknown_activations_are_refused(call):
 
 def test_functions_count_their_arguments():
     with pytest.raises(TypeError, match="arguments"):
-        wq._binding.quantize_rows(None, 0, 0, X)
+        wq._binding.quantize_rows(None, 0, STREAM, X)
