@@ -33,6 +33,21 @@ __device__ __forceinline__ float gradient_power(uint32_t top, int sign) {
 //   kInputGrad   dX: [dG | dU] of the tokens x the two weights, transposed: W(n, k) = W[k][n]
 enum ProductKind { kInt8, kInt8Gated, kGated, kInputGrad };
 
+template <int KIND>
+struct Kind {
+  static constexpr bool kCodes = KIND == kInt8 || KIND == kInt8Gated, kGate = KIND == kInt8Gated || KIND == kGated;
+  static constexpr bool kTransposed = KIND == kInputGrad;
+  static constexpr int kStepK = kCodes ? 128 : 64;  // values of a chunk
+};
+
+// What an accumulator stands for.
+template <bool CODES>
+__device__ __forceinline__ float value_of(uint32_t acc, float row, float col) {
+  if (CODES) return __int2float_rn((int)acc) * row * col;
+  return __uint_as_float(acc) * row;
+}
+__device__ __forceinline__ float gated(float g, float u, int act) { return g * logistic(gate_exponent(g, act)) * u; }
+
 struct Product {
   int kind, dtype, act;
   int64_t T, N, K;        // tokens, outputs, length of the sum (kInputGrad: of each of its two halves)

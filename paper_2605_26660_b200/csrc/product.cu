@@ -3,19 +3,24 @@
 //
 // A tile is 256 rows of weights x up to 256 tokens on a pair of thread blocks (cta_group::2: each holds half of either operand, so
 // that a block's shared memory feeds a product twice as large).  The weights are the rows of the accumulators and the tokens their
-// columns because the tokens are what is ragged: a tile takes as many as there are, in steps of 32, where rows come in 256.  A gated tile has both products of the same 128
-// outputs, 16 rows of one weight and 16 of the other in turns: a storing warp's 32 lanes hold g and u of 16 outputs, and read as
-// 16 x 8 fragments a thread has both in its registers.
+// columns because the tokens are what is ragged: a tile takes as many as there are, in steps of 32, where rows come in 256 (777
+// tokens x 2 x 13821 x 5120: 193 us, with the tokens as rows 209).  A gated tile has both products of the same 128 outputs, 16 rows
+// of one weight and 16 of the other in turns: a storing warp's 32 lanes hold g and u of 16 outputs, and read as 16 x 8 fragments a
+// thread has both in its registers.
 //
 // Outputs leave transposed, [token][output]: fragments go to shared memory by stmatrix.trans and on by TMA.
 //
 // Persistent over tiles with two accumulators, so that storing a tile overlaps the next.  Tiles that do not fill the GPU are cut along
 // K into equal shares, one a pair, where that saves more than it costs.  The pieces of a tile then go to scratch memory, and a second
-// kernel adds them, in order, and finishes the tile: nobody waits for another, and equal calls give equal bits.  (Tiles shared by a cluster, with sums through
-// distributed shared memory, came out slower: clusters of eight whole SMs fill few of a GPC's; one block adding all of a tile's
-// pieces, too: 100 tokens x 1024 x 4096 codes 19.5 us.)
+// kernel adds them, in order, and finishes the tile: nobody waits for another, and equal calls give equal bits.  (Tiles shared by a
+// cluster, with sums through distributed shared memory, came out slower: clusters of eight whole SMs fill few of a GPC's.  So did one
+// block that adds all of a tile's pieces: 100 tokens x 1024 x 4096 codes 19.5 us, now 10.)
 //
-// Warps: one issues TMA copies, one issues matrix products, four read the accumulators and store.
+// What bounds it: from about 2000 tokens on power (8192 x 14336 x 4096 codes: 305 us in a burst, 338 in a long run), below that the
+// copies from L2 (32 KB a chunk of K and block at 256 tokens, 13 TB/s over the GPU) and rounds that are not full.
+//
+// Warps: one issues TMA copies, one issues matrix products, four read the accumulators and store.  A block sets itself up, and brings
+// its first weights into L2, while the stream's kernel before ends, where that leaves room on the SM.
 #include <algorithm>
 
 #include "feed_forward.cuh"
@@ -54,13 +59,6 @@ struct Args {
 
 struct Barriers {
   uint64_t full[kMaxStages], empty[kMaxStages], done[2], free[2];
-};
-
-template <int KIND>
-struct Kind {
-  static constexpr bool kCodes = KIND == kInt8 || KIND == kInt8Gated, kGate = KIND == kInt8Gated || KIND == kGated;
-  static constexpr bool kTransposed = KIND == kInputGrad;
-  static constexpr int kStepK = kCodes ? 128 : 64;  // values of a chunk
 };
 
 // Tiles in an order that keeps a group of token tiles in L2 while the weights stream by.
@@ -111,13 +109,6 @@ struct Walk {
   __device__ __forceinline__ bool later() const { return (tile - p.whole_tiles) * p.chunks + c0 != begin; }
 };
 
-// What an accumulator stands for.
-template <bool CODES>
-__device__ __forceinline__ float value_of(uint32_t acc, float row, float col) {
-  if (CODES) return __int2float_rn((int)acc) * row * col;
-  return __uint_as_float(acc) * row;
-}
-__device__ __forceinline__ float gated(float g, float u, int act) { return g * logistic(gate_exponent(g, act)) * u; }
 // The four storing warps.
 __device__ __forceinline__ void barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
@@ -299,34 +290,50 @@ __global__ void __launch_bounds__(kThreads, 1)
   cluster_sync();  // the other block's barriers are ready
   tc_fence_after();
   launch_dependents();  // tensor memory is in hand
-  wait_for_predecessor();
   const uint32_t tmem = tmem_slot, boxes = base + p.stages * stage_bytes;
 
   if (warp == 0) {
+    int tt, wt, n0;
+    auto open = [&](int tile) {
+      tile_at(p, tile, tt, wt);
+      n0 = (2 * wt + me) * (K::kGate ? 64 : 128);
+    };
+    auto weights = [&](int c, auto take) {  // the boxes of a chunk: where in the stage, and where from
+      if (K::kTransposed) {
+        const bool other = c >= p.half_chunks;
+        const int k0 = (other ? c - p.half_chunks : c) * 64;
+        for (int b = 0; b < 2; b++) take(b * 8192, other ? &wmap1 : &wmap0, n0 + b * 64, k0);
+      } else if (K::kGate) {
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+          take(b * 4096, &wmap0, c * K::kStepK, n0 + b * 16);
+          take(b * 4096 + 2048, &wmap1, c * K::kStepK, n0 + b * 16);
+        }
+      } else {
+        take(0, &wmap0, c * K::kStepK, n0);
+      }
+    };
+    {
+      Walk first(p);
+      first.next();
+      open(first.tile);
+      if (elect_one())
+        for (int c = first.c0; c < min(first.c1, first.c0 + p.stages); c++)
+          weights(c, [&](int, const CUtensorMap* map, int x, int y) { tma_prefetch_2d(map, x, y); });
+      __syncwarp();
+    }
+    wait_for_predecessor();
     Ring at(p.stages);
     const uint32_t to = cluster_addr(full(0), 0);  // barriers of the issuing block
     for (Walk walk(p); walk.next();) {
-      int tt, wt;
-      tile_at(p, walk.tile, tt, wt);
-      const int t0 = tt * p.tokens + me * (p.tokens / 2), n0 = (2 * wt + me) * (K::kGate ? 64 : 128);
+      open(walk.tile);
+      const int t0 = tt * p.tokens + me * (p.tokens / 2);
       for (int c = walk.c0; c < walk.c1; c++) {
         mbar_wait(empty(at.s), at.phase ^ 1, dead_);
         const uint32_t dst = base + at.s * stage_bytes, bar = to + at.s * 8;
         if (elect_one() && !*(volatile int*)&dead) {
           if (me == 0) mbar_expect(full(at.s), 2 * stage_bytes);
-          if (K::kTransposed) {
-            const bool other = c >= p.half_chunks;
-            const int k0 = (other ? c - p.half_chunks : c) * 64;
-            for (int b = 0; b < 2; b++) tma_load_2d<true>(dst + b * 8192, other ? &wmap1 : &wmap0, n0 + b * 64, k0, bar);
-          } else if (K::kGate) {
-#pragma unroll
-            for (int b = 0; b < 4; b++) {
-              tma_load_2d<true>(dst + b * 4096, &wmap0, c * K::kStepK, n0 + b * 16, bar);
-              tma_load_2d<true>(dst + b * 4096 + 2048, &wmap1, c * K::kStepK, n0 + b * 16, bar);
-            }
-          } else {
-            tma_load_2d<true>(dst, &wmap0, c * K::kStepK, n0, bar);
-          }
+          weights(c, [&](int at, const CUtensorMap* map, int x, int y) { tma_load_2d<true>(dst + at, map, x, y, bar); });
           tma_load_2d<true>(dst + kWeightBytes, &xmap, c * K::kStepK, t0, bar);
         }
         __syncwarp();
@@ -334,6 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   } else if (warp == 1) {
+    wait_for_predecessor();
     if (me == 0) {
       const uint32_t idesc = K::kCodes ? instr_desc_i8(256, p.tokens) : instr_desc(p.dtype, K::kTransposed, false, 256, p.tokens);
       // a step of K further: 32 bytes in a K-major tile, two groups of 8 rows in an MN-major one
@@ -366,6 +374,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   } else {
+    wait_for_predecessor();
     Finish<KIND> out(p, &omap0, &omap1, &omap2, boxes, 64);
     int turn = 0;
     for (Walk walk(p); walk.next(); turn++) {
@@ -503,7 +512,8 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   p.token_tiles = (int)((q.T + p.tokens - 1) / p.tokens);
   const int outputs = gate ? 128 : 256;
   p.weight_tiles = (int)((q.N + outputs - 1) / outputs);
-  p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.token_tiles, (48ll << 20) / ((int64_t)p.chunks * kChunkBytes * p.tokens)));
+  // 24 MB of tokens: 4096 x 4096 x 22016 and its weights' gradients together 1205 us, with 48 MB 1240, with 96 1305
+  p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.token_tiles, (24ll << 20) / ((int64_t)p.chunks * kChunkBytes * p.tokens)));
   p.row_scale = q.row_scale;
   p.top = q.top;
   for (int k = 0; k < 2; k++) p.col_scale[k] = q.col_scale[k];
@@ -515,9 +525,9 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   p.whole_tiles = (int)tiles;
   int64_t pairs = std::min(tiles, slots);
   // Cutting saves the idle pairs' part of a tile (a chunk of K takes 0.2 us for 32 tokens, 0.36 for 256) and costs another kernel, 4
-  // us, and the pieces' way to memory and back, two for a pair at most.  333 tokens x 2048 x 16382: 32 + 9 us instead of 70.  Never
+  // us, and the pieces' way to memory and back, two for a pair at most.  333 tokens x 2048 x 16382: 30 + 7 us instead of 70.  Never
   // with a whole round and more: pairs at different places of K no longer meet in L2 (8192 x 14336 x 4096 codes: 356 instead of 339
-  // us; 256 tokens x 2 x 11008 x 4096: 63 instead of 55).
+  // us), and of a part of the last round alone nothing is won (256 tokens x 2 x 11008 x 4096: 56 us either way).
   if (tiles < slots && (slots - tiles) * p.chunks * (170 + p.tokens * 3 / 4) > (4000 + (slots + tiles) * p.tokens / 2) * slots) {
     p.whole_tiles = 0;
     pairs = std::min(slots, std::max(pairs, tiles * p.chunks / kLeastShare));

@@ -42,22 +42,7 @@ struct Barriers {
   uint64_t full[kMaxStages], empty[kMaxStages], done;
 };
 
-template <int KIND>
-struct Kind {
-  static constexpr bool kCodes = KIND == kInt8 || KIND == kInt8Gated, kGate = KIND == kInt8Gated || KIND == kGated;
-  static constexpr bool kTransposed = KIND == kInputGrad;
-  static constexpr int kStepK = kCodes ? 128 : 64;  // values of a chunk
-};
-
 __device__ __forceinline__ float scale_of(const float* s, int i, int n) { return i < n ? __ldg(s + i) : 0.0f; }
-// What an accumulator stands for.
-template <bool CODES>
-__device__ __forceinline__ float value_of(uint32_t acc, float row, float col) {
-  if (CODES) return __int2float_rn((int)acc) * row * col;
-  return __uint_as_float(acc) * row;
-}
-__device__ __forceinline__ float gated(float g, float u, int act) { return g * logistic(gate_exponent(g, act)) * u; }
-
 // Sums over a cluster's n blocks, in the order of their ranks, of U quads at base + offset[u] in each.  Distributed
 // shared memory answers after the better part of a microsecond: the loads of up to four blocks are in flight together.
 template <int U, bool CODES>

@@ -3,8 +3,9 @@
 //
 // A tile is 256 rows (outputs of the block) x up to 256 columns (channels) on a pair of thread blocks (cta_group::2: each holds half
 // of either operand); persistent over tiles with two accumulators, so that storing a tile overlaps the next.  Warps: one issues TMA
-// copies, one issues matrix products, eight read the accumulators and store (with four, storing took longer than the products of a short K:
-// 333 tokens x 8191 x 2048 30 us).
+// copies, one issues matrix products, eight read the accumulators and store (with four, storing took longer than the products of a
+// short K: 333 tokens x 8191 x 2048 30 us, now 27).  Bound by power for a long K, by writing the gradients for a short one (HBM takes
+// 3.9 TB/s of pure writes).
 //
 // Where the tiles do not fill the GPU, `splits` pairs (a cluster) share a tile along K and add their accumulators through
 // distributed shared memory, in rank order: equal calls give equal bits.
@@ -197,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (p.splits == 1) {
         // 32 rows x 64 columns at a time through shared memory (128-byte swizzle) and out by TMA
         for (int c = group * 64; c < 2 * p.block_cols; c += 128) {
-          const uint32_t to = staging + ((warp - 2) * 32 + lane) * 128;
+          const uint32_t box = staging + (warp - 2) * 4096, to = box + lane * 128;
           uint32_t r[4][16];
 #pragma unroll
           for (int h = 0; h < 4; h++) tmem_load16(d + c + h * 16, r[h]);
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const bool whole = n + 64 <= p.N || p.N % 8 == 0;
           if (lane == 0) {
             if (whole && m0 + quarter * 32 < p.F && n < p.N)
-              tma_store_2d(second ? &omap1 : &omap0, n, m0 + quarter * 32, staging + (warp - 2) * 4096);
+              tma_store_2d(second ? &omap1 : &omap0, n, m0 + quarter * 32, box);
             tma_store_commit();
           }
           if (!whole && m < p.F) {
@@ -313,7 +314,7 @@ windq_status launch_weight_gradient(windq_ctx* ctx, const WeightGradient& q, cud
     }
   }
   p.col_tiles = (int)((q.C + 2 * p.block_cols - 1) / (2 * p.block_cols));
-  p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.row_tiles, (48ll << 20) / (512 * q.T)));
+  p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.row_tiles, (24ll << 20) / (512 * q.T)));
   const int stage = kABytes + (p.block_cols + 63) / 64 * 8192, staging = p.splits > 1 ? 0 : kStaging;
   p.stages = std::min(kMaxStages, (kSmemLimit - 1024 - staging) / stage);
   p.accumulators = p.splits == 1 ? 2 : 1;

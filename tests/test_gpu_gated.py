@@ -87,6 +87,25 @@ def test_gates_far_out(wq, ctx, dtype, act):  # noqa: F811
         assert bool(got.isfinite().all())
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("T", [3, 70])
+def test_gates_of_any_size_in_bf16(wq, ctx, T, act):  # noqa: F811
+    """Gates whose squares and cubes leave binary32: open ones pass u on, shut ones nothing, and so do their gradients."""
+    C = F = 8
+    X = torch.zeros((T, C), dtype=BF, device="cuda")
+    X[:, 0], X[:, 1] = 1, 1
+    Wg, Wu = torch.zeros((F, C), dtype=BF, device="cuda"), torch.zeros((F, C), dtype=BF, device="cuda")
+    Wg[:, 0] = torch.tensor([1e10, -1e10, 1e20, -1e20, 1e36, -1e36, 200, -200], dtype=BF)
+    Wu[:, 1] = 2
+    f = wq.windq_gated_forward(ctx, X, Wg, Wu, activation=act, want_saved=True)
+    opened = Wg[:, 0] > 0
+    assert torch.equal(f["h"], torch.where(opened, 2 * Wg[:, 0], 0).expand(T, F))
+    dH = torch.ones((T, F), dtype=BF, device="cuda")
+    got = wq.windq_gated_backward(ctx, X, Wg, Wu, dH, gate=f["gate"], up=f["up"], activation=act, want_dx=False)
+    assert torch.equal(got["dWg"][:, 0], torch.where(opened, 2.0 * T, 0).to(BF))          # dG = dH u act'(g), act' one or zero
+    assert torch.allclose(got["dWu"][:, 1].float(), torch.where(opened, T * Wg[:, 0].float(), 0), rtol=2.0 ** -7, atol=1e-30)
+
+
 def exact_gradients(X, Wg, Wu, dH, g, u, act):
     x, dh, g, u = X.double(), dH.double(), g.double(), u.double()
     du, dg = dh * activation(g, act), dh * u * slope(g, act)
@@ -260,6 +279,31 @@ def test_graphs_and_streams(wq, T):  # noqa: F811
     torch.cuda.synchronize()
     wq.windq_destroy(a)
     wq.windq_destroy(b)
+
+
+@pytest.mark.parametrize("T,F,C", [(30, 600, 4096), (100, 200, 8192)])
+def test_reserved_scratch_is_enough_and_none_grows_while_captured(wq, T, F, C):  # noqa: F811
+    X, Wg, Wu = block(T, F, C, HALF, 4)
+    dH, c = integers((T, F), 8, HALF), wq.windq_create()
+    x, w, sx, sw = codes((T, C), 1), codes((F, C), 2), scales(T, 1), scales(F, 2)
+    want = wq.windq_gated_backward(c, X, Wg, Wu, dH)
+    y = wq.windq_int8_forward(c, x, sx, w, sw)
+    wq.windq_destroy(c)
+    c = wq.windq_create()
+    wq.windq_reserve(c, max(wq.windq_scratch_bytes_gated_backward(T, C, F, True), wq.windq_scratch_bytes_gated_forward(T, C, F),
+                            wq.windq_scratch_bytes_int8_forward(T, F, C)))
+    free = torch.cuda.mem_get_info()[0]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):                                       # a cudaMalloc in here would end the capture
+        got = wq.windq_gated_backward(c, X, Wg, Wu, dH)
+        z = wq.windq_int8_forward(c, x, sx, w, sw)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[k], want[k]) for k in want) and torch.equal(z, y)
+    assert free - torch.cuda.mem_get_info()[0] < 64 << 20
+    del graph
+    torch.cuda.synchronize()
+    wq.windq_destroy(c)
 
 
 def test_refusals(wq, ctx):  # noqa: F811
