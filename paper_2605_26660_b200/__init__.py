@@ -1234,7 +1234,7 @@ def windq_quantize_rows(ctx: Context, X: torch.Tensor, *, want_values: bool = Fa
     """8-bit codes of every row of X [T, C] (fp16 or bf16) with one scale a row: codes = round(127 X / a), scale = a / 127,
     a the row's largest magnitude.
 
-    Returns dict(codes int8 [T, C], whose rows are a multiple of 16 bytes apart, scale fp32 [T], values [T, C] of X's type
+    Returns dict(codes int8 [T, C], whose rows are C bytes apart or the next multiple of 128, scale fp32 [T], values [T, C] of X's type
     | None: what the codes stand for).  ``out`` may hold preallocated tensors under the same keys."""
     given = out or {}
     st, codes, scale, values = _binding.quantize_rows(ctx._h.value, ctx.device, stream, X, want_values, given.get("codes"),

@@ -51,10 +51,11 @@ Rows half_of(const Tensor& t, int device, const char* name) {
   TORCH_CHECK_TYPE(code_of(t.scalar_type()) >= 0, name, " must be torch.float16 or torch.bfloat16, got ", t.scalar_type());
   return rows_of(t, t.scalar_type(), device, 8, name);
 }
-// A caller's [rows, cols] output, or a new one whose rows are padded to a multiple of `step` elements.
+// A caller's [rows, cols] output, or a new one.  Rows of a new one that are no multiple of 32 bytes are padded to one of 128: copies
+// of rows that begin in the middle of 32 bytes take up to a third longer (500 tokens x 2 x 5000 x 5000 70 us, x 5056 57).
 Rows rows_out(PyObject* given, Tensor& t, int64_t rows, int64_t cols, at::ScalarType type, int device, int64_t step, const char* name) {
   if (given == Py_None) {
-    const int64_t ld = up(cols, step);
+    const int64_t size = (int64_t)c10::elementSize(type), ld = cols * size % 32 == 0 ? cols : up(cols, 128 / size);
     t = at::empty({rows, ld}, at::TensorOptions().dtype(type).device(at::kCUDA, (at::DeviceIndex)device));
     if (ld != cols) t = t.narrow(1, 0, cols);
     return Rows{t.data_ptr(), rows, cols, ld, type};

@@ -300,9 +300,12 @@ windq_status launch_few_tokens(windq_ctx* ctx, const Product& q, cudaStream_t st
   p.stalls = stalls_of(ctx);
   const int outputs = gate ? 64 : 128;
   const int64_t tiles = (q.N + outputs - 1) / outputs;
-  // Four splits at most: clusters of eight start and join slowly.
+  // As many as two blocks an SM hold: 48 tokens x 4096 x 11008 codes in two splits 20.3 us, in four 16.4; 33 tokens x 2 x 11008 x 4096,
+  // 172 tiles, whole 20.4, in two 27.9.  Clusters of four do not fill the last slots of every GPC (60 tokens x 2 x 4700 x 5056, 74
+  // tiles: in four splits, 296 blocks, 30.0 us, in two 22.1), and of eight start and join slowly.
   p.splits = 1;
-  while (p.splits < 4 && tiles * p.splits <= ctx->sm_count && p.chunks >= p.splits * 2 * 4) p.splits *= 2;
+  for (int splits = 2; splits <= 4; splits *= 2)
+    if (tiles * splits <= ctx->sm_count * 2 * (splits == 4 ? 9 : 10) / 10 && p.chunks >= splits * 4) p.splits = splits;
   const int stage = kWeightBytes + p.tokens * kChunkBytes;
   p.stages = std::min(kMaxStages, (kSmemLimit - 1024) / stage);
   p.columns = p.tokens <= 32 ? 32 : p.tokens <= 64 ? 64 : 128;
