@@ -228,7 +228,7 @@ def windq_fit_work(ctx: Context, reset: bool = False):
 
 
 def windq_stalls(ctx: Context, reset: bool = False) -> int:
-    """Thread blocks of the adapter calls whose bounded waits gave up (0 is expected).  Synchronises the device."""
+    """Thread blocks of the adapter and feed-forward calls whose bounded waits gave up (0 is expected).  Synchronises the device."""
     n = ctypes.c_int64(0)
     ctx._check(_lib.windq_stalls(ctx._h, ctypes.byref(n), 1 if reset else 0))
     return int(n.value)

@@ -2,10 +2,12 @@
 //
 //   q = round(127 x / a), ties to even, of the exact quotient;  a = max |x| of the row;  scale = a / 127
 // One pass: a row is held in registers between its maximum and its codes (up to 16384 values; of a longer one the rest is
-// read again, from L2).  Bound by memory: 2 bytes read, 1 written a value.  W warps share a row: as few as hold it where there
-// are many rows, more where there are few and the time is one row's latency.
+// read again, from L2).  Bound by memory: 2 bytes read, 1 written a value, 2 more with the values the codes stand for (4096 x 14336
+// with them: 46 us, 0.98 of the copy rate).  W warps share a row: as few as hold it where there are many rows, more where there are
+// few and the time is one row's latency (one row of 2048: 2.5 us).
 #include <algorithm>
 
+#include "fit_device.cuh"
 #include "tcgen05.cuh"
 #include "typed.cuh"
 
@@ -40,21 +42,23 @@ __device__ __forceinline__ uint32_t top_of(uint32_t top, const uint4& v) {
   return top;
 }
 
-// Codes of eight values.  x * inv is within 2^-23 of 127 x / a.  That quotient either is a border between two codes (8 bits) or
-// is at least 2^-18 of itself away from one (127 x has 18 bits, or 15), so rounding the product to 20 bits first puts both on
-// their side.  `lift` (1, or 2^60 for rows of tiny values, whose 127 / a would overflow) is a power of two.
-template <int DT, bool VALUES>
-__device__ __forceinline__ void encode(const uint4& v, float lift, float inv, float scale, uint2& codes, uint4& values) {
+// Codes of eight values.  y = x * inv is within 2^-23 of 127 x / a.  That quotient either is a border between two codes (8 bits) or
+// is at least 2^-18 of itself away from one (127 x has 18 bits, or 15), so rounding y to 20 bits first -- c - (c - y), c = 17 y --
+// puts both on their side.  Two values an instruction: with one, the kernel was bound by issue (8192 x 8192 5 us more of 43).
+// LIFT: rows of tiny values, whose 127 / a would overflow, are multiplied by 2^60 first.
+template <int DT, bool VALUES, bool LIFT>
+__device__ __forceinline__ void encode(const uint4& v, float inv, float scale, uint2& codes, uint4& values) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   float t[8];
 #pragma unroll
   for (int k = 0; k < 4; k++) {
-    const float2 x = unpack2(w[k], DT);
-#pragma unroll
-    for (int h = 0; h < 2; h++) {
-      const float y = (h ? x.y : x.x) * lift * inv, c = y * 17.0f;
-      t[2 * k + h] = (c - (c - y)) + 12582912.0f;  // 1.5 * 2^23: the integer, rounded, in the low bits
-    }
+    float2 x = unpack2(w[k], DT);
+    if (LIFT) x = make_float2(x.x * 0x1p60f, x.y * 0x1p60f);
+    const float2 y = mul2(x, make_float2(inv, inv)), c = fma2(y, make_float2(16.0f, 16.0f), y);
+    const float2 minus = make_float2(-1.0f, -1.0f), rest = fma2(y, minus, c);
+    const float2 q = add2(fma2(rest, minus, c), make_float2(12582912.0f, 12582912.0f));  // 1.5 * 2^23: the integer in the low bits
+    t[2 * k] = q.x;
+    t[2 * k + 1] = q.y;
   }
   uint32_t b[8];
 #pragma unroll
@@ -96,9 +100,10 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeArgs p
   if (!live) return;
   // a row with an infinity or a NaN: codes of zero and a scale of NaN, which spoil its row of every product
   const bool finite = top < (DT == WINDQ_F16 ? 0x7c00u : 0x7f80u);
-  const float a = finite ? unpack2(top, DT).x : 0.0f, lift = a < 0x1p-60f ? 0x1p60f : 1.0f;
+  const float a = finite ? unpack2(top, DT).x : 0.0f;
+  const bool lift = DT == WINDQ_BF16 && a < 0x1p-60f;
   const float scale = finite ? __fdiv_rn(a, 127.0f) : __uint_as_float(0x7fffffffu);
-  const float inv = a > 0.0f ? __fdiv_rn(127.0f, a * lift) : 0.0f;
+  const float inv = a > 0.0f ? __fdiv_rn(127.0f, lift ? a * 0x1p60f : a) : 0.0f;
   if (first == 0) p.scale[t] = scale;
   int8_t* q = p.q + t * p.ldq;
   uint16_t* out = VALUES ? p.values + t * p.ldv : nullptr;
@@ -106,7 +111,8 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeArgs p
     uint2 codes;
     uint4 values = make_uint4(0, 0, 0, 0);
     if (!finite) v = make_uint4(0, 0, 0, 0);
-    encode<DT, VALUES>(v, lift, inv, scale, codes, values);
+    if (lift) encode<DT, VALUES, true>(v, inv, scale, codes, values);
+    else encode<DT, VALUES, false>(v, inv, scale, codes, values);
     if (i * 8 + 8 <= p.C) {
       reinterpret_cast<uint2*>(q)[i] = codes;
       if (VALUES) reinterpret_cast<uint4*>(out)[i] = values;

@@ -40,3 +40,12 @@ def test_unknown_activations_are_refused(call):
 def test_functions_count_their_arguments():
     with pytest.raises(TypeError, match="arguments"):
         wq._binding.quantize_rows(None, 0, STREAM, X)
+
+
+def test_scratch_for_more_tokens_is_never_less():
+    """So that what is reserved for the longest batch serves every shorter one, captured or not."""
+    for bytes_of in (lambda T: wq.windq_scratch_bytes_int8_forward(T, 512, 512), lambda T: wq.windq_scratch_bytes_gated_forward(T, 512, 512),
+                     lambda T: wq.windq_scratch_bytes_gated_backward(T, 512, 512), lambda T: wq.windq_scratch_bytes_gated_backward(T, 512, 512, True)):
+        sizes = [bytes_of(T) for T in range(0, 1100)]
+        assert sizes == sorted(sizes)
+    assert wq.windq_scratch_bytes_int8_forward(-1, 5, 5) == 0 and wq.windq_scratch_bytes_gated_forward(4, 0, 5) == 0
