@@ -19,8 +19,9 @@
 // What bounds it: from about 2000 tokens on power (8192 x 14336 x 4096 codes: 305 us in a burst, 338 in a long run), below that the
 // copies from L2 (32 KB a chunk of K and block at 256 tokens, 13 TB/s over the GPU) and rounds that are not full.
 //
-// Warps: one issues TMA copies, one issues matrix products, four read the accumulators and store.  A block sets itself up, and brings
-// its first weights into L2, while the stream's kernel before ends, where that leaves room on the SM.
+// Warps: one issues TMA copies, one issues matrix products, four or eight read the accumulators and store, 64 tokens a group of four
+// at a time.  A block sets itself up, and brings its first weights
+// into L2, while the stream's kernel before ends, where that leaves room on the SM.
 #include <algorithm>
 
 #include "feed_forward.cuh"
@@ -29,14 +30,13 @@
 namespace windq {
 namespace {
 
-constexpr int kThreads = 192;
+constexpr int kMaxThreads = 64 + 2 * 128;      // the copying and the issuing warp, one or two groups of four that store
 constexpr int kMaxStages = 12;
 constexpr int kSmemLimit = 227 * 1024 - 2048;  // dynamic shared memory of one thread block per SM
 constexpr int kChunkBytes = 128;               // of K: 64 16-bit values or 128 codes
 constexpr int kWeightBytes = 128 * kChunkBytes;
 constexpr int kBoxBytes = 64 * 128;            // of a store: up to 64 tokens x 64 outputs
-constexpr int kBoxes = 4;                      // two turns of two (gated and stored g, u: two turns of three)
-constexpr int kBoxesSaved = 6;
+constexpr int kBoxes = 2, kBoxesSaved = 3;     // of a set (three: H, g and u); there are two sets
 constexpr int kMaxPairs = 74;
 constexpr int kLeastShare = 4;                 // chunks of K a pair, where tiles are cut
 
@@ -109,8 +109,8 @@ struct Walk {
   __device__ __forceinline__ bool later() const { return (tile - p.whole_tiles) * p.chunks + c0 != begin; }
 };
 
-// The four storing warps.
-__device__ __forceinline__ void barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// The four warps of a group that stores.
+__device__ __forceinline__ void barrier(int group) { asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory"); }
 
 // 16 lanes x 32 columns of accumulators: of every 8 columns a thread has lanes t / 4 and t / 4 + 8, columns 2 (t % 4) and the next.
 __device__ __forceinline__ void tmem_load_fragments(uint32_t addr, uint32_t (&r)[16]) {
@@ -164,22 +164,25 @@ __device__ __forceinline__ void add_quad(uint32_t* x, const uint4& y) {
   for (int e = 0; e < 4; e++) x[e] = CODES ? x[e] + v[e] : __float_as_uint(__uint_as_float(x[e]) + __uint_as_float(v[e]));
 }
 
-// What is done with whole sums, by the four storing warps.
+// What is done with whole sums, by a group of four storing warps.
 template <int KIND>
 struct Finish {
   using K = Kind<KIND>;
   const Args& p;
   const CUtensorMap *omap0, *omap1, *omap2;
-  const uint32_t boxes;
-  const int thread, lane, quarter;
+  uint32_t boxes;        // the set in use
+  const int other;       // from it to the other one, which a group of its own takes in turns with it
+  const int group, thread, lane, quarter;
   const bool saved, wanted;
   const float unscale;
-  uint32_t phase = 0;  // which half of the boxes
+  int flip = other;
   int n0, t0, tokens;  // of the tile
   float col[2][2];
-  __device__ Finish(const Args& p, const CUtensorMap* o0, const CUtensorMap* o1, const CUtensorMap* o2, uint32_t boxes, int first)
-      : p(p), omap0(o0), omap1(o1), omap2(o2), boxes(boxes), thread(threadIdx.x - first), lane(threadIdx.x & 31), quarter((threadIdx.x >> 5) & 3),
+  __device__ Finish(const Args& p, const CUtensorMap* o0, const CUtensorMap* o1, const CUtensorMap* o2, uint32_t sets, int groups, int group, int first)
+      : p(p), omap0(o0), omap1(o1), omap2(o2), boxes(sets + group * set_bytes(p)), other(groups == 1 ? set_bytes(p) : 0), group(group),
+        thread(threadIdx.x - first), lane(threadIdx.x & 31), quarter((threadIdx.x >> 5) & 3),
         saved(KIND == kGated && p.O[1]), wanted(KIND != kGated || p.O[0]), unscale(p.top ? gradient_power(*p.top, -1) : 1.0f) {}
+  static __device__ __forceinline__ int set_bytes(const Args& p) { return (KIND == kGated && p.O[1] ? kBoxesSaved : kBoxes) * kBoxBytes; }
   __device__ __forceinline__ void open(int tile, int me) {
     int tt, wt;
     tile_at(p, tile, tt, wt);
@@ -198,8 +201,11 @@ struct Finish {
   // `units` times 32 tokens of the tile from c on.
   template <int UNITS>
   __device__ __forceinline__ void put(const uint32_t (&r)[UNITS][2][16], int c, int units) {
-    const uint32_t turn = boxes + phase * (saved ? 3 : 2) * kBoxBytes;
-    phase ^= 1;
+    if (thread == 0) {  // what was sent from this set before has been read
+      if (other) tma_store_wait<1>();
+      else tma_store_wait<0>();
+    }
+    barrier(group);
 #pragma unroll
     for (int u = 0; u < UNITS; u++) {
       if (u >= units) break;
@@ -215,39 +221,40 @@ struct Finish {
         for (int k = 0; k < 16; k++) x[h][k] = value_of<K::kCodes>(r[u][h][k], row[(k >> 2) * 2 + (k & 1)], col[h][(k >> 1) & 1]);
       if (K::kGate) {
         if (saved) {
-          put_fragments(turn + kBoxBytes, u * 32, quarter * 2, lane, p.dtype, x[0]);
-          put_fragments(turn + 2 * kBoxBytes, u * 32, quarter * 2, lane, p.dtype, x[1]);
+          put_fragments(boxes + kBoxBytes, u * 32, quarter * 2, lane, p.dtype, x[0]);
+          put_fragments(boxes + 2 * kBoxBytes, u * 32, quarter * 2, lane, p.dtype, x[1]);
         }
         if (wanted) {
 #pragma unroll
           for (int k = 0; k < 16; k++) x[0][k] = gated(x[0][k], x[1][k], p.act);
-          put_fragments(turn, u * 32, quarter * 2, lane, p.dtype, x[0]);
+          put_fragments(boxes, u * 32, quarter * 2, lane, p.dtype, x[0]);
         }
       } else {
 #pragma unroll
-        for (int h = 0; h < 2; h++) put_fragments(turn + (quarter >> 1) * kBoxBytes, u * 32, (quarter & 1) * 4 + h * 2, lane, p.dtype, x[h]);
+        for (int h = 0; h < 2; h++) put_fragments(boxes + (quarter >> 1) * kBoxBytes, u * 32, (quarter & 1) * 4 + h * 2, lane, p.dtype, x[h]);
       }
     }
     fence_async_shared();
-    if (thread == 0) tma_store_wait<0>();  // of the boxes of the turn before, which the next one writes
-    barrier();
+    barrier(group);
     const int t = t0 + c, live = min(tokens - c, units * 32);
     if (K::kGate) {
-      if (wanted) send_box(p, turn, 0, omap0, n0, t, live, thread);
+      if (wanted) send_box(p, boxes, 0, omap0, n0, t, live, thread);
       if (saved) {
-        send_box(p, turn + kBoxBytes, 1, omap1, n0, t, live, thread);
-        send_box(p, turn + 2 * kBoxBytes, 2, omap2, n0, t, live, thread);
+        send_box(p, boxes + kBoxBytes, 1, omap1, n0, t, live, thread);
+        send_box(p, boxes + 2 * kBoxBytes, 2, omap2, n0, t, live, thread);
       }
     } else {
-      send_box(p, turn, 0, omap0, n0, t, live, thread);
-      send_box(p, turn + kBoxBytes, 0, omap0, n0 + 64, t, live, thread);
+      send_box(p, boxes, 0, omap0, n0, t, live, thread);
+      send_box(p, boxes + kBoxBytes, 0, omap0, n0 + 64, t, live, thread);
     }
     if (thread == 0) tma_store_commit();
+    boxes += flip;
+    flip = -flip;
   }
 };
 
 template <int KIND>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kMaxThreads, 1)
     product_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap0,
                    const __grid_constant__ CUtensorMap wmap1, const __grid_constant__ CUtensorMap omap0,
                    const __grid_constant__ CUtensorMap omap1, const __grid_constant__ CUtensorMap omap2,
@@ -277,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int b = 0; b < 2; b++) {
       mbar_init(done(b), 1);
-      mbar_init(free_(b), 8);
+      mbar_init(free_(b), 2 * (blockDim.x / 32 - 2));
     }
     dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -375,7 +382,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     wait_for_predecessor();
-    Finish<KIND> out(p, &omap0, &omap1, &omap2, boxes, 64);
+    const int group = (warp - 2) >> 2, groups = (blockDim.x - 64) / 128;
+    Finish<KIND> out(p, &omap0, &omap1, &omap2, boxes, groups, group, 64 + group * 128);
     int turn = 0;
     for (Walk walk(p); walk.next(); turn++) {
       const int b = turn & 1;
@@ -384,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_wait(done(b), (turn >> 1) & 1, dead_);
       tc_fence_after();
       if (walk.c1 - walk.c0 == p.chunks) {
-        for (int c = 0; c < out.tokens; c += 64) {
+        for (int c = group * 64; c < out.tokens; c += groups * 64) {
           const int units = c + 32 < out.tokens ? 2 : 1;
           uint32_t r[2][2][16];
 #pragma unroll
@@ -395,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       } else {
         uint32_t* piece = piece_of(p, walk.pair, walk.later(), me) + (out.quarter * 32 + lane) * 4;
-        for (int c = 0; c < out.tokens; c += 32) {
+        for (int c = group * 32; c < out.tokens; c += groups * 32) {
           uint32_t r[2][16];
           load_unit(d + c, r);
           tmem_load_wait();
@@ -428,11 +436,11 @@ template <int KIND>
 __global__ void __launch_bounds__(128)
     combine_kernel(const __grid_constant__ CUtensorMap omap0, const __grid_constant__ CUtensorMap omap1,
                    const __grid_constant__ CUtensorMap omap2, const __grid_constant__ Args p) {
-  __shared__ __align__(1024) uint8_t boxes[3 * kBoxBytes];
+  __shared__ __align__(1024) uint8_t boxes[kBoxesSaved * kBoxBytes];
   const int me = blockIdx.x & 1, cut = blockIdx.x >> 1, c = blockIdx.y * 32, s = cut * p.chunks;
   launch_dependents();
   wait_for_predecessor();
-  Finish<KIND> out(p, &omap0, &omap1, &omap2, smem_addr(boxes), 0);
+  Finish<KIND> out(p, &omap0, &omap1, &omap2, smem_addr(boxes), 2, 0, 0);
   out.open(p.whole_tiles + cut, me);
   int q = (int)((int64_t)p.pairs * cut / (p.token_tiles * p.weight_tiles - p.whole_tiles));  // near the pair that holds the first unit
   while (share(p, q + 1) <= s) q++;
@@ -476,12 +484,12 @@ int tile_tokens(int64_t T) {
 
 template <int KIND>
 windq_status launch(windq_ctx* ctx, const CUtensorMap& x, const CUtensorMap (&w)[2], const CUtensorMap (&o)[3], const Args& p, int blocks,
-                    int smem, cudaStream_t st) {
-  const windq_status ready = prepare_kernel(ctx, kProduct + KIND, product_kernel<KIND>, kThreads, kSmemLimit, false);
+                    int threads, int smem, cudaStream_t st) {
+  const windq_status ready = prepare_kernel(ctx, kProduct + KIND, product_kernel<KIND>, kMaxThreads, kSmemLimit, false);
   if (ready != WINDQ_OK) return ready;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attrs[2];
-  overlapped_launch(cfg, attrs, blocks, kThreads, 2, smem, st);
+  overlapped_launch(cfg, attrs, blocks, threads, 2, smem, st);
   WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, product_kernel<KIND>, x, w[0], w[1], o[0], o[1], o[2], p));
   const int cut = p.token_tiles * p.weight_tiles - p.whole_tiles;
   if (cut) {
@@ -537,8 +545,11 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
     pairs = std::min(slots, std::max(pairs, tiles * p.chunks / kLeastShare));
   }
   p.pairs = (int)pairs;
-  const int stage = kWeightBytes + p.tokens / 2 * kChunkBytes, extra = (q.kind == kGated && q.O[1] ? kBoxesSaved : kBoxes) * kBoxBytes;
+  const int stage = kWeightBytes + p.tokens / 2 * kChunkBytes, extra = 2 * (q.kind == kGated && q.O[1] ? kBoxesSaved : kBoxes) * kBoxBytes;
   p.stages = std::min(kMaxStages, (kSmemLimit - 1024 - extra) / stage);
+  // Of a short K storing a tile takes longer than its products: two groups of warps then (3000 tokens x 2 x 8192 x 2048 codes 107 ->
+  // 94 us, 700 x 2048 x 2048 16.4 -> 14.8).  Of a long one they only draw power (4096 x 2 x 8192 x 2048, 16 bits, 204 -> 208).
+  const int threads = p.chunks <= (codes ? 16 : 8) ? 64 + 256 : 64 + 128;
   const int smem = kSmemLimit;  // all of it, whatever is used: no block that wants tensor memory fits beside this one
 
   CUtensorMap x, w[2], o[3];
@@ -559,10 +570,10 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   for (int k = 0; k < 3; k++)
     if (!q.O[k]) o[k] = *any;  // not used
   switch (q.kind) {
-    case kInt8: return launch<kInt8>(ctx, x, w, o, p, (int)pairs * 2, smem, st);
-    case kInt8Gated: return launch<kInt8Gated>(ctx, x, w, o, p, (int)pairs * 2, smem, st);
-    case kGated: return launch<kGated>(ctx, x, w, o, p, (int)pairs * 2, smem, st);
-    default: return launch<kInputGrad>(ctx, x, w, o, p, (int)pairs * 2, smem, st);
+    case kInt8: return launch<kInt8>(ctx, x, w, o, p, (int)pairs * 2, threads, smem, st);
+    case kInt8Gated: return launch<kInt8Gated>(ctx, x, w, o, p, (int)pairs * 2, threads, smem, st);
+    case kGated: return launch<kGated>(ctx, x, w, o, p, (int)pairs * 2, threads, smem, st);
+    default: return launch<kInputGrad>(ctx, x, w, o, p, (int)pairs * 2, threads, smem, st);
   }
 }
 
