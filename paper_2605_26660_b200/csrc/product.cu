@@ -475,11 +475,41 @@ __global__ void __launch_bounds__(128)
   if (out.thread == 0) tma_store_wait<0>();
 }
 
-// Tokens of a tile: as few tiles as there can be, of equal size (one more, with narrower tiles: 777 tokens x 2 x 13821 x 5120 208
-// instead of 194 us, 300 x 2 x 11008 x 4096 80 instead of 65, 560 x 8192 x 8192 codes 43 instead of 44).
-int tile_tokens(int64_t T) {
-  const int64_t tiles = std::max<int64_t>(1, (T + 255) / 256);
-  return (int)std::max<int64_t>(round_up((T + tiles - 1) / tiles, 32), 32);
+// How the tokens are tiled, and whether the tiles are cut.
+struct Plan {
+  int tokens, pairs;
+  bool cut;
+};
+
+// The way that takes the least time.  A chunk of K takes max(200, 110 + tokens) ns: the copies from L2.  Whole tiles take rounds over
+// the pairs; up to three more token tiles than there need to be, narrower ones, may fill a round better (200 tokens x 2 x 4096 x 4096
+// 25.2 -> 23.2 us, 1500 x 4096 x 4096 codes 34.0 -> 29.5, 600 x 2048 x 8192 codes, which then need no cutting, 30.3 -> 23.1), but mostly
+// do not where there are several (777 tokens x 2 x 13821 x 5120 in five tiles 208 us, in four 194).  Cutting, below one round, gives every
+// pair an equal share and costs another kernel, about 8 us with what it starts up, and the pieces' way to memory and back, two for a
+// pair at most (333 tokens x 2048 x 16382: 30 + 7 us instead of 70); with a whole round and more it loses, because pairs at different
+// places of K do not meet in L2 (8192 x 14336 x 4096 codes: 356 us instead of 339).
+Plan plan_of(int64_t T, int64_t weight_tiles, int64_t chunks, int64_t slots) {
+  const int64_t least = std::max<int64_t>(1, (T + 255) / 256);
+  Plan best = {};
+  int64_t best_cost = INT64_MAX;
+  for (int64_t n = least; n < least + 4; n++) {
+    const int64_t tokens = std::max<int64_t>(round_up((T + n - 1) / n, 32), 32), tiles = (T + tokens - 1) / tokens * weight_tiles;
+    if (n > least && tokens == best.tokens) continue;
+    const int64_t chunk = std::max<int64_t>(200, 110 + tokens), rounds = (tiles + slots - 1) / slots;
+    const int64_t whole = 2000 + rounds * (chunks * chunk + 1000);
+    if (whole < best_cost - best_cost / 20) {
+      best = {(int)tokens, (int)std::min(tiles, slots), false};
+      best_cost = whole;
+    }
+    if (tiles >= slots) continue;
+    const int64_t pairs = std::min(slots, std::max(tiles, tiles * chunks / kLeastShare));
+    const int64_t cut = (tiles * chunks + pairs - 1) / pairs * chunk + 8000 + (pairs + tiles) * tokens / 2;
+    if (pairs > tiles && cut < best_cost - best_cost / 20) {
+      best = {(int)tokens, (int)pairs, true};
+      best_cost = cut;
+    }
+  }
+  return best;
 }
 
 template <int KIND>
@@ -520,10 +550,13 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   p.act = q.act;
   p.half_chunks = (int)((q.K + step - 1) / step);
   p.chunks = transposed ? 2 * p.half_chunks : p.half_chunks;
-  p.tokens = tile_tokens(q.T);
-  p.token_tiles = (int)((q.T + p.tokens - 1) / p.tokens);
   const int outputs = gate ? 128 : 256;
   p.weight_tiles = (int)((q.N + outputs - 1) / outputs);
+  const Plan plan = plan_of(q.T, p.weight_tiles, p.chunks, std::min(ctx->sm_count / 2, kMaxPairs));
+  p.tokens = plan.tokens;
+  p.pairs = plan.pairs;
+  p.token_tiles = (int)((q.T + p.tokens - 1) / p.tokens);
+  p.whole_tiles = plan.cut ? 0 : p.token_tiles * p.weight_tiles;
   // 24 MB of tokens: 4096 x 4096 x 22016 and its weights' gradients together 1205 us, with 48 MB 1240, with 96 1305
   p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.token_tiles, (24ll << 20) / ((int64_t)p.chunks * kChunkBytes * p.tokens)));
   p.row_scale = q.row_scale;
@@ -533,18 +566,6 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   p.partials = (uint32_t*)q.partials;
   p.stalls = stalls_of(ctx);
 
-  const int64_t tiles = (int64_t)p.token_tiles * p.weight_tiles, slots = std::min(ctx->sm_count / 2, kMaxPairs);
-  p.whole_tiles = (int)tiles;
-  int64_t pairs = std::min(tiles, slots);
-  // Cutting saves the idle pairs' part of a tile (a chunk of K takes 0.2 us for 32 tokens, 0.36 for 256) and costs another kernel, 4
-  // us, and the pieces' way to memory and back, two for a pair at most.  333 tokens x 2048 x 16382: 30 + 7 us instead of 70.  Never
-  // with a whole round and more: pairs at different places of K no longer meet in L2 (8192 x 14336 x 4096 codes: 356 instead of 339
-  // us), and of a part of the last round alone nothing is won (256 tokens x 2 x 11008 x 4096: 56 us either way).
-  if (tiles < slots && (slots - tiles) * p.chunks * (170 + p.tokens * 3 / 4) > (4000 + (slots + tiles) * p.tokens / 2) * slots) {
-    p.whole_tiles = 0;
-    pairs = std::min(slots, std::max(pairs, tiles * p.chunks / kLeastShare));
-  }
-  p.pairs = (int)pairs;
   const int stage = kWeightBytes + p.tokens / 2 * kChunkBytes, extra = 2 * (q.kind == kGated && q.O[1] ? kBoxesSaved : kBoxes) * kBoxBytes;
   p.stages = std::min(kMaxStages, (kSmemLimit - 1024 - extra) / stage);
   // Of a short K storing a tile takes longer than its products: two groups of warps then (3000 tokens x 2 x 8192 x 2048 codes 107 ->
@@ -570,10 +591,10 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   for (int k = 0; k < 3; k++)
     if (!q.O[k]) o[k] = *any;  // not used
   switch (q.kind) {
-    case kInt8: return launch<kInt8>(ctx, x, w, o, p, (int)pairs * 2, threads, smem, st);
-    case kInt8Gated: return launch<kInt8Gated>(ctx, x, w, o, p, (int)pairs * 2, threads, smem, st);
-    case kGated: return launch<kGated>(ctx, x, w, o, p, (int)pairs * 2, threads, smem, st);
-    default: return launch<kInputGrad>(ctx, x, w, o, p, (int)pairs * 2, threads, smem, st);
+    case kInt8: return launch<kInt8>(ctx, x, w, o, p, p.pairs * 2, threads, smem, st);
+    case kInt8Gated: return launch<kInt8Gated>(ctx, x, w, o, p, p.pairs * 2, threads, smem, st);
+    case kGated: return launch<kGated>(ctx, x, w, o, p, p.pairs * 2, threads, smem, st);
+    default: return launch<kInputGrad>(ctx, x, w, o, p, p.pairs * 2, threads, smem, st);
   }
 }
 
