@@ -65,8 +65,8 @@ struct Product {
 };
 windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st);
 int64_t product_scratch(int64_t T);
-// The same for up to so many tokens: see product_few.cu.
-constexpr int64_t kFewTokensMost = 64;
+// The same for up to so many tokens, gated or not: see product_few.cu.
+constexpr int64_t kMostFewGated = 128, kMostFew = 64;
 windq_status launch_few_tokens(windq_ctx* ctx, const Product& q, cudaStream_t st);
 
 // dWg = dG^T X, dWu = dU^T X from D = [dG | dU], [T][2 * half].

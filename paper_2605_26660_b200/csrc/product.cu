@@ -539,8 +539,8 @@ int64_t product_scratch(int64_t T) {  // never less for more tokens
 }
 
 windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
-  if (q.T <= kFewTokensMost) return launch_few_tokens(ctx, q, st);
   const bool codes = q.kind == kInt8 || q.kind == kInt8Gated, gate = q.kind == kInt8Gated || q.kind == kGated;
+  if (q.T <= (gate ? kMostFewGated : kMostFew)) return launch_few_tokens(ctx, q, st);
   const bool transposed = q.kind == kInputGrad;
   const int step = codes ? 128 : 64;
   Args p = {};

@@ -1,11 +1,13 @@
 // Few tokens times the weights of a feed-forward block: the shape of decoding, bound by the bytes of the weights.  The formulas
 // and what follows the products are those of product_kernel; its pairs of thread blocks, one tile at a time on a whole SM, start and
-// balance too coarsely here (33 tokens x 2 x 11008 x 4096 codes: 26.6 us against 18.5).
+// balance too coarsely here (33 tokens x 2 x 11008 x 4096 codes: 26.6 us against 18.5; 80 x 2 x 2048 x 2048 13.0 against 9.3).  Up to 64
+// tokens, or 128 of a gated product, whose tiles have half as many outputs to join (128 x 2048 x 2048 codes, not gated: 12.4 us, on
+// pairs 9.9).
 //
-// A tile is 128 rows of weights x up to 64 tokens, one a thread block and several blocks an SM, so that the loads of one run while
-// another starts or ends.  A gated tile has 64 rows of each weight, lanes n and n + 64 of the accumulators.  Sums leave through
-// shared memory, where they lie as the result does; where the tiles do not fill the GPU, `splits` blocks (a cluster) share a tile
-// along K and add their sums through distributed shared memory, in rank order: equal calls give equal bits.
+// A tile is 128 rows of weights x all tokens, one a thread block and two blocks an SM, so that the loads of one run while another
+// starts or ends.  A gated tile has 64 rows of each weight, lanes n and n + 64 of the accumulators.  Sums leave through shared memory,
+// where they lie as the result does; where the tiles do not fill the GPU, `splits` blocks (a cluster) share a tile along K and add their
+// sums through distributed shared memory, in rank order: equal calls give equal bits.
 //
 // A block starts while the stream's kernel before ends and first brings its first weights into L2.
 //

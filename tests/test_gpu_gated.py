@@ -106,6 +106,18 @@ def test_gates_of_any_size_in_bf16(wq, ctx, T, act):  # noqa: F811
     assert torch.allclose(got["dWu"][:, 1].float(), torch.where(opened, T * Wg[:, 0].float(), 0), rtol=2.0 ** -7, atol=1e-30)
 
 
+@pytest.mark.parametrize("T", [65, 96, 113, 128, 129])
+def test_from_few_tokens_to_many(wq, ctx, T):  # noqa: F811
+    X, Wg, Wu = block(T, 300, 1000, BF, T)
+    g, u = X.double() @ Wg.double().T, X.double() @ Wu.double().T
+    got = wq.windq_gated_forward(ctx, X, Wg, Wu, want_saved=True)
+    assert torch.equal(got["gate"], g.to(BF)) and torch.equal(got["up"], u.to(BF))
+    near(got["h"], activation(g, "silu") * u, BF)
+    x, wg, wu, s = codes((T, 1008), 1), codes((300, 1008), 2), codes((300, 1008), 3), scales(300, 2) * 0.05
+    h = wq.windq_gated_int8_forward(ctx, x, scales(T, 1), wg, s, wu, s)
+    near(h, activation(product(x, wg, scales(T, 1), s).double(), "silu") * product(x, wu, scales(T, 1), s).double(), HALF)
+
+
 def exact_gradients(X, Wg, Wu, dH, g, u, act):
     x, dh, g, u = X.double(), dH.double(), g.double(), u.double()
     du, dg = dh * activation(g, act), dh * u * slope(g, act)
