@@ -296,14 +296,15 @@ windq_status launch_weight_gradient(windq_ctx* ctx, const WeightGradient& q, cud
   p.ldo = q.ldw;
   p.stalls = stalls_of(ctx);
   // The width that takes the least time in rounds over the GPU (a chunk of K: 0.23 us at width 128, 0.27 at 192, 0.36 at 256;
-  // a tile 2 us more, 5 where it is split along K).  Tiles that fill less than half of the GPU are split.
+  // a tile 2 us more, 5 where it is split along K).  Tiles that fill less than half of the GPU are split, as far as clusters of
+  // whole SMs find room: 33 of four blocks, 15 of eight.
   const int64_t slots = ctx->sm_count / 2;
   int64_t best = INT64_MAX;
   for (int cols = 128; cols >= 64; cols -= 32) {
     const int width = 2 * cols;
     const int64_t tiles = p.row_tiles * ((q.C + width - 1) / width);
     int splits = 1;
-    while (splits < 4 && tiles * splits * 2 <= slots && p.chunks >= splits * 2 * 4) splits *= 2;
+    while (splits < 4 && tiles * splits * 2 <= slots * (splits == 1 ? 8 : 7) / 9 && p.chunks >= splits * 2 * 4) splits *= 2;
     const int64_t waves = (tiles * splits + slots - 1) / slots;
     const int chunk = std::max(210 + width / 5, width * 139 / 100) * (1256 - width) / 1000;
     const int64_t cost = waves * ((int64_t)(p.chunks + splits - 1) / splits * chunk + (splits > 1 ? 5000 : 2000));
