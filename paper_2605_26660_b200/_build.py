@@ -79,7 +79,7 @@ def binding_command(out: str):
             "-I", INCLUDE, "-I", include, "-I", os.path.join(include, "torch", "csrc", "api", "include"),
             "-I", os.path.join(os.path.dirname(os.path.dirname(nvcc_path())), "include"), "-I", sysconfig.get_paths()["include"],
             os.path.join(CSRC, "binding.cpp"), "-o", out, "-L", HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN",
-            "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+            "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
 
 
 def binding_hash() -> str:

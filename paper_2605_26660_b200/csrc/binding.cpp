@@ -1,10 +1,11 @@
-// Argument marshalling of the feed-forward calls, compiled.  Their kernels for a few tokens take 2 to 15 us, and checking
-// tensors, allocating outputs and converting a dozen arguments took Python 10 us a call; here it takes 2.  Nothing is computed:
-// every function checks its tensors, allocates the outputs it is not given, and calls the C ABI.
+// Argument marshalling of the feed-forward calls, compiled.  Their kernels for a few tokens take 2 to 15 us, and a call through
+// Python's checks, allocations and conversions of a dozen arguments 10 to 12; here it takes 4, of which a launch is 2.6.  Nothing is
+// computed: every function checks its tensors, allocates the outputs it is not given, and calls the C ABI.
 //
 // A function takes (handle, device, stream or None, ...) and returns a tuple whose first item is the status; wrong types raise
 // TypeError, wrong shapes ValueError, before anything is launched.
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -51,13 +52,26 @@ Rows half_of(const Tensor& t, int device, const char* name) {
   TORCH_CHECK_TYPE(code_of(t.scalar_type()) >= 0, name, " must be torch.float16 or torch.bfloat16, got ", t.scalar_type());
   return rows_of(t, t.scalar_type(), device, 8, name);
 }
+// Device memory for `bytes` bytes, straight from torch's allocator (through the dispatcher, with a view where rows are padded, a call
+// takes 1 to 3 us more).
+Tensor fresh(int64_t bytes, int device) {
+  return Tensor(at::detail::empty_cuda({bytes}, at::kByte, at::Device(at::kCUDA, (at::DeviceIndex)device), std::nullopt));
+}
+// A tensor of such memory, from byte `first` on.
+Tensor part_of(const Tensor& memory, at::ScalarType type, int64_t first, at::IntArrayRef sizes, at::IntArrayRef strides) {
+  Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(memory.storage()), c10::DispatchKeySet(c10::DispatchKey::CUDA),
+                                                      c10::scalarTypeToTypeMeta(type));
+  t.unsafeGetTensorImpl()->set_sizes_and_strides(sizes, strides, first / (int64_t)c10::elementSize(type));
+  return t;
+}
+int64_t row_length(int64_t cols, int64_t size) { return cols * size % 32 == 0 ? cols : up(cols, 128 / size); }
+
 // A caller's [rows, cols] output, or a new one.  Rows of a new one that are no multiple of 32 bytes are padded to one of 128: copies
 // of rows that begin in the middle of 32 bytes take up to a third longer (500 tokens x 2 x 5000 x 5000 70 us, x 5056 57).
 Rows rows_out(PyObject* given, Tensor& t, int64_t rows, int64_t cols, at::ScalarType type, int device, int64_t step, const char* name) {
   if (given == Py_None) {
-    const int64_t size = (int64_t)c10::elementSize(type), ld = cols * size % 32 == 0 ? cols : up(cols, 128 / size);
-    t = at::empty({rows, ld}, at::TensorOptions().dtype(type).device(at::kCUDA, (at::DeviceIndex)device));
-    if (ld != cols) t = t.narrow(1, 0, cols);
+    const int64_t size = (int64_t)c10::elementSize(type), ld = row_length(cols, size);
+    t = part_of(fresh(rows * ld * size, device), type, 0, {rows, cols}, {ld, 1});
     return Rows{t.data_ptr(), rows, cols, ld, type};
   }
   t = tensor_of(given, name);
@@ -129,9 +143,18 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   WINDQ_ARGUMENTS(8);
   const Rows x = half_of(tensor_of(a[3], "X"), c.device, "X");
   Tensor codes, scale, values;
-  const Rows q = rows_out(a[5], codes, x.rows, x.cols, at::kChar, c.device, 16, "codes");
-  if (a[6] == Py_None) scale = at::empty({x.rows}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, (at::DeviceIndex)c.device));
-  else scale = tensor_of(a[6], "scale");
+  Rows q;
+  if (a[5] == Py_None && a[6] == Py_None) {  // one allocation: neither is of use without the other
+    q = Rows{nullptr, x.rows, x.cols, row_length(x.cols, 1), at::kChar};
+    const int64_t size = up(x.rows * q.ld, 16);
+    const Tensor memory = fresh(size + 4 * x.rows, c.device);
+    codes = part_of(memory, at::kChar, 0, {x.rows, x.cols}, {q.ld, 1});
+    scale = part_of(memory, at::kFloat, size, {x.rows}, {1});
+    q.p = codes.data_ptr();
+  } else {
+    q = rows_out(a[5], codes, x.rows, x.cols, at::kChar, c.device, 16, "codes");
+    scale = a[6] == Py_None ? part_of(fresh(4 * x.rows, c.device), at::kFloat, 0, {x.rows}, {1}) : tensor_of(a[6], "scale");
+  }
   Rows v;
   if (truth(a[4])) v = rows_out(a[7], values, x.rows, x.cols, x.type, c.device, 8, "values");
   return result(windq_quantize_rows(c.ctx, code_of(x.type), x.p, x.rows, x.cols, x.ld, static_cast<int8_t*>(q.p), q.ld,
