@@ -674,7 +674,8 @@ windq_status windq_adamw_states(windq_ctx* ctx, const windq_adamw_job* jobs, int
  * plans quantise these matrices like any other.)  windq_gated_forward computes both and h in one kernel, windq_gated_backward
  * their gradients, for a consumer that trains on after a plan; windq_quantize_rows turns a weight's rows, when a model is
  * loaded, and every batch of tokens into 8-bit codes with one scale each, and windq_int8_forward (any projection) and
- * windq_gated_int8_forward multiply codes with codes. */
+ * windq_gated_int8_forward multiply codes with codes.  Channels and outputs below 2^26, tokens below 2^31 - 256 (2^28 in the backward
+ * call, whose sums run over them). */
 
 /* Rows of 16-bit values (tokens, or a weight's output channels) as 8-bit codes with one scale a row.  With a = max_j |X[t][j]|:
  *   q[t][j] = 127 X[t][j] / a, the exact quotient rounded to nearest (ties to even), in [-127, 127]

@@ -107,7 +107,8 @@ windq_status launch_gate_gradient(windq_ctx* ctx, const GateArgs& a, cudaStream_
 windq_status check_common(windq_ctx* ctx, const char* who, const void* X, int64_t T, int64_t C, int64_t ldx, int64_t R, int step) {
   WINDQ_REQUIRE(ctx, !*ctx->gave_up, WINDQ_ERR_CUDA, "%s: a wait of an earlier call gave up, its results are invalid (windq_stalls)", who);
   WINDQ_REQUIRE(ctx, T >= 0 && T < (1ll << 31) - 256, WINDQ_ERR_SHAPE, "%s: T = %lld", who, (long long)T);
-  WINDQ_REQUIRE(ctx, R > 0 && C > 0 && R < (1ll << 28) && C < (1ll << 28), WINDQ_ERR_SHAPE, "%s: %lld outputs of %lld channels", who,
+  // (a sum that ran for seconds would look like a stall)
+  WINDQ_REQUIRE(ctx, R > 0 && C > 0 && R < (1ll << 26) && C < (1ll << 26), WINDQ_ERR_SHAPE, "%s: %lld outputs of %lld channels", who,
                 (long long)R, (long long)C);
   WINDQ_REQUIRE(ctx, T == 0 || X, WINDQ_ERR_NULL, "%s: the tokens are NULL", who);
   WINDQ_REQUIRE(ctx, ldx >= C, WINDQ_ERR_SHAPE, "%s: ldx = %lld is below C = %lld", who, (long long)ldx, (long long)C);
@@ -249,6 +250,7 @@ windq_status windq_gated_backward(windq_ctx* ctx, int dtype, int activation, con
   WINDQ_TRY(check_act(ctx, who, activation));
   WINDQ_TRY(check_weight(ctx, who, "Wg", Wg, ldwg, C, 8));
   WINDQ_TRY(check_weight(ctx, who, "Wu", Wu, ldwu, C, 8));
+  WINDQ_REQUIRE(ctx, T < (1ll << 28), WINDQ_ERR_SHAPE, "%s: T = %lld", who, (long long)T);
   WINDQ_REQUIRE(ctx, !gate == !up, WINDQ_ERR_NULL, "%s: one of gate and up is NULL", who);
   if (gate) {
     WINDQ_TRY(check_rows(ctx, who, "gate", gate, ldg, F));

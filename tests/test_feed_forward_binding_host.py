@@ -49,3 +49,14 @@ def test_scratch_for_more_tokens_is_never_less():
         sizes = [bytes_of(T) for T in range(0, 1100)]
         assert sizes == sorted(sizes)
     assert wq.windq_scratch_bytes_int8_forward(-1, 5, 5) == 0 and wq.windq_scratch_bytes_gated_forward(4, 0, 5) == 0
+
+
+def test_a_missing_context_is_refused_by_the_library():
+    lib = wq._lib
+    for status in (lib.windq_quantize_rows(None, 0, None, 4, 64, 64, None, 64, None, None, 0, None),
+                   lib.windq_int8_forward(None, None, 4, 64, 64, None, None, 8, 64, None, 0, None, 8, None),
+                   lib.windq_gated_forward(None, 0, 0, None, 4, 64, 64, None, 64, None, 64, 8, None, 8, None, None, 0, None),
+                   lib.windq_gated_int8_forward(None, 0, None, 4, 64, 64, None, None, 64, None, None, 64, None, 8, 0, None, 8, None),
+                   lib.windq_gated_backward(None, 0, 0, None, 4, 64, 64, None, 64, None, 64, 8, None, None, 8, None, 8, None, 64, None, None,
+                                            64, None)):
+        assert status == 1 and b"ctx is NULL" in lib.windq_last_error(None)

@@ -338,6 +338,13 @@ def test_refusals(wq, ctx):  # noqa: F811
     with pytest.raises(wq.WindqError) as e:
         wq.windq_gated_backward(ctx, X, Wg, Wu, dH, want_dx=False, want_dw=False)
     assert e.value.status == 1
+    at = lambda t: t.data_ptr()  # noqa: E731
+    forward = lambda T, C, ld, F: wq._lib.windq_gated_forward(ctx._h, 0, 0, at(X), T, C, ld, at(Wg), ld, at(Wu), ld, F, at(dH),  # noqa: E731
+                                                              F + -F % 8, None, None, 0, None)
+    assert forward(4, 1 << 26, 1 << 26, 96) == 2 and forward(4, 64, 64, 1 << 26) == 2 and forward((1 << 31) - 256, 64, 64, 96) == 2
+    assert forward(-1, 64, 64, 96) == 2 and forward(4, 0, 64, 96) == 2 and forward(4, 65, 64, 96) == 2
+    assert wq._lib.windq_gated_backward(ctx._h, 0, 0, at(X), 1 << 28, 64, 64, at(Wg), 64, at(Wu), 64, 96, None, None, 0, at(dH), 96, at(X), 64,
+                                        None, None, 0, None) == 2
     odd = torch.zeros((4, 68), dtype=HALF, device="cuda")[:, :64]
     with pytest.raises(wq.WindqError) as e:
         wq.windq_gated_forward(ctx, odd, Wg, Wu)
