@@ -53,8 +53,7 @@ __global__ void __launch_bounds__(kThreads) gate_gradient_kernel(const GateArgs 
     power = gradient_power(top, 1);
     top = 0;
   }
-  const int f = (blockIdx.x * kThreads + threadIdx.x) * 8;
-  if (f < p.half) {
+  for (int f = (blockIdx.x * kThreads + threadIdx.x) * 8; f < p.half; f += gridDim.x * kThreads * 8) {
     const int live = min(8, p.F - f);
     for (int64_t t = blockIdx.y; t < p.T; t += gridDim.y) {
       float g[8], u[8], dh[8], dg[8], du[8];
@@ -94,7 +93,7 @@ constexpr int kMostBlocks = 8192;  // of the kernel above
 constexpr int64_t kTopBytes = 256 + 4 * kMostBlocks;
 template <int DT, bool TOP>
 windq_status launch_gate_gradient(windq_ctx* ctx, const GateArgs& a, cudaStream_t st) {
-  const int64_t across = (a.half + 8 * kThreads - 1) / (8 * kThreads);
+  const int64_t across = std::min<int64_t>((a.half + 8 * kThreads - 1) / (8 * kThreads), kMostBlocks);
   const int64_t down = std::max<int64_t>(1, std::min<int64_t>({a.T, (int64_t)ctx->sm_count * kBlocksPerSm / across, kMostBlocks / across}));
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attrs[2];

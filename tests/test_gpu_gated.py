@@ -230,6 +230,19 @@ def test_zero_and_nonfinite_gradients(wq, ctx, T, dtype):  # noqa: F811
     assert bool(got["dWg"][50].isnan().all()) and int(got["dWg"].isnan().any(dim=1).sum()) == 1
 
 
+def test_a_width_of_more_blocks_than_any(wq, ctx):  # noqa: F811
+    T, F, C = 2, 8192 * 2048 + 72, 8
+    X, Wg, Wu = integers((T, C), 1, HALF), integers((F, C), 2, HALF), integers((F, C), 3, HALF)
+    g, u, dH = integers((T, F), 5, HALF, 32, 64), integers((T, F), 6, HALF, -40, 41), torch.zeros((T, F), dtype=HALF, device="cuda")
+    dH[1, -1], dH[0, 3] = 2, 1                     # few, so that the sums of dX stay exact
+    got = wq.windq_gated_backward(ctx, X, Wg, Wu, dH, gate=g, up=u)
+    for t, f in ((1, F - 1), (0, 3)):
+        dg, du = dH[t, f].double() * u[t, f].double(), dH[t, f].double() * g[t, f].double()
+        assert torch.equal(got["dx"][t], (dg * Wg[f].double() + du * Wu[f].double()).half())
+        assert torch.equal(got["dWg"][f], (dg * X[t].double()).half()) and torch.equal(got["dWu"][f], (du * X[t].double()).half())
+    assert int((got["dWg"] != 0).any(dim=1).sum()) <= 2 and int((got["dWu"] != 0).any(dim=1).sum()) <= 2
+
+
 def test_no_tokens(wq, ctx):  # noqa: F811
     X, Wg, Wu = block(4, 96, 64, HALF, 2)
     f = wq.windq_gated_forward(ctx, X[:0], Wg, Wu, want_saved=True)
