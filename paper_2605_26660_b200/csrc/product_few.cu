@@ -58,28 +58,32 @@ __device__ __forceinline__ void sum_quads(uint32_t base, const uint32_t (&offset
                    : "memory");
     return;
   }
-  uint32_t y[4][U][4];
-#pragma unroll
-  for (int q = 0; q < 4; q++) {
-    if (q < n) {
-      const uint32_t from = cluster_addr(base, q);
-#pragma unroll
-      for (int u = 0; u < U; u++)
-        asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(y[q][u][0]), "=r"(y[q][u][1]), "=r"(y[q][u][2]), "=r"(y[q][u][3])
-                     : "r"(from + offset[u])
-                     : "memory");
-    }
-  }
 #pragma unroll
   for (int u = 0; u < U; u++)
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
-      x[u][k] = y[0][u][k];
+    for (int k = 0; k < 4; k++) x[u][k] = 0;
+  for (int q0 = 0; q0 < n; q0 += 4) {
+    uint32_t y[4][U][4];
 #pragma unroll
-      for (int q = 1; q < 4; q++)
-        if (q < n) x[u][k] = CODES ? x[u][k] + y[q][u][k] : __float_as_uint(__uint_as_float(x[u][k]) + __uint_as_float(y[q][u][k]));
+    for (int q = 0; q < 4; q++) {
+      if (q0 + q < n) {
+        const uint32_t from = cluster_addr(base, q0 + q);
+#pragma unroll
+        for (int u = 0; u < U; u++)
+          asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(y[q][u][0]), "=r"(y[q][u][1]), "=r"(y[q][u][2]), "=r"(y[q][u][3])
+                       : "r"(from + offset[u])
+                       : "memory");
+      }
     }
+#pragma unroll
+    for (int u = 0; u < U; u++)
+#pragma unroll
+      for (int k = 0; k < 4; k++)
+#pragma unroll
+        for (int q = 0; q < 4; q++)
+          if (q0 + q < n) x[u][k] = CODES ? x[u][k] + y[q][u][k] : __float_as_uint(__uint_as_float(x[u][k]) + __uint_as_float(y[q][u][k]));
+  }
 }
 
 // Four neighbouring values of an output row, the last of which may lie beyond its end.
@@ -304,10 +308,12 @@ windq_status launch_few_tokens(windq_ctx* ctx, const Product& q, cudaStream_t st
   const int64_t tiles = (q.N + outputs - 1) / outputs;
   // As many as two blocks an SM hold: 48 tokens x 4096 x 11008 codes in two splits 20.3 us, in four 16.4; 33 tokens x 2 x 11008 x 4096,
   // 172 tiles, whole 20.4, in two 27.9.  Clusters of four do not fill the last slots of every GPC (60 tokens x 2 x 4700 x 5056, 74
-  // tiles: in four splits, 296 blocks, 30.0 us, in two 22.1), and of eight start and join slowly.
+  // tiles: in four splits, 296 blocks, 30.0 us, in two 22.1).  Clusters of eight start and join slowly: for few tiles and a long K alone
+  // (8 x 2 x 1024 x 8192 11.8 -> 9.8, but 48 x 4096 x 11008 codes 16.3 -> 17.8).
   p.splits = 1;
   for (int splits = 2; splits <= 4; splits *= 2)
     if (tiles * splits <= ctx->sm_count * 2 * (splits == 4 ? 9 : 10) / 10 && p.chunks >= splits * 4) p.splits = splits;
+  if (tiles * 8 <= ctx->sm_count && p.chunks >= 8 * 12) p.splits = 8;
   const int stage = kWeightBytes + p.tokens * kChunkBytes;
   p.stages = std::min(kMaxStages, (kSmemLimit - 1024) / stage);
   p.columns = p.tokens <= 32 ? 32 : p.tokens <= 64 ? 64 : 128;

@@ -38,7 +38,7 @@ def test_sizes(wq, ctx, T, R, C, dtype):  # noqa: F811
     check(wq, ctx, T, R, C, dtype, seed=T + R)
 
 
-@pytest.mark.parametrize("T,R,C", [(1, 14336, 4096), (7, 4096, 14336), (48, 11008, 4096), (203, 8192, 1024), (256, 2048, 8192),
+@pytest.mark.parametrize("T,R,C", [(1, 14336, 4096), (7, 4096, 14336), (60, 512, 14336), (3, 100, 30000), (48, 11008, 4096), (203, 8192, 1024), (256, 2048, 8192),
                                    (777, 5120, 2824), (2000, 2056, 1000), (5000, 4093, 300), (600, 512, 16384)])
 def test_larger_sizes(wq, ctx, T, R, C):  # noqa: F811
     check(wq, ctx, T, R, C, BF if T % 2 else HALF, seed=3)
