@@ -728,12 +728,14 @@ windq_status windq_gated_int8_forward(windq_ctx* ctx, int activation, const int8
                                       int64_t ldwu, const float* wu_scale, int64_t F, int dtype, void* H, int64_t ldh, void* stream);
 
 /* Gradients of windq_gated_forward, given dH = the gradient of H:
- *   dU = dH act(g),  dG = dH u act'(g)           (binary32, rounded to `dtype` for the tensor cores)
+ *   dU = dH act(g),  dG = dH u act'(g)           (binary32; into the sums as values of `dtype`, see below)
  *   dX = dG Wg + dU Wu     [T][lddx], nullable
  *   dWg = dG^T X, dWu = dU^T X   [F][lddw], both or neither
  *   gate, up    [T][ldg], both or neither: what the forward call left.  Without them it is computed again, from X, and rounded
  *               as the forward call rounds it.
  *   dH [T][lddh];  lddh, ldg >= F, lddx, lddw >= C, multiples of 8
+ * Into the sums go dG and dU rounded to `dtype`, which costs the gradients about as much precision as their own rounding; of up to
+ * 64 tokens, or T C F up to 2^30, the sums of two such values, which costs none.
  * In fp16 dG and dU are kept times one power of two a call, which puts their largest near 2^15, and the products are
  * divided by it: small gradients lose nothing to fp16's range before they are rounded to the type of the result.
  * The outputs are overwritten, in an order of sums fixed by the sizes: equal calls give equal bits.  With T = 0 dWg and dWu

@@ -12,8 +12,8 @@ constexpr int kThreads = 256;
 struct GateArgs {
   const void *gate, *up, *dH;
   int64_t T, ldg, lddh, half;
-  int F, act;
-  uint16_t* D;     // [T][2 * half]: dG, dU; columns of a half behind F are zeros
+  int F, act, terms;
+  uint16_t* D;     // [T][terms * 2 * half]: dG, dU, and of two terms what rounding took off each; columns of a half behind F are zeros
   uint32_t* top;   // fp16: bits of the largest |dG|, |dU|; bf16: NULL
   uint32_t* tops;  // of every block, before that
 };
@@ -26,6 +26,9 @@ __device__ __forceinline__ void gate_gradient(float g, float u, float dh, int ac
   du = dh * (g * s);
   dg = dh * u * (t == 0.0f ? s : fmaf(slope, t, s));
 }
+
+// What rounding took off x; nothing where it left infinity or NaN, which then stand for themselves.
+__device__ __forceinline__ float rest_of(float x, float rounded) { return fabsf(rounded) < __uint_as_float(0x7f800000u) ? x - rounded : 0.0f; }
 
 // Eight columns a thread, rows gridDim.y apart.  Bound by memory: 6 bytes read and 4 written a value.  fp16's range does not hold
 // what small losses leave, so its values are stored times a power of two (see gradient_power) that a launch with TOP finds
@@ -77,8 +80,21 @@ __global__ void __launch_bounds__(kThreads) gate_gradient_kernel(const GateArgs 
         }
       }
       if (!TOP) {
-        store8(p.D, t * 2 * p.half + f, DT, dg);
-        store8(p.D, t * 2 * p.half + p.half + f, DT, du);
+        const int64_t at = t * p.terms * 2 * p.half + f;
+        store8(p.D, at, DT, dg);
+        store8(p.D, at + p.half, DT, du);
+        if (p.terms == 2) {
+#pragma unroll
+          for (int k = 0; k < 8; k += 2) {
+            const float2 g2 = unpack2(pack2(dg[k], dg[k + 1], DT), DT), u2 = unpack2(pack2(du[k], du[k + 1], DT), DT);
+            dg[k] = rest_of(dg[k], g2.x);
+            dg[k + 1] = rest_of(dg[k + 1], g2.y);
+            du[k] = rest_of(du[k], u2.x);
+            du[k + 1] = rest_of(du[k + 1], u2.y);
+          }
+          store8(p.D, at + 2 * p.half, DT, dg);
+          store8(p.D, at + 3 * p.half, DT, du);
+        }
       }
     }
   }
@@ -147,6 +163,12 @@ windq_status check_act(windq_ctx* ctx, const char* who, int act) {
     if (s_ != WINDQ_OK) return s_;         \
   } while (0)
 
+// Terms of dG and dU on the tensor cores.  One costs dX, dWg and dWu about as much precision as their own rounding does (1.41 times its
+// error; of few tokens, or where one hot channel has most of a gradient's norm, up to 1.8).  With two their own rounding is all there
+// is.  Two is what few tokens take, where they cost next to nothing, and up to 2^30 products, whose time is mostly that of starting kernels
+// (10 x 1000 x 800 13.8 -> 16.5 us, 1000 x 1000 x 1000 27.5 -> 41).
+int64_t two_term_tokens(int64_t C, int64_t F) { return std::max<int64_t>(kMostFew, (1ll << 30) / (C * F)); }
+
 // Sums of products of two codes stay in 32-bit integers up to here.
 constexpr int64_t kMaxCodes = 131071;
 
@@ -175,7 +197,7 @@ windq_status windq_int8_forward(windq_ctx* ctx, const int8_t* X, int64_t T, int6
   WINDQ_REQUIRE(ctx, Y, WINDQ_ERR_NULL, "%s: Y is NULL", who);
   DeviceGuard guard(ctx->device);
   WINDQ_TRY(ensure_scratch(ctx, product_scratch(T)));
-  Product q = {kInt8, dtype, 0, T, R, C, X, ldx, {W, nullptr}, {ldw, 0}, 0, x_scale, {w_scale, nullptr}, nullptr, {Y, nullptr, nullptr}, {ldy, 0, 0},
+  Product q = {kInt8, dtype, 0, T, R, C, X, ldx, {W, nullptr}, {ldw, 0}, 0, 0, x_scale, {w_scale, nullptr}, nullptr, {Y, nullptr, nullptr}, {ldy, 0, 0},
                ctx->scratch};
   return launch_product(ctx, q, (cudaStream_t)stream);
 }
@@ -200,7 +222,7 @@ windq_status windq_gated_int8_forward(windq_ctx* ctx, int activation, const int8
   WINDQ_REQUIRE(ctx, H, WINDQ_ERR_NULL, "%s: H is NULL", who);
   DeviceGuard guard(ctx->device);
   WINDQ_TRY(ensure_scratch(ctx, product_scratch(T)));
-  Product q = {kInt8Gated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, x_scale, {wg_scale, wu_scale}, nullptr,
+  Product q = {kInt8Gated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, 0, x_scale, {wg_scale, wu_scale}, nullptr,
                {H, nullptr, nullptr}, {ldh, 0, 0}, ctx->scratch};
   return launch_product(ctx, q, (cudaStream_t)stream);
 }
@@ -226,15 +248,18 @@ windq_status windq_gated_forward(windq_ctx* ctx, int dtype, int activation, cons
   WINDQ_REQUIRE(ctx, H, WINDQ_ERR_NULL, "%s: H is NULL", who);
   DeviceGuard guard(ctx->device);
   WINDQ_TRY(ensure_scratch(ctx, product_scratch(T)));
-  Product q = {kGated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, nullptr, {nullptr, nullptr}, nullptr,
+  Product q = {kGated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, 0, nullptr, {nullptr, nullptr}, nullptr,
                {H, gate_out, up_out}, {ldh, ldg, ldg}, ctx->scratch};
   return launch_product(ctx, q, (cudaStream_t)stream);
 }
 
 int64_t windq_scratch_bytes_gated_backward(int64_t T, int64_t C, int64_t F, int recompute) {
-  if (T < 0 || C <= 0 || F <= 0) return 0;
+  if (T < 0 || C <= 0 || F <= 0 || C >= 1ll << 26 || F >= 1ll << 26) return 0;
   const int64_t half = windq::round_up(F, 64);
-  return windq::kTopBytes + windq::round_up(4 * T * half, 256) * (recompute ? 2 : 1) + windq::product_scratch(T);
+  // never less for more tokens
+  const int64_t rows = std::max<int64_t>(T, 2 * std::min<int64_t>(T, windq::two_term_tokens(C, F)));
+  return windq::kTopBytes + windq::round_up(4 * rows * half, 256) + (recompute ? windq::round_up(4 * T * half, 256) : 0) +
+         windq::product_scratch(T);
 }
 
 windq_status windq_gated_backward(windq_ctx* ctx, int dtype, int activation, const void* X, int64_t T, int64_t C, int64_t ldx,
@@ -280,18 +305,19 @@ windq_status windq_gated_backward(windq_ctx* ctx, int dtype, int activation, con
     return p;
   };
   uint32_t* top = (uint32_t*)take(kTopBytes);
-  uint16_t* D = (uint16_t*)take(4 * T * half);
+  const int terms = T <= two_term_tokens(C, F) ? 2 : 1;
+  uint16_t* D = (uint16_t*)take(4 * T * half * terms);
   uint16_t* kept = gate ? nullptr : (uint16_t*)take(4 * T * half);
   void* partials = at;
   if (!gate) {
     gate = kept;
     up = kept + T * half;
     ldg = half;
-    Product q = {kGated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, nullptr, {nullptr, nullptr}, nullptr,
+    Product q = {kGated, dtype, activation, T, F, C, X, ldx, {Wg, Wu}, {ldwg, ldwu}, 0, 0, nullptr, {nullptr, nullptr}, nullptr,
                  {nullptr, kept, kept + T * half}, {0, half, half}, partials};
     WINDQ_TRY(launch_product(ctx, q, st));
   }
-  GateArgs a = {gate, up, dH, T, ldg, lddh, half, (int)F, activation, D, dtype == WINDQ_F16 ? top : nullptr, top + 64};
+  GateArgs a = {gate, up, dH, T, ldg, lddh, half, (int)F, activation, terms, D, dtype == WINDQ_F16 ? top : nullptr, top + 64};
   if (a.top) {
     WINDQ_TRY((launch_gate_gradient<WINDQ_F16, true>(ctx, a, st)));
     WINDQ_TRY((launch_gate_gradient<WINDQ_F16, false>(ctx, a, st)));
@@ -299,11 +325,11 @@ windq_status windq_gated_backward(windq_ctx* ctx, int dtype, int activation, con
     WINDQ_TRY((launch_gate_gradient<WINDQ_BF16, false>(ctx, a, st)));
   }
   if (dX) {
-    Product q = {kInputGrad, dtype, 0, T, C, F, D, 2 * half, {Wg, Wu}, {ldwg, ldwu}, half, nullptr, {nullptr, nullptr}, a.top,
+    Product q = {kInputGrad, dtype, 0, T, C, F, D, terms * 2 * half, {Wg, Wu}, {ldwg, ldwu}, half, terms, nullptr, {nullptr, nullptr}, a.top,
                  {dX, nullptr, nullptr}, {lddx, 0, 0}, partials};
     WINDQ_TRY(launch_product(ctx, q, st));
   }
-  if (dWg) WINDQ_TRY(launch_weight_gradient(ctx, WeightGradient{dtype, T, F, C, half, D, X, ldx, a.top, dWg, dWu, lddw}, st));
+  if (dWg) WINDQ_TRY(launch_weight_gradient(ctx, WeightGradient{dtype, terms, T, F, C, half, D, X, ldx, a.top, dWg, dWu, lddw}, st));
   return WINDQ_OK;
 }
 

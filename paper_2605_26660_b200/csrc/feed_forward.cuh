@@ -30,7 +30,8 @@ __device__ __forceinline__ float gradient_power(uint32_t top, int sign) {
 //   kInt8        codes of tokens x codes of a weight: O = D * row_scale[t] * col_scale[n]
 //   kInt8Gated   two weights: O = act(g) u, with g and u such products
 //   kGated       the same of 16-bit tokens and weights; optionally g and u are stored too
-//   kInputGrad   dX: [dG | dU] of the tokens x the two weights, transposed: W(n, k) = W[k][n]
+//   kInputGrad   dX: D of the tokens x the two weights, transposed: W(n, k) = W[k][n].  D is [dG | dU], or, of two terms, [dG | dU |
+//                what rounding took off dG | off dU]
 enum ProductKind { kInt8, kInt8Gated, kGated, kInputGrad };
 
 template <int KIND>
@@ -55,7 +56,8 @@ struct Product {
   int64_t ldx;
   const void* W[2];
   int64_t ldw[2];
-  int64_t half;           // kInputGrad: columns of each half of [dG | dU], a multiple of 64
+  int64_t half;           // kInputGrad: columns of dG in D, a multiple of 64
+  int terms;              // kInputGrad: of D
   const float* row_scale;
   const float* col_scale[2];
   const uint32_t* top;    // fp16 gradients: see gradient_power; nullable
@@ -69,9 +71,9 @@ int64_t product_scratch(int64_t T);
 constexpr int64_t kMostFewGated = 128, kMostFew = 64;
 windq_status launch_few_tokens(windq_ctx* ctx, const Product& q, cudaStream_t st);
 
-// dWg = dG^T X, dWu = dU^T X from D = [dG | dU], [T][2 * half].
+// dWg = dG^T X, dWu = dU^T X from D, [T][terms * 2 * half].
 struct WeightGradient {
-  int dtype;
+  int dtype, terms;
   int64_t T, F, C, half;
   const void* D;
   const void* X;

@@ -307,9 +307,10 @@ __global__ void __launch_bounds__(kMaxThreads, 1)
     };
     auto weights = [&](int c, auto take) {  // the boxes of a chunk: where in the stage, and where from
       if (K::kTransposed) {
-        const bool other = c >= p.half_chunks;
-        const int k0 = (other ? c - p.half_chunks : c) * 64;
-        for (int b = 0; b < 2; b++) take(b * 8192, other ? &wmap1 : &wmap0, n0 + b * 64, k0);
+        int k = c;
+        bool other = false;
+        for (; k >= p.half_chunks; k -= p.half_chunks) other = !other;  // the weights again for the second terms
+        for (int b = 0; b < 2; b++) take(b * 8192, other ? &wmap1 : &wmap0, n0 + b * 64, k * 64);
       } else if (K::kGate) {
 #pragma unroll
         for (int b = 0; b < 4; b++) {
@@ -549,7 +550,7 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   p.dtype = q.dtype;
   p.act = q.act;
   p.half_chunks = (int)((q.K + step - 1) / step);
-  p.chunks = transposed ? 2 * p.half_chunks : p.half_chunks;
+  p.chunks = transposed ? q.terms * 2 * p.half_chunks : p.half_chunks;
   const int outputs = gate ? 128 : 256;
   p.weight_tiles = (int)((q.N + outputs - 1) / outputs);
   const Plan plan = plan_of(q.T, p.weight_tiles, p.chunks, std::min(ctx->sm_count / 2, kMaxPairs));
@@ -576,7 +577,7 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   CUtensorMap x, w[2], o[3];
   WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
   const int type = codes ? -1 : q.dtype, bytes = codes ? 1 : 2;
-  bool ok = make_map_2d(&x, type, q.X, transposed ? 2 * q.half : q.K, q.T, q.ldx * bytes, step, p.tokens / 2);
+  bool ok = make_map_2d(&x, type, q.X, transposed ? q.terms * 2 * q.half : q.K, q.T, q.ldx * bytes, step, p.tokens / 2);
   for (int k = 0; ok && k < (q.W[1] ? 2 : 1); k++)
     ok = transposed ? make_map_2d(&w[k], type, q.W[k], q.N, q.K, q.ldw[k] * bytes, 64, 64)
                     : make_map_2d(&w[k], type, q.W[k], q.K, q.N, q.ldw[k] * bytes, step, gate ? 16 : 128);

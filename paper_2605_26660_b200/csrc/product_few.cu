@@ -30,7 +30,8 @@ constexpr int kWeightBytes = 128 * kChunkBytes;
 struct Args {
   int T, N, dtype, act;
   int chunks, half_chunks;  // of K; of the first weight (kInputGrad)
-  int tokens;               // of the tile: all of them, rounded up
+  int tokens;               // of the tile: all of them, rounded up, and once more where D has two terms
+  int second, half;         // kInputGrad: row of the second terms in the tile, or 0; columns of dG in D
   int splits, stages, columns;  // columns: of tensor memory
   const float* row_scale;
   const float* col_scale[2];
@@ -103,7 +104,7 @@ __device__ __forceinline__ void store_quad(void* O, int64_t ldo, int64_t m, int 
 template <int KIND>
 __device__ __forceinline__ void join(const Args& p, uint32_t base, int wt, int split) {
   using K = Kind<KIND>;
-  constexpr int U = K::kGate ? 2 : 4, outputs = K::kGate ? 64 : 128, quads = outputs / 4;
+  constexpr int U = K::kGate || K::kTransposed ? 2 : 4, outputs = K::kGate ? 64 : 128, quads = outputs / 4;
   const int n0 = wt * outputs, items = max(0, (p.T - split + p.splits - 1) / p.splits) * quads;
   const float unscale = p.top ? gradient_power(*p.top, -1) : 1.0f;
   for (int i = threadIdx.x; i < items; i += U * kThreads) {
@@ -114,6 +115,15 @@ __device__ __forceinline__ void join(const Args& p, uint32_t base, int wt, int s
       offset[u] = (uint32_t)((split + q / quads * p.splits) * kPitch + q % quads * 4) * 4;
     }
     sum_quads<U, K::kCodes>(base, offset, p.splits, x);
+    if (K::kTransposed && p.second) {
+#pragma unroll
+      for (int u = 0; u < U; u++) offset[u] += p.second * kPitch * 4;
+      sum_quads<U, false>(base, offset, p.splits, y);
+#pragma unroll
+      for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) x[u][k] = __float_as_uint(__uint_as_float(x[u][k]) + __uint_as_float(y[u][k]));
+    }
     if (K::kGate) {
 #pragma unroll
       for (int u = 0; u < U; u++) offset[u] += 64 * 4;
@@ -190,15 +200,14 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (warp == 0) {
     const int n0 = wt * (K::kGate ? 64 : 128);
     auto weights = [&](int c, auto take) {  // the two boxes of a chunk
-      const bool other = K::kTransposed && c >= p.half_chunks;
-      const CUtensorMap *first = other ? &wmap1 : &wmap0, *second = K::kGate || other ? &wmap1 : &wmap0;
       if (K::kTransposed) {
+        const bool other = c >= p.half_chunks;
         const int k0 = (other ? c - p.half_chunks : c) * 64;
-        take(0, first, n0, k0);
-        take(1, second, n0 + 64, k0);
+        take(0, other ? &wmap1 : &wmap0, n0, k0);
+        take(1, other ? &wmap1 : &wmap0, n0 + 64, k0);
       } else {
-        take(0, first, c * K::kStepK, n0);
-        take(1, second, c * K::kStepK, K::kGate ? n0 : n0 + 64);
+        take(0, &wmap0, c * K::kStepK, n0);
+        take(1, K::kGate ? &wmap1 : &wmap0, c * K::kStepK, K::kGate ? n0 : n0 + 64);
       }
     };
     if (elect_one())
@@ -214,6 +223,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         mbar_expect(bar, stage_bytes);
         weights(c, [&](int k, const CUtensorMap* map, int x, int y) { tma_load_2d<false>(dst + k * 8192, map, x, y, bar); });
         tma_load_2d<false>(dst + kWeightBytes, &xmap, c * K::kStepK, 0, bar);
+        if (K::kTransposed && p.second) tma_load_2d<false>(dst + kWeightBytes + p.second * kChunkBytes, &xmap, c * 64 + 2 * p.half, 0, bar);
       }
       __syncwarp();
       at.next();
@@ -298,7 +308,10 @@ windq_status launch_few_tokens(windq_ctx* ctx, const Product& q, cudaStream_t st
   p.act = q.act;
   p.half_chunks = (int)((q.K + step - 1) / step);
   p.chunks = transposed ? 2 * p.half_chunks : p.half_chunks;
-  p.tokens = (int)round_up(q.T, 16);
+  const int rows = (int)round_up(q.T, 16);
+  p.second = transposed && q.terms == 2 ? rows : 0;  // two terms of a token are two tokens: the weights are read once
+  p.tokens = rows + p.second;
+  p.half = (int)q.half;
   p.row_scale = q.row_scale;
   p.top = q.top;
   for (int k = 0; k < 2; k++) p.col_scale[k] = q.col_scale[k];
@@ -322,7 +335,7 @@ windq_status launch_few_tokens(windq_ctx* ctx, const Product& q, cudaStream_t st
   CUtensorMap x, w[2];
   WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
   const int type = codes ? -1 : q.dtype, bytes = codes ? 1 : 2;
-  bool ok = make_map_2d(&x, type, q.X, transposed ? 2 * q.half : q.K, q.T, q.ldx * bytes, step, p.tokens);
+  bool ok = make_map_2d(&x, type, q.X, transposed ? q.terms * 2 * q.half : q.K, q.T, q.ldx * bytes, step, rows);
   for (int k = 0; ok && k < (q.W[1] ? 2 : 1); k++)
     ok = make_map_2d(&w[k], type, q.W[k], transposed ? q.N : q.K, transposed ? q.K : q.N, q.ldw[k] * bytes, step, 64);
   if (!q.W[1]) w[1] = w[0];

@@ -1,5 +1,6 @@
 // Gradients of the two weights of a gated block: dWg = dG^T X, dWu = dU^T X, on the tensor cores (tcgen05, accumulators in tensor
-// memory, operands by TMA).  Both operands are transposed: K is the tokens, which are the rows of [dG | dU] and of X.
+// memory, operands by TMA).  Both operands are transposed: K is the tokens, which are the rows of D (see
+// ProductKind) and of X; where D has two terms, X goes by twice.
 //
 // A tile is 256 rows (outputs of the block) x up to 256 columns (channels) on a pair of thread blocks (cta_group::2: each holds half
 // of either operand); persistent over tiles with two accumulators, so that storing a tile overlaps the next.  Warps: one issues TMA
@@ -27,7 +28,8 @@ constexpr int kABytes = 2 * 8192;              // of a stage: 128 rows x 64 toke
 
 struct Args {
   int F, N, dtype;
-  int chunks, block_cols;         // of K (64 tokens each); columns of a thread block's half
+  int chunks, token_chunks;       // of K (64 tokens each, once a term of D); of the tokens
+  int block_cols;                 // columns of a thread block's half
   int row_tiles, col_tiles, group;
   int half_tiles, half;           // row tiles of the first gradient, columns of each half of [dG | dU]
   int splits, stages, accumulators, columns;  // columns: of tensor memory
@@ -145,8 +147,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t dst = base + at.s * stage_bytes, bar = to + at.s * 8;
         if (elect_one() && !*(volatile int*)&dead) {
           if (me == 0) mbar_expect(full(at.s), 2 * stage_bytes);
-          for (int b = 0; b < 2; b++) tma_load_2d<true>(dst + b * 8192, &amap, m0 + b * 64, c * 64, bar);
-          for (int b = 0; b < b_boxes; b++) tma_load_2d<true>(dst + kABytes + b * 8192, &bmap, n0 + b * 64, c * 64, bar);
+          const bool second = c >= p.token_chunks;
+          const int x = m0 + (second ? 2 * p.half : 0), y = (second ? c - p.token_chunks : c) * 64;
+          for (int b = 0; b < 2; b++) tma_load_2d<true>(dst + b * 8192, &amap, x + b * 64, y, bar);
+          for (int b = 0; b < b_boxes; b++) tma_load_2d<true>(dst + kABytes + b * 8192, &bmap, n0 + b * 64, y, bar);
         }
         __syncwarp();
         at.next();
@@ -286,7 +290,8 @@ windq_status launch_weight_gradient(windq_ctx* ctx, const WeightGradient& q, cud
   p.F = (int)q.F;
   p.N = (int)q.C;
   p.dtype = q.dtype;
-  p.chunks = (int)((q.T + 63) / 64);
+  p.token_chunks = (int)((q.T + 63) / 64);
+  p.chunks = q.terms * p.token_chunks;
   p.half = (int)q.half;
   p.half_tiles = (int)((q.F + 255) / 256);
   p.row_tiles = 2 * p.half_tiles;
@@ -326,7 +331,7 @@ windq_status launch_weight_gradient(windq_ctx* ctx, const WeightGradient& q, cud
 
   CUtensorMap a, b, o[2];
   WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
-  const bool ok = make_map_2d(&a, q.dtype, q.D, 2 * q.half, q.T, 4 * q.half, 64, 64) && make_map_2d(&b, q.dtype, q.X, q.C, q.T, 2 * q.ldx, 64, 64) &&
+  const bool ok = make_map_2d(&a, q.dtype, q.D, q.terms * 2 * q.half, q.T, q.terms * 4 * q.half, 64, 64) && make_map_2d(&b, q.dtype, q.X, q.C, q.T, 2 * q.ldx, 64, 64) &&
                   make_map_2d(&o[0], q.dtype, q.dWg, q.C, q.F, 2 * q.ldw, 64, 32) && make_map_2d(&o[1], q.dtype, q.dWu, q.C, q.F, 2 * q.ldw, 64, 32);
   WINDQ_REQUIRE(ctx, ok, WINDQ_ERR_CUDA, "a tensor map could not be made");
   const windq_status ready = prepare_kernel(ctx, kWeightGradient, weight_gradient_kernel, kThreads, kSmemLimit, false);

@@ -154,7 +154,8 @@ def bound(dtype, want, terms):
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 @pytest.mark.parametrize("dtype", [HALF, BF])
-@pytest.mark.parametrize("T,F,C", [(1, 200, 300), (50, 333, 520), (300, 1000, 264), (700, 520, 1000)])
+@pytest.mark.parametrize("T,F,C", [(1, 200, 300), (50, 333, 520), (64, 5000, 4000), (300, 1000, 264), (700, 520, 1000), (65, 6000, 3000),
+                                   (400, 2100, 1400)])
 def test_gradients_against_the_formula(wq, ctx, T, F, C, dtype, act):  # noqa: F811
     gen = torch.Generator(device="cuda").manual_seed(T)
     r = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
@@ -172,6 +173,10 @@ def test_gradients_against_the_formula(wq, ctx, T, F, C, dtype, act):  # noqa: F
         assert bool((off <= bound(dtype, want[k], terms[k])).all()), k
         # a rounding of each term and one of the result, independent of one another: well below twice a rounding in the mean
         assert float(off.norm() / want[k].norm()) < 2 * u, k
+        if T <= 64 or T * F * C <= 1 << 30:
+            # two terms: what is left beside the last rounding, FAST and what the tensor cores cut off (together below 2^-14.5 of the
+            # norm, fp16's rounding above 2^-12.5 of it), adds in squares, below 4 %
+            assert float(off.norm()) < 1.04 * float((want[k].to(dtype).double() - want[k]).norm()), k
     again = wq.windq_gated_backward(ctx, X, Wg, Wu, dH, activation=act)     # computed again from X
     for k in want:
         assert torch.equal(again[k], got[k]), k
