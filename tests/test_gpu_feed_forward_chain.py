@@ -90,3 +90,24 @@ def test_two_contexts_on_two_streams(wq):  # noqa: F811
             assert all(same(a, b) for a, b in zip(run, want[k]))
         assert wq.windq_stalls(contexts[k]) == 0
         wq.windq_destroy(contexts[k])
+
+
+@pytest.mark.parametrize("T,R,C", [(1, 4096, 2048), (20, 2048, 4096), (90, 3000, 1024), (300, 2048, 2048), (1000, 1024, 1024)])
+def test_a_weight_that_the_kernel_before_still_writes(wq, ctx, T, R, C):  # noqa: F811
+    """The product brings its first weights into L2 while the quantiser that writes them runs: it must multiply with what that leaves."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    weights = [torch.randn((R, C), generator=g, device="cuda").half() for _ in range(3)]
+    x = wq.windq_quantize_rows(ctx, torch.randn((T, C), generator=g, device="cuda").half())
+    want = []
+    for w in weights:
+        q = wq.windq_quantize_rows(ctx, w)
+        torch.cuda.synchronize()
+        want.append(wq.windq_int8_forward(ctx, x["codes"], x["scale"], q["codes"], q["scale"]))
+        torch.cuda.synchronize()
+    out = wq.windq_quantize_rows(ctx, weights[0])
+    got = []
+    for k in range(60):
+        wq.windq_quantize_rows(ctx, weights[k % 3], out=out)
+        got.append(wq.windq_int8_forward(ctx, x["codes"], x["scale"], out["codes"], out["scale"]))
+    for k, y in enumerate(got):
+        assert torch.equal(y, want[k % 3]), k
