@@ -164,7 +164,8 @@ __device__ __forceinline__ void add_quad(uint32_t* x, const uint4& y) {
   for (int e = 0; e < 4; e++) x[e] = CODES ? x[e] + v[e] : __float_as_uint(__uint_as_float(x[e]) + __uint_as_float(v[e]));
 }
 
-// What is done with whole sums, by a group of four storing warps.
+// What is done with whole sums, by a group of four storing warps.  (Scales are not read by __ldg, which wants memory that nothing writes
+// while the kernel lives: the kernel before may still have been writing them when this one came.)
 template <int KIND>
 struct Finish {
   using K = Kind<KIND>;
@@ -195,7 +196,7 @@ struct Finish {
 #pragma unroll
       for (int e = 0; e < 2; e++) {
         const int n = n0 + (K::kGate ? quarter * 16 : quarter * 32 + h * 16) + e * 8 + (lane >> 2);
-        col[h][e] = K::kCodes && n < p.N ? __ldg(p.col_scale[K::kGate ? h : 0] + n) : 0.0f;
+        col[h][e] = K::kCodes && n < p.N ? p.col_scale[K::kGate ? h : 0][n] : 0.0f;
       }
   }
   // `units` times 32 tokens of the tile from c on.
@@ -213,7 +214,7 @@ struct Finish {
 #pragma unroll
       for (int k = 0; k < 8; k++) {
         const int t = t0 + c + u * 32 + (k >> 1) * 8 + (lane & 3) * 2 + (k & 1);
-        row[k] = K::kCodes ? (t < p.T ? __ldg(p.row_scale + t) : 0.0f) : unscale;
+        row[k] = K::kCodes ? (t < p.T ? p.row_scale[t] : 0.0f) : unscale;
       }
 #pragma unroll
       for (int h = 0; h < 2; h++)

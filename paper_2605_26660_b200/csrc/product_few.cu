@@ -45,7 +45,8 @@ struct Barriers {
   uint64_t full[kMaxStages], empty[kMaxStages], done;
 };
 
-__device__ __forceinline__ float scale_of(const float* s, int i, int n) { return i < n ? __ldg(s + i) : 0.0f; }
+// (Not __ldg, which wants memory that nothing writes while the kernel lives: the kernel before may still write scales when this one comes.)
+__device__ __forceinline__ float scale_of(const float* s, int i, int n) { return i < n ? s[i] : 0.0f; }
 // Sums over a cluster's n blocks, in the order of their ranks, of U quads at base + offset[u] in each.  Distributed
 // shared memory answers after the better part of a microsecond: the loads of up to four blocks are in flight together.
 template <int U, bool CODES>
@@ -109,10 +110,16 @@ __device__ __forceinline__ void join(const Args& p, uint32_t base, int wt, int s
   const float unscale = p.top ? gradient_power(*p.top, -1) : 1.0f;
   for (int i = threadIdx.x; i < items; i += U * kThreads) {
     uint32_t offset[U], x[U][4], y[U][4];
+    float row[U], col[U][K::kGate ? 2 : 1][4];  // scales, on their way while the sums are read
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const int q = min(i + u * kThreads, items - 1);
-      offset[u] = (uint32_t)((split + q / quads * p.splits) * kPitch + q % quads * 4) * 4;
+      const int q = min(i + u * kThreads, items - 1), t = split + q / quads * p.splits, n = n0 + q % quads * 4;
+      offset[u] = (uint32_t)(t * kPitch + q % quads * 4) * 4;
+      row[u] = K::kCodes ? p.row_scale[t] : unscale;
+#pragma unroll
+      for (int w = 0; w < (K::kGate ? 2 : 1); w++)
+#pragma unroll
+        for (int k = 0; k < 4; k++) col[u][w][k] = K::kCodes ? scale_of(p.col_scale[w], n + k, p.N) : 1.0f;
     }
     sum_quads<U, K::kCodes>(base, offset, p.splits, x);
     if (K::kTransposed && p.second) {
@@ -133,13 +140,12 @@ __device__ __forceinline__ void join(const Args& p, uint32_t base, int wt, int s
     for (int u = 0; u < U; u++) {
       const int q = i + u * kThreads, t = split + q / quads * p.splits, n = n0 + q % quads * 4;
       if (q >= items || n >= p.N) continue;
-      const float row = K::kCodes ? __ldg(p.row_scale + t) : unscale;
       float a[4], b[4], h[4];
 #pragma unroll
       for (int k = 0; k < 4; k++) {
-        a[k] = value_of<K::kCodes>(x[u][k], row, K::kCodes ? scale_of(p.col_scale[0], n + k, p.N) : 1.0f);
+        a[k] = value_of<K::kCodes>(x[u][k], row[u], col[u][0][k]);
         if (K::kGate) {
-          b[k] = value_of<K::kCodes>(y[u][k], row, K::kCodes ? scale_of(p.col_scale[1], n + k, p.N) : 1.0f);
+          b[k] = value_of<K::kCodes>(y[u][k], row[u], col[u][1][k]);
           h[k] = gated(a[k], b[k], p.act);
         }
       }

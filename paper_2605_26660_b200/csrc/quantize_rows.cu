@@ -27,9 +27,10 @@ struct QuantizeArgs {
   int64_t ldv;
 };
 
-// Eight values of a row as they are stored; what lies behind its end reads as zero and is not touched.
+// Eight values of a row as they are stored; what lies behind its end reads as zero and is not touched.  (Not __ldg, which wants memory
+// that nothing writes while the kernel lives: this one is there before the kernel that writes X has ended.)
 __device__ __forceinline__ uint4 load_piece(const uint16_t* row, int i, int C) {
-  if (i * 8 + 8 <= C) return __ldg(reinterpret_cast<const uint4*>(row) + i);
+  if (i * 8 + 8 <= C) return reinterpret_cast<const uint4*>(row)[i];
   uint32_t w[4] = {0, 0, 0, 0};
   for (int k = 0; i * 8 + k < C; k++) w[k >> 1] |= (uint32_t)row[i * 8 + k] << (16 * (k & 1));
   return make_uint4(w[0], w[1], w[2], w[3]);
