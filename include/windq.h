@@ -736,8 +736,10 @@ windq_status windq_gated_int8_forward(windq_ctx* ctx, int activation, const int8
  *   dH [T][lddh];  lddh, ldg >= F, lddx, lddw >= C, multiples of 8
  * Into the sums go dG and dU rounded to `dtype`, which costs the gradients about as much precision as their own rounding; of up to
  * 64 tokens, or T C F up to 2^30, the sums of two such values, which costs none.
- * In fp16 dG and dU are kept times one power of two a call, which puts their largest near 2^15, and the products are
- * divided by it: small gradients lose nothing to fp16's range before they are rounded to the type of the result.
+ * In fp16 dG and dU are kept times one power of two a call, which puts the largest of the finite ones near 2^15, and the products
+ * are divided by it: values down to 2^-28 of the largest lose nothing to fp16's range before they are rounded to the type of the
+ * result; smaller ones are rounded to steps of at most 2^-38 of the largest (a token that far below the others keeps as much).
+ * An infinity or a NaN among them spoils dX of its token and dWg and dWu of its output, and nothing else.
  * The outputs are overwritten, in an order of sums fixed by the sizes: equal calls give equal bits.  With T = 0 dWg and dWu
  * become zero.  Scratch: windq_scratch_bytes_gated_backward (recompute: 1 without gate and up). */
 int64_t windq_scratch_bytes_gated_backward(int64_t T, int64_t C, int64_t F, int recompute);

@@ -14,7 +14,7 @@ struct GateArgs {
   int64_t T, ldg, lddh, half;
   int F, act, terms;
   uint16_t* D;     // [T][terms * 2 * half]: dG, dU, and of two terms what rounding took off each; columns of a half behind F are zeros
-  uint32_t* top;   // fp16: bits of the largest |dG|, |dU|; bf16: NULL
+  uint32_t* top;   // fp16: bits of the largest finite |dG|, |dU|; bf16: NULL
   uint32_t* tops;  // of every block, before that
 };
 
@@ -29,6 +29,12 @@ __device__ __forceinline__ void gate_gradient(float g, float u, float dh, int ac
 
 // What rounding took off x; nothing where it left infinity or NaN, which then stand for themselves.
 __device__ __forceinline__ float rest_of(float x, float rounded) { return fabsf(rounded) < __uint_as_float(0x7f800000u) ? x - rounded : 0.0f; }
+
+// The bits of |x|; of an infinity or a NaN zero: it spoils its own token and output, not the power of two of all others.
+__device__ __forceinline__ uint32_t finite_magnitude(float x) {
+  const uint32_t bits = __float_as_uint(x) & 0x7fffffffu;
+  return bits < 0x7f800000u ? bits : 0;
+}
 
 // Eight columns a thread, rows gridDim.y apart.  Bound by memory: 6 bytes read and 4 written a value.  fp16's range does not hold
 // what small losses leave, so its values are stored times a power of two (see gradient_power) that a launch with TOP finds
@@ -73,7 +79,7 @@ __global__ void __launch_bounds__(kThreads) gate_gradient_kernel(const GateArgs 
       for (int k = 0; k < 8; k++) {
         gate_gradient(g[k], u[k], dh[k], p.act, dg[k], du[k]);
         if (TOP) {
-          top = max(top, max(__float_as_uint(dg[k]) & 0x7fffffffu, __float_as_uint(du[k]) & 0x7fffffffu));
+          top = max(top, max(finite_magnitude(dg[k]), finite_magnitude(du[k])));
         } else {
           dg[k] *= power;
           du[k] *= power;

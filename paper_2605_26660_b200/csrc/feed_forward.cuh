@@ -18,11 +18,10 @@ __device__ __forceinline__ float logistic(float y) {
 }
 
 // The power of two that the gradients of the two products are multiplied with before they are rounded to fp16 (and its
-// inverse, for the products formed from them): their largest then is in [2^14, 2^15).  `top`: bits of the largest |value|.
+// inverse, for the products formed from them): their largest then is in [2^14, 2^15).  `top`: bits of the largest finite |value|.
 __device__ __forceinline__ float gradient_power(uint32_t top, int sign) {
-  const int e = (int)(top >> 23);
-  if (top == 0 || e == 255) return 1.0f;
-  const int shift = min(max(14 + 127 - e, -112), 112);
+  if (top == 0) return 1.0f;
+  const int shift = min(max(14 + 127 - (int)(top >> 23), -112), 112);
   return __uint_as_float((uint32_t)(127 + sign * shift) << 23);
 }
 
