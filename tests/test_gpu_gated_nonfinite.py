@@ -1,9 +1,10 @@
-"""Gradients of the gated block in fp16 where a value is not finite: it spoils its own token and output, and nothing else."""
+"""Gradients of the gated block where a value is not finite: it spoils its own token and output, and nothing else; and gates so far out
+that the forward pass leaves infinities of them, which are shut all the same."""
 import pytest
 import torch
 
 from test_gpu_gated import exact_gradients
-from test_gpu_quantize_rows import HALF, ctx, wq  # noqa: F401
+from test_gpu_quantize_rows import BF, HALF, ctx, wq  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +44,45 @@ def test_no_finite_value_at_all(wq, ctx):  # noqa: F811
     g = torch.ones((70, 72), dtype=HALF, device="cuda")
     got = wq.windq_gated_backward(ctx, X, W, W, torch.full_like(g, float("nan")), gate=g, up=g)
     assert all(bool(got[k].isnan().all()) for k in got)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("T", [20, 300])
+def test_shut_gates_beyond_fp16(wq, ctx, T, act):  # noqa: F811
+    """g = -120000 in every second output, u = +-120000 in every third: kept as infinities, while H is 0 and so are dG and dU."""
+    F, C = 96, 64
+    X = torch.zeros((T, C), dtype=HALF, device="cuda")
+    X[:, 0] = 2
+    Wg, Wu = torch.full((F, C), 0.5, dtype=HALF, device="cuda"), torch.full((F, C), 0.25, dtype=HALF, device="cuda")
+    Wg[:, 0], Wu[:, 0] = 20, 1                            # open gates, g = 40
+    Wg[::2, 0] = -60000
+    Wu[::6, 0], Wu[2::6, 0] = 60000, -60000               # of shut gates alone
+    f = wq.windq_gated_forward(ctx, X, Wg, Wu, activation=act, want_saved=True)
+    assert bool((f["gate"][:, ::2] == float("-inf")).all()) and bool((f["up"][:, ::6] == float("inf")).all())
+    assert bool((f["h"][:, ::2] == 0).all()) and bool((f["h"][:, 1::2] == 80).all())
+    dH = torch.ones((T, F), dtype=HALF, device="cuda")
+    for saved in (dict(gate=f["gate"], up=f["up"]), {}):
+        got = wq.windq_gated_backward(ctx, X, Wg, Wu, dH, activation=act, **saved)
+        # open gates: dG = u = 2, dU = g = 40 (exp(-40) is below a rounding), sums of integers
+        assert bool((got["dWg"][::2] == 0).all()) and bool((got["dWu"][::2] == 0).all())
+        assert bool((got["dWg"][1::2, 0] == 4 * T).all())
+        assert torch.equal(got["dWu"][1::2, 0], torch.full((F // 2,), 80.0 * T, device="cuda").half())
+        assert bool((got["dx"][:, 1:] == 48 * (2 * 0.5 + 40 * 0.25)).all()) and bool((got["dx"][:, 0] == 48 * (2 * 20 + 40)).all())
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", [HALF, BF])
+def test_what_a_shut_gate_does_not_hide(wq, ctx, dtype, act):  # noqa: F811
+    """A NaN in the gate, in up or in the gradient of H is a mistake of the caller's and stays visible."""
+    T, F, C = 7, 64, 64
+    X, W = torch.ones((T, C), dtype=dtype, device="cuda"), torch.ones((F, C), dtype=dtype, device="cuda")
+    for name in ("gate", "up", "dH"):
+        a = dict(gate=torch.full((T, F), float("-inf"), dtype=dtype, device="cuda"), up=torch.full((T, F), float("inf"), dtype=dtype, device="cuda"),
+                 dH=torch.ones((T, F), dtype=dtype, device="cuda"))
+        a[name][2, 5] = float("nan")
+        got = wq.windq_gated_backward(ctx, X, W, W, a.pop("dH"), activation=act, **a)
+        rows = torch.arange(T, device="cuda") != 2
+        assert bool(got["dx"][2].isnan().all()) and bool((got["dx"][rows] == 0).all())
+        outputs = torch.arange(F, device="cuda") != 5
+        assert bool((got["dWg"][outputs] == 0).all()) and bool((got["dWu"][outputs] == 0).all())
+        assert bool(got["dWg"][5].isnan().all())
