@@ -1219,6 +1219,10 @@ def windq_adamw_states(ctx: Context, tensors: AdamwTensors, m_out=None, v_out=No
 
 
 # ---- the feed-forward block: trained in 16 bits, served in 8 ----
+#
+# Rows of a new output that are no multiple of 32 bytes are padded to a multiple of 128, which the kernels copy faster: its stride(0)
+# then is more than its width, it is not contiguous, and it wants reshape where a contiguous tensor takes view.  Only the gradients of
+# weights whose width is a multiple of 8 are always contiguous, as AdamwTensors takes them.  Tensors given as ``out`` are used as they are.
 
 ACTIVATIONS = {"silu": 0, "gelu": 1}   # windq_activation of the header; gelu is its tanh form
 
@@ -1234,8 +1238,9 @@ def windq_quantize_rows(ctx: Context, X: torch.Tensor, *, want_values: bool = Fa
     """8-bit codes of every row of X [T, C] (fp16 or bf16) with one scale a row: codes = round(127 X / a), scale = a / 127,
     a the row's largest magnitude.
 
-    Returns dict(codes int8 [T, C], whose rows are C bytes apart or the next multiple of 128, scale fp32 [T], values [T, C] of X's type
-    | None: what the codes stand for).  ``out`` may hold preallocated tensors under the same keys."""
+    Returns dict(codes int8 [T, C], scale fp32 [T], values [T, C] of X's type | None: what the codes stand for).  ``out`` may hold
+    preallocated tensors under the same keys; the rows of new codes and values are C values apart, or, where that is no multiple of
+    32 bytes, the next multiple of 128 bytes: then they are not contiguous."""
     given = out or {}
     st, codes, scale, values = _binding.quantize_rows(ctx._h.value, ctx.device, stream, X, want_values, given.get("codes"),
                                                       given.get("scale"), given.get("values"))
@@ -1249,7 +1254,8 @@ def windq_int8_forward(ctx: Context, codes: torch.Tensor, scale: torch.Tensor, w
     """Y[t, r] = (sum_j codes[t, j] w_codes[r, j]) scale[t] w_scale[r], the sum exact.
 
     codes int8 [T, C], w_codes int8 [R, C] (rows a multiple of 16 bytes apart, as windq_quantize_rows leaves them); scale
-    fp32 [T], w_scale fp32 [R].  Returns Y [T, R] of ``dtype``, fp16 or bf16 (``out`` if given, whose type counts)."""
+    fp32 [T], w_scale fp32 [R].  Returns Y [T, R] of ``dtype``, fp16 or bf16 (``out`` if given, whose type counts).  The rows of a new Y
+    are R values apart, or, where that is no multiple of 32 bytes, the next multiple of 128 bytes: then it is not contiguous."""
     st, out = _binding.int8_forward(ctx._h.value, ctx.device, stream, codes, scale, w_codes, w_scale, dtype, out)
     if st:
         ctx._check(st)
@@ -1260,7 +1266,7 @@ def windq_gated_int8_forward(ctx: Context, codes: torch.Tensor, scale: torch.Ten
                              wu_codes: torch.Tensor, wu_scale: torch.Tensor, *, activation: str = "silu",
                              dtype: torch.dtype = torch.float16, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """H = act(g) u with g and u as windq_int8_forward forms them from the two weights [F, C], before its rounding to 16
-    bits.  Returns H [T, F] of ``dtype``, fp16 or bf16 (``out`` if given, whose type counts)."""
+    bits.  Returns H [T, F] of ``dtype``, fp16 or bf16 (``out`` if given, whose type counts), its rows apart as windq_int8_forward's."""
     st, out = _binding.gated_int8_forward(ctx._h.value, ctx.device, stream, codes, scale, wg_codes, wg_scale, wu_codes,
                                           wu_scale, _activation(activation), dtype, out)
     if st:
@@ -1274,7 +1280,8 @@ def windq_gated_forward(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: tor
     (the tanh form).
 
     Returns dict(h [T, F], gate, up [T, F] | None: both products, rounded, for windq_gated_backward).  ``out`` may hold
-    preallocated tensors under the same keys.  Autograd records nothing: the gradients are windq_gated_backward's."""
+    preallocated tensors under the same keys; the rows of new ones are F values apart, or, where that is no multiple of 32 bytes, the
+    next multiple of 128 bytes: then they are not contiguous.  Autograd records nothing: the gradients are windq_gated_backward's."""
     given = out or {}
     st, h, gate, up = _binding.gated_forward(ctx._h.value, ctx.device, stream, X, Wg, Wu, _activation(activation), want_saved,
                                              given.get("h"), given.get("gate"), given.get("up"))
@@ -1302,7 +1309,8 @@ def windq_gated_backward(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: to
     without them they are computed again.
 
     Returns dict(dx [T, C] | None, dWg, dWu [F, C] | None), of X's type, overwritten, not added to.  ``out`` may hold
-    preallocated tensors under the same keys."""
+    preallocated tensors under the same keys.  New dWg and dWu are contiguous where C is a multiple of 8; the rows of a new dx are C
+    values apart, or, where that is no multiple of 32 bytes, the next multiple of 128 bytes."""
     given = out or {}
     st, dx, dWg, dWu = _binding.gated_backward(ctx._h.value, ctx.device, stream, X, Wg, Wu, _activation(activation), dH, gate, up,
                                                want_dx, want_dw, given.get("dx"), given.get("dWg"), given.get("dWu"))

@@ -67,10 +67,12 @@ Tensor part_of(const Tensor& memory, at::ScalarType type, int64_t first, at::Int
 int64_t row_length(int64_t cols, int64_t size) { return cols * size % 32 == 0 ? cols : up(cols, 128 / size); }
 
 // A caller's [rows, cols] output, or a new one.  Rows of a new one that are no multiple of 32 bytes are padded to one of 128: copies
-// of rows that begin in the middle of 32 bytes take up to a third longer (500 tokens x 2 x 5000 x 5000 70 us, x 5056 57).
+// of rows that begin in the middle of 32 bytes take up to a third longer (500 tokens x 2 x 5000 x 5000 70 us, x 5056 57).  A new DENSE
+// one is padded only where the library wants its rows apart.
+template <bool DENSE = false>
 Rows rows_out(PyObject* given, Tensor& t, int64_t rows, int64_t cols, at::ScalarType type, int device, int64_t step, const char* name) {
   if (given == Py_None) {
-    const int64_t size = (int64_t)c10::elementSize(type), ld = row_length(cols, size);
+    const int64_t size = (int64_t)c10::elementSize(type), ld = DENSE && cols % step == 0 ? cols : row_length(cols, size);
     t = part_of(fresh(rows * ld * size, device), type, 0, {rows, cols}, {ld, 1});
     return Rows{t.data_ptr(), rows, cols, ld, type};
   }
@@ -249,8 +251,8 @@ PyObject* gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Tensor dX, dWg, dWu;
   if (truth(a[10])) dx = rows_out(a[12], dX, T, C, q.x.type, c.device, 8, "dx");
   if (truth(a[11])) {
-    dg = rows_out(a[13], dWg, F, C, q.x.type, c.device, 8, "dWg");
-    du = rows_out(a[14], dWu, F, C, q.x.type, c.device, 8, "dWu");
+    dg = rows_out<true>(a[13], dWg, F, C, q.x.type, c.device, 8, "dWg");  // the optimiser takes contiguous gradients
+    du = rows_out<true>(a[14], dWu, F, C, q.x.type, c.device, 8, "dWu");
     TORCH_CHECK_VALUE(dg.ld == du.ld, "dWg and dWu must have the same stride between rows");
   }
   return result(windq_gated_backward(c.ctx, code_of(q.x.type), act, q.x.p, T, C, q.x.ld, q.g.p, q.g.ld, q.u.p, q.u.ld, F, g.p, u.p, g.ld, dh.p,
