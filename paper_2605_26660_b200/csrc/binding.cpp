@@ -3,7 +3,8 @@
 // computed: every function checks its tensors, allocates the outputs it is not given, and calls the C ABI.
 //
 // A function takes (handle, device, stream or None, ...) and returns a tuple whose first item is the status; wrong types raise
-// TypeError, wrong shapes ValueError, before anything is launched.
+// TypeError, wrong shapes ValueError, before anything is launched.  The interpreter lock is released while memory is allocated and the
+// library runs.
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
@@ -52,9 +53,25 @@ Rows half_of(const Tensor& t, int device, const char* name) {
   TORCH_CHECK_TYPE(code_of(t.scalar_type()) >= 0, name, " must be torch.float16 or torch.bfloat16, got ", t.scalar_type());
   return rows_of(t, t.scalar_type(), device, 8, name);
 }
+// Gives the interpreter lock to other threads for as long as it lives: a launch waits where the stream's queue is full, an allocation for
+// the device, and what the stream waits for may be another Python thread's to do.  No Python object is touched meanwhile.
+class Unlocked {
+  PyThreadState* state_ = PyEval_SaveThread();
+
+ public:
+  Unlocked() = default;
+  Unlocked(const Unlocked&) = delete;
+  ~Unlocked() { PyEval_RestoreThread(state_); }
+};
+template <class F, class... A>
+windq_status unlocked(F call, const A&... arguments) {
+  const Unlocked others;
+  return call(arguments...);
+}
 // Device memory for `bytes` bytes, straight from torch's allocator (through the dispatcher, with a view where rows are padded, a call
 // takes 1 to 3 us more).
 Tensor fresh(int64_t bytes, int device) {
+  const Unlocked others;
   return Tensor(at::detail::empty_cuda({bytes}, at::kByte, at::Device(at::kCUDA, (at::DeviceIndex)device), std::nullopt));
 }
 // A tensor of such memory, from byte `first` on.
@@ -159,7 +176,7 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   Rows v;
   if (truth(a[4])) v = rows_out(a[7], values, x.rows, x.cols, x.type, c.device, 8, "values");
-  return result(windq_quantize_rows(c.ctx, code_of(x.type), x.p, x.rows, x.cols, x.ld, static_cast<int8_t*>(q.p), q.ld,
+  return result(unlocked(windq_quantize_rows, c.ctx, code_of(x.type), x.p, x.rows, x.cols, x.ld, static_cast<int8_t*>(q.p), q.ld,
                                     scales_of(scale, x.rows, c.device, "scale"), v.p, v.ld, c.stream),
                 codes, scale, values);
   END_HANDLE_TH_ERRORS
@@ -175,7 +192,7 @@ PyObject* int8_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const float* sw = scales_of(tensor_of(a[6], "w_scale"), w.rows, c.device, "w_scale");
   Tensor out;
   const Rows y = rows_out(a[8], out, x.rows, w.rows, out_type(a[7], a[8]), c.device, 8, "out");
-  return result(windq_int8_forward(c.ctx, static_cast<int8_t*>(x.p), x.rows, x.cols, x.ld, sx, static_cast<int8_t*>(w.p), w.rows, w.ld, sw,
+  return result(unlocked(windq_int8_forward, c.ctx, static_cast<int8_t*>(x.p), x.rows, x.cols, x.ld, sx, static_cast<int8_t*>(w.p), w.rows, w.ld, sw,
                                    code_of(y.type), y.p, y.ld, c.stream),
                 out);
   END_HANDLE_TH_ERRORS
@@ -195,7 +212,7 @@ PyObject* gated_int8_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (PyErr_Occurred()) throw python_error();
   Tensor out;
   const Rows h = rows_out(a[11], out, x.rows, g.rows, out_type(a[10], a[11]), c.device, 8, "out");
-  return result(windq_gated_int8_forward(c.ctx, act, static_cast<int8_t*>(x.p), x.rows, x.cols, x.ld, sx, static_cast<int8_t*>(g.p), g.ld, sg,
+  return result(unlocked(windq_gated_int8_forward, c.ctx, act, static_cast<int8_t*>(x.p), x.rows, x.cols, x.ld, sx, static_cast<int8_t*>(g.p), g.ld, sg,
                                          static_cast<int8_t*>(u.p), u.ld, su, g.rows, code_of(h.type), h.p, h.ld, c.stream),
                 out);
   END_HANDLE_TH_ERRORS
@@ -225,7 +242,7 @@ PyObject* gated_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     u = rows_out(a[10], up_, T, F, q.x.type, c.device, 8, "up");
     TORCH_CHECK_VALUE(g.ld == u.ld, "gate and up must have the same stride between rows");
   }
-  return result(windq_gated_forward(c.ctx, code_of(q.x.type), act, q.x.p, T, q.x.cols, q.x.ld, q.g.p, q.g.ld, q.u.p, q.u.ld, F, o.p, o.ld, g.p,
+  return result(unlocked(windq_gated_forward, c.ctx, code_of(q.x.type), act, q.x.p, T, q.x.cols, q.x.ld, q.g.p, q.g.ld, q.u.p, q.u.ld, F, o.p, o.ld, g.p,
                                     u.p, g.ld, c.stream),
                 h, gate, up_);
   END_HANDLE_TH_ERRORS
@@ -255,7 +272,7 @@ PyObject* gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     du = rows_out<true>(a[14], dWu, F, C, q.x.type, c.device, 8, "dWu");
     TORCH_CHECK_VALUE(dg.ld == du.ld, "dWg and dWu must have the same stride between rows");
   }
-  return result(windq_gated_backward(c.ctx, code_of(q.x.type), act, q.x.p, T, C, q.x.ld, q.g.p, q.g.ld, q.u.p, q.u.ld, F, g.p, u.p, g.ld, dh.p,
+  return result(unlocked(windq_gated_backward, c.ctx, code_of(q.x.type), act, q.x.p, T, C, q.x.ld, q.g.p, q.g.ld, q.u.p, q.u.ld, F, g.p, u.p, g.ld, dh.p,
                                      dh.ld, dx.p, dx.ld, dg.p, du.p, dg.ld, c.stream),
                 dX, dWg, dWu);
   END_HANDLE_TH_ERRORS
