@@ -4,9 +4,9 @@ Every function below has the name of the C-ABI entry point it calls
 (``include/windq.h``) and does nothing but check tensor types, allocate output
 tensors with torch, pass raw device pointers and the current CUDA stream, and
 turn a non-zero status into ``WindqError`` (for the feed-forward calls most of
-that is compiled: ``csrc/binding.cpp``).  All arithmetic happens in the CUDA
-kernels.  There is no CPU fallback: if the shared library is missing and cannot
-be built, importing this package raises.
+that is compiled: ``csrc/binding.cpp``, loaded by the first of them).  All
+arithmetic happens in the CUDA kernels.  There is no CPU fallback: if the shared
+library is missing and cannot be built, importing this package raises.
 """
 from __future__ import annotations
 
@@ -15,6 +15,7 @@ import ctypes
 import importlib
 import operator
 import os
+import threading
 
 import torch
 
@@ -127,18 +128,29 @@ def _load() -> ctypes.CDLL:
     return lib
 
 
+_binding_lock = threading.Lock()
+
+
 def _load_binding():
-    """The compiled marshalling of the feed-forward calls (csrc/binding.cpp)."""
-    try:
-        _build.build_binding()
-    except Exception as exc:  # no compiler, or a compile error
-        if not os.path.exists(_build.BINDING):
-            raise ImportError("the compiled binding is not built and cannot be built here: %s" % exc) from exc
-    return importlib.import_module("._binding", __name__)
+    """The compiled marshalling of the feed-forward calls (csrc/binding.cpp), built first where it is not current: one for another
+    torch, Python or header is never loaded."""
+    with _binding_lock:
+        try:
+            _build.build_binding()
+        except Exception as exc:  # no compiler, a torch without CUDA, or a compile error
+            raise ImportError("the compiled binding is not current and cannot be built here: %s" % exc) from exc
+        return importlib.import_module("._binding", __name__)
+
+
+class _Unloaded:
+    """Stands for the compiled binding until a feed-forward call needs it; importing the module then puts it in this one's place."""
+
+    def __getattr__(self, name):
+        return getattr(_load_binding(), name)
 
 
 _lib = _load()
-_binding = _load_binding()
+_binding = _Unloaded()
 LIBRARY_PATH = _build.LIB
 
 

@@ -68,14 +68,16 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 # ---- the compiled binding: csrc/binding.cpp against torch's headers, linked to the library beside it ----
 
+BINDING_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden"]
+
+
 def binding_command(out: str):
     import sysconfig
 
     import torch
     base = os.path.dirname(torch.__file__)
     include = os.path.join(base, "include")
-    return [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
-            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+    return [shutil.which("g++") or "g++", *BINDING_FLAGS, "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
             "-I", INCLUDE, "-I", include, "-I", os.path.join(include, "torch", "csrc", "api", "include"),
             "-I", os.path.join(os.path.dirname(os.path.dirname(nvcc_path())), "include"), "-I", sysconfig.get_paths()["include"],
             os.path.join(CSRC, "binding.cpp"), "-o", out, "-L", HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN",
@@ -83,8 +85,11 @@ def binding_command(out: str):
 
 
 def binding_hash() -> str:
+    """Of all that a built binding fits: its sources, this Python and this torch.  Needs no compiler."""
+    import sys
+
     import torch
-    h = hashlib.sha256((torch.__version__ + " ".join(binding_command("")[1:6])).encode())
+    h = hashlib.sha256(" ".join([torch.__version__, str(torch._C._GLIBCXX_USE_CXX11_ABI), sys.version, *BINDING_FLAGS]).encode())
     for f in (os.path.join(CSRC, "binding.cpp"), os.path.join(INCLUDE, "windq.h")):
         with open(f, "rb") as fh:
             h.update(fh.read())
