@@ -74,11 +74,11 @@ Tensor fresh(int64_t bytes, int device) {
   const Unlocked others;
   return Tensor(at::detail::empty_cuda({bytes}, at::kByte, at::Device(at::kCUDA, (at::DeviceIndex)device), std::nullopt));
 }
-// A tensor of such memory, from byte `first` on.
-Tensor part_of(const Tensor& memory, at::ScalarType type, int64_t first, at::IntArrayRef sizes, at::IntArrayRef strides) {
+// A tensor of such memory.
+Tensor tensor_in(const Tensor& memory, at::ScalarType type, at::IntArrayRef sizes, at::IntArrayRef strides) {
   Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(memory.storage()), c10::DispatchKeySet(c10::DispatchKey::CUDA),
                                                       c10::scalarTypeToTypeMeta(type));
-  t.unsafeGetTensorImpl()->set_sizes_and_strides(sizes, strides, first / (int64_t)c10::elementSize(type));
+  t.unsafeGetTensorImpl()->set_sizes_and_strides(sizes, strides);
   return t;
 }
 int64_t row_length(int64_t cols, int64_t size) { return cols * size % 32 == 0 ? cols : up(cols, 128 / size); }
@@ -90,7 +90,7 @@ template <bool DENSE = false>
 Rows rows_out(PyObject* given, Tensor& t, int64_t rows, int64_t cols, at::ScalarType type, int device, int64_t step, const char* name) {
   if (given == Py_None) {
     const int64_t size = (int64_t)c10::elementSize(type), ld = DENSE && cols % step == 0 ? cols : row_length(cols, size);
-    t = part_of(fresh(rows * ld * size, device), type, 0, {rows, cols}, {ld, 1});
+    t = tensor_in(fresh(rows * ld * size, device), type, {rows, cols}, {ld, 1});
     return Rows{t.data_ptr(), rows, cols, ld, type};
   }
   t = tensor_of(given, name);
@@ -162,18 +162,10 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   WINDQ_ARGUMENTS(8);
   const Rows x = half_of(tensor_of(a[3], "X"), c.device, "X");
   Tensor codes, scale, values;
-  Rows q;
-  if (a[5] == Py_None && a[6] == Py_None) {  // one allocation: neither is of use without the other
-    q = Rows{nullptr, x.rows, x.cols, row_length(x.cols, 1), at::kChar};
-    const int64_t size = up(x.rows * q.ld, 16);
-    const Tensor memory = fresh(size + 4 * x.rows, c.device);
-    codes = part_of(memory, at::kChar, 0, {x.rows, x.cols}, {q.ld, 1});
-    scale = part_of(memory, at::kFloat, size, {x.rows}, {1});
-    q.p = codes.data_ptr();
-  } else {
-    q = rows_out(a[5], codes, x.rows, x.cols, at::kChar, c.device, 16, "codes");
-    scale = a[6] == Py_None ? part_of(fresh(4 * x.rows, c.device), at::kFloat, 0, {x.rows}, {1}) : tensor_of(a[6], "scale");
-  }
+  // Memory of its own for each: who keeps or saves a weight's scales does not keep its codes with them.
+  const Rows q = rows_out(a[5], codes, x.rows, x.cols, at::kChar, c.device, 16, "codes");
+  if (a[6] == Py_None) scale = tensor_in(fresh(4 * x.rows, c.device), at::kFloat, {x.rows}, {1});
+  else scale = tensor_of(a[6], "scale");
   Rows v;
   if (truth(a[4])) v = rows_out(a[7], values, x.rows, x.cols, x.type, c.device, 8, "values");
   return result(unlocked(windq_quantize_rows, c.ctx, code_of(x.type), x.p, x.rows, x.cols, x.ld, static_cast<int8_t*>(q.p), q.ld,
