@@ -45,8 +45,8 @@ struct Args {
   int chunks, half_chunks;      // of K; of the first weight (kInputGrad)
   int tokens;                   // of a tile
   int token_tiles, weight_tiles, group;
-  int whole_tiles;              // dealt out; the tiles after them are cut
-  int pairs;                    // that the cut ones are cut for
+  int pairs;
+  bool cut;                     // tiles, along K, into a share for each pair; otherwise whole ones are dealt out
   int stages;
   const float* row_scale;
   const float* col_scale[2];
@@ -69,10 +69,8 @@ __device__ __forceinline__ void tile_at(const Args& p, int tile, int& tt, int& w
   tt = g * p.group + rest - wt * rows;
 }
 
-// The cut tiles as units of a chunk of a tile, tile by tile: where the share of pair i begins.
-__device__ __forceinline__ int share(const Args& p, int i) {
-  return (int)((int64_t)(p.token_tiles * p.weight_tiles - p.whole_tiles) * p.chunks * i / p.pairs);
-}
+// Cut tiles as units of a chunk of a tile, tile by tile: where the share of pair i begins.
+__device__ __forceinline__ int share(const Args& p, int i) { return (int)((int64_t)p.token_tiles * p.weight_tiles * p.chunks * i / p.pairs); }
 // Where a pair's piece lies: its share has at most two, the first, and one that begins a tile later.  As the threads hold it: 32
 // tokens as eight times 16 bytes a lane of the accumulators.
 __device__ __forceinline__ uint32_t* piece_of(const Args& p, int pair, int later, int me) {
@@ -82,31 +80,32 @@ __device__ __forceinline__ uint32_t* piece_of(const Args& p, int pair, int later
 // What a pair does, in order; every warp walks through the same.
 struct Walk {
   const Args& p;
-  const int pair, pairs;
-  int begin, at, end, next_tile;  // of its share of units; the next of its whole tiles
-  int tile, c0, c1;               // now
-  __device__ explicit Walk(const Args& p) : p(p), pair(blockIdx.x >> 1), pairs(gridDim.x >> 1) {
-    next_tile = pair;
-    at = begin = share(p, min(pair, p.pairs));
-    end = share(p, min(pair + 1, p.pairs));
+  const int pair;
+  int begin = 0, at = 0, end = 0;  // of its share of units
+  int next_tile;                   // of its whole tiles
+  int tile, c0, c1;                // now
+  __device__ explicit Walk(const Args& p) : p(p), pair(blockIdx.x >> 1), next_tile(blockIdx.x >> 1) {
+    if (p.cut) {
+      at = begin = share(p, pair);
+      end = share(p, pair + 1);
+    }
   }
   __device__ __forceinline__ bool next() {
-    if (next_tile < p.whole_tiles) {
-      tile = next_tile;
-      next_tile += pairs;
-      c0 = 0;
-      c1 = p.chunks;
+    if (p.cut) {
+      if (at >= end) return false;
+      tile = at / p.chunks;
+      c0 = at - tile * p.chunks;
+      c1 = min(p.chunks, end - tile * p.chunks);
+      at += c1 - c0;
       return true;
     }
-    if (at >= end) return false;
-    const int k = at / p.chunks;
-    tile = p.whole_tiles + k;
-    c0 = at - k * p.chunks;
-    c1 = min(p.chunks, end - k * p.chunks);
-    at += c1 - c0;
-    return true;
+    tile = next_tile;
+    next_tile += p.pairs;
+    c0 = 0;
+    c1 = p.chunks;
+    return tile < p.token_tiles * p.weight_tiles;
   }
-  __device__ __forceinline__ bool later() const { return (tile - p.whole_tiles) * p.chunks + c0 != begin; }
+  __device__ __forceinline__ bool later() const { return tile * p.chunks + c0 != begin; }
 };
 
 // The four warps of a group that stores.
@@ -439,12 +438,12 @@ __global__ void __launch_bounds__(128)
     combine_kernel(const __grid_constant__ CUtensorMap omap0, const __grid_constant__ CUtensorMap omap1,
                    const __grid_constant__ CUtensorMap omap2, const __grid_constant__ Args p) {
   __shared__ __align__(1024) uint8_t boxes[kBoxesSaved * kBoxBytes];
-  const int me = blockIdx.x & 1, cut = blockIdx.x >> 1, c = blockIdx.y * 32, s = cut * p.chunks;
+  const int me = blockIdx.x & 1, tile = blockIdx.x >> 1, c = blockIdx.y * 32, s = tile * p.chunks;
   launch_dependents();
   wait_for_predecessor();
   Finish<KIND> out(p, &omap0, &omap1, &omap2, smem_addr(boxes), 2, 0, 0);
-  out.open(p.whole_tiles + cut, me);
-  int q = (int)((int64_t)p.pairs * cut / (p.token_tiles * p.weight_tiles - p.whole_tiles));  // near the pair that holds the first unit
+  out.open(tile, me);
+  int q = (int)((int64_t)p.pairs * tile / (p.token_tiles * p.weight_tiles));  // near the pair that holds the first unit
   while (share(p, q + 1) <= s) q++;
   while (share(p, q) > s) q--;
   if (share(p, q + 1) >= s + p.chunks || c >= out.tokens) return;  // one pair had all of it; or no such tokens
@@ -523,10 +522,9 @@ windq_status launch(windq_ctx* ctx, const CUtensorMap& x, const CUtensorMap (&w)
   cudaLaunchAttribute attrs[2];
   overlapped_launch(cfg, attrs, blocks, threads, 2, smem, st);
   WINDQ_CUDA(ctx, cudaLaunchKernelEx(&cfg, product_kernel<KIND>, x, w[0], w[1], o[0], o[1], o[2], p));
-  const int cut = p.token_tiles * p.weight_tiles - p.whole_tiles;
-  if (cut) {
+  if (p.cut) {
     cudaLaunchConfig_t second = {};
-    overlapped_launch(second, attrs, cut * 2, 128, 1, 0, st);
+    overlapped_launch(second, attrs, p.token_tiles * p.weight_tiles * 2, 128, 1, 0, st);
     second.gridDim.y = (p.tokens + 31) / 32;
     WINDQ_CUDA(ctx, cudaLaunchKernelEx(&second, combine_kernel<KIND>, o[0], o[1], o[2], p));
   }
@@ -557,8 +555,8 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   const Plan plan = plan_of(q.T, p.weight_tiles, p.chunks, std::min(ctx->sm_count / 2, kMaxPairs));
   p.tokens = plan.tokens;
   p.pairs = plan.pairs;
+  p.cut = plan.cut;
   p.token_tiles = (int)((q.T + p.tokens - 1) / p.tokens);
-  p.whole_tiles = plan.cut ? 0 : p.token_tiles * p.weight_tiles;
   // 24 MB of tokens: 4096 x 4096 x 22016 and its weights' gradients together 1205 us, with 48 MB 1240, with 96 1305
   p.group = (int)std::max<int64_t>(1, std::min<int64_t>(p.token_tiles, (24ll << 20) / ((int64_t)p.chunks * kChunkBytes * p.tokens)));
   p.row_scale = q.row_scale;
@@ -578,15 +576,15 @@ windq_status launch_product(windq_ctx* ctx, const Product& q, cudaStream_t st) {
   CUtensorMap x, w[2], o[3];
   WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
   const int type = codes ? -1 : q.dtype, bytes = codes ? 1 : 2;
-  bool ok = make_map_2d(&x, type, q.X, transposed ? q.terms * 2 * q.half : q.K, q.T, q.ldx * bytes, step, p.tokens / 2);
+  bool ok = make_map_2d(&x, type, q.X, transposed ? q.terms * 2 * q.half : q.K, q.T, q.ldx * bytes, p.tokens / 2);
   for (int k = 0; ok && k < (q.W[1] ? 2 : 1); k++)
-    ok = transposed ? make_map_2d(&w[k], type, q.W[k], q.N, q.K, q.ldw[k] * bytes, 64, 64)
-                    : make_map_2d(&w[k], type, q.W[k], q.K, q.N, q.ldw[k] * bytes, step, gate ? 16 : 128);
+    ok = transposed ? make_map_2d(&w[k], type, q.W[k], q.N, q.K, q.ldw[k] * bytes, 64)
+                    : make_map_2d(&w[k], type, q.W[k], q.K, q.N, q.ldw[k] * bytes, gate ? 16 : 128);
   if (!q.W[1]) w[1] = w[0];
   const CUtensorMap* any = nullptr;
   for (int k = 0; ok && k < 3; k++) {
     if (!q.O[k]) continue;
-    ok = make_map_2d(&o[k], q.dtype, q.O[k], q.N, q.T, q.ldo[k] * 2, 64, 32);
+    ok = make_map_2d(&o[k], q.dtype, q.O[k], q.N, q.T, q.ldo[k] * 2, 32);
     any = &o[k];
   }
   WINDQ_REQUIRE(ctx, ok, WINDQ_ERR_CUDA, "a tensor map could not be made");

@@ -341,9 +341,9 @@ windq_status launch_few_tokens(windq_ctx* ctx, const Product& q, cudaStream_t st
   CUtensorMap x, w[2];
   WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
   const int type = codes ? -1 : q.dtype, bytes = codes ? 1 : 2;
-  bool ok = make_map_2d(&x, type, q.X, transposed ? q.terms * 2 * q.half : q.K, q.T, q.ldx * bytes, step, rows);
+  bool ok = make_map_2d(&x, type, q.X, transposed ? q.terms * 2 * q.half : q.K, q.T, q.ldx * bytes, rows);
   for (int k = 0; ok && k < (q.W[1] ? 2 : 1); k++)
-    ok = make_map_2d(&w[k], type, q.W[k], transposed ? q.N : q.K, transposed ? q.K : q.N, q.ldw[k] * bytes, step, 64);
+    ok = make_map_2d(&w[k], type, q.W[k], transposed ? q.N : q.K, transposed ? q.K : q.N, q.ldw[k] * bytes, 64);
   if (!q.W[1]) w[1] = w[0];
   WINDQ_REQUIRE(ctx, ok, WINDQ_ERR_CUDA, "a tensor map could not be made");
   const int blocks = (int)(tiles * p.splits);

@@ -321,19 +321,16 @@ inline bool make_map(CUtensorMap* map, int dtype, const void* base, int64_t inne
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// A row-major array [rows][inner] of 16-bit values, or of bytes (dtype < 0), its rows `row_bytes` apart, in boxes of
-// box_rows x box_inner: with the 128-byte swizzle where a box is 128 bytes wide, else as rows one after another.
-inline bool make_map_2d(CUtensorMap* map, int dtype, const void* base, int64_t inner, int64_t rows, int64_t row_bytes, int box_inner,
-                        int box_rows) {
+// A row-major array [rows][inner] of 16-bit values, or of bytes (dtype < 0), its rows `row_bytes` apart, in boxes of box_rows x 128
+// bytes with the 128-byte swizzle.
+inline bool make_map_2d(CUtensorMap* map, int dtype, const void* base, int64_t inner, int64_t rows, int64_t row_bytes, int box_rows) {
   const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)row_bytes};
-  const cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+  const cuuint32_t box[2] = {dtype < 0 ? 128u : 64u, (cuuint32_t)box_rows}, ones[2] = {1, 1};
   const CUtensorMapDataType type = dtype < 0              ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                    : dtype == WINDQ_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                                         : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-  const bool swizzled = box_inner * (dtype < 0 ? 1 : 2) == 128;
   return encode_tiled()(map, type, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // A launch that may begin while its predecessor in the stream ends (the kernel waits for it, see above).

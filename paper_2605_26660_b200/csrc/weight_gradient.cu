@@ -331,8 +331,8 @@ windq_status launch_weight_gradient(windq_ctx* ctx, const WeightGradient& q, cud
 
   CUtensorMap a, b, o[2];
   WINDQ_REQUIRE(ctx, encode_tiled(), WINDQ_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
-  const bool ok = make_map_2d(&a, q.dtype, q.D, q.terms * 2 * q.half, q.T, q.terms * 4 * q.half, 64, 64) && make_map_2d(&b, q.dtype, q.X, q.C, q.T, 2 * q.ldx, 64, 64) &&
-                  make_map_2d(&o[0], q.dtype, q.dWg, q.C, q.F, 2 * q.ldw, 64, 32) && make_map_2d(&o[1], q.dtype, q.dWu, q.C, q.F, 2 * q.ldw, 64, 32);
+  const bool ok = make_map_2d(&a, q.dtype, q.D, q.terms * 2 * q.half, q.T, q.terms * 4 * q.half, 64) && make_map_2d(&b, q.dtype, q.X, q.C, q.T, 2 * q.ldx, 64) &&
+                  make_map_2d(&o[0], q.dtype, q.dWg, q.C, q.F, 2 * q.ldw, 32) && make_map_2d(&o[1], q.dtype, q.dWu, q.C, q.F, 2 * q.ldw, 32);
   WINDQ_REQUIRE(ctx, ok, WINDQ_ERR_CUDA, "a tensor map could not be made");
   const windq_status ready = prepare_kernel(ctx, kWeightGradient, weight_gradient_kernel, kThreads, kSmemLimit, false);
   if (ready != WINDQ_OK) return ready;
