@@ -44,8 +44,9 @@ __device__ __forceinline__ uint32_t top_of(uint32_t top, const uint4& v) {
 }
 
 // Codes of eight values.  y = x * inv is within 2^-23 of 127 x / a.  That quotient either is a border between two codes (8 bits) or
-// is at least 2^-18 of itself away from one (127 x has 18 bits, or 15), so rounding y to 20 bits first -- c - (c - y), c = 17 y --
-// puts both on their side.  Two values an instruction: with one, the kernel was bound by issue (8192 x 8192 5 us more of 43).
+// is at least 2^-19 of itself away from one (the closest: 127 * 2025 / 2033 = 126.50025, 2^-18.97), and rounding y to 20 bits first --
+// c - (c - y), c = 17 y -- moves it by 2^-20 at most: a border comes out as itself, what is not one stays on its side.  Two values an
+// instruction: with one, the kernel was bound by issue (8192 x 8192 5 us more of 43).
 // LIFT: rows of tiny values, whose 127 / a would overflow, are multiplied by 2^60 first.
 template <int DT, bool VALUES, bool LIFT>
 __device__ __forceinline__ void encode(const uint4& v, float inv, float scale, uint2& codes, uint4& values) {
