@@ -1,13 +1,13 @@
 // Argument marshalling of the feed-forward calls, compiled.  Their kernels for a few tokens take 2 to 15 us, and a call through
-// Python's checks, allocations and conversions of a dozen arguments 10 to 12; here it takes 4, of which a launch is 2.6.  Nothing is
+// Python's checks, allocations and conversions of a dozen arguments 10 to 12; here it takes 4.5, of which a launch is 2.6.  Nothing is
 // computed: every function checks its tensors, allocates the outputs it is not given, and calls the C ABI.
 //
 // A function takes (handle, device, stream or None, ...) and returns a tuple whose first item is the status; wrong types raise
 // TypeError, wrong shapes ValueError, before anything is launched.  The interpreter lock is released while memory is allocated and the
 // library runs.
 #include <ATen/ATen.h>
-#include <ATen/cuda/EmptyTensor.h>
-#include <c10/cuda/CUDAStream.h>
+#include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -68,15 +68,13 @@ windq_status unlocked(F call, const A&... arguments) {
   const Unlocked others;
   return call(arguments...);
 }
-// Device memory for `bytes` bytes, straight from torch's allocator (through the dispatcher, with a view where rows are padded, a call
-// takes 1 to 3 us more).
-Tensor fresh(int64_t bytes, int device) {
+// A new tensor in memory of its own, straight from torch's allocator (through the dispatcher, with a view where rows are padded, a call
+// takes 1 to 3 us more; through a tensor of bytes 0.1 each).
+Tensor fresh(int64_t bytes, int device, at::ScalarType type, at::IntArrayRef sizes, at::IntArrayRef strides) {
   const Unlocked others;
-  return Tensor(at::detail::empty_cuda({bytes}, at::kByte, at::Device(at::kCUDA, (at::DeviceIndex)device), std::nullopt));
-}
-// A tensor of such memory.
-Tensor tensor_in(const Tensor& memory, at::ScalarType type, at::IntArrayRef sizes, at::IntArrayRef strides) {
-  Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(memory.storage()), c10::DispatchKeySet(c10::DispatchKey::CUDA),
+  const c10::cuda::CUDAGuard on((c10::DeviceIndex)device);
+  c10::Storage memory(c10::Storage::use_byte_size_t(), bytes, c10::cuda::CUDACachingAllocator::get(), /*resizable=*/true);
+  Tensor t = at::detail::make_tensor<c10::TensorImpl>(std::move(memory), c10::DispatchKeySet(c10::DispatchKey::CUDA),
                                                       c10::scalarTypeToTypeMeta(type));
   t.unsafeGetTensorImpl()->set_sizes_and_strides(sizes, strides);
   return t;
@@ -90,7 +88,7 @@ template <bool DENSE = false>
 Rows rows_out(PyObject* given, Tensor& t, int64_t rows, int64_t cols, at::ScalarType type, int device, int64_t step, const char* name) {
   if (given == Py_None) {
     const int64_t size = (int64_t)c10::elementSize(type), ld = DENSE && cols % step == 0 ? cols : row_length(cols, size);
-    t = tensor_in(fresh(rows * ld * size, device), type, {rows, cols}, {ld, 1});
+    t = fresh(rows * ld * size, device, type, {rows, cols}, {ld, 1});
     return Rows{t.data_ptr(), rows, cols, ld, type};
   }
   t = tensor_of(given, name);
@@ -164,7 +162,7 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Tensor codes, scale, values;
   // Memory of its own for each: who keeps or saves a weight's scales does not keep its codes with them.
   const Rows q = rows_out(a[5], codes, x.rows, x.cols, at::kChar, c.device, 16, "codes");
-  if (a[6] == Py_None) scale = tensor_in(fresh(4 * x.rows, c.device), at::kFloat, {x.rows}, {1});
+  if (a[6] == Py_None) scale = fresh(4 * x.rows, c.device, at::kFloat, {x.rows}, {1});
   else scale = tensor_of(a[6], "scale");
   Rows v;
   if (truth(a[4])) v = rows_out(a[7], values, x.rows, x.cols, x.type, c.device, 8, "values");
