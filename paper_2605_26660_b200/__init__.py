@@ -1232,6 +1232,9 @@ def windq_adamw_states(ctx: Context, tensors: AdamwTensors, m_out=None, v_out=No
 
 # ---- the feed-forward block: trained in 16 bits, served in 8 ----
 #
+# With ``stream`` given new outputs come from that stream's memory, as if it were the current one.  (Those of the calls above come from
+# the current stream's: where ``stream`` is another, let it wait for the current one first, or give the outputs.)
+#
 # Rows of a new output that are no multiple of 32 bytes are padded to a multiple of 128, which the kernels copy faster: its stride(0)
 # then is more than its width, it is not contiguous, and it wants reshape where a contiguous tensor takes view.  Only the gradients of
 # weights whose width is a multiple of 8 are always contiguous, as AdamwTensors takes them.  Tensors given as ``out`` are used as they are.

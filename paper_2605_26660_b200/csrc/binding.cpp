@@ -68,11 +68,33 @@ windq_status unlocked(F call, const A&... arguments) {
   const Unlocked others;
   return call(arguments...);
 }
+struct Call {
+  windq_ctx* ctx;
+  int device;
+  void* stream;
+  bool given;  // the stream, by the caller
+  Call(PyObject* const* a)
+      : ctx(reinterpret_cast<windq_ctx*>(a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]))), device((int)PyLong_AsLong(a[1])), given(a[2] != Py_None) {
+    if (!given) {
+      stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
+    } else {  // a torch.cuda.Stream
+      PyObject* handle = PyObject_GetAttrString(a[2], "cuda_stream");
+      if (!handle) throw python_error();
+      stream = PyLong_AsVoidPtr(handle);
+      Py_DECREF(handle);
+    }
+    if (PyErr_Occurred()) throw python_error();
+  }
+};
+
 // A new tensor in memory of its own, straight from torch's allocator (through the dispatcher, with a view where rows are padded, a call
-// takes 1 to 3 us more; through a tensor of bytes 0.1 each).
-Tensor fresh(int64_t bytes, int device, at::ScalarType type, at::IntArrayRef sizes, at::IntArrayRef strides) {
+// takes 1 to 3 us more; through a tensor of bytes 0.1 each), and of the stream that writes it: memory of the current stream's pool may
+// still be in use there when another stream comes to it.
+Tensor fresh(int64_t bytes, const Call& c, at::ScalarType type, at::IntArrayRef sizes, at::IntArrayRef strides) {
   const Unlocked others;
-  const c10::cuda::CUDAGuard on((c10::DeviceIndex)device);
+  const c10::cuda::CUDAGuard on((c10::DeviceIndex)c.device);
+  c10::cuda::OptionalCUDAStreamGuard stream;
+  if (c.given) stream.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(c.stream), (c10::DeviceIndex)c.device));
   c10::Storage memory(c10::Storage::use_byte_size_t(), bytes, c10::cuda::CUDACachingAllocator::get(), /*resizable=*/true);
   Tensor t = at::detail::make_tensor<c10::TensorImpl>(std::move(memory), c10::DispatchKeySet(c10::DispatchKey::CUDA),
                                                       c10::scalarTypeToTypeMeta(type));
@@ -85,14 +107,14 @@ int64_t row_length(int64_t cols, int64_t size) { return cols * size % 32 == 0 ? 
 // of rows that begin in the middle of 32 bytes take up to a third longer (500 tokens x 2 x 5000 x 5000 70 us, x 5056 57).  A new DENSE
 // one is padded only where the library wants its rows apart.
 template <bool DENSE = false>
-Rows rows_out(PyObject* given, Tensor& t, int64_t rows, int64_t cols, at::ScalarType type, int device, int64_t step, const char* name) {
+Rows rows_out(PyObject* given, Tensor& t, int64_t rows, int64_t cols, at::ScalarType type, const Call& c, int64_t step, const char* name) {
   if (given == Py_None) {
     const int64_t size = (int64_t)c10::elementSize(type), ld = DENSE && cols % step == 0 ? cols : row_length(cols, size);
-    t = fresh(rows * ld * size, device, type, {rows, cols}, {ld, 1});
+    t = fresh(rows * ld * size, c, type, {rows, cols}, {ld, 1});
     return Rows{t.data_ptr(), rows, cols, ld, type};
   }
   t = tensor_of(given, name);
-  const Rows r = rows_of(t, type, device, step, name);
+  const Rows r = rows_of(t, type, c.device, step, name);
   TORCH_CHECK_VALUE(r.rows == rows && r.cols == cols, name, " must be a [", rows, ", ", cols, "] tensor");
   return r;
 }
@@ -113,24 +135,6 @@ at::ScalarType out_type(PyObject* dtype, PyObject* out) {
   TORCH_CHECK_TYPE(code_of(type) >= 0, "the output must be torch.float16 or torch.bfloat16, got ", type);
   return type;
 }
-
-struct Call {
-  windq_ctx* ctx;
-  int device;
-  void* stream;
-  Call(PyObject* const* a)
-      : ctx(reinterpret_cast<windq_ctx*>(a[0] == Py_None ? nullptr : PyLong_AsVoidPtr(a[0]))), device((int)PyLong_AsLong(a[1])) {
-    if (a[2] == Py_None) {
-      stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
-    } else {  // a torch.cuda.Stream
-      PyObject* handle = PyObject_GetAttrString(a[2], "cuda_stream");
-      if (!handle) throw python_error();
-      stream = PyLong_AsVoidPtr(handle);
-      Py_DECREF(handle);
-    }
-    if (PyErr_Occurred()) throw python_error();
-  }
-};
 
 bool truth(PyObject* o) {
   const int t = PyObject_IsTrue(o);
@@ -161,11 +165,11 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const Rows x = half_of(tensor_of(a[3], "X"), c.device, "X");
   Tensor codes, scale, values;
   // Memory of its own for each: who keeps or saves a weight's scales does not keep its codes with them.
-  const Rows q = rows_out(a[5], codes, x.rows, x.cols, at::kChar, c.device, 16, "codes");
-  if (a[6] == Py_None) scale = fresh(4 * x.rows, c.device, at::kFloat, {x.rows}, {1});
+  const Rows q = rows_out(a[5], codes, x.rows, x.cols, at::kChar, c, 16, "codes");
+  if (a[6] == Py_None) scale = fresh(4 * x.rows, c, at::kFloat, {x.rows}, {1});
   else scale = tensor_of(a[6], "scale");
   Rows v;
-  if (truth(a[4])) v = rows_out(a[7], values, x.rows, x.cols, x.type, c.device, 8, "values");
+  if (truth(a[4])) v = rows_out(a[7], values, x.rows, x.cols, x.type, c, 8, "values");
   return result(unlocked(windq_quantize_rows, c.ctx, code_of(x.type), x.p, x.rows, x.cols, x.ld, static_cast<int8_t*>(q.p), q.ld,
                                     scales_of(scale, x.rows, c.device, "scale"), v.p, v.ld, c.stream),
                 codes, scale, values);
@@ -181,7 +185,7 @@ PyObject* int8_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const float* sx = scales_of(tensor_of(a[4], "scale"), x.rows, c.device, "scale");
   const float* sw = scales_of(tensor_of(a[6], "w_scale"), w.rows, c.device, "w_scale");
   Tensor out;
-  const Rows y = rows_out(a[8], out, x.rows, w.rows, out_type(a[7], a[8]), c.device, 8, "out");
+  const Rows y = rows_out(a[8], out, x.rows, w.rows, out_type(a[7], a[8]), c, 8, "out");
   return result(unlocked(windq_int8_forward, c.ctx, static_cast<int8_t*>(x.p), x.rows, x.cols, x.ld, sx, static_cast<int8_t*>(w.p), w.rows, w.ld, sw,
                                    code_of(y.type), y.p, y.ld, c.stream),
                 out);
@@ -201,7 +205,7 @@ PyObject* gated_int8_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int act = (int)PyLong_AsLong(a[9]);
   if (PyErr_Occurred()) throw python_error();
   Tensor out;
-  const Rows h = rows_out(a[11], out, x.rows, g.rows, out_type(a[10], a[11]), c.device, 8, "out");
+  const Rows h = rows_out(a[11], out, x.rows, g.rows, out_type(a[10], a[11]), c, 8, "out");
   return result(unlocked(windq_gated_int8_forward, c.ctx, act, static_cast<int8_t*>(x.p), x.rows, x.cols, x.ld, sx, static_cast<int8_t*>(g.p), g.ld, sg,
                                          static_cast<int8_t*>(u.p), u.ld, su, g.rows, code_of(h.type), h.p, h.ld, c.stream),
                 out);
@@ -225,11 +229,11 @@ PyObject* gated_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (PyErr_Occurred()) throw python_error();
   const int64_t T = q.x.rows, F = q.g.rows;
   Tensor h, gate, up_;
-  const Rows o = rows_out(a[8], h, T, F, q.x.type, c.device, 8, "h");
+  const Rows o = rows_out(a[8], h, T, F, q.x.type, c, 8, "h");
   Rows g, u;
   if (truth(a[7])) {
-    g = rows_out(a[9], gate, T, F, q.x.type, c.device, 8, "gate");
-    u = rows_out(a[10], up_, T, F, q.x.type, c.device, 8, "up");
+    g = rows_out(a[9], gate, T, F, q.x.type, c, 8, "gate");
+    u = rows_out(a[10], up_, T, F, q.x.type, c, 8, "up");
     TORCH_CHECK_VALUE(g.ld == u.ld, "gate and up must have the same stride between rows");
   }
   return result(unlocked(windq_gated_forward, c.ctx, code_of(q.x.type), act, q.x.p, T, q.x.cols, q.x.ld, q.g.p, q.g.ld, q.u.p, q.u.ld, F, o.p, o.ld, g.p,
@@ -256,10 +260,10 @@ PyObject* gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
                       "] tensors with the same stride between rows");
   }
   Tensor dX, dWg, dWu;
-  if (truth(a[10])) dx = rows_out(a[12], dX, T, C, q.x.type, c.device, 8, "dx");
+  if (truth(a[10])) dx = rows_out(a[12], dX, T, C, q.x.type, c, 8, "dx");
   if (truth(a[11])) {
-    dg = rows_out<true>(a[13], dWg, F, C, q.x.type, c.device, 8, "dWg");  // the optimiser takes contiguous gradients
-    du = rows_out<true>(a[14], dWu, F, C, q.x.type, c.device, 8, "dWu");
+    dg = rows_out<true>(a[13], dWg, F, C, q.x.type, c, 8, "dWg");  // the optimiser takes contiguous gradients
+    du = rows_out<true>(a[14], dWu, F, C, q.x.type, c, 8, "dWu");
     TORCH_CHECK_VALUE(dg.ld == du.ld, "dWg and dWu must have the same stride between rows");
   }
   return result(unlocked(windq_gated_backward, c.ctx, code_of(q.x.type), act, q.x.p, T, C, q.x.ld, q.g.p, q.g.ld, q.u.p, q.u.ld, F, g.p, u.p, g.ld, dh.p,
