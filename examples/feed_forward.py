@@ -57,7 +57,8 @@ def main(verbose=True):
             first |= dict(dWg=grads[0].clone(), dWu=grads[1].clone())
         wq.windq_adamw_step(ctx, tensors, step=step, lr=2e-3)
 
-    # serving: codes of the trained weights, made once, and of every batch of tokens
+    # serving: codes of the trained weights, made once, and of every batch of tokens.  They are a second rounding, with one scale a row:
+    # a plan's own codes have a zero point and a scale for each group, which no integer product reads.
     coded = [wq.windq_quantize_rows(ctx, W) for W in (*copies, down)]
     X = torch.randn(6, C, device="cuda").half()
     x = wq.windq_quantize_rows(ctx, X)

@@ -94,8 +94,8 @@ windq_status windq_fit_work(windq_ctx* ctx, int64_t* evaluated_out, int64_t* sea
 
 /* Thread blocks of the adapter calls (windq_lora_*) and the products of the feed-forward calls (windq_int8_forward,
  * windq_gated_*) in which a wait on a copy or a matrix product gave up after about two seconds: 0 unless the GPU or the
- * library is broken; the results of a call that adds to it are invalid.  Once one did, these calls refuse to run (WINDQ_ERR_CUDA) until the counter is put back; the replay of a captured call does
- * not look.  (Every wait on a barrier of shared memory is bounded, so that such a fault ends the kernel instead of hanging
+ * library is broken; the results of a call that adds to it are invalid.  Once one did, these calls refuse to run
+ * (WINDQ_ERR_CUDA) until the counter is put back; the replay of a captured call does not look.  (Every wait on a barrier of shared memory is bounded, so that such a fault ends the kernel instead of hanging
  * the GPU.  What waits without a limit -- for tensor memory, for the other blocks of a cluster, for the kernel before --
  * waits for blocks that run to that point by themselves.)
  *   n_out: HOST pointer to one int64; reset != 0 puts the counter back to zero.  Synchronises the device first: every
@@ -737,11 +737,11 @@ windq_status windq_gated_int8_forward(windq_ctx* ctx, int activation, const int8
  * Into the sums go dG and dU rounded to `dtype`, which costs the gradients about as much precision as their own rounding; of up to
  * 64 tokens, or T C F up to 2^30, the sums of two such values, which costs none.
  * In fp16 dG and dU are kept times one power of two a call, which puts the largest of the finite ones near 2^15, and the products
- * are divided by it: values down to 2^-28 of the largest lose nothing to fp16's range before they are rounded to the type of the
- * result; smaller ones are rounded to steps of at most 2^-38 of the largest (a token that far below the others keeps as much).
- * An infinity or a NaN among them spoils dX of its token and dWg and dWu of its output, and nothing else.
- * The outputs are overwritten, in an order of sums fixed by the sizes: equal calls give equal bits.  With T = 0 dWg and dWu
- * become zero.  Scratch: windq_scratch_bytes_gated_backward (recompute: 1 without gate and up). */
+ * are divided by it: those down to 2^-28 of the largest keep fp16's full precision.  Smaller ones are rounded to steps of at most
+ * 2^-38 of the largest: a token whose gradients are that far below another's loses them.  An infinity or a NaN among them spoils dX of
+ * its token and dWg and dWu of its output, and nothing else.
+ * The outputs are overwritten, in an order of sums fixed by the sizes: equal calls give equal bits.  They must not overlap one another
+ * or an input.  With T = 0 dWg and dWu become zero.  Scratch: windq_scratch_bytes_gated_backward (recompute: 1 without gate and up). */
 int64_t windq_scratch_bytes_gated_backward(int64_t T, int64_t C, int64_t F, int recompute);
 windq_status windq_gated_backward(windq_ctx* ctx, int dtype, int activation, const void* X, int64_t T, int64_t C, int64_t ldx,
                                   const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu, int64_t F, const void* gate,
