@@ -86,3 +86,28 @@ def test_what_a_shut_gate_does_not_hide(wq, ctx, dtype, act):  # noqa: F811
         outputs = torch.arange(F, device="cuda") != 5
         assert bool((got["dWg"][outputs] == 0).all()) and bool((got["dWu"][outputs] == 0).all())
         assert bool(got["dWg"][5].isnan().all())
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("T", [20, 300])
+def test_tokens_without_a_gradient(wq, ctx, T, act):  # noqa: F811
+    """Padding, and tokens outside the loss: their gates and ups may be beyond fp16, their dH is 0, and so is what they add."""
+    F, C = 96, 64
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    r = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    X, Wg, Wu = r(T, C).half(), (0.1 * r(F, C)).half(), (0.1 * r(F, C)).half()
+    Wg[:, 0], Wu[:, 0] = 30, -30
+    X[:, 0] = 0
+    masked = torch.arange(T, device="cuda") % 3 == 1
+    X[masked, 0] = 30000                                  # g = 900000, u = -900000
+    dH = r(T, F).half()
+    dH[masked] = 0
+    f = wq.windq_gated_forward(ctx, X, Wg, Wu, activation=act, want_saved=True)
+    assert bool(f["gate"][masked].isinf().all()) and bool(f["up"][masked].isinf().all()) and bool(f["h"][~masked].isfinite().all())
+    kept = wq.windq_gated_backward(ctx, X[~masked].contiguous(), Wg, Wu, dH[~masked].contiguous(), activation=act)
+    for saved in (dict(gate=f["gate"], up=f["up"]), {}):
+        got = wq.windq_gated_backward(ctx, X, Wg, Wu, dH, activation=act, **saved)
+        assert bool((got["dx"][masked] == 0).all())
+        # the same sums beside zeros: what differs is where the tensor cores cut them off, below a rounding of the result
+        for a, b in ((got["dx"][~masked], kept["dx"]), (got["dWg"], kept["dWg"]), (got["dWu"], kept["dWu"])):
+            assert bool(a.isfinite().all()) and float((a.double() - b.double()).norm() / b.double().norm()) < 2.0 ** -11
